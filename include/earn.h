@@ -276,6 +276,97 @@ earn_status_t earn_beam_topk(int32_t batch, int32_t beams, int32_t n_live, int32
                              const float* beam_scores_or_null, int32_t* parent, int32_t* token, float* new_scores,
                              void* workspace, size_t workspace_bytes, earn_stream_t stream);
 
+/* ---- Evictable cache of a layer l < k ---------------------------------------------------------------------------------
+ * The full layers keep every prompt row, which is what is left of a model's cache once the register layers hold R rows
+ * (Eq. 9: k L of k L + (N - k) R entries).  The four calls below hold such a layer to a budget of rows per sequence and kv
+ * head: its first and last tokens' rows and, of the others, those that received the most attention so far (not part of the
+ * paper's method; it is what the systems it compares itself with do to a cache, and goes with the split as well):
+ *
+ *   prompt : earn_prefill_attn (with lse) -> earn_key_weights -> earn_evict_prompt_kv      packed K/V -> budgeted pages
+ *   step   : earn_paged_decode_attn -> earn_evict_kv                                       one new token, then back to the budget
+ *
+ * Every kv head of a sequence holds the same number of rows, but not the rows of the same tokens: slot s of head h is a
+ * row of its own, and pos says which token it came from.  K arrives rotated, so the order of the slots does not matter. */
+
+/* Paged K/V cache of one layer.  Row j of sequence b is slot j % 16 of page block_table[b * pages_per_seq + j / 16].
+ * The pages of different sequences are disjoint.  A table entry outside [0, n_pages) reads a wrong page, never outside the
+ * cache; a row that would be written there is dropped.  The per-row arrays that go with it (weight, pos) are
+ * [B, Hkv, 16 * pages_per_seq]; rows at or past a sequence's length are neither read nor written in any of them. */
+typedef struct {
+  void* k_pages;              /* device [n_pages, 16, Hkv, D] */
+  void* v_pages;              /* device, same shape */
+  const int32_t* block_table; /* device [B, pages_per_seq], or NULL: page p of sequence b is b*pages_per_seq+p */
+  int32_t pages_per_seq;
+  int32_t n_pages;
+  const int32_t* seq_len;     /* device [B]: rows the sequence holds, the new token of earn_paged_decode_attn included.
+                                 0: the sequence takes no part.  The calls read it and never write it (one array serves
+                                 all layers of a step); earn_evict_prompt_kv does not use it and accepts NULL. */
+  int32_t max_len;            /* host: no seq_len exceeds it (a longer one counts as max_len); 1 .. 16 * pages_per_seq */
+} earn_paged_cache_t;
+
+/* What stays when a sequence holds more than `budget` rows: the rows of the first n_first tokens and of the last n_last
+ * tokens, and of the others those with the largest weight (equal weights: the lower row number; NaN counts as -inf).
+ * n_first + n_last <= budget. */
+typedef struct {
+  int32_t budget;  /* >= 1 rows per sequence and kv head */
+  int32_t n_first; /* >= 0; at least the prefix registers, as a rule */
+  int32_t n_last;  /* >= 0; at least the suffix registers, as a rule */
+} earn_evict_t;
+
+/* Bytes of scratch that cover the three calls on a paged cache for n_seq sequences (256 for a malformed request).  Host
+ * only; the first 256 bytes are the status block, as in earn_workspace_bytes, and earn_workspace_init prepares it. */
+size_t earn_paged_workspace_bytes(const earn_model_t* model, int32_t n_seq, const earn_paged_cache_t* cache);
+
+/* Accumulated attention weight of every prompt row of a layer l < k: with W_b the last min(n_obs, L_b) rows of sequence b,
+ *   weight[h, j] = sum_{i in W_b, i >= j} sum_{query heads a of h} exp( Q[i,a].K[j,h] * scale - lse[a,i] ).
+ * q: device [total_tokens, Hq, D]; k: device [total_tokens, Hkv, D]; lse: device fp32 [Hq, total_tokens] as
+ * earn_prefill_attn writes it (rows outside the windows are not read); weight: device fp32 [Hkv, total_tokens], overwritten.
+ * fp32 logits, exponentials and sums, in an order that depends on the shapes only.
+ * workspace: at least earn_workspace_bytes(model, batch, 1) bytes.
+ * Errors: layer outside [0, k), n_obs < 1, NULL or misaligned tensors -> INVALID_ARG; workspace -> WORKSPACE. */
+earn_status_t earn_key_weights(const earn_model_t* model, const earn_batch_t* batch, int32_t layer, int32_t n_obs,
+                               const void* q, const void* k, const float* lse, float* weight,
+                               void* workspace, size_t workspace_bytes, earn_stream_t stream);
+
+/* The prompt's budget of rows, from the packed K/V into the pages: row m of head h is a bit copy of the m-th kept position
+ * of the sequence in increasing order, pos_out[b, h, m] that position and weight_out[b, h, m] (if not NULL) its weight.
+ * A prompt of at most `budget` rows is copied whole.  weight: device fp32 [Hkv, total_tokens] (earn_key_weights).
+ * The sequence then holds min(L_b, budget) rows, which the caller puts into seq_len.
+ * Errors: layer outside [0, k), min(max L_b, budget) > 16 * pages_per_seq, a malformed policy or cache, NULL or misaligned
+ * tensors -> INVALID_ARG; workspace -> WORKSPACE. */
+earn_status_t earn_evict_prompt_kv(const earn_model_t* model, const earn_batch_t* batch, int32_t layer,
+                                   const earn_evict_t* policy, const void* k, const void* v, const float* weight,
+                                   const earn_paged_cache_t* cache, float* weight_out_or_null, int32_t* pos_out,
+                                   void* workspace, size_t workspace_bytes, earn_stream_t stream);
+
+/* One new token per sequence over the paged cache of a layer l < k (Eq. 4: append, then attend, self included).
+ * The new row k_new[b], v_new[b] (device [n_seq, Hkv, D]; both NULL: the row is there already) is stored as row
+ * seq_len[b] - 1; q, o: device [n_seq, Hq, D]; o of a sequence with seq_len 0 is zero.
+ * weight_out (if not NULL): weight_out[b,h,j] = weight[b,h,j] + sum over the query heads of h of the softmax weight of row
+ * j, for j < seq_len[b]; the appended row starts from zero, and weight == NULL stands for zeros.  weight_out == weight adds
+ * in place.  pos (if not NULL, with new_pos): pos[b, h, seq_len[b] - 1] = new_pos[b], device int32 [n_seq].
+ * Logits, softmax and sums in fp32; with bf16 the weights are rounded to bf16 in front of the product with V only.
+ * Errors: layer outside [0, k), weight without weight_out, only one of k_new / v_new or of new_pos / pos, a malformed
+ * cache, NULL or misaligned tensors -> INVALID_ARG; more than 1024 query heads per kv head, n_seq > 65535 or kv heads >
+ * 65535 -> UNSUPPORTED; workspace -> WORKSPACE. */
+earn_status_t earn_paged_decode_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, const void* q,
+                                     const void* k_new_or_null, const void* v_new_or_null,
+                                     const earn_paged_cache_t* cache, void* o, const float* weight_or_null,
+                                     float* weight_out_or_null, const int32_t* new_pos_or_null, int32_t* pos_or_null,
+                                     void* workspace, size_t workspace_bytes, earn_stream_t stream);
+
+/* Back to the budget, in place: in a sequence that holds more than `budget` rows, the kept rows (earn_evict_t; the first
+ * tokens are those with pos < n_first, the last those with pos > max pos - n_last) that lie at or past row `budget` move,
+ * in increasing order, into the rows below it that are not kept, in increasing order.  No other row of the pages changes.
+ * weight_out, pos_out receive the rows below min(seq_len, budget) as they are afterwards; each may be the input array
+ * itself (otherwise it must not overlap it).  The sequence then holds min(seq_len[b], budget) rows, which the caller puts
+ * into seq_len once the call of every layer has been enqueued.
+ * Errors: layer outside [0, k), a malformed policy or cache, NULL or misaligned tensors -> INVALID_ARG; workspace ->
+ * WORKSPACE. */
+earn_status_t earn_evict_kv(const earn_model_t* model, int32_t n_seq, int32_t layer, const earn_evict_t* policy,
+                            const earn_paged_cache_t* cache, const float* weight, const int32_t* pos, float* weight_out,
+                            int32_t* pos_out, void* workspace, size_t workspace_bytes, earn_stream_t stream);
+
 /* Number of kernels this library has launched in this process so far (host counter, all streams). */
 uint64_t earn_launch_count(void);
 

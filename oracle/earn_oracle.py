@@ -33,6 +33,9 @@ What pins each function (see tests/test_oracle_pins.py):
                           on the participating rows and the same gradients, zero on every prompt row
   beam_topk             : python's sorted() on (score, index) tuples; hand-made cases (a dominant beam, exact ties,
                           the first step with one live beam); greedy decoding (one beam) = argmax
+  key_weights           : column sums of the scalar definition; over the whole prompt the weights of a sequence sum to the
+                          number of (query row, head) pairs
+  keep_rows, evict_moves : python's sorted() on (protected, weight, row) tuples; a budget of every row keeps every row
 Attention values have no printed worked example in the paper, so beyond those
 pins they are parity unpinned.
 """
@@ -482,3 +485,59 @@ def sinks(p: np.ndarray, t_head: int = 3, tail_span: int = 3) -> Tuple[float, fl
     """Eq. 15 with 1-based positions: Sink_head = sum_{i<=T_h} p_i, Sink_tail = sum_{i>=n-tail_span} p_i."""
     n = len(p)
     return float(np.sum(p[:t_head])), float(np.sum(p[max(n - tail_span - 1, 0):]))
+
+
+# ---------------------------------------------------------------------------
+# Evictable cache (not in the paper: a budget of rows per sequence and kv head for the layers in front of the split)
+# ---------------------------------------------------------------------------
+def key_weights(q, k, lse, cu_seqlens, n_obs: int, scale: Optional[float] = None) -> np.ndarray:
+    """weight[h, j] = sum over the last n_obs query rows i >= j of j's sequence and over the query heads a of kv head h of
+    exp(q[i, a] . k[j, h] * scale - lse[a, i]).  lse [Hq, total] natural log."""
+    q, k, lse = np.asarray(q, np.float64), np.asarray(k, np.float64), np.asarray(lse, np.float64)
+    hq, hkv, sc = q.shape[1], k.shape[1], _scale(q.shape[2], scale)
+    out = np.zeros((hkv, q.shape[0]))
+    for b in range(len(cu_seqlens) - 1):
+        lo, hi = int(cu_seqlens[b]), int(cu_seqlens[b + 1])
+        for i in range(max(lo, hi - n_obs), hi):
+            for a in range(hq):
+                h = a // (hq // hkv)
+                out[h, lo:i + 1] += np.exp(k[lo:i + 1, h] @ q[i, a] * sc - lse[a, i])
+    return out
+
+
+def keep_rows(weight, pos, budget: int, n_first: int, n_last: int) -> np.ndarray:
+    """Row numbers (increasing) that stay of the len(weight) rows of one (sequence, kv head)."""
+    n = len(weight)
+    if n <= budget:
+        return np.arange(n)
+    last = max(int(p) for p in pos)
+
+    def rank(j):
+        w = float(weight[j])
+        protected = pos[j] < n_first or pos[j] > last - n_last
+        return (0 if protected else 1, 0.0 if protected else -(float("-inf") if np.isnan(w) else w), j)
+
+    return np.asarray(sorted(sorted(range(n), key=rank)[:budget]), dtype=np.int64)
+
+
+def evict_moves(weight, pos, budget: int, n_first: int, n_last: int) -> Tuple[np.ndarray, np.ndarray]:
+    """(from, to): the kept rows at or past `budget` and the rows below it that go, each in increasing order."""
+    keep = keep_rows(weight, pos, budget, n_first, n_last)
+    free = np.setdiff1d(np.arange(min(budget, len(weight))), keep)
+    return keep[keep >= budget], free
+
+
+def paged_decode(q, keys, values, scale: Optional[float] = None) -> Tuple[np.ndarray, np.ndarray]:
+    """q [Hq, D], keys / values [n, Hkv, D] of one sequence, the new token's row included: (o [Hq, D], the softmax weight
+    every row receives, summed over the query heads of its kv head [Hkv, n])."""
+    q, keys, values = (np.asarray(x, np.float64) for x in (q, keys, values))
+    hq, hkv = q.shape[0], keys.shape[1]
+    o, w = np.zeros(q.shape), np.zeros((hkv, keys.shape[0]))
+    if keys.shape[0] == 0:
+        return o, w
+    for a in range(hq):
+        h = a // (hq // hkv)
+        p = attention_scores(q[a], keys[:, h], scale)
+        o[a] = p @ values[:, h]
+        w[h] += p
+    return o, w

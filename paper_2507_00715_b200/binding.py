@@ -48,6 +48,15 @@ class EarnProj(C.Structure):
                 ("rope_cos", C.c_void_p), ("rope_sin", C.c_void_p)]
 
 
+class EarnPagedCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("block_table", C.c_void_p),
+                ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("seq_len", C.c_void_p), ("max_len", C.c_int32)]
+
+
+class EarnEvict(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32)]
+
+
 SYMBOLS = {
     "earn_workspace_bytes": (C.c_size_t, [C.POINTER(EarnModel), C.POINTER(EarnBatch), C.c_int32]),
     "earn_workspace_init": (C.c_int, [C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -81,6 +90,17 @@ SYMBOLS = {
     "earn_beam_topk_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     "earn_beam_topk": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "earn_paged_workspace_bytes": (C.c_size_t, [C.POINTER(EarnModel), C.c_int32, C.POINTER(EarnPagedCache)]),
+    "earn_key_weights": (C.c_int, [C.POINTER(EarnModel), C.POINTER(EarnBatch), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "earn_evict_prompt_kv": (C.c_int, [C.POINTER(EarnModel), C.POINTER(EarnBatch), C.c_int32, C.POINTER(EarnEvict), C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.POINTER(EarnPagedCache), C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]),
+    "earn_paged_decode_attn": (C.c_int, [C.POINTER(EarnModel), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.POINTER(EarnPagedCache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_size_t, C.c_void_p]),
+    "earn_evict_kv": (C.c_int, [C.POINTER(EarnModel), C.c_int32, C.c_int32, C.POINTER(EarnEvict), C.POINTER(EarnPagedCache),
+                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "earn_launch_count": (C.c_uint64, []),
     "earn_status_string": (C.c_char_p, [C.c_int]),
     "earn_version": (C.c_int32, []),
@@ -285,3 +305,122 @@ def earn_train_attn_bwd(model, batch: Batch, layer, n_target, q, k, v, o, lse, d
     _check(lib().earn_train_attn_bwd(C.byref(model), C.byref(batch.c), layer, n_target, _ptr(q), _ptr(k), _ptr(v), _ptr(o),
                                      _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), p, n, _stream()),
            "earn_train_attn_bwd")
+
+
+# ---- evictable paged cache of the full layers.  These wrappers check what the C ABI cannot see: element types, density,
+# sizes and the device of every tensor (a ValueError names the argument); the library checks the rest.
+_TORCH_DTYPE = {EARN_F32: torch.float32, EARN_BF16: torch.bfloat16}
+
+
+def _tensor(t, what: str, dtype: torch.dtype, numel: int) -> Optional[int]:
+    """Address of a dense CUDA tensor of `dtype` on the current device with at least `numel` elements (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: not contiguous")
+    if t.numel() < numel:
+        raise ValueError(f"{what}: {t.numel()} elements, expected at least {numel}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: on {t.device}, expected the current CUDA device")
+    return t.data_ptr()
+
+
+def make_evict(budget: int, n_first: int = 0, n_last: int = 0) -> EarnEvict:
+    return EarnEvict(budget, n_first, n_last)
+
+
+def make_paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: Optional[torch.Tensor] = None,
+                     seq_len: Optional[torch.Tensor] = None, max_len: Optional[int] = None,
+                     pages_per_seq: Optional[int] = None) -> EarnPagedCache:
+    """k_pages, v_pages [n_pages, 16, Hkv, D]; block_table int32 [n_seq, pages_per_seq] (None: identity, then
+    pages_per_seq is required); seq_len int32 [n_seq].  max_len defaults to 16 * pages_per_seq.  The caller keeps the
+    tensors alive."""
+    for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if t.dim() != 4 or t.shape[1] != PAGE_TOKENS or t.shape != k_pages.shape or t.dtype != k_pages.dtype:
+            raise ValueError(f"{what}: expected [n_pages, {PAGE_TOKENS}, Hkv, D], the same for k and v")
+        _tensor(t, what, t.dtype, 0)
+    if block_table is not None:
+        if block_table.dim() != 2:
+            raise ValueError("block_table: expected [n_seq, pages_per_seq]")
+        pages_per_seq = block_table.shape[1]
+    if pages_per_seq is None:
+        raise ValueError("pages_per_seq is needed without a block table")
+    cache = EarnPagedCache(_ptr(k_pages), _ptr(v_pages), _tensor(block_table, "block_table", torch.int32, 0), pages_per_seq,
+                           k_pages.shape[0], _tensor(seq_len, "seq_len", torch.int32, 0),
+                           PAGE_TOKENS * pages_per_seq if max_len is None else max_len)
+    # what the calls check against the model and the number of sequences
+    cache.kind = (k_pages.dtype, k_pages.shape[2], k_pages.shape[3])
+    cache.rows = (None if block_table is None else block_table.shape[0], None if seq_len is None else seq_len.numel())
+    return cache
+
+
+def _check_cache(model: EarnModel, n_seq: int, cache: EarnPagedCache) -> int:
+    """Rows of the per-row arrays (weight, pos) of one sequence and head; raises if the cache is not this model's."""
+    if cache.kind != (_TORCH_DTYPE[model.dtype], model.n_kv_heads, model.head_dim):
+        raise ValueError(f"cache of {cache.kind}, model of {(_TORCH_DTYPE[model.dtype], model.n_kv_heads, model.head_dim)}")
+    if any(r is not None and r < n_seq for r in cache.rows):
+        raise ValueError(f"block_table / seq_len hold fewer than {n_seq} sequences")
+    return PAGE_TOKENS * cache.pages_per_seq
+
+
+def earn_paged_workspace_bytes(model: EarnModel, n_seq: int, cache: EarnPagedCache) -> int:
+    return lib().earn_paged_workspace_bytes(C.byref(model), n_seq, C.byref(cache))
+
+
+def earn_key_weights(model: EarnModel, batch: Batch, layer: int, n_obs: int, q, k, lse, weight, workspace) -> None:
+    """q [total, Hq, D], k [total, Hkv, D], lse fp32 [Hq, total] (earn_prefill_attn) -> weight fp32 [Hkv, total]."""
+    n, dt = batch.c.total_tokens, _TORCH_DTYPE[model.dtype]
+    p, size = _ws(workspace)
+    _check(lib().earn_key_weights(C.byref(model), C.byref(batch.c), layer, n_obs,
+                                  _tensor(q, "q", dt, n * model.n_q_heads * model.head_dim),
+                                  _tensor(k, "k", dt, n * model.n_kv_heads * model.head_dim),
+                                  _tensor(lse, "lse", torch.float32, n * model.n_q_heads),
+                                  _tensor(weight, "weight", torch.float32, n * model.n_kv_heads), p, size, _stream()),
+           "earn_key_weights")
+
+
+def earn_evict_prompt_kv(model: EarnModel, batch: Batch, layer: int, policy: EarnEvict, k, v, weight, cache: EarnPagedCache,
+                         weight_out, pos_out, workspace) -> None:
+    """k, v [total, Hkv, D], weight fp32 [Hkv, total] -> the pages, weight_out fp32 (or None) and pos_out int32
+    [B, Hkv, 16 * pages_per_seq].  Sequence b then holds min(L_b, budget) rows: put that into seq_len."""
+    n, dt, rows = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], batch.batch * model.n_kv_heads
+    cap = _check_cache(model, batch.batch, cache)
+    p, size = _ws(workspace)
+    _check(lib().earn_evict_prompt_kv(C.byref(model), C.byref(batch.c), layer, C.byref(policy),
+                                      _tensor(k, "k", dt, n * model.n_kv_heads * model.head_dim),
+                                      _tensor(v, "v", dt, n * model.n_kv_heads * model.head_dim),
+                                      _tensor(weight, "weight", torch.float32, n * model.n_kv_heads), C.byref(cache),
+                                      _tensor(weight_out, "weight_out", torch.float32, rows * cap),
+                                      _tensor(pos_out, "pos_out", torch.int32, rows * cap), p, size, _stream()),
+           "earn_evict_prompt_kv")
+
+
+def earn_paged_decode_attn(model: EarnModel, n_seq: int, layer: int, q, k_new, v_new, cache: EarnPagedCache, o, weight=None,
+                           weight_out=None, new_pos=None, pos=None, workspace=None) -> None:
+    """q, o [n_seq, Hq, D], k_new, v_new [n_seq, Hkv, D] (or None), weight, weight_out fp32 and pos int32
+    [n_seq, Hkv, 16 * pages_per_seq] (or None), new_pos int32 [n_seq]; weight_out may be weight."""
+    dt, rows = _TORCH_DTYPE[model.dtype], n_seq * model.n_kv_heads
+    cap = _check_cache(model, n_seq, cache)
+    nq, nk = n_seq * model.n_q_heads * model.head_dim, rows * model.head_dim
+    p, size = _ws(workspace)
+    _check(lib().earn_paged_decode_attn(C.byref(model), n_seq, layer, _tensor(q, "q", dt, nq), _tensor(k_new, "k_new", dt, nk),
+                                        _tensor(v_new, "v_new", dt, nk), C.byref(cache), _tensor(o, "o", dt, nq),
+                                        _tensor(weight, "weight", torch.float32, rows * cap),
+                                        _tensor(weight_out, "weight_out", torch.float32, rows * cap),
+                                        _tensor(new_pos, "new_pos", torch.int32, n_seq),
+                                        _tensor(pos, "pos", torch.int32, rows * cap), p, size, _stream()),
+           "earn_paged_decode_attn")
+
+
+def earn_evict_kv(model: EarnModel, n_seq: int, layer: int, policy: EarnEvict, cache: EarnPagedCache, weight, pos, weight_out,
+                  pos_out, workspace) -> None:
+    """weight fp32 and pos int32 [n_seq, Hkv, 16 * pages_per_seq]; weight_out / pos_out may be the same tensors.  Sequence b
+    then holds min(seq_len[b], budget) rows: put that into seq_len."""
+    n = n_seq * model.n_kv_heads * _check_cache(model, n_seq, cache)
+    p, size = _ws(workspace)
+    _check(lib().earn_evict_kv(C.byref(model), n_seq, layer, C.byref(policy), C.byref(cache),
+                               _tensor(weight, "weight", torch.float32, n), _tensor(pos, "pos", torch.int32, n),
+                               _tensor(weight_out, "weight_out", torch.float32, n),
+                               _tensor(pos_out, "pos_out", torch.int32, n), p, size, _stream()), "earn_evict_kv")

@@ -195,6 +195,59 @@ earn_status_t validate_decode(const earn_model_t* model, const earn_batch_t* bat
   return EARN_OK;
 }
 
+// ---- evictable paged cache: shared checks
+static inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static earn_status_t check_paged(const earn_paged_cache_t* c, int64_t n_seq, bool needs_len) {
+  if (c == nullptr) return EARN_ERR_INVALID_ARG;
+  if (c->k_pages == nullptr || c->v_pages == nullptr || !aligned16(c->k_pages) || !aligned16(c->v_pages)) return EARN_ERR_INVALID_ARG;
+  if (c->pages_per_seq < 1 || c->n_pages < 1) return EARN_ERR_INVALID_ARG;
+  if ((int64_t)c->pages_per_seq * EARN_PAGE_TOKENS > INT32_MAX) return EARN_ERR_UNSUPPORTED;   // row numbers are 32-bit
+  if (c->max_len < 1 || (int64_t)c->max_len > (int64_t)c->pages_per_seq * EARN_PAGE_TOKENS) return EARN_ERR_INVALID_ARG;
+  if (c->block_table == nullptr && (int64_t)c->n_pages < n_seq * c->pages_per_seq) return EARN_ERR_INVALID_ARG;
+  if (!aligned4(c->block_table) || !aligned4(c->seq_len) || (needs_len && c->seq_len == nullptr)) return EARN_ERR_INVALID_ARG;
+  return EARN_OK;
+}
+
+static earn_status_t check_policy(const earn_evict_t* p) {
+  if (p == nullptr || p->budget < 1 || p->n_first < 0 || p->n_last < 0) return EARN_ERR_INVALID_ARG;
+  return (int64_t)p->n_first + p->n_last <= p->budget ? EARN_OK : EARN_ERR_INVALID_ARG;
+}
+
+static PagedSource paged_rows(const earn_paged_cache_t* c) {
+  PagedSource s{};
+  s.k = reinterpret_cast<char*>(c->k_pages); s.v = reinterpret_cast<char*>(c->v_pages);
+  s.block_table = c->block_table; s.seq_len = c->seq_len;
+  s.pages_per_seq = c->pages_per_seq; s.n_pages = c->n_pages; s.max_len = c->max_len;
+  return s;
+}
+
+// Workspace of the calls on a paged cache: status block, then either the decode call's scratch (logits, partials and
+// their denominators) or the eviction's (moves and their numbers).
+struct PagedLayout {
+  size_t scores, part_o, part_lse;   // byte offsets, decode
+  size_t n_moves, moves;             // byte offsets, eviction
+  size_t total;
+  int chunk, n_splits, score_ld, list;
+};
+static PagedLayout paged_layout(const earn_model_t* m, int32_t n_seq, const earn_paged_cache_t* c) {
+  PagedLayout l{};
+  const int g = m->n_q_heads / m->n_kv_heads;
+  const size_t units = (size_t)n_seq * m->n_kv_heads;
+  plan_paged_decode(n_seq, m->n_kv_heads, g, c->max_len, &l.chunk, &l.n_splits);
+  l.score_ld = (int)round_up((size_t)c->max_len, EARN_PAGE_TOKENS);
+  l.scores = kStatusBytes;
+  l.part_o = l.scores + round_up(units * g * (size_t)l.score_ld * 4, 256);
+  l.part_lse = l.part_o + round_up(units * l.n_splits * g * (size_t)m->head_dim * 4, 256);
+  const size_t decode_end = l.part_lse + round_up(units * l.n_splits * g * 4, 256);
+  l.list = c->max_len / 2 + 1;   // a move takes a row below the budget and one behind it: at most half the rows
+  l.n_moves = kStatusBytes;
+  l.moves = l.n_moves + round_up(units * 4, 256);
+  const size_t evict_end = l.moves + round_up(units * 2 * (size_t)l.list * 4, 256);
+  l.total = decode_end > evict_end ? decode_end : evict_end;
+  return l;
+}
+
 }  // namespace earn
 
 using namespace earn;
@@ -559,6 +612,137 @@ earn_status_t earn_beam_topk(int32_t batch, int32_t beams, int32_t n_live, int32
                                    workspace, (cudaStream_t)stream) == cudaSuccess;
   note_call(stream, ok ? CALL_LEAVES_CACHE : CALL_UNKNOWN);   // ordinary launches that write the beam tables only
   return ok ? EARN_OK : EARN_ERR_CUDA;
+}
+
+size_t earn_paged_workspace_bytes(const earn_model_t* model, int32_t n_seq, const earn_paged_cache_t* cache) {
+  if (check_model(model) != EARN_OK || n_seq < 0 || check_paged(cache, n_seq, false) != EARN_OK) return kStatusBytes;
+  return paged_layout(model, n_seq, cache).total;
+}
+
+earn_status_t earn_key_weights(const earn_model_t* model, const earn_batch_t* batch, int32_t layer, int32_t n_obs,
+                               const void* q, const void* k, const float* lse, float* weight, void* workspace,
+                               size_t workspace_bytes, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  s = check_batch(batch);
+  if (s != EARN_OK) return s;
+  if (layer < 0 || layer >= model->split_k || n_obs < 1) return EARN_ERR_INVALID_ARG;
+  if (batch->total_tokens == 0) return EARN_OK;
+  if (!q || !k || !lse || !weight || !aligned16(q) || !aligned16(k) || !aligned4(lse) || !aligned4(weight)) return EARN_ERR_INVALID_ARG;
+  if (model->n_kv_heads > 65535) return EARN_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < workspace_need(model, batch, 1)) return EARN_ERR_WORKSPACE;
+  KeyWeightArgs a{};
+  a.q = q; a.k = k; a.lse = lse; a.weight = weight; a.cu_seqlens = batch->cu_seqlens;
+  a.batch = batch->batch; a.total = batch->total_tokens; a.max_seqlen = batch->max_seqlen; a.n_obs = n_obs;
+  a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
+  a.scale = scale_of(model);
+  note_call(stream, CALL_UNKNOWN);
+  return launch_key_weights_simt(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+earn_status_t earn_evict_prompt_kv(const earn_model_t* model, const earn_batch_t* batch, int32_t layer,
+                                   const earn_evict_t* policy, const void* k, const void* v, const float* weight,
+                                   const earn_paged_cache_t* cache, float* weight_out_or_null, int32_t* pos_out,
+                                   void* workspace, size_t workspace_bytes, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  s = check_batch(batch);
+  if (s != EARN_OK) return s;
+  if (layer < 0 || layer >= model->split_k) return EARN_ERR_INVALID_ARG;
+  s = check_policy(policy);
+  if (s != EARN_OK) return s;
+  s = check_paged(cache, batch->batch, false);
+  if (s != EARN_OK) return s;
+  int longest = 0;
+  for (int i = 0; i < batch->batch; ++i) {
+    const int len = batch->cu_seqlens_host[i + 1] - batch->cu_seqlens_host[i];
+    longest = len > longest ? len : longest;
+  }
+  const int kept = longest < policy->budget ? longest : policy->budget;
+  if ((int64_t)kept > (int64_t)cache->pages_per_seq * EARN_PAGE_TOKENS) return EARN_ERR_INVALID_ARG;
+  if ((int64_t)batch->batch * model->n_kv_heads > INT32_MAX) return EARN_ERR_UNSUPPORTED;
+  if (batch->total_tokens == 0) return EARN_OK;
+  if (!k || !v || !weight || !pos_out || !aligned16(k) || !aligned16(v) || !aligned4(weight) || !aligned4(weight_out_or_null) ||
+      !aligned4(pos_out))
+    return EARN_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < paged_layout(model, batch->batch, cache).total)
+    return EARN_ERR_WORKSPACE;
+  EvictArgs a{};
+  a.cache = paged_rows(cache);
+  a.k_packed = k; a.v_packed = v; a.cu_seqlens = batch->cu_seqlens; a.weight = weight;
+  a.weight_out = weight_out_or_null; a.pos_out = pos_out;
+  a.n_seq = batch->batch; a.total = batch->total_tokens; a.max_rows = longest; a.Hkv = model->n_kv_heads;
+  a.row_bytes = (int)(model->head_dim * elem_size(model));
+  a.budget = policy->budget; a.n_first = policy->n_first; a.n_last = policy->n_last;
+  note_call(stream, CALL_UNKNOWN);
+  return launch_evict(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+earn_status_t earn_paged_decode_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, const void* q,
+                                     const void* k_new_or_null, const void* v_new_or_null,
+                                     const earn_paged_cache_t* cache, void* o, const float* weight_or_null,
+                                     float* weight_out_or_null, const int32_t* new_pos_or_null, int32_t* pos_or_null,
+                                     void* workspace, size_t workspace_bytes, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  if (n_seq < 0 || layer < 0 || layer >= model->split_k) return EARN_ERR_INVALID_ARG;
+  s = check_paged(cache, n_seq, true);
+  if (s != EARN_OK) return s;
+  const int g = model->n_q_heads / model->n_kv_heads;
+  if (n_seq > 65535 || model->n_kv_heads > 65535 || g > 1024) return EARN_ERR_UNSUPPORTED;
+  if ((k_new_or_null == nullptr) != (v_new_or_null == nullptr) || (new_pos_or_null == nullptr) != (pos_or_null == nullptr) ||
+      (weight_or_null != nullptr && weight_out_or_null == nullptr))
+    return EARN_ERR_INVALID_ARG;
+  if (n_seq == 0) return EARN_OK;
+  if (!q || !o || !aligned16(q) || !aligned16(o) || !aligned16(k_new_or_null) || !aligned16(v_new_or_null) ||
+      !aligned16(weight_or_null) || !aligned16(weight_out_or_null) || !aligned4(new_pos_or_null) || !aligned4(pos_or_null))
+    return EARN_ERR_INVALID_ARG;
+  const PagedLayout l = paged_layout(model, n_seq, cache);
+  if ((int64_t)l.n_splits * ((g + 15) / 16) > 65535) return EARN_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < l.total) return EARN_ERR_WORKSPACE;
+  PagedDecodeArgs a{};
+  char* ws = reinterpret_cast<char*>(workspace);
+  a.q = q; a.k_new = k_new_or_null; a.v_new = v_new_or_null; a.o = o;
+  a.cache = paged_rows(cache);
+  a.weight = weight_or_null; a.weight_out = weight_out_or_null; a.new_pos = new_pos_or_null; a.pos = pos_or_null;
+  a.scores = reinterpret_cast<float*>(ws + l.scores);
+  a.part_o = reinterpret_cast<float*>(ws + l.part_o);
+  a.part_lse = reinterpret_cast<float*>(ws + l.part_lse);
+  a.n_seq = n_seq; a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
+  a.g = g; a.chunk = l.chunk; a.n_splits = l.n_splits; a.score_ld = l.score_ld;
+  a.scale = scale_of(model);
+  note_call(stream, CALL_UNKNOWN);
+  return launch_paged_decode(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+earn_status_t earn_evict_kv(const earn_model_t* model, int32_t n_seq, int32_t layer, const earn_evict_t* policy,
+                            const earn_paged_cache_t* cache, const float* weight, const int32_t* pos, float* weight_out,
+                            int32_t* pos_out, void* workspace, size_t workspace_bytes, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  if (n_seq < 0 || layer < 0 || layer >= model->split_k) return EARN_ERR_INVALID_ARG;
+  s = check_policy(policy);
+  if (s != EARN_OK) return s;
+  s = check_paged(cache, n_seq, true);
+  if (s != EARN_OK) return s;
+  if ((int64_t)n_seq * model->n_kv_heads > INT32_MAX) return EARN_ERR_UNSUPPORTED;
+  if (n_seq == 0) return EARN_OK;
+  if (!weight || !pos || !weight_out || !pos_out || !aligned4(weight) || !aligned4(pos) || !aligned4(weight_out) || !aligned4(pos_out))
+    return EARN_ERR_INVALID_ARG;
+  const PagedLayout l = paged_layout(model, n_seq, cache);
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < l.total) return EARN_ERR_WORKSPACE;
+  EvictArgs a{};
+  char* ws = reinterpret_cast<char*>(workspace);
+  a.cache = paged_rows(cache);
+  a.weight = weight; a.pos = pos; a.weight_out = weight_out; a.pos_out = pos_out;
+  a.n_moves = reinterpret_cast<int32_t*>(ws + l.n_moves);
+  a.moves = reinterpret_cast<int32_t*>(ws + l.moves);
+  a.list = l.list;
+  a.n_seq = n_seq; a.max_rows = cache->max_len; a.Hkv = model->n_kv_heads;
+  a.row_bytes = (int)(model->head_dim * elem_size(model));
+  a.budget = policy->budget; a.n_first = policy->n_first; a.n_last = policy->n_last;
+  note_call(stream, CALL_UNKNOWN);
+  return launch_evict(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }
 
 }  // extern "C"

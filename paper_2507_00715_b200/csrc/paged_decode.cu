@@ -1,0 +1,418 @@
+// One new token per sequence over the paged cache of a full layer (Eq. 4: append K_t, V_t, then attend over K_{1:t}), with
+// the attention weight every row received added to its accumulated weight.
+//
+// HBM-bound: K and V of every row are read once.  The key list of a (sequence, kv head) is cut into chunks; a warp takes
+// one chunk under 16 query rows (the group's heads), page by page -- a page is a tile of 16 positions -- through a ring
+// of cp.async stages, and leaves a normalised partial with its log2-domain softmax denominator.  A second kernel joins
+// the partials.  The weight of a row needs the denominator of the whole list, so the first kernel also leaves the scaled
+// logits (4 bytes per query head and row beside the 4 D bytes of K and V: 6 % at a group of 8 and D = 128, written and read
+// while they are in L2), and the second kernel turns them into weights: sum over the heads of 2^(logit - LSE).
+// No atomics: every sum has one order.
+#include "decode_tile.cuh"
+#include "sm100_ptx.cuh"
+
+namespace earn {
+namespace {
+using namespace dec;
+
+constexpr int STAGES = 4;
+
+// ------------------------------------------------------------------------------------------------ bf16: one warp per chunk
+template <int D, bool WEIGH>
+__global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
+  using G = Geo<D>;
+  constexpr int CH = G::CH, RPI = G::RPI, NIT = KT / RPI, NTILES = D / 8;
+  extern __shared__ __align__(128) uint8_t smem[];
+  pdl_wait();
+  const int lane = threadIdx.x;
+  const int kvh = blockIdx.x, b = blockIdx.z;
+  const int row_tiles = (a.g + 15) / 16;
+  const int split = blockIdx.y / row_tiles, row0 = (blockIdx.y % row_tiles) * 16;
+  const int len = paged_len(a.cache, b);
+  const int begin = split * a.chunk, n = min(len - begin, a.chunk);
+  if (n <= 0) return;
+  const int n_tiles = (n + KT - 1) / KT;
+  const float scale_log2 = a.scale * kLog2e;
+  RowMap rm;
+  rm.b = b; rm.kvh = kvh; rm.row0 = row0; rm.g = a.g; rm.W = 1; rm.n_rows = a.g; rm.Hq = a.Hq;
+  const bf16 *kp = reinterpret_cast<const bf16*>(a.cache.k), *vp = reinterpret_cast<const bf16*>(a.cache.v);
+  const bf16 *kn = reinterpret_cast<const bf16*>(a.k_new), *vn = reinterpret_cast<const bf16*>(a.v_new);
+
+  // lane t holds the page of tile t (a chunk has at most 32 tiles)
+  bool page_ok = true;
+  int page = 0;
+  if (lane < n_tiles) page = paged_page(a.cache, b, begin / KT + lane, page_ok);
+
+  const uint32_t ring = ptx::smem_u32(smem);
+  const int ch = lane % CH, r0 = lane / CH;
+  const uint32_t dst0 = (uint32_t)r0 * G::PITCH + (uint32_t)ch * 16;
+  const int64_t rowstride = (int64_t)a.Hkv * D;
+  const int newest = kn != nullptr ? len - 1 - begin : -1;   // position of the appended row in this chunk's list (or outside)
+  const int64_t new_off = ((int64_t)b * a.Hkv + kvh) * D + ch * 8;
+
+  auto issue_tile = [&](int t) {
+    const int pg = __shfl_sync(0xffffffffu, page, t);
+    const uint32_t kdst = ring + (t % STAGES) * G::STAGE_B + dst0, vdst = kdst + G::TILE_B;
+    const int64_t off = (((int64_t)pg * KT + r0) * a.Hkv + kvh) * D + ch * 8;
+    if ((t + 1) * KT <= n && (newest < t * KT || newest >= (t + 1) * KT)) {
+#pragma unroll
+      for (int i = 0; i < NIT; ++i) {
+        cp_async16(kdst + i * RPI * G::PITCH, kp + off + i * RPI * rowstride);
+        cp_async16(vdst + i * RPI * G::PITCH, vp + off + i * RPI * rowstride);
+      }
+    } else {   // rows past the list are zero-filled; the appended row comes from k_new / v_new
+#pragma unroll
+      for (int i = 0; i < NIT; ++i) {
+        const int p = t * KT + r0 + i * RPI;
+        const bool fresh = p == newest;
+        const bf16* ks = fresh ? kn + new_off : kp + off + i * RPI * rowstride;
+        const bf16* vs = fresh ? vn + new_off : vp + off + i * RPI * rowstride;
+        cp_async16(kdst + i * RPI * G::PITCH, ks, p < n ? 16 : 0);
+        cp_async16(vdst + i * RPI * G::PITCH, vs, p < n ? 16 : 0);
+      }
+    }
+  };
+  // tiles are consumed in pairs: two in use, STAGES - 2 in flight
+  constexpr int PRE = STAGES - 2;
+#pragma unroll
+  for (int s = 0; s < PRE; ++s) {
+    if (s < n_tiles) issue_tile(s);
+    cp_async_commit();
+  }
+  RowTile<D> t;
+  t.init(reinterpret_cast<const bf16*>(a.q), rm, lane);
+
+  // logits of tile `tile` (8-column blocks 0 .. NB - 1 from its first position on) -> scores, this lane's two rows
+  const int q0 = row0 + (lane >> 2), q1 = q0 + 8, c2 = (lane & 3) * 2;
+  float* s_base = WEIGH ? a.scores + ((int64_t)b * a.Hkv + kvh) * a.g * a.score_ld + begin : nullptr;
+  auto store = [&](int tile, const float* s0, int blk) {   // s0: the four fragment values of 8-column block blk
+    if (!WEIGH) return;
+    const int c = tile * KT + blk * 8 + c2;
+    if (q0 < a.g) *reinterpret_cast<float2*>(s_base + (int64_t)q0 * a.score_ld + c) = make_float2(s0[0] * scale_log2, s0[1] * scale_log2);
+    if (q1 < a.g) *reinterpret_cast<float2*>(s_base + (int64_t)q1 * a.score_ld + c) = make_float2(s0[2] * scale_log2, s0[3] * scale_log2);
+  };
+  struct Sink2 { decltype(store)& f; __device__ __forceinline__ void operator()(int tile, const float (&s)[2][4]) const { f(tile, s[0], 0); f(tile, s[1], 1); } };
+  struct Sink4 { decltype(store)& f; __device__ __forceinline__ void operator()(int tile, const float (&s)[4][4]) const { f(tile, s[0], 0); f(tile, s[1], 1); f(tile, s[2], 2); f(tile, s[3], 3); } };
+  const Sink2 sink2{store};
+  const Sink4 sink4{store};
+  auto visible_in = [&](int tile) { return [=](int c, bool) { return tile * KT + c < n; }; };
+
+  for (int it = 0; it < n_tiles; it += 2) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (it + PRE + u < n_tiles) issue_tile(it + PRE + u);
+      cp_async_commit();
+    }
+    cp_async_wait<PRE>();
+    __syncwarp();
+    const uint32_t ks = ring + (it % STAGES) * G::STAGE_B, vs = ks + G::TILE_B;
+    const uint32_t ks2 = ring + ((it + 1) % STAGES) * G::STAGE_B, vs2 = ks2 + G::TILE_B;
+    if ((it + 2) * KT <= n) {
+      t.attend2(ks, vs, ks2, vs2, scale_log2, lane, sink4, it);
+    } else {
+      t.attend(ks, vs, scale_log2, lane, (it + 1) * KT > n, visible_in(it), sink2, it);
+      if (it + 1 < n_tiles) t.attend(ks2, vs2, scale_log2, lane, true, visible_in(it + 1), sink2, it + 1);
+    }
+    __syncwarp();
+  }
+  cp_async_wait<0>();
+  // ---- append: nothing in this launch reads the stored row
+  if (newest >= 0 && newest < n && row0 == 0) {
+    const int pt = newest / KT;
+    const bool ok = __shfl_sync(0xffffffffu, (int)page_ok, pt) != 0;
+    const int64_t dst = (((int64_t)__shfl_sync(0xffffffffu, page, pt) * KT + newest % KT) * a.Hkv + kvh) * D;
+    if (ok && lane < 2 * CH) {
+      const bf16* s = (lane < CH ? kn : vn) + ((int64_t)b * a.Hkv + kvh) * D;
+      bf16* d = reinterpret_cast<bf16*>(lane < CH ? a.cache.k : a.cache.v) + dst;
+      *reinterpret_cast<uint4*>(d + (lane % CH) * 8) = *reinterpret_cast<const uint4*>(s + (lane % CH) * 8);
+    }
+  }
+  pdl_launch_dependents();
+  t.reduce_sums();
+  // ---- the partial: normalised rows and their log2-domain denominators
+  const int64_t prow = (((int64_t)b * a.Hkv + kvh) * a.n_splits + split) * a.g;
+  const float i0 = t.l0 == 0.f ? 0.f : 1.f / t.l0, i1 = t.l1 == 0.f ? 0.f : 1.f / t.l1;   // (0: every logit of the chunk is -inf)
+  if (q0 < a.g) {
+    float* p0 = a.part_o + (prow + q0) * D + c2;
+#pragma unroll
+    for (int k = 0; k < NTILES; ++k) *reinterpret_cast<float2*>(p0 + k * 8) = make_float2(t.o[k][0] * i0, t.o[k][1] * i0);
+    if ((lane & 3) == 0) a.part_lse[prow + q0] = t.m0 + log2f(t.l0);
+  }
+  if (q1 < a.g) {
+    float* p1 = a.part_o + (prow + q1) * D + c2;
+#pragma unroll
+    for (int k = 0; k < NTILES; ++k) *reinterpret_cast<float2*>(p1 + k * 8) = make_float2(t.o[k][2] * i1, t.o[k][3] * i1);
+    if ((lane & 3) == 0) a.part_lse[prow + q1] = t.m1 + log2f(t.l1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ fp32
+// 128 threads per (sequence, kv head, chunk, 16 query rows), tiles of 32 rows in shared memory.  Logits: a lane per row of
+// the tile, a warp per query row (each K element read once per query row); P V: a thread per column.
+constexpr int FT = 32;   // rows per tile
+template <int D>
+struct F32Smem {
+  static constexpr int PITCH = D + 4;   // floats; lanes a row apart hit different banks with 16-byte reads
+  float k[2][FT][PITCH], v[2][FT][D];
+  float q[16][D];
+  float s[16][FT];
+  float alpha[16];
+};
+
+template <int D, bool WEIGH>
+__global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a) {
+  using S = F32Smem<D>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  S& sh = *reinterpret_cast<S*>(smem);
+  pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int kvh = blockIdx.x, b = blockIdx.z;
+  const int row_tiles = (a.g + 15) / 16;
+  const int split = blockIdx.y / row_tiles, row0 = (blockIdx.y % row_tiles) * 16;
+  const int rows = min(a.g - row0, 16);
+  const int len = paged_len(a.cache, b);
+  const int begin = split * a.chunk, n = min(len - begin, a.chunk);
+  if (n <= 0) return;
+  const int n_tiles = (n + FT - 1) / FT;
+  const float scale_log2 = a.scale * kLog2e;
+  const float *kp = reinterpret_cast<const float*>(a.cache.k), *vp = reinterpret_cast<const float*>(a.cache.v);
+  const float *kn = reinterpret_cast<const float*>(a.k_new), *vn = reinterpret_cast<const float*>(a.v_new);
+  const int newest = kn != nullptr ? len - 1 - begin : -1;
+  const int64_t new_off = ((int64_t)b * a.Hkv + kvh) * D;
+  for (int i = tid; i < 16 * D; i += 128)
+    sh.q[i / D][i % D] = i / D < rows ? reinterpret_cast<const float*>(a.q)[((int64_t)b * a.Hq + kvh * a.g + row0) * D + i] : 0.f;
+
+  constexpr int CH = D / 4;   // 16-byte pieces of a row
+  auto issue_tile = [&](int t) {
+    for (int i = tid; i < FT * CH; i += 128) {
+      const int r = i / CH, c = (i % CH) * 4, p = t * FT + r;
+      bool ok;
+      const int page = p < n ? paged_page(a.cache, b, (begin + p) / EARN_PAGE_TOKENS, ok) : 0;
+      const int64_t off = (((int64_t)page * EARN_PAGE_TOKENS + p % EARN_PAGE_TOKENS) * a.Hkv + kvh) * D;   // (begin is a multiple of 16)
+      const bool fresh = p == newest;
+      cp_async16(ptx::smem_u32(&sh.k[t & 1][r][c]), (fresh ? kn + new_off : kp + off) + c, p < n ? 16 : 0);
+      cp_async16(ptx::smem_u32(&sh.v[t & 1][r][c]), (fresh ? vn + new_off : vp + off) + c, p < n ? 16 : 0);
+    }
+    cp_async_commit();
+  };
+  issue_tile(0);
+  constexpr int HALVES = 128 / D, MY = 16 / HALVES;   // P V: a thread per column; at D = 64 each half of the CTA takes 8 query rows
+  const int col = tid % D, half = tid / D;
+  float acc[MY];
+#pragma unroll
+  for (int r = 0; r < MY; ++r) acc[r] = 0.f;
+  float m[4], l[4];   // rows warp, warp + 4, ..: kept by every lane of the warp
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+  float* s_base = WEIGH ? a.scores + ((int64_t)b * a.Hkv + kvh) * a.g * a.score_ld + begin : nullptr;
+
+  for (int t = 0; t < n_tiles; ++t) {
+    if (t + 1 < n_tiles) issue_tile(t + 1);
+    else cp_async_commit();
+    cp_async_wait<1>();
+    __syncthreads();
+    const int buf = t & 1, p = t * FT + lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = warp + 4 * i;
+      if (r < rows) {   // warp-uniform
+        float x = 0.f, y = 0.f;
+#pragma unroll 8
+        for (int d = 0; d < D; d += 4) {
+          const float4 kk = *reinterpret_cast<const float4*>(&sh.k[buf][lane][d]);
+          const float4 qq = *reinterpret_cast<const float4*>(&sh.q[r][d]);
+          x = fmaf(kk.x, qq.x, x); y = fmaf(kk.y, qq.y, y);
+          x = fmaf(kk.z, qq.z, x); y = fmaf(kk.w, qq.w, y);
+        }
+        const float s = p < n ? (x + y) * scale_log2 : -INFINITY;
+        if (WEIGH && p < n) s_base[(int64_t)(row0 + r) * a.score_ld + p] = s;
+        float mx = s;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float mn = fmaxf(m[i], mx), mu = mn == -INFINITY ? 0.f : mn;
+        const float al = exp2f(m[i] - mu), e = exp2f(s - mu);
+        float sum = e;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        l[i] = l[i] * al + sum;
+        m[i] = mn;
+        sh.s[r][lane] = e;
+        if (lane == 0) sh.alpha[r] = al;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MY; ++i) {
+      const int r = half * MY + i;
+      if (r < rows) {
+        float x = acc[i] * sh.alpha[r];
+#pragma unroll 8
+        for (int j = 0; j < FT; j += 4) {
+          const float4 pp = *reinterpret_cast<const float4*>(&sh.s[r][j]);
+          x = fmaf(pp.x, sh.v[buf][j][col], x);
+          x = fmaf(pp.y, sh.v[buf][j + 1][col], x);
+          x = fmaf(pp.z, sh.v[buf][j + 2][col], x);
+          x = fmaf(pp.w, sh.v[buf][j + 3][col], x);
+        }
+        acc[i] = x;
+      }
+    }
+    __syncthreads();   // the tile and the probabilities have been read
+  }
+  cp_async_wait<0>();
+  if (newest >= 0 && newest < n && row0 == 0) {
+    bool ok;
+    const int page = paged_page(a.cache, b, (begin + newest) / EARN_PAGE_TOKENS, ok);
+    const int64_t dst = (((int64_t)page * EARN_PAGE_TOKENS + newest % EARN_PAGE_TOKENS) * a.Hkv + kvh) * D;
+    if (ok && tid < D) {
+      reinterpret_cast<float*>(a.cache.k)[dst + tid] = kn[new_off + tid];
+      reinterpret_cast<float*>(a.cache.v)[dst + tid] = vn[new_off + tid];
+    }
+  }
+  pdl_launch_dependents();
+  const int64_t prow = (((int64_t)b * a.Hkv + kvh) * a.n_splits + split) * a.g + row0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = warp + 4 * i;
+    if (r < rows && lane == 0) {
+      sh.alpha[r] = l[i] == 0.f ? 0.f : 1.f / l[i];   // (0: every logit of the chunk is -inf)
+      a.part_lse[prow + r] = m[i] + log2f(l[i]);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MY; ++i) {
+    const int r = half * MY + i;
+    if (r < rows) a.part_o[(prow + r) * D + col] = acc[i] * sh.alpha[r];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ join
+// Block x < g: query row x of the (sequence, kv head): the partials, weighted by 2^(their LSE - LSE of all).
+// Block x >= g: rows (x - g) * JOIN_KEYS .. of the list: their weights.
+constexpr int JOIN_THREADS = 256, JOIN_KEYS = 4 * JOIN_THREADS, JOIN_MAX_G = 1024;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArgs a) {
+  __shared__ float lse_all[JOIN_MAX_G];
+  __shared__ float4 part[JOIN_THREADS];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int kvh = blockIdx.y, b = blockIdx.z, g = a.g;
+  const int64_t unit = (int64_t)b * a.Hkv + kvh;
+  const int len = paged_len(a.cache, b);
+  const int live = (len + a.chunk - 1) / a.chunk;   // splits that hold rows
+  const float* lse = a.part_lse + unit * a.n_splits * g;
+  const bool o_block = (int)blockIdx.x < g;
+  const int key0 = ((int)blockIdx.x - g) * JOIN_KEYS;
+  if (!o_block && key0 >= len) return;
+  // ---- denominators over the whole list (one row, or all of the group's)
+  for (int r = o_block ? (warp == 0 ? (int)blockIdx.x : g) : warp; r < (o_block ? (int)blockIdx.x + 1 : g); r += JOIN_THREADS / 32) {
+    float mx = -INFINITY;
+    for (int s = lane; s < live; s += 32) mx = fmaxf(mx, lse[s * g + r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float mu = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f;
+    for (int s = lane; s < live; s += 32) sum += exp2f(lse[s * g + r] - mu);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) lse_all[r] = mu + log2f(sum);
+  }
+  __syncthreads();
+  if (o_block) {
+    constexpr int V4 = D / 4, GROUPS = JOIN_THREADS / V4;   // float4 per row; splits walked side by side
+    const int r = blockIdx.x, c = tid % V4, grp = tid / V4;
+    const float all = lse_all[r];
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = grp; s < live; s += GROUPS) {
+      const float w = exp2f(lse[s * g + r] - all);
+      const float4 x = reinterpret_cast<const float4*>(a.part_o + ((unit * a.n_splits + s) * g + r) * D)[c];
+      acc.x = fmaf(w, x.x, acc.x); acc.y = fmaf(w, x.y, acc.y); acc.z = fmaf(w, x.z, acc.z); acc.w = fmaf(w, x.w, acc.w);
+    }
+    part[tid] = acc;
+    __syncthreads();
+    if (tid < V4) {
+      float y[4] = {0.f, 0.f, 0.f, 0.f};   // (a sequence without rows: zeros)
+      for (int k = 0; k < GROUPS; ++k) {
+        const float4 x = part[k * V4 + tid];
+        y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+      }
+      Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)b * a.Hq + kvh * g + r) * D + tid * 4, y);
+    }
+    if (r == 0 && tid == 0 && a.pos != nullptr && len > 0)
+      a.pos[unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq + len - 1] = a.new_pos[b];
+    return;
+  }
+  // ---- weights
+  const int j = key0 + tid * 4;
+  if (j >= len) return;
+  const float* s = a.scores + unit * g * a.score_ld + j;
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int r = 0; r < g; ++r) {
+    const float4 x = *reinterpret_cast<const float4*>(s + (int64_t)r * a.score_ld);   // (columns past the list are not used)
+    const float d = lse_all[r];
+    w[0] += exp2f(x.x - d); w[1] += exp2f(x.y - d); w[2] += exp2f(x.z - d); w[3] += exp2f(x.w - d);
+  }
+  const int64_t at = unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq + j;
+  const int fresh = a.k_new != nullptr ? len - 1 : -1;   // the appended row starts from zero
+  if (j + 4 <= len && (fresh < j || fresh >= j + 4)) {
+    float4 x = a.weight ? *reinterpret_cast<const float4*>(a.weight + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    x.x += w[0]; x.y += w[1]; x.z += w[2]; x.w += w[3];
+    *reinterpret_cast<float4*>(a.weight_out + at) = x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (j + i < len) a.weight_out[at + i] = (a.weight && j + i != fresh ? a.weight[at + i] : 0.f) + w[i];
+  }
+}
+
+template <int D, bool WEIGH>
+cudaError_t launch_main(const PagedDecodeArgs& a, cudaStream_t st) {
+  const dim3 grid(a.Hkv, a.n_splits * ((a.g + 15) / 16), a.n_seq);
+  cudaError_t e;
+  if (a.dtype == EARN_BF16) {
+    constexpr int smem = STAGES * Geo<D>::STAGE_B;
+    e = ensure_dynamic_smem<paged_decode_kernel<D, WEIGH>>(smem);
+    if (e == cudaSuccess) e = launch_pdl(paged_decode_kernel<D, WEIGH>, grid, dim3(32), smem, st, a);
+  } else {
+    constexpr int smem = (int)sizeof(F32Smem<D>);
+    e = ensure_dynamic_smem<paged_decode_f32_kernel<D, WEIGH>>(smem);
+    if (e == cudaSuccess) e = launch_pdl(paged_decode_f32_kernel<D, WEIGH>, grid, dim3(128), smem, st, a);
+  }
+  note_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_d(const PagedDecodeArgs& a, cudaStream_t st) {
+  cudaError_t e = a.weight_out ? launch_main<D, true>(a, st) : launch_main<D, false>(a, st);
+  if (e != cudaSuccess) return e;
+  const dim3 grid(a.g + (a.weight_out ? (a.cache.max_len + JOIN_KEYS - 1) / JOIN_KEYS : 0), a.Hkv, a.n_seq);
+  e = a.dtype == EARN_BF16 ? launch_pdl(paged_join_kernel<bf16, D>, grid, dim3(JOIN_THREADS), 0, st, a)
+                           : launch_pdl(paged_join_kernel<float, D>, grid, dim3(JOIN_THREADS), 0, st, a);
+  note_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+void plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int* chunk, int* n_splits) {
+  // about three chunks per warp slot (six one-warp CTAs an SM), so that uneven lists even out; a chunk of at least 32 rows
+  const int64_t units = (int64_t)n_seq * n_kv_heads * ((g + 15) / 16), slots = 18LL * sm_count();
+  int64_t c = (units * max_len + slots - 1) / slots;
+  c = (c + 31) / 32 * 32;
+  if (c < 32) c = 32;
+  if (c > kPagedMaxChunk) c = kPagedMaxChunk;
+  *chunk = (int)c;
+  *n_splits = (int)((max_len + c - 1) / c);
+}
+
+cudaError_t launch_paged_decode(const PagedDecodeArgs& a, cudaStream_t st) {
+  return a.D == 64 ? launch_d<64>(a, st) : launch_d<128>(a, st);
+}
+
+}  // namespace earn
