@@ -637,7 +637,12 @@ earn_status_t earn_key_weights(const earn_model_t* model, const earn_batch_t* ba
   a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
   a.scale = scale_of(model);
   note_call(stream, CALL_UNKNOWN);
-  return launch_key_weights_simt(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+  const int entries = prefill_plan_entries(*batch, key_weights_tc_rows());
+  const cudaError_t e = key_weights_tc_supported(a, entries)
+                            ? launch_key_weights_tc(a, entries, reinterpret_cast<char*>(workspace) + kStatusBytes,
+                                                    reinterpret_cast<int32_t*>(workspace), (cudaStream_t)stream)
+                            : launch_key_weights_simt(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }
 
 earn_status_t earn_evict_prompt_kv(const earn_model_t* model, const earn_batch_t* batch, int32_t layer,

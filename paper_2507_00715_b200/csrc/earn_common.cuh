@@ -265,6 +265,10 @@ struct KeyWeightArgs {
   float scale;
 };
 cudaError_t launch_key_weights_simt(const KeyWeightArgs& a, cudaStream_t st);
+// tensor-core path (bf16, groups of at most 128 heads): one plan entry per key_weights_tc_rows() keys of a sequence
+int key_weights_tc_rows();
+bool key_weights_tc_supported(const KeyWeightArgs& a, int64_t plan_entries);
+cudaError_t launch_key_weights_tc(const KeyWeightArgs& a, int plan_entries, void* plan, int32_t* status_word, cudaStream_t st);
 
 struct EvictArgs {
   PagedSource cache;

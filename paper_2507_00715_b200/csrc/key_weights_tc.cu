@@ -1,0 +1,398 @@
+// Accumulated attention weight of the prompt's rows (earn_key_weights) on the Blackwell tensor cores: bf16 Q and K,
+// head_dim 64 or 128, fp32 logits, exponentials and sums.
+//
+//   weight[h, j] = sum over the window's queries i >= j and the heads a of h's group of exp(q_ia . k_jh * scale - lse_ai)
+//
+// The logits are computed transposed, S^T = K Q^T, keys along the 128 rows of the accumulator: a softmax thread then owns
+// one key and sums along its own TMEM lane, with no exchange between threads until one 4-byte store per key.  The columns
+// are (token, head of the group) pairs -- g heads of a token are contiguous in Q, so one TMA box of T = 128 / g tokens is a
+// tile of T g columns, and a window of a few queries fills one tile for the whole group.
+//
+// Work item = 256 keys of one (sequence, kv head) (two accumulators that share every Q tile), over all Q tiles of the window
+// that see them.  A planning kernel lists the blocks, most queries first; the main kernel is persistent, one CTA per SM.
+//   warp 0      TMA: the two K tiles of the next item (double-buffered), a ring of Q tiles
+//   warp 2      the softmax denominators of a Q tile's columns, negated and scaled into the log2 domain -> shared memory
+//   warp 1      one thread issues tcgen05.mma into two TMEM buffers per accumulator
+//   warps 4..   one warpgroup per accumulator: 2^(S * scale - lse) summed per key
+// Bound by the special-function unit and the tensor core (a tile of 128 x 128 logits costs 1024 clocks of exponentials at
+// 16 per clock against 512 of MMA at D = 128) when the window is long, by HBM (K read once) when it is short.
+//
+// Every mbarrier wait is bounded; when one runs out the CTA raises its abort flag, writes EARN_ERR_TIMEOUT to the status
+// word, drains what it has in flight, frees its TMEM and returns.
+#include <algorithm>
+#include <type_traits>
+
+#include "earn_common.cuh"
+#include "sm100_ptx.cuh"
+#include "tc_maps.cuh"
+
+namespace earn {
+namespace {
+using namespace ptx;
+
+constexpr int BM = 128, BC = 128, NT = 2;          // keys per accumulator, columns per Q tile, accumulators per item
+constexpr long long WAIT_LIMIT = 2000000000LL;     // about one second of SM clocks
+
+template <int HD>
+struct Cfg {
+  static constexpr int HALF = BM * 128;              // one 64-column block of a tile (128 rows x 128 B)
+  static constexpr int TILE = HALF * (HD / 64);
+  static constexpr int NSTAGE = 3;                   // Q ring
+  static constexpr int OFF_K = 0;                    // [2][NT] tiles
+  static constexpr int OFF_Q = OFF_K + 2 * NT * TILE;
+  static constexpr int OFF_LSE = OFF_Q + NSTAGE * TILE;
+  static constexpr int OFF_BAR = OFF_LSE + NSTAGE * BC * 4;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;   // + alignment slack
+  static constexpr int TMEM_COLS = NT * 2 * BC;
+  static constexpr int THREADS = 32 * (4 + 4 * NT);
+  static constexpr int BAR_KFULL = 0, BAR_KFREE = 2, BAR_QFULL = 4, BAR_QFREE = BAR_QFULL + NSTAGE, BAR_LFULL = BAR_QFREE + NSTAGE,
+                       BAR_LFREE = BAR_LFULL + NSTAGE, BAR_SFULL = BAR_LFREE + NSTAGE, BAR_SFREE = BAR_SFULL + 2 * NT,
+                       BAR_DRAIN = BAR_SFREE + 2 * NT, N_BARS = BAR_DRAIN + 1;
+  static_assert(8 * N_BARS + 16 <= 256 && SMEM_BYTES <= 232448, "shared memory");
+};
+
+struct KwParams {
+  const float* lse;
+  float* weight;
+  const int4* plan;          // {first global row of the block, rows of the sequence from there, block, sequence}
+  const int32_t* cu_seqlens;
+  int32_t* status;
+  int Hq, Hkv, g, T, n_obs, total, n_items;
+  float scale_log2;
+};
+
+struct Item {
+  int lo, len, kvh;   // the sequence's first row and length
+  int key0;           // first key of the block (position in the sequence)
+  int first;          // first query of the window that sees any of these keys
+  int n_qt;           // Q tiles
+};
+
+// The planner orders blocks by their number, highest first (for queries that is the longest key range).  Here block t has
+// the more queries the lower it is, so the order is read backwards within the sequence.
+__device__ __forceinline__ Item load_item(const KwParams& p, int i) {
+  const int e = i / p.Hkv;
+  const int4 t = __ldg(p.plan + e);
+  Item it;
+  it.kvh = i - e * p.Hkv;
+  it.lo = __ldg(p.cu_seqlens + t.w);
+  it.len = t.z * (NT * BM) + t.y;
+  it.key0 = ((it.len + NT * BM - 1) / (NT * BM) - 1 - t.z) * (NT * BM);
+  it.first = max(max(it.len - p.n_obs, 0), it.key0);
+  it.n_qt = (it.len - it.first + p.T - 1) / p.T;
+  return it;
+}
+// Does accumulator x take part in Q tile i: does the tile's last query see the accumulator's first key?
+__device__ __forceinline__ bool active(const KwParams& p, const Item& it, int x, int i) {
+  return min(it.first + (i + 1) * p.T, it.len) - 1 >= it.key0 + x * BM;
+}
+
+// (d0, d1) = (a0, a1) * b + (c0, c1), (d0, d1) += (a0, a1): packed fp32 pairs
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c0, float c1) {
+  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %4};\n\tmov.b64 rc, {%5, %6};\n\t"
+      "fma.rn.ftz.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
+  asm("{\n\t.reg .b64 ra, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rd, {%0, %1};\n\tadd.rn.ftz.f32x2 rd, rd, ra;\n\t"
+      "mov.b64 {%0, %1}, rd;\n\t}"
+      : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1));
+}
+
+template <int HD>
+__global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
+key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, KwParams p) {
+  using C = Cfg<HD>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;    // swizzled tiles need 1024-byte alignment
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sK = base + C::OFF_K, sQ = base + C::OFF_Q, bars = base + C::OFF_BAR;
+  auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_BAR + 8 * C::N_BARS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 8);
+  float* s_lse = reinterpret_cast<float*>(gen + C::OFF_LSE);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tile_rows = p.T * p.g;                        // columns a TMA box fills
+  const uint32_t q_bytes = (uint32_t)tile_rows * HD * 2;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(C::BAR_KFULL + s), 1);
+      mbar_init(bar(C::BAR_KFREE + s), 1);
+    }
+    for (int s = 0; s < C::NSTAGE; ++s) {
+      mbar_init(bar(C::BAR_QFULL + s), 1);
+      mbar_init(bar(C::BAR_QFREE + s), 1);
+      mbar_init(bar(C::BAR_LFULL + s), 32);
+      mbar_init(bar(C::BAR_LFREE + s), 4 * NT);
+    }
+    for (int s = 0; s < 2 * NT; ++s) {
+      mbar_init(bar(C::BAR_SFULL + s), 1);
+      mbar_init(bar(C::BAR_SFREE + s), 4);
+    }
+    mbar_init(bar(C::BAR_DRAIN), 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
+  }
+  // The rows of a Q tile that no box fills (128 is not a multiple of g) stay zero: a logit of 0 against a denominator of
+  // +inf, where leftover bits could be a NaN.
+  for (int i = threadIdx.x; i < C::NSTAGE * (HD / 64) * (BC - tile_rows) * 8; i += C::THREADS) {
+    const int piece = i & 7, r = tile_rows + (i >> 3) % (BC - tile_rows), blk = (i >> 3) / (BC - tile_rows);
+    st_shared_v4(sQ + blk * C::HALF + (uint32_t)r * 128 + piece * 16, 0u, 0u, 0u, 0u);
+  }
+  fence_async_smem();
+  if (warp == 1) {
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int n_cta = gridDim.x;
+  // passes of gridDim.x items, forwards and backwards in turn: the list is sorted, most work first
+  auto item_at = [&](int k) { return k * n_cta + ((k & 1) ? n_cta - 1 - (int)blockIdx.x : (int)blockIdx.x); };
+  pdl_launch_dependents();
+  pdl_wait();   // the plan (written by the kernel launched just before this one) and every tensor are read below
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int e = 0, n = 0;   // Q tiles and items issued so far
+      bool ok = true;
+      for (int i = item_at(0); i < p.n_items && ok; i = item_at(n)) {
+        const Item it = load_item(p, i);
+        const int kb = n & 1;
+        if (n >= 2 && !mbar_wait_bounded(bar(C::BAR_KFREE + kb), ((n >> 1) - 1) & 1, abort_flag, WAIT_LIMIT)) { ok = false; break; }
+        const int tiles = it.key0 + BM < it.len ? NT : 1;   // the second accumulator may lie past the sequence
+        mbar_expect_tx(bar(C::BAR_KFULL + kb), tiles * C::TILE);
+        for (int x = 0; x < tiles; ++x)
+          for (int h = 0; h < HD / 64; ++h)
+            tma_load_3d(sK + (kb * NT + x) * C::TILE + h * C::HALF, &map_k, bar(C::BAR_KFULL + kb), h * 64, it.kvh, it.lo + it.key0 + x * BM);
+        ++n;
+        for (int t = 0; t < it.n_qt; ++t, ++e) {
+          const int st = e % C::NSTAGE;
+          if (e >= C::NSTAGE && !mbar_wait_bounded(bar(C::BAR_QFREE + st), ((e / C::NSTAGE) - 1) & 1, abort_flag, WAIT_LIMIT)) { ok = false; break; }
+          mbar_expect_tx(bar(C::BAR_QFULL + st), q_bytes);
+          for (int h = 0; h < HD / 64; ++h)
+            tma_load_3d(sQ + st * C::TILE + h * C::HALF, &map_q, bar(C::BAR_QFULL + st), h * 64, it.kvh * p.g, it.lo + it.first + t * p.T);
+        }
+      }
+      if (*abort_flag) {
+        // let the copies already in flight land before the CTA gives its shared memory back
+        int none = 0;
+        for (int f = max(e - C::NSTAGE, 0); f < e; ++f) mbar_wait_bounded(bar(C::BAR_QFULL + f % C::NSTAGE), (f / C::NSTAGE) & 1, &none, WAIT_LIMIT);
+        for (int f = max(n - 2, 0); f < n; ++f) mbar_wait_bounded(bar(C::BAR_KFULL + (f & 1)), (f >> 1) & 1, &none, WAIT_LIMIT);
+      }
+    }
+  } else if (warp == 2) {
+    // ------------------------------------------------------------------ denominators of the columns
+    int tok[4];
+    int64_t at[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int col = lane + 32 * c;
+      tok[c] = col < tile_rows ? col / p.g : INT32_MAX / 2;
+      at[c] = (int64_t)(col % p.g) * p.total + (col < tile_rows ? col / p.g : 0);
+    }
+    int e = 0;
+    bool ok = true;
+    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
+      const Item it = load_item(p, i);
+      const float* src = p.lse + (int64_t)it.kvh * p.g * p.total + it.lo;
+      auto fetch = [&](float (&v)[4], int t) {
+        const int tok0 = it.first + t * p.T;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = tok0 + tok[c] < it.len ? __ldg(src + at[c] + tok0) * -kLog2e : -INFINITY;
+      };
+      float cur[4], nxt[4];
+      fetch(cur, 0);
+      for (int t = 0; t < it.n_qt; ++t, ++e) {
+        if (t + 1 < it.n_qt) fetch(nxt, t + 1);   // (in flight while this tile's slot comes free)
+        const int st = e % C::NSTAGE;
+        if (e >= C::NSTAGE &&
+            !__all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_LFREE + st), ((e / C::NSTAGE) - 1) & 1, abort_flag, WAIT_LIMIT))) {
+          ok = false;
+          break;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s_lse[st * BC + lane + 32 * c] = cur[c];
+        mbar_arrive(bar(C::BAR_LFULL + st));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) cur[c] = nxt[c];
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    const bool leader = lane == 0;
+    const uint32_t idesc = idesc_bf16_f32(BM, (tile_rows + 31) / 32 * 32, 0, 0);   // K (K-major) x Q^T (K-major); whole 32-column chunks
+    constexpr uint32_t desc_hi = smem_desc_hi_sw128(1024);
+    const uint32_t k_lo = smem_desc_lo(sK, 16), q_lo = smem_desc_lo(sQ, 16);
+    auto wait = [&](int b, int parity) {   // warp-uniform result
+      return __all_sync(0xffffffffu, mbar_wait_bounded(bar(b), (uint32_t)parity & 1u, abort_flag, WAIT_LIMIT));
+    };
+    int e = 0, ns[NT] = {0, 0};
+    bool ok = true;
+    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
+      const Item it = load_item(p, i);
+      const int kb = n & 1;
+      ok = wait(C::BAR_KFULL + kb, n >> 1);
+      for (int t = 0; t < it.n_qt && ok; ++t, ++e) {
+        const int st = e % C::NSTAGE;
+        ok = wait(C::BAR_QFULL + st, e / C::NSTAGE);
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+          if (!ok || !active(p, it, x, t)) continue;
+          const int buf = ns[x] & 1;
+          if (ns[x] >= 2) ok = wait(C::BAR_SFREE + x * 2 + buf, (ns[x] >> 1) - 1);
+          if (!ok) continue;
+          ++ns[x];
+          tc_fence_after();
+          const uint32_t a0 = k_lo + (kb * NT + x) * (C::TILE >> 4), b0 = q_lo + st * (C::TILE >> 4);
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) {
+              const uint32_t off = ((kk >> 2) * C::HALF + (kk & 3) * 32) >> 4;
+              umma_ss_lohi(tmem + (x * 2 + buf) * BC, a0 + off, desc_hi, b0 + off, desc_hi, idesc, kk > 0);
+            }
+            umma_commit(bar(C::BAR_SFULL + x * 2 + buf));
+          }
+        }
+        if (leader && ok) umma_commit(bar(C::BAR_QFREE + st));
+      }
+      if (leader && ok) umma_commit(bar(C::BAR_KFREE + kb));
+    }
+    if (leader && *abort_flag) {
+      int none = 0;
+      umma_commit(bar(C::BAR_DRAIN));   // everything this thread issued has retired once this fires
+      mbar_wait_bounded(bar(C::BAR_DRAIN), 0, &none, WAIT_LIMIT);
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------------ one key per thread
+    const int x = (warp - 4) >> 2;
+    const int wq = warp & 3;            // a warp may only touch TMEM lanes 32*(warp % 4) ..
+    const uint32_t t_s = tmem + ((uint32_t)(wq * 32) << 16) + x * 2 * BC;
+    const float sl2 = p.scale_log2;
+    int e = 0, ns = 0;
+    bool ok = true;
+    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
+      const Item it = load_item(p, i);
+      const int key = it.key0 + x * BM + wq * 32 + lane, key_hi = it.key0 + x * BM + wq * 32 + 31;   // this thread's, the warp's last
+      float acc0 = 0.f, acc1 = 0.f;
+      for (int t = 0; t < it.n_qt; ++t, ++e) {
+        const int st = e % C::NSTAGE;
+        // (a warp that skips the tile waits for its denominators all the same: it must not arrive twice in one phase)
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_LFULL + st), (e / C::NSTAGE) & 1, abort_flag, WAIT_LIMIT));
+        if (!ok) break;
+        if (!active(p, it, x, t)) {   // warp-uniform
+          if (lane == 0) mbar_arrive(bar(C::BAR_LFREE + st));
+          continue;
+        }
+        const int buf = ns & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_SFULL + x * 2 + buf), (ns >> 1) & 1, abort_flag, WAIT_LIMIT));
+        if (!ok) break;
+        ++ns;
+        tc_fence_after();
+        const uint32_t t_b = t_s + buf * BC;
+        const float4* l4 = reinterpret_cast<const float4*>(s_lse + st * BC);
+        const int tok0 = it.first + t * p.T, toks = min(p.T, it.len - tok0);
+        // columns [c_lo, c_hi) are visible to this key: tokens at or after it, tokens of the sequence
+        const int c_hi = toks * p.g, c_lo = max(key - tok0, 0) * p.g;
+        const bool interior = toks == p.T && tok0 >= key_hi;   // warp-uniform
+        // 32-column chunks with any token of the sequence
+        const int n_chunks = (c_hi + 31) >> 5;
+        uint32_t a[32], b[32];
+        tmem_ld_32x32(t_b, a);
+        tmem_wait_ld(a);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (q < n_chunks) {
+            uint32_t(&cur)[32] = (q & 1) ? b : a;
+            uint32_t(&nxt)[32] = (q & 1) ? a : b;
+            if (q + 1 < 4 && q + 1 < n_chunks) tmem_ld_32x32(t_b + (q + 1) * 32, nxt);
+            if (interior) {
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) {
+                const float4 l = l4[q * 8 + (c >> 2)];
+                float e0, e1, e2, e3;
+                fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, l.x, l.y);
+                fma2(e2, e3, __uint_as_float(cur[c + 2]), __uint_as_float(cur[c + 3]), sl2, l.z, l.w);
+                add2(acc0, acc1, ex2(e0), ex2(e1));
+                add2(acc0, acc1, ex2(e2), ex2(e3));
+              }
+            } else {
+              const uint32_t width = (uint32_t)max(c_hi - c_lo, 0);
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) {
+                const float4 l = l4[q * 8 + (c >> 2)];
+                const float ll[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {   // what is not visible may be anything, a NaN included: selected away
+                  const float v = ex2(fmaf(__uint_as_float(cur[c + k]), sl2, ll[k]));
+                  acc0 += (uint32_t)(q * 32 + c + k - c_lo) < width ? v : 0.f;
+                }
+              }
+            }
+            if (q + 1 < 4 && q + 1 < n_chunks) tmem_wait_ld(nxt);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(C::BAR_SFREE + x * 2 + buf));
+          mbar_arrive(bar(C::BAR_LFREE + st));
+        }
+      }
+      if (ok && key < it.len) p.weight[(int64_t)it.kvh * p.total + it.lo + key] = acc0 + acc1;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, (int32_t)EARN_ERR_TIMEOUT);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, C::TMEM_COLS);
+  }
+}
+
+template <int HD>
+cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int32_t* status, cudaStream_t st) {
+  const int g = a.Hq / a.Hkv, T = BC / g;
+  CUtensorMap mq, mk;
+  if (!tcmap::make_map(&mq, a.q, a.Hq, a.total, T, HD, g) || !tcmap::make_map(&mk, a.k, a.Hkv, a.total, BM, HD)) return cudaErrorInvalidValue;
+  // sequences per group of the plan: about 32 MB of the windows' Q rows, which every block of a sequence re-reads
+  const int64_t window = std::min<int64_t>(a.n_obs, a.total / std::max(a.batch, 1) + 1);
+  const int group_seqs = (int)std::max<int64_t>(1, (32LL << 20) / std::max<int64_t>(window * a.Hq * HD * 2, 1));
+  cudaError_t e = launch_tile_plan(a.cu_seqlens, a.batch, a.max_seqlen, NT * BM, group_seqs, plan, st);
+  if (e != cudaSuccess) return e;
+  KwParams p{};
+  p.lse = a.lse; p.weight = a.weight; p.plan = reinterpret_cast<const int4*>(plan); p.cu_seqlens = a.cu_seqlens; p.status = status;
+  p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = g; p.T = T; p.n_obs = a.n_obs; p.total = a.total;
+  p.n_items = plan_entries * a.Hkv;
+  p.scale_log2 = a.scale * kLog2e;
+  e = ensure_dynamic_smem<key_weights_tc_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mk, p);
+  note_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+int key_weights_tc_rows() { return NT * BM; }
+
+// (a group of at most 128 heads; the planner orders at most 2048 blocks a sequence; item numbers are 32-bit)
+bool key_weights_tc_supported(const KeyWeightArgs& a, int64_t plan_entries) {
+  return a.dtype == EARN_BF16 && a.Hq / a.Hkv <= BC && a.total >= BM && (a.max_seqlen + NT * BM - 1) / (NT * BM) <= 2048 &&
+         plan_entries * a.Hkv < (1LL << 30);
+}
+
+cudaError_t launch_key_weights_tc(const KeyWeightArgs& a, int plan_entries, void* plan, int32_t* status_word, cudaStream_t st) {
+  return a.D == 64 ? launch_hd<64>(a, plan_entries, plan, status_word, st) : launch_hd<128>(a, plan_entries, plan, status_word, st);
+}
+
+}  // namespace earn
