@@ -13,7 +13,7 @@
 //   warp 0      TMA: the two K tiles of the next item (double-buffered), a ring of Q tiles
 //   warp 2      the softmax denominators of a Q tile's columns, negated and scaled into the log2 domain -> shared memory
 //   warp 1      one thread issues tcgen05.mma into two TMEM buffers per accumulator
-//   warps 4..   one warpgroup per accumulator: 2^(S * scale - lse) summed per key
+//   warps 4..   two warpgroups per accumulator, 64 columns each: 2^(S * scale - lse) summed per key
 // Bound by the special-function unit and the tensor core (a tile of 128 x 128 logits costs 1024 clocks of exponentials at
 // 16 per clock against 512 of MMA at D = 128) when the window is long, by HBM (K read once) when it is short.
 //
@@ -41,13 +41,14 @@ struct Cfg {
   static constexpr int OFF_K = 0;                    // [2][NT] tiles
   static constexpr int OFF_Q = OFF_K + 2 * NT * TILE;
   static constexpr int OFF_LSE = OFF_Q + NSTAGE * TILE;
-  static constexpr int OFF_BAR = OFF_LSE + NSTAGE * BC * 4;
-  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;   // + alignment slack
+  static constexpr int OFF_SUM = OFF_LSE + NSTAGE * BC * 4;   // [NT][128] halves of the keys' sums
+  static constexpr int OFF_BAR = OFF_SUM + NT * BM * 4;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256;
   static constexpr int TMEM_COLS = NT * 2 * BC;
-  static constexpr int THREADS = 32 * (4 + 4 * NT);
+  static constexpr int THREADS = 32 * (4 + 8 * NT);
   static constexpr int BAR_KFULL = 0, BAR_KFREE = 2, BAR_QFULL = 4, BAR_QFREE = BAR_QFULL + NSTAGE, BAR_LFULL = BAR_QFREE + NSTAGE,
                        BAR_LFREE = BAR_LFULL + NSTAGE, BAR_SFULL = BAR_LFREE + NSTAGE, BAR_SFREE = BAR_SFULL + 2 * NT,
-                       BAR_DRAIN = BAR_SFREE + 2 * NT, N_BARS = BAR_DRAIN + 1;
+                       BAR_SUM = BAR_SFREE + 2 * NT, BAR_SUMFREE = BAR_SUM + NT, BAR_DRAIN = BAR_SUMFREE + NT, N_BARS = BAR_DRAIN + 1;
   static_assert(8 * N_BARS + 16 <= 256 && SMEM_BYTES <= 232448, "shared memory");
 };
 
@@ -103,9 +104,9 @@ template <int HD>
 __global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
 key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, KwParams p) {
   using C = Cfg<HD>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;    // swizzled tiles need 1024-byte alignment
-  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t smem_raw[];   // (swizzled tiles need 1024-byte alignment)
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* gen = smem_raw;
   const uint32_t sK = base + C::OFF_K, sQ = base + C::OFF_Q, bars = base + C::OFF_BAR;
   auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_BAR + 8 * C::N_BARS);
@@ -124,11 +125,15 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       mbar_init(bar(C::BAR_QFULL + s), 1);
       mbar_init(bar(C::BAR_QFREE + s), 1);
       mbar_init(bar(C::BAR_LFULL + s), 32);
-      mbar_init(bar(C::BAR_LFREE + s), 4 * NT);
+      mbar_init(bar(C::BAR_LFREE + s), 8 * NT);
     }
     for (int s = 0; s < 2 * NT; ++s) {
       mbar_init(bar(C::BAR_SFULL + s), 1);
-      mbar_init(bar(C::BAR_SFREE + s), 4);
+      mbar_init(bar(C::BAR_SFREE + s), 8);
+    }
+    for (int x = 0; x < NT; ++x) {
+      mbar_init(bar(C::BAR_SUM + x), 4);
+      mbar_init(bar(C::BAR_SUMFREE + x), 4);
     }
     mbar_init(bar(C::BAR_DRAIN), 1);
     *abort_flag = 0;
@@ -271,11 +276,15 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
     __syncwarp();
   } else if (warp >= 4) {
-    // ------------------------------------------------------------------ one key per thread
-    const int x = (warp - 4) >> 2;
+    // ------------------------------------------------------------------ one key per thread, half of a tile's columns
+    const int x = (warp - 4) >> 3, half = ((warp - 4) >> 2) & 1;
     const int wq = warp & 3;            // a warp may only touch TMEM lanes 32*(warp % 4) ..
-    const uint32_t t_s = tmem + ((uint32_t)(wq * 32) << 16) + x * 2 * BC;
+    const uint32_t t_s = tmem + ((uint32_t)(wq * 32) << 16) + x * 2 * BC + half * 64;
+    float* s_sum = reinterpret_cast<float*>(gen + C::OFF_SUM) + x * BM + wq * 32 + lane;
     const float sl2 = p.scale_log2;
+    int tok_lo[2], tok_hi[2];   // first and last token of the half's two 32-column chunks
+#pragma unroll
+    for (int q = 0; q < 2; ++q) { tok_lo[q] = (half * 64 + q * 32) / p.g; tok_hi[q] = (half * 64 + q * 32 + 31) / p.g; }
     int e = 0, ns = 0;
     bool ok = true;
     for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
@@ -296,57 +305,82 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         if (!ok) break;
         ++ns;
         tc_fence_after();
-        const uint32_t t_b = t_s + buf * BC;
-        const float4* l4 = reinterpret_cast<const float4*>(s_lse + st * BC);
         const int tok0 = it.first + t * p.T, toks = min(p.T, it.len - tok0);
-        // columns [c_lo, c_hi) are visible to this key: tokens at or after it, tokens of the sequence
-        const int c_hi = toks * p.g, c_lo = max(key - tok0, 0) * p.g;
-        const bool interior = toks == p.T && tok0 >= key_hi;   // warp-uniform
-        // 32-column chunks with any token of the sequence
-        const int n_chunks = (c_hi + 31) >> 5;
-        uint32_t a[32], b[32];
-        tmem_ld_32x32(t_b, a);
-        tmem_wait_ld(a);
+        // columns [c_lo, c_lo + width) of this half are visible to this key: tokens at or after it, tokens of the sequence
+        const int c_lo = max(key - tok0, 0) * p.g - half * 64;
+        const uint32_t width = (uint32_t)max(toks * p.g - half * 64 - c_lo, 0);
+        const float4* l4 = reinterpret_cast<const float4*>(s_lse + st * BC + half * 64);
+        uint32_t a[32];
+        auto load = [&](int q) {
+          tmem_ld_32x32(t_s + buf * BC + q * 32, a);
+          tmem_wait_ld(a);
+        };
+        auto release = [&]() {   // the accumulator is free as soon as it has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::BAR_SFREE + x * 2 + buf));
+        };
+        auto add_all = [&](int q) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (q < n_chunks) {
-            uint32_t(&cur)[32] = (q & 1) ? b : a;
-            uint32_t(&nxt)[32] = (q & 1) ? a : b;
-            if (q + 1 < 4 && q + 1 < n_chunks) tmem_ld_32x32(t_b + (q + 1) * 32, nxt);
-            if (interior) {
+          for (int c = 0; c < 32; c += 4) {
+            const float4 l = l4[q * 8 + (c >> 2)];
+            float e0, e1, e2, e3;
+            fma2(e0, e1, __uint_as_float(a[c]), __uint_as_float(a[c + 1]), sl2, l.x, l.y);
+            fma2(e2, e3, __uint_as_float(a[c + 2]), __uint_as_float(a[c + 3]), sl2, l.z, l.w);
+            add2(acc0, acc1, ex2(e0), ex2(e1));   // (a share of the exponentials as polynomials on the FMA pipe: no faster,
+            add2(acc0, acc1, ex2(e2), ex2(e3));   // 620 us with none, 643 with a quarter, 729 with half at 8 x 4096 tokens)
+          }
+        };
+        // The interior takes straight-line code of its own: with a test per chunk in between, 641 us instead of 620.
+        if (toks == p.T && tok0 >= key_hi) {
+          load(0);
+          add_all(0);
+          load(1);
+          release();
+          add_all(1);
+        } else {
 #pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                const float4 l = l4[q * 8 + (c >> 2)];
-                float e0, e1, e2, e3;
-                fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, l.x, l.y);
-                fma2(e2, e3, __uint_as_float(cur[c + 2]), __uint_as_float(cur[c + 3]), sl2, l.z, l.w);
-                add2(acc0, acc1, ex2(e0), ex2(e1));
-                add2(acc0, acc1, ex2(e2), ex2(e3));
-              }
-            } else {
-              const uint32_t width = (uint32_t)max(c_hi - c_lo, 0);
+          for (int q = 0; q < 2; ++q) {
+            // (warp-uniform) a chunk none of whose tokens any of the warp's keys sees, or all of them, or some
+            if (tok_lo[q] >= toks || tok0 + tok_hi[q] < key_hi - 31) continue;
+            load(q);
+            if (tok0 + tok_lo[q] >= key_hi && (toks == p.T || tok_hi[q] < toks)) {
+              add_all(q);
+              continue;
+            }
+            // what is not visible may be anything, a NaN included: it is selected away
 #pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                const float4 l = l4[q * 8 + (c >> 2)];
-                const float ll[4] = {l.x, l.y, l.z, l.w};
+            for (int c = 0; c < 32; c += 4) {
+              const float4 l = l4[q * 8 + (c >> 2)];
+              const float ll[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {   // what is not visible may be anything, a NaN included: selected away
-                  const float v = ex2(fmaf(__uint_as_float(cur[c + k]), sl2, ll[k]));
-                  acc0 += (uint32_t)(q * 32 + c + k - c_lo) < width ? v : 0.f;
-                }
+              for (int k = 0; k < 4; ++k) {
+                const float v = ex2(fmaf(__uint_as_float(a[c + k]), sl2, ll[k]));
+                acc0 += (uint32_t)(q * 32 + c + k - c_lo) < width ? v : 0.f;
               }
             }
-            if (q + 1 < 4 && q + 1 < n_chunks) tmem_wait_ld(nxt);
           }
+          release();
         }
-        tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar(C::BAR_SFREE + x * 2 + buf));
-          mbar_arrive(bar(C::BAR_LFREE + st));
-        }
+        if (lane == 0) mbar_arrive(bar(C::BAR_LFREE + st));
       }
-      if (ok && key < it.len) p.weight[(int64_t)it.kvh * p.total + it.lo + key] = acc0 + acc1;
+      if (!ok) break;
+      // ---- the two halves of a key's sum meet in shared memory
+      if (half == 1) {
+        if (n > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_SUMFREE + x), (n - 1) & 1, abort_flag, WAIT_LIMIT));
+        if (!ok) break;
+        *s_sum = acc0 + acc1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::BAR_SUM + x));
+      } else {
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_SUM + x), n & 1, abort_flag, WAIT_LIMIT));
+        if (!ok) break;
+        const float other = *s_sum;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::BAR_SUMFREE + x));
+        if (key < it.len) p.weight[(int64_t)it.kvh * p.total + it.lo + key] = (acc0 + acc1) + other;
+      }
     }
   }
 
@@ -364,10 +398,10 @@ cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int3
   const int g = a.Hq / a.Hkv, T = BC / g;
   CUtensorMap mq, mk;
   if (!tcmap::make_map(&mq, a.q, a.Hq, a.total, T, HD, g) || !tcmap::make_map(&mk, a.k, a.Hkv, a.total, BM, HD)) return cudaErrorInvalidValue;
-  // sequences per group of the plan: about 32 MB of the windows' Q rows, which every block of a sequence re-reads
-  const int64_t window = std::min<int64_t>(a.n_obs, a.total / std::max(a.batch, 1) + 1);
-  const int group_seqs = (int)std::max<int64_t>(1, (32LL << 20) / std::max<int64_t>(window * a.Hq * HD * 2, 1));
-  cudaError_t e = launch_tile_plan(a.cu_seqlens, a.batch, a.max_seqlen, NT * BM, group_seqs, plan, st);
+  // The whole batch is one group of the plan: sorted by work over all sequences and dealt back and forth the CTAs' loads
+  // come out within 2 % of the mean (8 x 4096 tokens, 8 kv heads), where groups of a few sequences left them 15 to 40 %
+  // apart.  The blocks of a (sequence, head) that run side by side still read its Q tiles through L2 together.
+  cudaError_t e = launch_tile_plan(a.cu_seqlens, a.batch, a.max_seqlen, NT * BM, 0, plan, st);
   if (e != cudaSuccess) return e;
   KwParams p{};
   p.lse = a.lse; p.weight = a.weight; p.plan = reinterpret_cast<const int4*>(plan); p.cu_seqlens = a.cu_seqlens; p.status = status;
