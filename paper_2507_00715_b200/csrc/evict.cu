@@ -228,7 +228,189 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a, bool move
     for (int i = warp; i < n_moves; i += NT / 32) move_row(a, b, kvh, from[i], to[i], lane, 32);
 }
 
-// The step form's moves, MOVES_PER_CTA of one (sequence, kv head) per CTA; a warp's lanes are dealt to rows of row_bytes / 16
+// ---- lists of at most NT * IPT rows: every key in a register (row j0 + 32 i + lane of a warp's stretch), read once.
+// Four digits of 8 bits: the CTA counts a digit's 256 bins in shared memory (a histogram of its own per digit, so a digit
+// costs one barrier) and every warp finds the bin by itself.  Ranks over the warps come from one count per warp and one
+// barrier as well.  (Eleven-bit digits and full scans: 20 us for 512 lists of 1025 rows; a search bit by bit: 17 us.)
+constexpr int MOVES_HERE = 64;   // moves the selecting CTA makes itself
+
+template <int NT>
+struct RegShared {
+  int hist[4][256];
+  int2 ranks[2][NT / 32];
+  int last[NT / 32];
+  int from[MOVES_HERE], to[MOVES_HERE];
+};
+
+// sum over the warps in front of this one (x, y) and over all of them, of one pair per warp
+template <int NW>
+__device__ __forceinline__ int2 rank_base(int2 mine, int2* slots, int2& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) slots[warp] = mine;
+  __syncthreads();
+  const int2 v = lane < NW ? slots[lane] : make_int2(0, 0);
+  total = make_int2(__reduce_add_sync(0xffffffffu, v.x), __reduce_add_sync(0xffffffffu, v.y));
+  const bool before = lane < warp;
+  return make_int2(__reduce_add_sync(0xffffffffu, before ? v.x : 0), __reduce_add_sync(0xffffffffu, before ? v.y : 0));
+}
+
+template <int NT, int IPT, bool PROMPT>
+__global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool move_here) {
+  constexpr int NW = NT / 32;
+  __shared__ RegShared<NT> sh;
+  pdl_wait();   // everything below reads or writes global memory
+  pdl_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int unit = blockIdx.x, b = unit / a.Hkv, kvh = unit - b * a.Hkv;
+  const int64_t cap = (int64_t)EARN_PAGE_TOKENS * a.cache.pages_per_seq;
+  const int lo = PROMPT ? a.cu_seqlens[b] : 0;
+  const int n = PROMPT ? min(a.cu_seqlens[b + 1] - lo, a.max_rows) : paged_len(a.cache, b);
+  const float* weight = PROMPT ? a.weight + (int64_t)kvh * a.total + lo : a.weight + unit * cap;
+  const int32_t* pos = PROMPT ? nullptr : a.pos + unit * cap;
+  float* w_out = a.weight_out ? a.weight_out + unit * cap : nullptr;
+  int32_t* p_out = a.pos_out + unit * cap;
+  const bool copy_w = w_out != nullptr && w_out != weight, copy_p = p_out != pos;
+  const int budget = a.budget;
+  const int ipt = (n + NT - 1) / NT, j0 = warp * ipt * 32 + lane;   // this lane's rows: j0 + 32 i, i < ipt
+  if (n <= budget) {   // nothing goes
+    for (int j = tid; j < n; j += NT) {
+      if (copy_w) w_out[j] = weight[j];
+      if (copy_p) p_out[j] = PROMPT ? j : pos[j];
+    }
+    if (!PROMPT && tid == 0) a.n_moves[unit] = 0;
+    return;
+  }
+  for (int i = tid; i < 4 * 256; i += NT) sh.hist[0][i] = 0;
+  // ---- keys
+  uint32_t u[IPT];
+  int last = n - 1;
+  {
+    float w[IPT];
+    int p[IPT];
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+      const int j = j0 + 32 * i;
+      const bool in = i < ipt && j < n;
+      w[i] = in ? weight[j] : 0.f;
+      p[i] = PROMPT ? j : in ? pos[j] : INT_MIN;
+    }
+    if (!PROMPT) {   // the newest token's position
+      int m = INT_MIN;
+#pragma unroll
+      for (int i = 0; i < IPT; ++i) m = max(m, p[i]);
+      m = __reduce_max_sync(0xffffffffu, m);
+      if (lane == 0) sh.last[warp] = m;
+    }
+    __syncthreads();   // (the histograms are cleared, too)
+    if (!PROMPT) last = __reduce_max_sync(0xffffffffu, sh.last[lane % NW]);
+    const int64_t after = (int64_t)last - a.n_last;
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+      const bool in = i < ipt && j0 + 32 * i < n;
+      u[i] = !in ? 0u : (p[i] < a.n_first || p[i] > after) ? KEY_PROTECTED : weight_key(w[i]);
+    }
+  }
+  // ---- the budget-th largest key T, digit by digit from the top: `want` of the keys that agree with T so far stay.  (No
+  // row's key is 0, so the key 0 of a lane without a row is never counted.)
+  uint32_t T = 0;
+  int want = budget, equal = 0;
+#pragma unroll
+  for (int d = 3; d >= 0; --d) {
+    int* hist = sh.hist[d];
+#pragma unroll
+    for (int i = 0; i < IPT; ++i)
+      if (u[i] != 0u && (d == 3 || (u[i] >> (8 * d + 8)) == (T >> (8 * d + 8)))) atomicAdd(&hist[(u[i] >> (8 * d)) & 255u], 1);
+    __syncthreads();
+    // lane l owns bins 255 - 8 l .. 248 - 8 l; the bins of the lanes below it hold larger digits
+    const int4 h0 = reinterpret_cast<const int4*>(hist)[63 - 2 * lane], h1 = reinterpret_cast<const int4*>(hist)[62 - 2 * lane];
+    const int c[8] = {h0.w, h0.z, h0.y, h0.x, h1.w, h1.z, h1.y, h1.x};   // from the largest digit down
+    int sum = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += c[k];
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    const int owner = __ffs(__ballot_sync(0xffffffffu, incl >= want)) - 1;
+    int above = incl - sum, digit = 0, rest = 0, cnt = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (above < want && want <= above + c[k]) { digit = 255 - 8 * lane - k; rest = want - above; cnt = c[k]; }
+      above += c[k];
+    }
+    T |= (uint32_t)__shfl_sync(0xffffffffu, digit, owner) << (8 * d);
+    want = __shfl_sync(0xffffffffu, rest, owner);
+    equal = __shfl_sync(0xffffffffu, cnt, owner);
+  }
+  // ---- rows with a larger key stay, and the first `want` of the `equal` rows with key T
+  const uint32_t lt = (1u << lane) - 1u;
+  uint32_t keep = 0;   // bit i: row j0 + 32 i stays
+  int2 total;
+  if (want == equal) {   // block-uniform
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) keep |= u[i] >= T ? 1u << i : 0u;
+  } else {
+    int eq = 0;
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) eq += __popc(__ballot_sync(0xffffffffu, u[i] == T));
+    int seen = rank_base<NW>(make_int2(eq, 0), sh.ranks[0], total).x;
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+      const uint32_t eqs = __ballot_sync(0xffffffffu, u[i] == T);
+      if (u[i] > T || (u[i] == T && seen + __popc(eqs & lt) < want)) keep |= 1u << i;
+      seen += __popc(eqs);
+    }
+  }
+  // ---- ranks (x: kept rows, or free rows below the budget; y: kept rows behind it) and the lists
+  auto is_x = [&](int i) { return PROMPT ? (keep >> i & 1u) != 0u : i < ipt && j0 + 32 * i < budget && !(keep >> i & 1u); };
+  auto is_y = [&](int i) { return !PROMPT && (keep >> i & 1u) && j0 + 32 * i >= budget; };
+  int cx = 0, cy = 0;
+#pragma unroll
+  for (int i = 0; i < IPT; ++i) {
+    cx += __popc(__ballot_sync(0xffffffffu, is_x(i)));
+    if (!PROMPT) cy += __popc(__ballot_sync(0xffffffffu, is_y(i)));
+  }
+  const int2 base = rank_base<NW>(make_int2(cx, cy), sh.ranks[1], total);
+  int rx = base.x, ry = base.y;
+  int32_t* from = PROMPT ? nullptr : move_here ? sh.from : a.moves + (int64_t)unit * 2 * a.list;
+  int32_t* to = PROMPT ? nullptr : move_here ? sh.to : a.moves + (int64_t)unit * 2 * a.list + a.list;
+#pragma unroll
+  for (int i = 0; i < IPT; ++i) {
+    if (i >= ipt) break;
+    const int j = j0 + 32 * i;
+    const uint32_t bx = __ballot_sync(0xffffffffu, is_x(i)), by = PROMPT ? 0u : __ballot_sync(0xffffffffu, is_y(i));
+    if (PROMPT) {
+      if (is_x(i)) {
+        const int slot = rx + __popc(bx & lt);
+        p_out[slot] = j;
+        if (copy_w) w_out[slot] = weight[j];
+      }
+    } else {
+      if (is_x(i)) to[rx + __popc(bx & lt)] = j;
+      if (is_y(i)) from[ry + __popc(by & lt)] = j;
+      if ((keep >> i & 1u) && j < budget) {
+        if (copy_w) w_out[j] = weight[j];
+        if (copy_p) p_out[j] = pos[j];
+      }
+    }
+    rx += __popc(bx);
+    ry += __popc(by);
+  }
+  if (PROMPT) return;
+  const int n_moves = total.y;
+  __syncthreads();   // the lists are written, and nobody reads a row below the budget any more
+  if (tid == NT - 1) a.n_moves[unit] = n_moves;
+  for (int i = NT - 1 - tid; i < n_moves; i += NT) {   // (from the last warp down: the first ones move rows meanwhile)
+    w_out[to[i]] = weight[from[i]];
+    p_out[to[i]] = pos[from[i]];
+  }
+  if (move_here)
+    for (int i = warp; i < n_moves; i += NW) move_row(a, b, kvh, from[i], to[i], lane, 32);
+}
+
+// The step form's moves, ROWS_PER_CTA of one (sequence, kv head) per CTA; 8, 16 or 32 threads a row
 constexpr int ROWS_PER_CTA = 64;
 
 __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
@@ -241,7 +423,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a) {
   const int b = unit / a.Hkv, kvh = unit - b * a.Hkv;
   const int32_t* from = a.moves + (int64_t)unit * 2 * a.list + i0;
   const int32_t* to = from + a.list;
-  const int per_row = a.row_bytes / 16, rows_at_once = 256 / per_row;   // 8, 16 or 32 threads a row
+  const int per_row = a.row_bytes / 16, rows_at_once = 256 / per_row;
   for (int i = threadIdx.x / per_row; i < n; i += rows_at_once) move_row(a, b, kvh, from[i], to[i], threadIdx.x % per_row, per_row);
 }
 
@@ -284,15 +466,25 @@ cudaError_t launch_select(const EvictArgs& a, bool move_here, cudaStream_t st) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
+template <int NT, int IPT, bool PROMPT>
+cudaError_t launch_select_regs(const EvictArgs& a, bool move_here, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(evict_select_regs_kernel<NT, IPT, PROMPT>, dim3((unsigned)a.n_seq * a.Hkv), dim3(NT), 0, st, a, move_here);
+  note_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 template <bool PROMPT>
 cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
-  // the most moves a (sequence, kv head) can need; up to 64 are made by the selecting CTA
+  // the most moves a (sequence, kv head) can need; up to MOVES_HERE are made by the selecting CTA
   const int most = a.max_rows > a.budget ? (a.max_rows - a.budget < a.budget ? a.max_rows - a.budget : a.budget) : 0;
-  const bool move_here = !PROMPT && most <= ROWS_PER_CTA;
+  const bool move_here = !PROMPT && most <= MOVES_HERE;
   cudaError_t e;
   if (a.max_rows > STAGE_ROWS) e = launch_select<1024, PROMPT, false>(a, move_here, st);
-  else if (a.max_rows > 2048) e = launch_select<1024, PROMPT, true>(a, move_here, st);
-  else e = launch_select<256, PROMPT, true>(a, move_here, st);
+  else if (a.max_rows > 1024 * 16) e = launch_select<1024, PROMPT, true>(a, move_here, st);
+  else if (a.max_rows > 512 * 16) e = launch_select_regs<1024, 16, PROMPT>(a, move_here, st);
+  else if (a.max_rows > 256 * 8) e = launch_select_regs<512, 16, PROMPT>(a, move_here, st);
+  else if (a.max_rows > 128 * 4) e = launch_select_regs<256, 8, PROMPT>(a, move_here, st);
+  else e = launch_select_regs<128, 4, PROMPT>(a, move_here, st);
   const int rows = PROMPT ? (a.max_rows < a.budget ? a.max_rows : a.budget) : most;
   if (e != cudaSuccess || move_here || rows == 0) return e;
   const unsigned units = (unsigned)a.n_seq * a.Hkv, gy = units < 32768u ? units : 32768u;
