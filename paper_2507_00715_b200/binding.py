@@ -312,19 +312,24 @@ def earn_train_attn_bwd(model, batch: Batch, layer, n_target, q, k, v, o, lse, d
 _TORCH_DTYPE = {EARN_F32: torch.float32, EARN_BF16: torch.bfloat16}
 
 
-def _tensor(t, what: str, dtype: torch.dtype, numel: int) -> Optional[int]:
-    """Address of a dense CUDA tensor of `dtype` on the current device with at least `numel` elements (None stays None)."""
+def _tensor(t, what: str, dtype: torch.dtype, numel: int, device: int) -> Optional[int]:
+    """Address of a dense tensor of `dtype` on CUDA device `device` with at least `numel` elements (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: not contiguous")
     if t.numel() < numel:
         raise ValueError(f"{what}: {t.numel()} elements, expected at least {numel}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: on {t.device}, expected the current CUDA device")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, expected the current CUDA device ({device})")
     return t.data_ptr()
+
+
+def _stream_of(device: int) -> Optional[int]:
+    """torch's current stream on `device` (the raw handle; building a torch.cuda.Stream costs a few microseconds a call)."""
+    return torch._C._cuda_getCurrentRawStream(device) or None
 
 
 def make_evict(budget: int, n_first: int = 0, n_last: int = 0) -> EarnEvict:
@@ -340,28 +345,32 @@ def make_paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: 
     for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if t.dim() != 4 or t.shape[1] != PAGE_TOKENS or t.shape != k_pages.shape or t.dtype != k_pages.dtype:
             raise ValueError(f"{what}: expected [n_pages, {PAGE_TOKENS}, Hkv, D], the same for k and v")
-        _tensor(t, what, t.dtype, 0)
     if block_table is not None:
         if block_table.dim() != 2:
             raise ValueError("block_table: expected [n_seq, pages_per_seq]")
         pages_per_seq = block_table.shape[1]
     if pages_per_seq is None:
         raise ValueError("pages_per_seq is needed without a block table")
-    cache = EarnPagedCache(_ptr(k_pages), _ptr(v_pages), _tensor(block_table, "block_table", torch.int32, 0), pages_per_seq,
-                           k_pages.shape[0], _tensor(seq_len, "seq_len", torch.int32, 0),
+    dev = torch.cuda.current_device()
+    cache = EarnPagedCache(_tensor(k_pages, "k_pages", k_pages.dtype, 0, dev), _tensor(v_pages, "v_pages", v_pages.dtype, 0, dev),
+                           _tensor(block_table, "block_table", torch.int32, 0, dev), pages_per_seq, k_pages.shape[0],
+                           _tensor(seq_len, "seq_len", torch.int32, 0, dev),
                            PAGE_TOKENS * pages_per_seq if max_len is None else max_len)
-    # what the calls check against the model and the number of sequences
+    # what the calls check against the model, the number of sequences and the current device
     cache.kind = (k_pages.dtype, k_pages.shape[2], k_pages.shape[3])
-    cache.rows = (None if block_table is None else block_table.shape[0], None if seq_len is None else seq_len.numel())
+    cache.n_seq = min([len(t) for t in (block_table, seq_len) if t is not None], default=k_pages.shape[0])
+    cache.device = dev
     return cache
 
 
-def _check_cache(model: EarnModel, n_seq: int, cache: EarnPagedCache) -> int:
+def _check_cache(model: EarnModel, n_seq: int, cache: EarnPagedCache, dt: torch.dtype, hkv: int, d: int, dev: int) -> int:
     """Rows of the per-row arrays (weight, pos) of one sequence and head; raises if the cache is not this model's."""
-    if cache.kind != (_TORCH_DTYPE[model.dtype], model.n_kv_heads, model.head_dim):
-        raise ValueError(f"cache of {cache.kind}, model of {(_TORCH_DTYPE[model.dtype], model.n_kv_heads, model.head_dim)}")
-    if any(r is not None and r < n_seq for r in cache.rows):
+    if cache.kind != (dt, hkv, d):
+        raise ValueError(f"cache of {cache.kind}, model of {(dt, hkv, d)}")
+    if cache.n_seq < n_seq:
         raise ValueError(f"block_table / seq_len hold fewer than {n_seq} sequences")
+    if cache.device != dev:
+        raise ValueError(f"cache on CUDA device {cache.device}, expected the current one ({dev})")
     return PAGE_TOKENS * cache.pages_per_seq
 
 
@@ -371,13 +380,12 @@ def earn_paged_workspace_bytes(model: EarnModel, n_seq: int, cache: EarnPagedCac
 
 def earn_key_weights(model: EarnModel, batch: Batch, layer: int, n_obs: int, q, k, lse, weight, workspace) -> None:
     """q [total, Hq, D], k [total, Hkv, D], lse fp32 [Hq, total] (earn_prefill_attn) -> weight fp32 [Hkv, total]."""
-    n, dt = batch.c.total_tokens, _TORCH_DTYPE[model.dtype]
+    n, dt, dev = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], torch.cuda.current_device()
+    hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
     p, size = _ws(workspace)
-    _check(lib().earn_key_weights(C.byref(model), C.byref(batch.c), layer, n_obs,
-                                  _tensor(q, "q", dt, n * model.n_q_heads * model.head_dim),
-                                  _tensor(k, "k", dt, n * model.n_kv_heads * model.head_dim),
-                                  _tensor(lse, "lse", torch.float32, n * model.n_q_heads),
-                                  _tensor(weight, "weight", torch.float32, n * model.n_kv_heads), p, size, _stream()),
+    _check(lib().earn_key_weights(model, batch.c, layer, n_obs, _tensor(q, "q", dt, n * hq * d, dev),
+                                  _tensor(k, "k", dt, n * hkv * d, dev), _tensor(lse, "lse", torch.float32, n * hq, dev),
+                                  _tensor(weight, "weight", torch.float32, n * hkv, dev), p, size, _stream_of(dev)),
            "earn_key_weights")
 
 
@@ -385,15 +393,15 @@ def earn_evict_prompt_kv(model: EarnModel, batch: Batch, layer: int, policy: Ear
                          weight_out, pos_out, workspace) -> None:
     """k, v [total, Hkv, D], weight fp32 [Hkv, total] -> the pages, weight_out fp32 (or None) and pos_out int32
     [B, Hkv, 16 * pages_per_seq].  Sequence b then holds min(L_b, budget) rows: put that into seq_len."""
-    n, dt, rows = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], batch.batch * model.n_kv_heads
-    cap = _check_cache(model, batch.batch, cache)
+    n, n_seq, dt, dev = batch.c.total_tokens, batch.c.batch, _TORCH_DTYPE[model.dtype], torch.cuda.current_device()
+    hkv, d = model.n_kv_heads, model.head_dim
+    rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
     p, size = _ws(workspace)
-    _check(lib().earn_evict_prompt_kv(C.byref(model), C.byref(batch.c), layer, C.byref(policy),
-                                      _tensor(k, "k", dt, n * model.n_kv_heads * model.head_dim),
-                                      _tensor(v, "v", dt, n * model.n_kv_heads * model.head_dim),
-                                      _tensor(weight, "weight", torch.float32, n * model.n_kv_heads), C.byref(cache),
-                                      _tensor(weight_out, "weight_out", torch.float32, rows * cap),
-                                      _tensor(pos_out, "pos_out", torch.int32, rows * cap), p, size, _stream()),
+    _check(lib().earn_evict_prompt_kv(model, batch.c, layer, policy, _tensor(k, "k", dt, n * hkv * d, dev),
+                                      _tensor(v, "v", dt, n * hkv * d, dev),
+                                      _tensor(weight, "weight", torch.float32, n * hkv, dev), cache,
+                                      _tensor(weight_out, "weight_out", torch.float32, rows, dev),
+                                      _tensor(pos_out, "pos_out", torch.int32, rows, dev), p, size, _stream_of(dev)),
            "earn_evict_prompt_kv")
 
 
@@ -401,26 +409,25 @@ def earn_paged_decode_attn(model: EarnModel, n_seq: int, layer: int, q, k_new, v
                            weight_out=None, new_pos=None, pos=None, workspace=None) -> None:
     """q, o [n_seq, Hq, D], k_new, v_new [n_seq, Hkv, D] (or None), weight, weight_out fp32 and pos int32
     [n_seq, Hkv, 16 * pages_per_seq] (or None), new_pos int32 [n_seq]; weight_out may be weight."""
-    dt, rows = _TORCH_DTYPE[model.dtype], n_seq * model.n_kv_heads
-    cap = _check_cache(model, n_seq, cache)
-    nq, nk = n_seq * model.n_q_heads * model.head_dim, rows * model.head_dim
+    dt, dev, f32, i32 = _TORCH_DTYPE[model.dtype], torch.cuda.current_device(), torch.float32, torch.int32
+    hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
+    rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
+    nq, nk = n_seq * hq * d, n_seq * hkv * d
     p, size = _ws(workspace)
-    _check(lib().earn_paged_decode_attn(C.byref(model), n_seq, layer, _tensor(q, "q", dt, nq), _tensor(k_new, "k_new", dt, nk),
-                                        _tensor(v_new, "v_new", dt, nk), C.byref(cache), _tensor(o, "o", dt, nq),
-                                        _tensor(weight, "weight", torch.float32, rows * cap),
-                                        _tensor(weight_out, "weight_out", torch.float32, rows * cap),
-                                        _tensor(new_pos, "new_pos", torch.int32, n_seq),
-                                        _tensor(pos, "pos", torch.int32, rows * cap), p, size, _stream()),
-           "earn_paged_decode_attn")
+    _check(lib().earn_paged_decode_attn(model, n_seq, layer, _tensor(q, "q", dt, nq, dev), _tensor(k_new, "k_new", dt, nk, dev),
+                                        _tensor(v_new, "v_new", dt, nk, dev), cache, _tensor(o, "o", dt, nq, dev),
+                                        _tensor(weight, "weight", f32, rows, dev), _tensor(weight_out, "weight_out", f32, rows, dev),
+                                        _tensor(new_pos, "new_pos", i32, n_seq, dev), _tensor(pos, "pos", i32, rows, dev),
+                                        p, size, _stream_of(dev)), "earn_paged_decode_attn")
 
 
 def earn_evict_kv(model: EarnModel, n_seq: int, layer: int, policy: EarnEvict, cache: EarnPagedCache, weight, pos, weight_out,
                   pos_out, workspace) -> None:
     """weight fp32 and pos int32 [n_seq, Hkv, 16 * pages_per_seq]; weight_out / pos_out may be the same tensors.  Sequence b
     then holds min(seq_len[b], budget) rows: put that into seq_len."""
-    n = n_seq * model.n_kv_heads * _check_cache(model, n_seq, cache)
+    dt, dev, hkv, d = _TORCH_DTYPE[model.dtype], torch.cuda.current_device(), model.n_kv_heads, model.head_dim
+    n = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
     p, size = _ws(workspace)
-    _check(lib().earn_evict_kv(C.byref(model), n_seq, layer, C.byref(policy), C.byref(cache),
-                               _tensor(weight, "weight", torch.float32, n), _tensor(pos, "pos", torch.int32, n),
-                               _tensor(weight_out, "weight_out", torch.float32, n),
-                               _tensor(pos_out, "pos_out", torch.int32, n), p, size, _stream()), "earn_evict_kv")
+    _check(lib().earn_evict_kv(model, n_seq, layer, policy, cache, _tensor(weight, "weight", torch.float32, n, dev),
+                               _tensor(pos, "pos", torch.int32, n, dev), _tensor(weight_out, "weight_out", torch.float32, n, dev),
+                               _tensor(pos_out, "pos_out", torch.int32, n, dev), p, size, _stream_of(dev)), "earn_evict_kv")

@@ -228,18 +228,19 @@ struct PagedLayout {
   size_t scores, part_o, part_lse;   // byte offsets, decode
   size_t n_moves, moves;             // byte offsets, eviction
   size_t total;
-  int chunk, n_splits, score_ld, list;
+  PagedPlan plan;
+  int score_ld, list;
 };
 static PagedLayout paged_layout(const earn_model_t* m, int32_t n_seq, const earn_paged_cache_t* c) {
   PagedLayout l{};
   const int g = m->n_q_heads / m->n_kv_heads;
   const size_t units = (size_t)n_seq * m->n_kv_heads;
-  plan_paged_decode(n_seq, m->n_kv_heads, g, c->max_len, &l.chunk, &l.n_splits);
-  l.score_ld = (int)round_up((size_t)c->max_len, EARN_PAGE_TOKENS);
+  l.plan = plan_paged_decode(n_seq, m->n_kv_heads, g, c->max_len, m->dtype);
+  l.score_ld = l.plan.cluster > 0 ? 0 : (int)round_up((size_t)c->max_len, EARN_PAGE_TOKENS);
   l.scores = kStatusBytes;
   l.part_o = l.scores + round_up(units * g * (size_t)l.score_ld * 4, 256);
-  l.part_lse = l.part_o + round_up(units * l.n_splits * g * (size_t)m->head_dim * 4, 256);
-  const size_t decode_end = l.part_lse + round_up(units * l.n_splits * g * 4, 256);
+  l.part_lse = l.part_o + round_up(units * l.plan.n_splits * g * (size_t)m->head_dim * 4, 256);
+  const size_t decode_end = l.part_lse + round_up(units * l.plan.n_splits * g * 4, 256);
   l.list = c->max_len / 2 + 1;   // a move takes a row below the budget and one behind it: at most half the rows
   l.n_moves = kStatusBytes;
   l.moves = l.n_moves + round_up(units * 4, 256);
@@ -703,7 +704,7 @@ earn_status_t earn_paged_decode_attn(const earn_model_t* model, int32_t n_seq, i
       !aligned16(weight_or_null) || !aligned16(weight_out_or_null) || !aligned4(new_pos_or_null) || !aligned4(pos_or_null))
     return EARN_ERR_INVALID_ARG;
   const PagedLayout l = paged_layout(model, n_seq, cache);
-  if ((int64_t)l.n_splits * ((g + 15) / 16) > 65535) return EARN_ERR_UNSUPPORTED;
+  if ((int64_t)l.plan.n_splits * ((g + 15) / 16) > 65535) return EARN_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < l.total) return EARN_ERR_WORKSPACE;
   PagedDecodeArgs a{};
   char* ws = reinterpret_cast<char*>(workspace);
@@ -714,7 +715,7 @@ earn_status_t earn_paged_decode_attn(const earn_model_t* model, int32_t n_seq, i
   a.part_o = reinterpret_cast<float*>(ws + l.part_o);
   a.part_lse = reinterpret_cast<float*>(ws + l.part_lse);
   a.n_seq = n_seq; a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
-  a.g = g; a.chunk = l.chunk; a.n_splits = l.n_splits; a.score_ld = l.score_ld;
+  a.g = g; a.cluster = l.plan.cluster; a.chunk = l.plan.chunk; a.n_splits = l.plan.n_splits; a.score_ld = l.score_ld;
   a.scale = scale_of(model);
   note_call(stream, CALL_UNKNOWN);
   return launch_paged_decode(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;

@@ -295,12 +295,16 @@ struct PagedDecodeArgs {
   float* scores;               // [B, Hkv, g, score_ld] scaled log2-domain logits (only with weight_out)
   float* part_o;               // [B, Hkv, n_splits, g, D]
   float* part_lse;             // [B, Hkv, n_splits, g] (log2 domain)
-  int n_seq, Hq, Hkv, D, dtype, g, chunk, n_splits, score_ld;
+  int n_seq, Hq, Hkv, D, dtype, g, cluster, chunk, n_splits, score_ld;
   float scale;
 };
-// how the key lists are cut: n_splits chunks of `chunk` rows each (a multiple of 16, at most kPagedMaxChunk)
+// How the key lists are cut.  cluster > 0: to the CTAs of a cluster, at most `chunk` rows each, in one launch without scratch
+// (n_splits 0).  Otherwise n_splits chunks of `chunk` rows (a multiple of 16) and a second kernel that joins them.
+struct PagedPlan {
+  int cluster, chunk, n_splits;
+};
 constexpr int kPagedMaxChunk = 512;
-void plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int* chunk, int* n_splits);
+PagedPlan plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int dtype);
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, cudaStream_t st);
 
 // ---- element helpers ----

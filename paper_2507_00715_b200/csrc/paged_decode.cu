@@ -7,7 +7,13 @@
 // the partials.  The weight of a row needs the denominator of the whole list, so the first kernel also leaves the scaled
 // logits (4 bytes per query head and row beside the 4 D bytes of K and V: 6 % at a group of 8 and D = 128, written and read
 // while they are in L2), and the second kernel turns them into weights: sum over the heads of 2^(logit - LSE).
+// 32/8 heads of 128, with weights: 166 us over 8 lists of 20000 to 32768 rows (5.5 TB/s, 0.85 of a copy; the first kernel
+// alone 151 us), 51 us over 64 of 700 to 1044 (44 us alone).  The last warp of a (sequence, kv head) joining by itself
+// instead of a second kernel cost 66 us there: one warp is too few for the logits.
+// Small calls: one launch, the chunks of a list in a cluster (below).
 // No atomics: every sum has one order.
+#include <climits>
+
 #include "decode_tile.cuh"
 #include "sm100_ptx.cuh"
 
@@ -17,20 +23,69 @@ using namespace dec;
 
 constexpr int STAGES = 4;
 
+// four rows' weights: out[0..3] = before + w for the rows j + i < n; row `fresh` (the appended one, or outside) starts from zero
+__device__ __forceinline__ void add_weights(float* out, const float4& before, int j, int n, int fresh, const float (&w)[4]) {
+  const float x[4] = {(fresh == j ? 0.f : before.x) + w[0], (fresh == j + 1 ? 0.f : before.y) + w[1],
+                      (fresh == j + 2 ? 0.f : before.z) + w[2], (fresh == j + 3 ? 0.f : before.w) + w[3]};
+  if (j + 4 <= n) {
+    *reinterpret_cast<float4*>(out) = make_float4(x[0], x[1], x[2], x[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (j + i < n) out[i] = x[i];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ thread-block clusters
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// address of the same shared-memory location in CTA `rank` of the cluster, and loads from there
+__device__ __forceinline__ uint32_t peer_smem(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float peer_ld(uint32_t addr) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(addr) : "memory");
+  return x;
+}
+__device__ __forceinline__ float4 peer_ld4(uint32_t addr) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+  return x;
+}
+
 // ------------------------------------------------------------------------------------------------ bf16: one warp per chunk
-template <int D, bool WEIGH>
+// CLUSTER: the list of a (sequence, kv head) is shared out to the one-warp CTAs of a cluster (a.cluster of them, at most 512
+// rows each).  Logits stay in shared memory, the CTAs read each other's maxima, sums and partial rows through distributed
+// shared memory, and each finishes its share of the output and the weights of its rows: one launch, nothing through L2.
+// Behind the ring: logits [g][chunk + 8] (with weights), maxima and sums [2][16], what a CTA's partial counts [8][16], LSE [16].
+constexpr int kMaxCluster = 8;
+template <int D>
+__host__ __device__ constexpr int cluster_smem(int g, int chunk, bool weigh) {
+  return STAGES * Geo<D>::STAGE_B + (weigh ? g * (chunk + 8) * 4 : 0) + (2 + kMaxCluster + 1) * 16 * 4;
+}
+
+template <int D, bool WEIGH, bool CLUSTER>
 __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
   using G = Geo<D>;
   constexpr int CH = G::CH, RPI = G::RPI, NIT = KT / RPI, NTILES = D / 8;
   extern __shared__ __align__(128) uint8_t smem[];
   pdl_wait();
   const int lane = threadIdx.x;
-  const int kvh = blockIdx.x, b = blockIdx.z;
   const int row_tiles = (a.g + 15) / 16;
-  const int split = blockIdx.y / row_tiles, row0 = (blockIdx.y % row_tiles) * 16;
+  const int kvh = CLUSTER ? blockIdx.x / a.cluster : blockIdx.x, b = blockIdx.z;
+  const int split = CLUSTER ? (int)cluster_rank() : (int)blockIdx.y / row_tiles, row0 = CLUSTER ? 0 : (blockIdx.y % row_tiles) * 16;
   const int len = paged_len(a.cache, b);
-  const int begin = split * a.chunk, n = min(len - begin, a.chunk);
-  if (n <= 0) return;
+  const int chunk = CLUSTER ? ((len + KT - 1) / KT + a.cluster - 1) / a.cluster * KT : a.chunk;   // rows of a CTA
+  const int begin = split * chunk, n = min(len - begin, chunk);
+  if (!CLUSTER && n <= 0) return;
   const int n_tiles = (n + KT - 1) / KT;
   const float scale_log2 = a.scale * kLog2e;
   RowMap rm;
@@ -84,12 +139,14 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
 
   // logits of tile `tile` (8-column blocks 0 .. NB - 1 from its first position on) -> scores, this lane's two rows
   const int q0 = row0 + (lane >> 2), q1 = q0 + 8, c2 = (lane & 3) * 2;
-  float* s_base = WEIGH ? a.scores + ((int64_t)b * a.Hkv + kvh) * a.g * a.score_ld + begin : nullptr;
+  float* s_base = !WEIGH ? nullptr : CLUSTER ? reinterpret_cast<float*>(smem + STAGES * G::STAGE_B)
+                                             : a.scores + ((int64_t)b * a.Hkv + kvh) * a.g * a.score_ld + begin;
+  const int64_t s_ld = CLUSTER ? chunk + 8 : a.score_ld;   // (+ 8: the rows of a fragment's store fall into different banks)
   auto store = [&](int tile, const float* s0, int blk) {   // s0: the four fragment values of 8-column block blk
     if (!WEIGH) return;
     const int c = tile * KT + blk * 8 + c2;
-    if (q0 < a.g) *reinterpret_cast<float2*>(s_base + (int64_t)q0 * a.score_ld + c) = make_float2(s0[0] * scale_log2, s0[1] * scale_log2);
-    if (q1 < a.g) *reinterpret_cast<float2*>(s_base + (int64_t)q1 * a.score_ld + c) = make_float2(s0[2] * scale_log2, s0[3] * scale_log2);
+    if (q0 < a.g) *reinterpret_cast<float2*>(s_base + q0 * s_ld + c) = make_float2(s0[0] * scale_log2, s0[1] * scale_log2);
+    if (q1 < a.g) *reinterpret_cast<float2*>(s_base + q1 * s_ld + c) = make_float2(s0[2] * scale_log2, s0[3] * scale_log2);
   };
   struct Sink2 { decltype(store)& f; __device__ __forceinline__ void operator()(int tile, const float (&s)[2][4]) const { f(tile, s[0], 0); f(tile, s[1], 1); } };
   struct Sink4 { decltype(store)& f; __device__ __forceinline__ void operator()(int tile, const float (&s)[4][4]) const { f(tile, s[0], 0); f(tile, s[1], 1); f(tile, s[2], 2); f(tile, s[3], 3); } };
@@ -129,6 +186,77 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
   }
   pdl_launch_dependents();
   t.reduce_sums();
+  if constexpr (CLUSTER) {
+    float* s_o = reinterpret_cast<float*>(smem);   // [16][D], over the ring
+    float* s_ml = reinterpret_cast<float*>(smem + STAGES * G::STAGE_B + (WEIGH ? a.g * (a.chunk + 8) * 4 : 0));
+    float *s_wt = s_ml + 32, *s_lse = s_wt + kMaxCluster * 16;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < NTILES; ++k) {
+      *reinterpret_cast<float2*>(s_o + q0 * D + k * 8 + c2) = make_float2(t.o[k][0], t.o[k][1]);
+      *reinterpret_cast<float2*>(s_o + q1 * D + k * 8 + c2) = make_float2(t.o[k][2], t.o[k][3]);
+    }
+    if ((lane & 3) == 0) {
+      s_ml[q0] = t.m0; s_ml[q1] = t.m1;
+      s_ml[16 + q0] = t.l0; s_ml[16 + q1] = t.l1;
+    }
+    cluster_arrive();
+    cluster_wait();
+    // lane r < g: row r's denominator over the whole list, and what each CTA's partial counts
+    if (lane < a.g) {
+      float m[kMaxCluster], mx = -INFINITY, sum = 0.f;
+      const uint32_t at = ptx::smem_u32(s_ml + lane);
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) {
+        m[k] = k < a.cluster ? peer_ld(peer_smem(at, k)) : -INFINITY;
+        mx = fmaxf(mx, m[k]);
+      }
+      const float mu = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) {
+        m[k] = ex2(m[k] - mu);
+        if (k < a.cluster) sum += m[k] * peer_ld(peer_smem(at + 64, k));
+      }
+      const float inv = len > 0 ? 1.f / sum : 0.f;   // (a sequence without rows: zeros)
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) s_wt[k * 16 + lane] = m[k] * inv;
+      s_lse[lane] = mu + log2f(sum);
+    }
+    __syncwarp();
+    constexpr int V4 = D / 4;
+    const uint32_t o_at = ptx::smem_u32(s_o);
+    for (int i = split * 32 + lane; i < a.g * V4; i += a.cluster * 32) {
+      const int r = i / V4;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k) {
+        if (k < a.cluster) {
+          const float4 x = peer_ld4(peer_smem(o_at + i * 16, k));
+          const float w = s_wt[k * 16 + r];
+          acc.x = fmaf(w, x.x, acc.x); acc.y = fmaf(w, x.y, acc.y); acc.z = fmaf(w, x.z, acc.z); acc.w = fmaf(w, x.w, acc.w);
+        }
+      }
+      reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.o) + ((int64_t)b * a.Hq + kvh * a.g) * D)[i] =
+          make_uint2(pack2(acc.x, acc.y), pack2(acc.z, acc.w));
+    }
+    cluster_arrive();   // (what is left reads this CTA's own memory)
+    const int64_t cap_row = ((int64_t)b * a.Hkv + kvh) * EARN_PAGE_TOKENS * a.cache.pages_per_seq;
+    if (split == 0 && lane == 0 && a.pos != nullptr && len > 0) a.pos[cap_row + len - 1] = a.new_pos[b];
+    if (WEIGH) {
+      for (int j = lane * 4; j < n; j += 128) {
+        float w[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < a.g; ++r) {
+          const float4 x = *reinterpret_cast<const float4*>(s_base + r * s_ld + j);   // (columns past the list are not used)
+          const float d = s_lse[r];
+          w[0] += ex2(x.x - d); w[1] += ex2(x.y - d); w[2] += ex2(x.z - d); w[3] += ex2(x.w - d);
+        }
+        const float4 before = a.weight ? *reinterpret_cast<const float4*>(a.weight + cap_row + begin + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        add_weights(a.weight_out + cap_row + begin + j, before, j, n, newest, w);
+      }
+    }
+    cluster_wait();   // the other CTAs have read this one's shared memory
+    return;
+  }
   // ---- the partial: normalised rows and their log2-domain denominators
   const int64_t prow = (((int64_t)b * a.Hkv + kvh) * a.n_splits + split) * a.g;
   const float i0 = t.l0 == 0.f ? 0.f : 1.f / t.l0, i1 = t.l1 == 0.f ? 0.f : 1.f / t.l1;   // (0: every logit of the chunk is -inf)
@@ -288,9 +416,27 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// Block x < g: query row x of the (sequence, kv head): the partials, weighted by 2^(their LSE - LSE of all).
-// Block x >= g: rows (x - g) * JOIN_KEYS .. of the list: their weights.
-constexpr int JOIN_THREADS = 256, JOIN_KEYS = 4 * JOIN_THREADS, JOIN_MAX_G = 1024;
+// The first ceil(g / 4) blocks of a (sequence, kv head) take four output rows each, two warps to a row: the partials, weighted
+// by 2^(their LSE - LSE of all).  The blocks behind them take JOIN_KEYS rows of the list each: their weights.  What a block
+// reads does not depend on the length (only what it uses does), so the denominators, partials and logits are all asked for
+// at once: one round trip to L2 instead of the chain length -> denominators -> partials, and few enough blocks for one wave.
+constexpr int JOIN_THREADS = 256, JOIN_ROWS = 4, JOIN_KEYS = 8 * JOIN_THREADS, JOIN_AHEAD = 4, JOIN_MAX_G = 1024;
+
+// log2-domain denominator of query row r over `live` splits, by one warp; x0, x1: the lane's splits lane and lane + 32
+__device__ __forceinline__ float join_lse(const float* lse, int g, int r, int live, int lane, float x0, float x1) {
+  x0 = lane < live ? x0 : -INFINITY;
+  x1 = lane + 32 < live ? x1 : -INFINITY;
+  float mx = fmaxf(x0, x1);
+  for (int s = lane + 64; s < live; s += 32) mx = fmaxf(mx, lse[s * g + r]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  const float mu = mx == -INFINITY ? 0.f : mx;
+  float sum = ex2(x0 - mu) + ex2(x1 - mu);
+  for (int s = lane + 64; s < live; s += 32) sum += ex2(lse[s * g + r] - mu);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return mu + log2f(sum);
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArgs a) {
@@ -301,73 +447,116 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int kvh = blockIdx.y, b = blockIdx.z, g = a.g;
   const int64_t unit = (int64_t)b * a.Hkv + kvh;
-  const int len = paged_len(a.cache, b);
-  const int live = (len + a.chunk - 1) / a.chunk;   // splits that hold rows
   const float* lse = a.part_lse + unit * a.n_splits * g;
-  const bool o_block = (int)blockIdx.x < g;
-  const int key0 = ((int)blockIdx.x - g) * JOIN_KEYS;
-  if (!o_block && key0 >= len) return;
-  // ---- denominators over the whole list (one row, or all of the group's)
-  for (int r = o_block ? (warp == 0 ? (int)blockIdx.x : g) : warp; r < (o_block ? (int)blockIdx.x + 1 : g); r += JOIN_THREADS / 32) {
-    float mx = -INFINITY;
-    for (int s = lane; s < live; s += 32) mx = fmaxf(mx, lse[s * g + r]);
+  const int o_blocks = (g + JOIN_ROWS - 1) / JOIN_ROWS;
+  if ((int)blockIdx.x < o_blocks) {
+    constexpr int V4 = D / 4, SUB = 32 / V4, STEP = 2 * SUB, AHEAD = 4;   // float4 per row; splits a warp, a row's two warps take at once
+    const int r = (int)blockIdx.x * JOIN_ROWS + warp / 2;
+    const int first = (warp & 1) * SUB + lane / V4;
+    const float4* po = reinterpret_cast<const float4*>(a.part_o) + (unit * a.n_splits * g + r) * V4 + lane % V4;
+    const bool in = r < g;
+    float4 y[AHEAD];
+    float ly[AHEAD];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float mu = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f;
-    for (int s = lane; s < live; s += 32) sum += exp2f(lse[s * g + r] - mu);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) lse_all[r] = mu + log2f(sum);
-  }
-  __syncthreads();
-  if (o_block) {
-    constexpr int V4 = D / 4, GROUPS = JOIN_THREADS / V4;   // float4 per row; splits walked side by side
-    const int r = blockIdx.x, c = tid % V4, grp = tid / V4;
-    const float all = lse_all[r];
+    for (int k = 0; k < AHEAD; ++k) {
+      const int s = first + k * STEP;
+      const bool ok = in && s < a.n_splits;
+      ly[k] = ok ? lse[s * g + r] : 0.f;
+      y[k] = ok ? po[(int64_t)s * g * V4] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    const float x0 = in && lane < a.n_splits ? lse[lane * g + r] : 0.f, x1 = in && lane + 32 < a.n_splits ? lse[(lane + 32) * g + r] : 0.f;
+    const int len = paged_len(a.cache, b), live = (len + a.chunk - 1) / a.chunk;   // splits that hold rows
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int s = grp; s < live; s += GROUPS) {
-      const float w = exp2f(lse[s * g + r] - all);
-      const float4 x = reinterpret_cast<const float4*>(a.part_o + ((unit * a.n_splits + s) * g + r) * D)[c];
-      acc.x = fmaf(w, x.x, acc.x); acc.y = fmaf(w, x.y, acc.y); acc.z = fmaf(w, x.z, acc.z); acc.w = fmaf(w, x.w, acc.w);
+    if (in) {   // (warp-uniform)
+      const float all = join_lse(lse, g, r, live, lane, x0, x1);
+      auto add = [&](float l, const float4& z) {
+        const float w = ex2(l - all);
+        acc.x = fmaf(w, z.x, acc.x); acc.y = fmaf(w, z.y, acc.y); acc.z = fmaf(w, z.z, acc.z); acc.w = fmaf(w, z.w, acc.w);
+      };
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (first + k * STEP < live) add(ly[k], y[k]);
+#pragma unroll 8
+      for (int s = first + AHEAD * STEP; s < live; s += STEP) add(lse[s * g + r], po[(int64_t)s * g * V4]);
     }
     part[tid] = acc;
     __syncthreads();
-    if (tid < V4) {
-      float y[4] = {0.f, 0.f, 0.f, 0.f};   // (a sequence without rows: zeros)
-      for (int k = 0; k < GROUPS; ++k) {
-        const float4 x = part[k * V4 + tid];
-        y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+    if (in && (warp & 1) == 0 && lane < V4) {
+      float o[4] = {0.f, 0.f, 0.f, 0.f};   // (a sequence without rows: zeros)
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) {
+        const float4 z = part[warp * 32 + k * V4 + lane];
+        o[0] += z.x; o[1] += z.y; o[2] += z.z; o[3] += z.w;
       }
-      Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)b * a.Hq + kvh * g + r) * D + tid * 4, y);
+      Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)b * a.Hq + kvh * g + r) * D + lane * 4, o);
     }
-    if (r == 0 && tid == 0 && a.pos != nullptr && len > 0)
+    if (blockIdx.x == 0 && tid == 0 && a.pos != nullptr && len > 0)
       a.pos[unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq + len - 1] = a.new_pos[b];
     return;
   }
   // ---- weights
-  const int j = key0 + tid * 4;
-  if (j >= len) return;
-  const float* s = a.scores + unit * g * a.score_ld + j;
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int r = 0; r < g; ++r) {
-    const float4 x = *reinterpret_cast<const float4*>(s + (int64_t)r * a.score_ld);   // (columns past the list are not used)
-    const float d = lse_all[r];
-    w[0] += exp2f(x.x - d); w[1] += exp2f(x.y - d); w[2] += exp2f(x.z - d); w[3] += exp2f(x.w - d);
-  }
-  const int64_t at = unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq + j;
-  const int fresh = a.k_new != nullptr ? len - 1 : -1;   // the appended row starts from zero
-  if (j + 4 <= len && (fresh < j || fresh >= j + 4)) {
-    float4 x = a.weight ? *reinterpret_cast<const float4*>(a.weight + at) : make_float4(0.f, 0.f, 0.f, 0.f);
-    x.x += w[0]; x.y += w[1]; x.z += w[2]; x.w += w[3];
-    *reinterpret_cast<float4*>(a.weight_out + at) = x;
-  } else {
+  const int key0 = ((int)blockIdx.x - o_blocks) * JOIN_KEYS + tid * 4;
+  const float* sc = a.scores + unit * g * a.score_ld + key0;
+  float4 x[2][JOIN_AHEAD];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (j + i < len) a.weight_out[at + i] = (a.weight && j + i != fresh ? a.weight[at + i] : 0.f) + w[i];
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int r = 0; r < JOIN_AHEAD; ++r)
+      if (r < g && key0 + h * (JOIN_KEYS / 2) < a.score_ld)
+        x[h][r] = *reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (JOIN_KEYS / 2));   // (columns past the list are not used)
+  const int64_t row0 = unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq;
+  float4 in[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    in[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.weight && key0 + h * (JOIN_KEYS / 2) < a.score_ld) in[h] = *reinterpret_cast<const float4*>(a.weight + row0 + key0 + h * (JOIN_KEYS / 2));
   }
+  const int len = paged_len(a.cache, b), live = (len + a.chunk - 1) / a.chunk;
+  for (int r = warp; r < g; r += JOIN_THREADS / 32) {
+    const float x0 = lane < a.n_splits ? lse[lane * g + r] : 0.f, x1 = lane + 32 < a.n_splits ? lse[(lane + 32) * g + r] : 0.f;
+    const float all = join_lse(lse, g, r, live, lane, x0, x1);
+    if (lane == 0) lse_all[r] = all;
+  }
+  __syncthreads();
+  const int fresh = a.k_new != nullptr ? len - 1 : -1;   // the appended row starts from zero
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = key0 + h * (JOIN_KEYS / 2);
+    if (j >= len) return;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float4& y, float d) { w[0] += ex2(y.x - d); w[1] += ex2(y.y - d); w[2] += ex2(y.z - d); w[3] += ex2(y.w - d); };
+#pragma unroll
+    for (int r = 0; r < JOIN_AHEAD; ++r)
+      if (r < g) add(x[h][r], lse_all[r]);
+#pragma unroll 4
+    for (int r = JOIN_AHEAD; r < g; ++r)
+      add(*reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (JOIN_KEYS / 2)), lse_all[r]);
+    add_weights(a.weight_out + row0 + j, in[h], j, len, fresh, w);
+  }
+}
+
+// cluster form: a.cluster CTAs per (sequence, kv head), launched as one cluster
+template <int D, bool WEIGH>
+cudaError_t launch_cluster(const PagedDecodeArgs& a, cudaStream_t st) {
+  const int smem = cluster_smem<D>(a.g, a.chunk, WEIGH);
+  cudaError_t e = ensure_dynamic_smem<paged_decode_kernel<D, WEIGH, true>>(cluster_smem<D>(16, kPagedMaxChunk, WEIGH));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(a.Hkv * a.cluster, 1, a.n_seq);
+  cfg.blockDim = dim3(32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  e = cudaLaunchKernelEx(&cfg, paged_decode_kernel<D, WEIGH, true>, a);
+  note_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <int D, bool WEIGH>
@@ -376,8 +565,8 @@ cudaError_t launch_main(const PagedDecodeArgs& a, cudaStream_t st) {
   cudaError_t e;
   if (a.dtype == EARN_BF16) {
     constexpr int smem = STAGES * Geo<D>::STAGE_B;
-    e = ensure_dynamic_smem<paged_decode_kernel<D, WEIGH>>(smem);
-    if (e == cudaSuccess) e = launch_pdl(paged_decode_kernel<D, WEIGH>, grid, dim3(32), smem, st, a);
+    e = ensure_dynamic_smem<paged_decode_kernel<D, WEIGH, false>>(smem);
+    if (e == cudaSuccess) e = launch_pdl(paged_decode_kernel<D, WEIGH, false>, grid, dim3(32), smem, st, a);
   } else {
     constexpr int smem = (int)sizeof(F32Smem<D>);
     e = ensure_dynamic_smem<paged_decode_f32_kernel<D, WEIGH>>(smem);
@@ -389,9 +578,10 @@ cudaError_t launch_main(const PagedDecodeArgs& a, cudaStream_t st) {
 
 template <int D>
 cudaError_t launch_d(const PagedDecodeArgs& a, cudaStream_t st) {
+  if (a.cluster > 0) return a.weight_out ? launch_cluster<D, true>(a, st) : launch_cluster<D, false>(a, st);
   cudaError_t e = a.weight_out ? launch_main<D, true>(a, st) : launch_main<D, false>(a, st);
   if (e != cudaSuccess) return e;
-  const dim3 grid(a.g + (a.weight_out ? (a.cache.max_len + JOIN_KEYS - 1) / JOIN_KEYS : 0), a.Hkv, a.n_seq);
+  const dim3 grid((a.g + JOIN_ROWS - 1) / JOIN_ROWS + (a.weight_out ? (a.cache.max_len + JOIN_KEYS - 1) / JOIN_KEYS : 0), a.Hkv, a.n_seq);
   e = a.dtype == EARN_BF16 ? launch_pdl(paged_join_kernel<bf16, D>, grid, dim3(JOIN_THREADS), 0, st, a)
                            : launch_pdl(paged_join_kernel<float, D>, grid, dim3(JOIN_THREADS), 0, st, a);
   note_launch();
@@ -400,15 +590,29 @@ cudaError_t launch_d(const PagedDecodeArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-void plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int* chunk, int* n_splits) {
+// A call with less work than a wave of chunks is a chain of latencies, and one launch with the join inside the cluster beats
+// two: 64 (sequence, kv head) pairs of 1000 rows 12.0 us against 14.7, 192 of 50 to 200 rows 8.7 against 9.4 (group of 7),
+// 512 of 300 rows 22.4 against 23.7.  Past that a cluster's CTAs sit out the exchange without a load in flight (512 pairs of
+// 700 to 1044 rows: 54.5 us against 51.3), and more than 256 rows a warp take too long (16 pairs of 2000 rows: level).
+PagedPlan plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int dtype) {
+  PagedPlan p{};
+  const int64_t units = (int64_t)n_seq * n_kv_heads * ((g + 15) / 16), sms = sm_count();
+  constexpr int ROWS = kPagedMaxChunk / 2;
+  if (dtype == EARN_BF16 && g <= 16 && max_len <= kMaxCluster * ROWS && units * max_len <= 6 * sms * ROWS) {
+    int c = 1;   // enough CTAs for half the warp slots, unless their lists come to less than two tiles
+    while (c < kMaxCluster && ((max_len + c - 1) / c > ROWS || (units * c < 3 * sms && max_len > 2 * KT * c))) c *= 2;
+    p.cluster = c;
+    p.chunk = ((max_len + KT - 1) / KT + c - 1) / c * KT;
+    return p;
+  }
   // about three chunks per warp slot (six one-warp CTAs an SM), so that uneven lists even out; a chunk of at least 32 rows
-  const int64_t units = (int64_t)n_seq * n_kv_heads * ((g + 15) / 16), slots = 18LL * sm_count();
-  int64_t c = (units * max_len + slots - 1) / slots;
+  int64_t c = (units * max_len + 18 * sms - 1) / (18 * sms);
   c = (c + 31) / 32 * 32;
   if (c < 32) c = 32;
   if (c > kPagedMaxChunk) c = kPagedMaxChunk;
-  *chunk = (int)c;
-  *n_splits = (int)((max_len + c - 1) / c);
+  p.chunk = (int)c;
+  p.n_splits = (int)((max_len + c - 1) / c);
+  return p;
 }
 
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, cudaStream_t st) {

@@ -116,9 +116,9 @@ def test_evict_rows(lib):  # noqa: F811
 
 
 def test_workspace_size(lib):  # noqa: F811
-    c = cache(per_seq=64, n_pages=128, max_len=1024)
+    c = cache(per_seq=512, n_pages=1024, max_len=8192)
     need = lib.earn_paged_workspace_bytes(C.byref(MODEL), 2, C.byref(c))
-    assert need >= 256 + 2 * 2 * 4 * 1024 * 4                               # one logit per (sequence, query head, row)
+    assert need >= 256 + 2 * 2 * 4 * 8192 * 4                               # one logit per (sequence, query head, row)
     assert lib.earn_paged_workspace_bytes(C.byref(MODEL), 2, C.byref(cache(max_len=0))) == 256
     assert lib.earn_paged_workspace_bytes(C.byref(MODEL), -1, C.byref(c)) == 256
 
@@ -126,21 +126,25 @@ def test_workspace_size(lib):  # noqa: F811
 def test_the_binding_turns_down_what_the_library_cannot_see():
     x = torch.zeros(4, 8, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="q: torch.bfloat16"):
-        B._tensor(x, "q", torch.float32, 1)
+        B._tensor(x, "q", torch.float32, 1, 0)
     with pytest.raises(ValueError, match="not contiguous"):
-        B._tensor(x.t(), "q", torch.bfloat16, 1)
+        B._tensor(x.t(), "q", torch.bfloat16, 1, 0)
     with pytest.raises(ValueError, match="at least 33"):
-        B._tensor(x, "q", torch.bfloat16, 33)
+        B._tensor(x, "q", torch.bfloat16, 33, 0)
     with pytest.raises(ValueError, match="expected the current CUDA device"):
-        B._tensor(x, "q", torch.bfloat16, 32)
-    assert B._tensor(None, "q", torch.float32, 1) is None
+        B._tensor(x, "q", torch.bfloat16, 32, 0)
+    assert B._tensor(None, "q", torch.float32, 1, 0) is None
     with pytest.raises(ValueError, match="n_pages"):
         B.make_paged_cache(torch.zeros(2, 8, 2, 64), torch.zeros(2, 8, 2, 64), pages_per_seq=1)
-    other = cache()
-    other.kind, other.rows = (torch.bfloat16, 4, 128), (2, 2)
+    with pytest.raises(ValueError, match="pages_per_seq"):
+        B.make_paged_cache(torch.zeros(2, 16, 2, 64), torch.zeros(2, 16, 2, 64))
+    other, bf16 = cache(), torch.bfloat16
+    other.kind, other.n_seq, other.device = (bf16, 4, 128), 2, 0
     with pytest.raises(ValueError, match="cache of"):
-        B._check_cache(MODEL, 2, other)
-    other.kind = (torch.bfloat16, 2, 128)
+        B._check_cache(MODEL, 2, other, bf16, 2, 128, 0)
+    other.kind = (bf16, 2, 128)
     with pytest.raises(ValueError, match="fewer than 3"):
-        B._check_cache(MODEL, 3, other)
-    assert B._check_cache(MODEL, 2, other) == 64
+        B._check_cache(MODEL, 3, other, bf16, 2, 128, 0)
+    with pytest.raises(ValueError, match="cache on CUDA device"):
+        B._check_cache(MODEL, 2, other, bf16, 2, 128, 1)
+    assert B._check_cache(MODEL, 2, other, bf16, 2, 128, 0) == 64
