@@ -229,16 +229,22 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a, bool move
 }
 
 // ---- lists of at most NT * IPT rows: every key in a register (row j0 + 32 i + lane of a warp's stretch), read once.
-// Four digits of 8 bits: the CTA counts a digit's 256 bins in shared memory (a histogram of its own per digit, so a digit
-// costs one barrier) and every warp finds the bin by itself.  Ranks over the warps come from one count per warp and one
-// barrier as well.  (Eleven-bit digits and full scans: 20 us for 512 lists of 1025 rows; a search bit by bit: 17 us.)
+// Four digits of 8 bits, the CTA counting a digit's 256 bins in shared memory (a histogram of its own per digit, cleared
+// once; four copies of the first digit's, where every row counts and most fall into a few bins).  Ranks over the warps come
+// from one count per warp and one barrier.  (Eleven-bit digits and full scans: 20 us for 512 lists of 1025 rows; a search
+// bit by bit: 17 us.)  In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one
+// instead, by a minimum over the CTA each.
 constexpr int MOVES_HERE = 64;   // moves the selecting CTA makes itself
+constexpr int FEW = 8;           // rows too many that are taken out one by one
 
 template <int NT>
 struct RegShared {
-  int hist[4][256];
+  int hist[4][256], more[3][256];   // digit d; copies of the first digit's (d = 3)
   int2 ranks[2][NT / 32];
   int last[NT / 32];
+  int bin, rest, equal;
+  uint32_t low_key[2][NT / 32];
+  int low_row[2][NT / 32];
   int from[MOVES_HERE], to[MOVES_HERE];
 };
 
@@ -280,13 +286,15 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
     if (!PROMPT && tid == 0) a.n_moves[unit] = 0;
     return;
   }
-  for (int i = tid; i < 4 * 256; i += NT) sh.hist[0][i] = 0;
+  const bool few = !PROMPT && n - budget <= FEW;   // block-uniform
+  if (!few)
+    for (int i = tid; i < 7 * 256; i += NT) (&sh.hist[0][0])[i] = 0;
   // ---- keys
   uint32_t u[IPT];
+  float w[IPT];
+  int p[IPT];
   int last = n - 1;
   {
-    float w[IPT];
-    int p[IPT];
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       const int j = j0 + 32 * i;
@@ -310,39 +318,114 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
       u[i] = !in ? 0u : (p[i] < a.n_first || p[i] > after) ? KEY_PROTECTED : weight_key(w[i]);
     }
   }
+  if (few) {
+    // ---- the last rows of the order, one by one: the smallest key, and of equal ones the highest row
+    int gone[FEW];
+#pragma unroll
+    for (int m = 0; m < FEW; ++m) {
+      gone[m] = INT_MAX;
+      if (m >= n - budget) continue;   // block-uniform
+      uint32_t low = 0xffffffffu;
+      int row = -1;
+#pragma unroll
+      for (int i = 0; i < IPT; ++i)   // (a lane's rows rise with i; key 0: no row, or one that is out already)
+        if (u[i] != 0u && u[i] <= low) { low = u[i]; row = j0 + 32 * i; }
+      const uint32_t wlow = __reduce_min_sync(0xffffffffu, low);
+      const int wrow = __reduce_max_sync(0xffffffffu, low == wlow ? row : -1);
+      if (lane == 0) { sh.low_key[m & 1][warp] = wlow; sh.low_row[m & 1][warp] = wrow; }
+      __syncthreads();
+      const uint32_t k = lane < NW ? sh.low_key[m & 1][lane] : 0xffffffffu;
+      const int r = lane < NW ? sh.low_row[m & 1][lane] : -1;   // (-1: a warp without rows)
+      const uint32_t least = __reduce_min_sync(0xffffffffu, r >= 0 ? k : 0xffffffffu);
+      gone[m] = __reduce_max_sync(0xffffffffu, k == least ? r : -1);
+#pragma unroll
+      for (int i = 0; i < IPT; ++i)
+        if (j0 + 32 * i == gone[m]) u[i] = 0u;
+    }
+    // rows below the budget that stay; kept row budget + t moves into the place of its rank's free row
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+      const int j = j0 + 32 * i;
+      if (u[i] != 0u && j < budget) {
+        if (copy_w) w_out[j] = w[i];
+        if (copy_p) p_out[j] = p[i];
+      }
+    }
+    int from = -1, to = -1;   // thread t < FEW: row budget + t
+    if (tid < FEW && budget + tid < n) {
+      from = budget + tid;
+      int rank = tid;         // kept rows behind the budget in front of this one
+#pragma unroll
+      for (int m = 0; m < FEW; ++m) {
+        if (gone[m] == budget + tid) from = -1;
+        if (gone[m] >= budget && gone[m] < budget + tid) --rank;
+      }
+#pragma unroll
+      for (int m = 0; m < FEW; ++m) {   // the free row with `rank` free rows below it
+        int below = 0;
+#pragma unroll
+        for (int k = 0; k < FEW; ++k) below += gone[k] < gone[m] ? 1 : 0;
+        if (gone[m] < budget && below == rank) to = gone[m];
+      }
+    }
+    // (nobody reads a row below the budget any more: the rows were read ahead of the barriers)
+    if (from >= 0) {
+      w_out[to] = weight[from];
+      p_out[to] = pos[from];
+    }
+    const uint32_t moving = __ballot_sync(0xffffffffu, from >= 0);
+    if (tid == 0) a.n_moves[unit] = move_here ? 0 : __popc(moving);
+    if (warp == 0) {
+      int32_t* list = a.moves + (int64_t)unit * 2 * a.list;
+      for (int t = 0; t < FEW; ++t) {
+        const int f = __shfl_sync(0xffffffffu, from, t), g = __shfl_sync(0xffffffffu, to, t);
+        if (f < 0) continue;
+        if (move_here) move_row(a, b, kvh, f, g, lane, 32);
+        else if (lane == 0) { const int k = __popc(moving & ((1u << t) - 1u)); list[k] = f; list[a.list + k] = g; }
+      }
+    }
+    return;
+  }
   // ---- the budget-th largest key T, digit by digit from the top: `want` of the keys that agree with T so far stay.  (No
   // row's key is 0, so the key 0 of a lane without a row is never counted.)
   uint32_t T = 0;
   int want = budget, equal = 0;
 #pragma unroll
   for (int d = 3; d >= 0; --d) {
-    int* hist = sh.hist[d];
+    int* hist = d == 3 && (lane & 3) ? sh.more[(lane & 3) - 1] : sh.hist[d];
 #pragma unroll
     for (int i = 0; i < IPT; ++i)
       if (u[i] != 0u && (d == 3 || (u[i] >> (8 * d + 8)) == (T >> (8 * d + 8)))) atomicAdd(&hist[(u[i] >> (8 * d)) & 255u], 1);
     __syncthreads();
-    // lane l owns bins 255 - 8 l .. 248 - 8 l; the bins of the lanes below it hold larger digits
-    const int4 h0 = reinterpret_cast<const int4*>(hist)[63 - 2 * lane], h1 = reinterpret_cast<const int4*>(hist)[62 - 2 * lane];
-    const int c[8] = {h0.w, h0.z, h0.y, h0.x, h1.w, h1.z, h1.y, h1.x};   // from the largest digit down
-    int sum = 0;
+    if (warp == 0) {
+      // lane l owns bins 255 - 8 l .. 248 - 8 l; the bins of the lanes below it hold larger digits
+      int c[8];   // from the largest digit down
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += c[k];
-    int incl = sum;
+      for (int k = 0; k < 8; ++k) {
+        const int bin = 255 - 8 * lane - k;
+        c[k] = sh.hist[d][bin];
+        if (d == 3) c[k] += sh.more[0][bin] + sh.more[1][bin] + sh.more[2][bin];
+      }
+      int sum = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
+      for (int k = 0; k < 8; ++k) sum += c[k];
+      int incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+      }
+      int above = incl - sum;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (above < want && want <= above + c[k]) { sh.bin = 255 - 8 * lane - k; sh.rest = want - above; sh.equal = c[k]; }   // one lane
+        above += c[k];
+      }
     }
-    const int owner = __ffs(__ballot_sync(0xffffffffu, incl >= want)) - 1;
-    int above = incl - sum, digit = 0, rest = 0, cnt = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (above < want && want <= above + c[k]) { digit = 255 - 8 * lane - k; rest = want - above; cnt = c[k]; }
-      above += c[k];
-    }
-    T |= (uint32_t)__shfl_sync(0xffffffffu, digit, owner) << (8 * d);
-    want = __shfl_sync(0xffffffffu, rest, owner);
-    equal = __shfl_sync(0xffffffffu, cnt, owner);
+    __syncthreads();
+    T |= (uint32_t)sh.bin << (8 * d);
+    want = sh.rest;
+    equal = sh.equal;
   }
   // ---- rows with a larger key stay, and the first `want` of the `equal` rows with key T
   const uint32_t lt = (1u << lane) - 1u;
@@ -376,6 +459,14 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
   int rx = base.x, ry = base.y;
   int32_t* from = PROMPT ? nullptr : move_here ? sh.from : a.moves + (int64_t)unit * 2 * a.list;
   int32_t* to = PROMPT ? nullptr : move_here ? sh.to : a.moves + (int64_t)unit * 2 * a.list + a.list;
+  // (what stays is read again, all of it ahead of the first store: the outputs may be the inputs, so the compiler would not)
+#pragma unroll
+  for (int i = 0; i < IPT; ++i) {
+    const int j = j0 + 32 * i;
+    const bool stays = (keep >> i & 1u) && (PROMPT || j < budget);
+    if (stays && copy_w) w[i] = weight[j];
+    if (!PROMPT && stays && copy_p) p[i] = pos[j];
+  }
 #pragma unroll
   for (int i = 0; i < IPT; ++i) {
     if (i >= ipt) break;
@@ -385,14 +476,14 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
       if (is_x(i)) {
         const int slot = rx + __popc(bx & lt);
         p_out[slot] = j;
-        if (copy_w) w_out[slot] = weight[j];
+        if (copy_w) w_out[slot] = w[i];
       }
     } else {
       if (is_x(i)) to[rx + __popc(bx & lt)] = j;
       if (is_y(i)) from[ry + __popc(by & lt)] = j;
       if ((keep >> i & 1u) && j < budget) {
-        if (copy_w) w_out[j] = weight[j];
-        if (copy_p) p_out[j] = pos[j];
+        if (copy_w) w_out[j] = w[i];
+        if (copy_p) p_out[j] = p[i];
       }
     }
     rx += __popc(bx);
