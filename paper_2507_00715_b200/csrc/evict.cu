@@ -1,17 +1,16 @@
 // Eviction from a cache by accumulated attention weight: which rows of every (sequence, kv head) stay within the budget,
 // and their way into (prompt form) or inside (step form) the paged cache.
 //
-// Selection: one CTA per (sequence, kv head).  Every row gets a 32-bit key that orders as the policy does (a protected
-// row the largest key of all, otherwise the weight's bits made monotone), kept in shared memory while the list fits
-// there.  The budget-th largest key is found digit by digit (11 + 11 + 10 bits, a histogram in shared memory per
-// digit); of the rows that equal it the first ones stay.  Row numbers in order come from ballots: a warp owns a contiguous
-// stretch of the list, so a count per warp and one scan over the warps turn into ranks.  Exact, and no result depends on
-// the order in which threads arrive.
-//   prompt form: the m-th kept position goes to pos_out[m]; a second kernel copies the K / V rows (bit copies, 16-byte
-//   vectors) from the packed prompt into the pages.
-//   step form: the i-th free row below the budget and the i-th kept row behind it form a move; sources and destinations
-//   are disjoint, so the moves run in any order.  A few moves (a step's worth) are made by the selecting CTA itself, more
-//   of them by a second kernel over the whole GPU.
+// Selection: every row gets a 32-bit key that orders as the policy does (a protected row the largest key of all, otherwise
+// the weight's bits made monotone), and the budget-th largest key is found digit by digit with a histogram in shared memory;
+// of the rows that equal it the first ones stay.  Row numbers in order come from ballots: a warp owns a contiguous stretch of
+// the list, so a count per warp turns into ranks.  Exact, and no result depends on the order in which threads arrive.
+//   prompt form: the m-th kept position goes to pos_out[m], its K / V rows (bit copies, 16-byte vectors) from the packed
+//   prompt into row m of the pages;
+//   step form: the i-th free row below the budget and the i-th kept row behind it form a move; sources and destinations are
+//   disjoint, so the moves run in any order.
+// Lists of up to 32768 rows take one launch (evict_cluster_kernel), longer ones a selecting kernel of one CTA per list, keys
+// in shared memory while they fit, and a copying kernel behind it.
 #include <climits>
 
 #include "earn_common.cuh"
@@ -81,7 +80,7 @@ __device__ __forceinline__ void move_row(const EvictArgs& a, int b, int kvh, int
 }
 
 template <int NT, bool PROMPT, bool STAGED>
-__global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a, bool move_here) {
+__global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
   extern __shared__ uint32_t staged[];
   __shared__ SelectShared sh;
   pdl_wait();   // everything below reads or writes global memory
@@ -224,50 +223,84 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a, bool move
     w_out[to[i]] = weight[from[i]];
     p_out[to[i]] = pos[from[i]];
   }
-  if (move_here)
-    for (int i = warp; i < n_moves; i += NT / 32) move_row(a, b, kvh, from[i], to[i], lane, 32);
 }
 
-// ---- lists of at most NT * IPT rows: every key in a register (row j0 + 32 i + lane of a warp's stretch), read once.
-// Four digits of 8 bits, the CTA counting a digit's 256 bins in shared memory (a histogram of its own per digit, cleared
-// once; four copies of the first digit's, where every row counts and most fall into a few bins).  Ranks over the warps come
-// from one count per warp and one barrier.  (Eleven-bit digits and full scans: 20 us for 512 lists of 1025 rows; a search
-// bit by bit: 17 us.)  In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one
-// instead, by a minimum over the CTA each.
-constexpr int MOVES_HERE = 64;   // moves the selecting CTA makes itself
+// ---- lists of at most 32768 rows: one launch.  A cluster of C CTAs of 256 threads owns a (sequence, kv head); every key is in
+// a register (CTA r holds the r-th stretch of the list, a warp a stretch of that, row j0 + 32 i + lane), read once.
+// Four digits of 8 bits: each CTA counts a digit's 256 bins in its shared memory (a histogram of its own per digit, cleared
+// once; four copies of the first digit's, where every row counts and most fall into a few bins), the counts of the cluster
+// are added through distributed shared memory, and the search ends with the first digit whose bin stays whole.  Ranks come
+// from one count per warp and one per CTA.  The CTAs then copy the rows they have found themselves (prompt form) or a share
+// of the moves (in place), without a second launch: while one list is still being searched, others are being copied.
+// In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one instead, by a minimum
+// over the CTA each.
+// Measured (8 kv heads, bf16, D = 128): 8 prompts of 12000 to 16384 rows to 2048 in 40 us, of which the copies are 20 at 6.7 TB/s
+// and the search with its exchanges 8 (fetching the rows that a first digit had settled into L2 meanwhile: 43 us); 64 lists of
+// 8192 rows halved in 40 us; 512 lists of 1025 rows to 1024 in 5.5 us (20 us with 11-bit digits and full scans over the
+// CTA, 17 with a search bit by bit).
+constexpr int NT = 256, NW = NT / 32, MAX_CLUSTER = 8, MAX_IPT = 16;
 constexpr int FEW = 8;           // rows too many that are taken out one by one
+constexpr int ROWS_EACH = 1024;  // rows of a list a CTA of a cluster is worth
 
-template <int NT>
-struct RegShared {
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return (int)r;
+}
+// an int of the same place in the shared memory of CTA `rank` of the cluster
+__device__ __forceinline__ int peer_int(const int* p, int rank) {
+  uint32_t at = (uint32_t)__cvta_generic_to_shared(p);
+  int x;
+  asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(rank));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+
+template <int IPT>
+struct ClusterShared {
   int hist[4][256], more[3][256];   // digit d; copies of the first digit's (d = 3)
-  int2 ranks[2][NT / 32];
-  int last[NT / 32];
+  int sum[256];                     // the digit's bins over the cluster
+  int2 ranks[2][NW];
+  int2 cta_total[2];
+  int last[NW], cta_last;
   int bin, rest, equal;
-  uint32_t low_key[2][NT / 32];
-  int low_row[2][NT / 32];
-  int from[MOVES_HERE], to[MOVES_HERE];
+  uint32_t low_key[2][NW];
+  int low_row[2][NW];
+  int src[NT * IPT];                // prompt form: the rows this CTA keeps, in order
 };
 
-// sum over the warps in front of this one (x, y) and over all of them, of one pair per warp
-template <int NW>
-__device__ __forceinline__ int2 rank_base(int2 mine, int2* slots, int2& total) {
+// sum over the warps in front of this one, CTAs of lower rank included (x, y), and over all of them, of one pair per warp
+__device__ __forceinline__ int2 rank_base(int2 mine, int2* slots, int2* cta_total, int rank, int n_cta, int2& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (lane == 0) slots[warp] = mine;
   __syncthreads();
   const int2 v = lane < NW ? slots[lane] : make_int2(0, 0);
   total = make_int2(__reduce_add_sync(0xffffffffu, v.x), __reduce_add_sync(0xffffffffu, v.y));
   const bool before = lane < warp;
-  return make_int2(__reduce_add_sync(0xffffffffu, before ? v.x : 0), __reduce_add_sync(0xffffffffu, before ? v.y : 0));
+  int2 base = make_int2(__reduce_add_sync(0xffffffffu, before ? v.x : 0), __reduce_add_sync(0xffffffffu, before ? v.y : 0));
+  if (n_cta > 1) {
+    if (threadIdx.x == 0) *cta_total = total;
+    cluster_sync();
+    const int2 c = lane < n_cta ? make_int2(peer_int(&cta_total->x, lane), peer_int(&cta_total->y, lane)) : make_int2(0, 0);
+    base.x += __reduce_add_sync(0xffffffffu, lane < rank ? c.x : 0);
+    base.y += __reduce_add_sync(0xffffffffu, lane < rank ? c.y : 0);
+    total = make_int2(__reduce_add_sync(0xffffffffu, c.x), __reduce_add_sync(0xffffffffu, c.y));
+  }
+  return base;
 }
 
-template <int NT, int IPT, bool PROMPT>
-__global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool move_here) {
-  constexpr int NW = NT / 32;
-  __shared__ RegShared<NT> sh;
+template <int IPT, bool PROMPT>
+__global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n_cta, bool copy_here) {
+  __shared__ ClusterShared<IPT> sh;
   pdl_wait();   // everything below reads or writes global memory
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int unit = blockIdx.x, b = unit / a.Hkv, kvh = unit - b * a.Hkv;
+  const int rank = n_cta > 1 ? cluster_rank() : 0;
+  const int unit = blockIdx.x / n_cta, b = unit / a.Hkv, kvh = unit - b * a.Hkv;
   const int64_t cap = (int64_t)EARN_PAGE_TOKENS * a.cache.pages_per_seq;
   const int lo = PROMPT ? a.cu_seqlens[b] : 0;
   const int n = PROMPT ? min(a.cu_seqlens[b + 1] - lo, a.max_rows) : paged_len(a.cache, b);
@@ -277,16 +310,48 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
   int32_t* p_out = a.pos_out + unit * cap;
   const bool copy_w = w_out != nullptr && w_out != weight, copy_p = p_out != pos;
   const int budget = a.budget;
-  const int ipt = (n + NT - 1) / NT, j0 = warp * ipt * 32 + lane;   // this lane's rows: j0 + 32 i, i < ipt
+  const int per_cta = ((n + n_cta - 1) / n_cta + 31) / 32 * 32;   // rows of a CTA
+  const int c0 = min(rank * per_cta, n), c1 = min(c0 + per_cta, n);
+  const int ipt = (c1 - c0 + NT - 1) / NT, j0 = c0 + warp * ipt * 32 + lane;   // this lane's rows: j0 + 32 i < c1, i < ipt
+  const int per_row = a.row_bytes / 16, rows_at_once = NT / per_row, part = (tid % per_row) * 16;
+  // rows src(i), i0 <= i < i1, of the packed prompt (counted from the sequence's first) -> rows i of the pages
+  auto copy_prompt = [&](int i0, int i1, auto src) {
+    const char *kp = reinterpret_cast<const char*>(a.k_packed), *vp = reinterpret_cast<const char*>(a.v_packed);
+    constexpr int U = 4;   // rows a thread has in flight
+    for (int i = i0 + tid / per_row; i < i1; i += U * rows_at_once) {
+      uint4 x[U], y[U];
+      int64_t dst[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int m = i + k * rows_at_once;
+        dst[k] = -1;
+        if (m >= i1) continue;
+        bool ok;
+        const int page = paged_page(a.cache, b, m / EARN_PAGE_TOKENS, ok);
+        if (!ok) continue;
+        dst[k] = (((int64_t)page * EARN_PAGE_TOKENS + m % EARN_PAGE_TOKENS) * a.Hkv + kvh) * a.row_bytes + part;
+        const int64_t at = (((int64_t)lo + src(m)) * a.Hkv + kvh) * a.row_bytes + part;
+        x[k] = __ldg(reinterpret_cast<const uint4*>(kp + at));
+        y[k] = __ldg(reinterpret_cast<const uint4*>(vp + at));
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (dst[k] < 0) continue;
+        *reinterpret_cast<uint4*>(a.cache.k + dst[k]) = x[k];
+        *reinterpret_cast<uint4*>(a.cache.v + dst[k]) = y[k];
+      }
+    }
+  };
   if (n <= budget) {   // nothing goes
-    for (int j = tid; j < n; j += NT) {
+    for (int j = c0 + tid; j < c1; j += NT) {
       if (copy_w) w_out[j] = weight[j];
       if (copy_p) p_out[j] = PROMPT ? j : pos[j];
     }
-    if (!PROMPT && tid == 0) a.n_moves[unit] = 0;
-    return;
+    if (PROMPT && copy_here) copy_prompt(c0, c1, [](int m) { return m; });
+    if (!PROMPT && !copy_here && rank == 0 && tid == 0) a.n_moves[unit] = 0;
+    return;   // (the whole cluster leaves here)
   }
-  const bool few = !PROMPT && n - budget <= FEW;   // block-uniform
+  const bool few = !PROMPT && n_cta == 1 && n - budget <= FEW;   // block-uniform
   if (!few)
     for (int i = tid; i < 7 * 256; i += NT) (&sh.hist[0][0])[i] = 0;
   // ---- keys
@@ -294,29 +359,34 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
   float w[IPT];
   int p[IPT];
   int last = n - 1;
-  {
 #pragma unroll
-    for (int i = 0; i < IPT; ++i) {
-      const int j = j0 + 32 * i;
-      const bool in = i < ipt && j < n;
-      w[i] = in ? weight[j] : 0.f;
-      p[i] = PROMPT ? j : in ? pos[j] : INT_MIN;
-    }
-    if (!PROMPT) {   // the newest token's position
-      int m = INT_MIN;
+  for (int i = 0; i < IPT; ++i) {
+    const int j = j0 + 32 * i;
+    const bool in = i < ipt && j < c1;
+    w[i] = in ? weight[j] : 0.f;
+    p[i] = PROMPT ? j : in ? pos[j] : INT_MIN;
+  }
+  if (!PROMPT) {   // the newest token's position
+    int m = INT_MIN;
 #pragma unroll
-      for (int i = 0; i < IPT; ++i) m = max(m, p[i]);
-      m = __reduce_max_sync(0xffffffffu, m);
-      if (lane == 0) sh.last[warp] = m;
+    for (int i = 0; i < IPT; ++i) m = max(m, p[i]);
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (lane == 0) sh.last[warp] = m;
+  }
+  __syncthreads();   // (the histograms are cleared, too)
+  if (!PROMPT) {
+    last = __reduce_max_sync(0xffffffffu, sh.last[lane % NW]);
+    if (n_cta > 1) {
+      if (tid == 0) sh.cta_last = last;
+      cluster_sync();
+      last = __reduce_max_sync(0xffffffffu, lane < n_cta ? peer_int(&sh.cta_last, lane) : INT_MIN);
     }
-    __syncthreads();   // (the histograms are cleared, too)
-    if (!PROMPT) last = __reduce_max_sync(0xffffffffu, sh.last[lane % NW]);
-    const int64_t after = (int64_t)last - a.n_last;
+  }
+  const int64_t after = (int64_t)last - a.n_last;
 #pragma unroll
-    for (int i = 0; i < IPT; ++i) {
-      const bool in = i < ipt && j0 + 32 * i < n;
-      u[i] = !in ? 0u : (p[i] < a.n_first || p[i] > after) ? KEY_PROTECTED : weight_key(w[i]);
-    }
+  for (int i = 0; i < IPT; ++i) {
+    const bool in = i < ipt && j0 + 32 * i < c1;
+    u[i] = !in ? 0u : (p[i] < a.n_first || p[i] > after) ? KEY_PROTECTED : weight_key(w[i]);
   }
   if (few) {
     // ---- the last rows of the order, one by one: the smallest key, and of equal ones the highest row
@@ -373,42 +443,46 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
       w_out[to] = weight[from];
       p_out[to] = pos[from];
     }
-    const uint32_t moving = __ballot_sync(0xffffffffu, from >= 0);
-    if (tid == 0) a.n_moves[unit] = move_here ? 0 : __popc(moving);
     if (warp == 0) {
-      int32_t* list = a.moves + (int64_t)unit * 2 * a.list;
       for (int t = 0; t < FEW; ++t) {
         const int f = __shfl_sync(0xffffffffu, from, t), g = __shfl_sync(0xffffffffu, to, t);
-        if (f < 0) continue;
-        if (move_here) move_row(a, b, kvh, f, g, lane, 32);
-        else if (lane == 0) { const int k = __popc(moving & ((1u << t) - 1u)); list[k] = f; list[a.list + k] = g; }
+        if (f >= 0) move_row(a, b, kvh, f, g, lane, 32);
       }
     }
     return;
   }
-  // ---- the budget-th largest key T, digit by digit from the top: `want` of the keys that agree with T so far stay.  (No
-  // row's key is 0, so the key 0 of a lane without a row is never counted.)
+  // ---- the budget-th largest key T, digit by digit from the top: `want` of the `equal` keys that agree with T so far stay.
+  // (No row's key is 0, so the key 0 of a lane without a row is never counted.)
   uint32_t T = 0;
   int want = budget, equal = 0;
 #pragma unroll
   for (int d = 3; d >= 0; --d) {
+    if (d < 3 && want == equal) break;   // cluster-uniform: every key that agrees with T stays
     int* hist = d == 3 && (lane & 3) ? sh.more[(lane & 3) - 1] : sh.hist[d];
 #pragma unroll
     for (int i = 0; i < IPT; ++i)
       if (u[i] != 0u && (d == 3 || (u[i] >> (8 * d + 8)) == (T >> (8 * d + 8)))) atomicAdd(&hist[(u[i] >> (8 * d)) & 255u], 1);
     __syncthreads();
+    int count = 0;
+    if (n_cta > 1) {
+      if (d == 3) {
+        sh.hist[3][tid] += sh.more[0][tid] + sh.more[1][tid] + sh.more[2][tid];
+      }
+      cluster_sync();
+#pragma unroll
+      for (int r = 0; r < MAX_CLUSTER; ++r)
+        if (r < n_cta) count += peer_int(&sh.hist[d][tid], r);
+    } else {
+      count = sh.hist[d][tid];
+      if (d == 3) count += sh.more[0][tid] + sh.more[1][tid] + sh.more[2][tid];
+    }
+    sh.sum[tid] = count;
+    __syncthreads();
     if (warp == 0) {
       // lane l owns bins 255 - 8 l .. 248 - 8 l; the bins of the lanes below it hold larger digits
-      int c[8];   // from the largest digit down
+      int c[8], sum = 0;   // from the largest digit down
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int bin = 255 - 8 * lane - k;
-        c[k] = sh.hist[d][bin];
-        if (d == 3) c[k] += sh.more[0][bin] + sh.more[1][bin] + sh.more[2][bin];
-      }
-      int sum = 0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum += c[k];
+      for (int k = 0; k < 8; ++k) { c[k] = sh.sum[255 - 8 * lane - k]; sum += c[k]; }
       int incl = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -427,18 +501,18 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
     want = sh.rest;
     equal = sh.equal;
   }
-  // ---- rows with a larger key stay, and the first `want` of the `equal` rows with key T
+  // ---- rows with a larger key stay, and the first `want` of the `equal` rows that agree with T
   const uint32_t lt = (1u << lane) - 1u;
   uint32_t keep = 0;   // bit i: row j0 + 32 i stays
   int2 total;
-  if (want == equal) {   // block-uniform
+  if (want == equal) {   // cluster-uniform
 #pragma unroll
-    for (int i = 0; i < IPT; ++i) keep |= u[i] >= T ? 1u << i : 0u;
+    for (int i = 0; i < IPT; ++i) keep |= u[i] >= T && u[i] != 0u ? 1u << i : 0u;
   } else {
     int eq = 0;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) eq += __popc(__ballot_sync(0xffffffffu, u[i] == T));
-    int seen = rank_base<NW>(make_int2(eq, 0), sh.ranks[0], total).x;
+    int seen = rank_base(make_int2(eq, 0), sh.ranks[0], &sh.cta_total[0], rank, n_cta, total).x;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       const uint32_t eqs = __ballot_sync(0xffffffffu, u[i] == T);
@@ -446,8 +520,8 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
       seen += __popc(eqs);
     }
   }
-  // ---- ranks (x: kept rows, or free rows below the budget; y: kept rows behind it) and the lists
-  auto is_x = [&](int i) { return PROMPT ? (keep >> i & 1u) != 0u : i < ipt && j0 + 32 * i < budget && !(keep >> i & 1u); };
+  // ---- ranks (x: kept rows, or free rows below the budget; y: kept rows behind it)
+  auto is_x = [&](int i) { return PROMPT ? (keep >> i & 1u) != 0u : i < ipt && j0 + 32 * i < min(c1, budget) && !(keep >> i & 1u); };
   auto is_y = [&](int i) { return !PROMPT && (keep >> i & 1u) && j0 + 32 * i >= budget; };
   int cx = 0, cy = 0;
 #pragma unroll
@@ -455,26 +529,22 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
     cx += __popc(__ballot_sync(0xffffffffu, is_x(i)));
     if (!PROMPT) cy += __popc(__ballot_sync(0xffffffffu, is_y(i)));
   }
-  const int2 base = rank_base<NW>(make_int2(cx, cy), sh.ranks[1], total);
+  const int2 base = rank_base(make_int2(cx, cy), sh.ranks[1], &sh.cta_total[1], rank, n_cta, total);
   int rx = base.x, ry = base.y;
-  int32_t* from = PROMPT ? nullptr : move_here ? sh.from : a.moves + (int64_t)unit * 2 * a.list;
-  int32_t* to = PROMPT ? nullptr : move_here ? sh.to : a.moves + (int64_t)unit * 2 * a.list + a.list;
-  // (what stays is read again, all of it ahead of the first store: the outputs may be the inputs, so the compiler would not)
+  int32_t* from = PROMPT ? nullptr : a.moves + (int64_t)unit * 2 * a.list;
+  int32_t* to = PROMPT ? nullptr : from + a.list;
+  // the CTA's first slot: its warp 0's base
+  if (PROMPT && tid == 0) sh.bin = base.x;
+  if (PROMPT) __syncthreads();
+  const int slot0 = PROMPT ? sh.bin : 0;
 #pragma unroll
   for (int i = 0; i < IPT; ++i) {
-    const int j = j0 + 32 * i;
-    const bool stays = (keep >> i & 1u) && (PROMPT || j < budget);
-    if (stays && copy_w) w[i] = weight[j];
-    if (!PROMPT && stays && copy_p) p[i] = pos[j];
-  }
-#pragma unroll
-  for (int i = 0; i < IPT; ++i) {
-    if (i >= ipt) break;
     const int j = j0 + 32 * i;
     const uint32_t bx = __ballot_sync(0xffffffffu, is_x(i)), by = PROMPT ? 0u : __ballot_sync(0xffffffffu, is_y(i));
     if (PROMPT) {
       if (is_x(i)) {
         const int slot = rx + __popc(bx & lt);
+        sh.src[slot - slot0] = j;
         p_out[slot] = j;
         if (copy_w) w_out[slot] = w[i];
       }
@@ -489,16 +559,50 @@ __global__ void __launch_bounds__(NT) evict_select_regs_kernel(EvictArgs a, bool
     rx += __popc(bx);
     ry += __popc(by);
   }
-  if (PROMPT) return;
-  const int n_moves = total.y;
-  __syncthreads();   // the lists are written, and nobody reads a row below the budget any more
-  if (tid == NT - 1) a.n_moves[unit] = n_moves;
-  for (int i = NT - 1 - tid; i < n_moves; i += NT) {   // (from the last warp down: the first ones move rows meanwhile)
-    w_out[to[i]] = weight[from[i]];
-    p_out[to[i]] = pos[from[i]];
+  if (PROMPT) {
+    if (copy_here) __syncthreads();
+    int kept = 0;   // by this CTA
+#pragma unroll
+    for (int k = 0; k < NW; ++k) kept += sh.ranks[1][k].x;
+    if (copy_here) copy_prompt(slot0, slot0 + kept, [&](int m) { return sh.src[m - slot0]; });
+  } else {
+    // the lists are written, and nobody reads a row below the budget any more
+    if (n_cta > 1) cluster_sync();
+    else __syncthreads();
+    const int n_moves = total.y, share = (n_moves + n_cta - 1) / n_cta, i0 = rank * share, i1 = min(i0 + share, n_moves);
+    for (int i = i0 + tid; i < i1; i += NT) {
+      const int f = from[i], t = to[i];
+      w_out[t] = weight[f];
+      p_out[t] = pos[f];
+    }
+    if (!copy_here && rank == 0 && tid == 0) a.n_moves[unit] = n_moves;
+    constexpr int U = 4;   // rows a thread has in flight
+    for (int i = copy_here ? i0 + tid / per_row : i1; i < i1; i += U * rows_at_once) {
+      uint4 x[U], y[U];
+      int64_t dst[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int m = i + k * rows_at_once;
+        dst[k] = -1;
+        if (m >= i1) continue;
+        const int f = from[m], t = to[m];
+        bool ok_from, ok_to;
+        const int pf = paged_page(a.cache, b, f / EARN_PAGE_TOKENS, ok_from), pt = paged_page(a.cache, b, t / EARN_PAGE_TOKENS, ok_to);
+        if (!ok_to) continue;
+        dst[k] = (((int64_t)pt * EARN_PAGE_TOKENS + t % EARN_PAGE_TOKENS) * a.Hkv + kvh) * a.row_bytes + part;
+        const int64_t at = (((int64_t)pf * EARN_PAGE_TOKENS + f % EARN_PAGE_TOKENS) * a.Hkv + kvh) * a.row_bytes + part;
+        x[k] = *reinterpret_cast<const uint4*>(a.cache.k + at);
+        y[k] = *reinterpret_cast<const uint4*>(a.cache.v + at);
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (dst[k] < 0) continue;
+        *reinterpret_cast<uint4*>(a.cache.k + dst[k]) = x[k];
+        *reinterpret_cast<uint4*>(a.cache.v + dst[k]) = y[k];
+      }
+    }
   }
-  if (move_here)
-    for (int i = warp; i < n_moves; i += NW) move_row(a, b, kvh, from[i], to[i], lane, 32);
+  if (n_cta > 1) cluster_sync();   // the other CTAs have read this one's shared memory
 }
 
 // The step form's moves, ROWS_PER_CTA of one (sequence, kv head) per CTA; 8, 16 or 32 threads a row
@@ -545,41 +649,65 @@ __global__ void __launch_bounds__(256) evict_gather_kernel(EvictArgs a) {
   }
 }
 
-template <int NT, bool PROMPT, bool STAGED>
-cudaError_t launch_select(const EvictArgs& a, bool move_here, cudaStream_t st) {
+template <int THREADS, bool PROMPT, bool STAGED>
+cudaError_t launch_select(const EvictArgs& a, cudaStream_t st) {
   const int smem = STAGED ? (a.max_rows + 3) / 4 * 16 : 0;
   if (STAGED) {
-    const cudaError_t e = ensure_dynamic_smem<evict_select_kernel<NT, PROMPT, STAGED>>(STAGE_ROWS * 4);
+    const cudaError_t e = ensure_dynamic_smem<evict_select_kernel<THREADS, PROMPT, STAGED>>(STAGE_ROWS * 4);
     if (e != cudaSuccess) return e;
   }
-  const cudaError_t e = launch_pdl(evict_select_kernel<NT, PROMPT, STAGED>, dim3((unsigned)a.n_seq * a.Hkv), dim3(NT), smem, st, a, move_here);
+  const cudaError_t e = launch_pdl(evict_select_kernel<THREADS, PROMPT, STAGED>, dim3((unsigned)a.n_seq * a.Hkv), dim3(THREADS), smem, st, a);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <int NT, int IPT, bool PROMPT>
-cudaError_t launch_select_regs(const EvictArgs& a, bool move_here, cudaStream_t st) {
-  const cudaError_t e = launch_pdl(evict_select_regs_kernel<NT, IPT, PROMPT>, dim3((unsigned)a.n_seq * a.Hkv), dim3(NT), 0, st, a, move_here);
+template <int IPT, bool PROMPT>
+cudaError_t launch_cluster(const EvictArgs& a, int n_cta, bool copy_here, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)a.n_seq * a.Hkv * n_cta);
+  cfg.blockDim = dim3(NT);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = n_cta;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = n_cta > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_cluster_kernel<IPT, PROMPT>, a, n_cta, copy_here);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <bool PROMPT>
 cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
-  // the most moves a (sequence, kv head) can need; up to MOVES_HERE are made by the selecting CTA
-  const int most = a.max_rows > a.budget ? (a.max_rows - a.budget < a.budget ? a.max_rows - a.budget : a.budget) : 0;
-  const bool move_here = !PROMPT && most <= MOVES_HERE;
+  const int64_t units = (int64_t)a.n_seq * a.Hkv;
+  const int excess = a.max_rows > a.budget ? a.max_rows - a.budget : 0;   // rows that go, at most
+  bool copied = false;
   cudaError_t e;
-  if (a.max_rows > STAGE_ROWS) e = launch_select<1024, PROMPT, false>(a, move_here, st);
-  else if (a.max_rows > 1024 * 16) e = launch_select<1024, PROMPT, true>(a, move_here, st);
-  else if (a.max_rows > 512 * 16) e = launch_select_regs<1024, 16, PROMPT>(a, move_here, st);
-  else if (a.max_rows > 256 * 8) e = launch_select_regs<512, 16, PROMPT>(a, move_here, st);
-  else if (a.max_rows > 128 * 4) e = launch_select_regs<256, 8, PROMPT>(a, move_here, st);
-  else e = launch_select_regs<128, 4, PROMPT>(a, move_here, st);
-  const int rows = PROMPT ? (a.max_rows < a.budget ? a.max_rows : a.budget) : most;
-  if (e != cudaSuccess || move_here || rows == 0) return e;
-  const unsigned units = (unsigned)a.n_seq * a.Hkv, gy = units < 32768u ? units : 32768u;
-  const dim3 grid((rows + ROWS_PER_CTA - 1) / ROWS_PER_CTA, gy, (units + gy - 1) / gy);
+  if (a.max_rows <= MAX_CLUSTER * NT * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
+    // CTAs per list: one if only a few rows go, otherwise as many as leave them ROWS_EACH rows while the grid
+    // stays within what is resident at once (four CTAs an SM)
+    int c = 1;
+    while (c < MAX_CLUSTER && (a.max_rows > c * NT * MAX_IPT ||
+                               ((PROMPT || excess > FEW) && a.max_rows >= 2 * c * ROWS_EACH && units * 2 * c <= 4 * sm_count())))
+      c *= 2;
+    const int per_thread = (a.max_rows + c * NT - 1) / (c * NT);
+    // A grid of more than one wave leaves the copies to a kernel of their own: CTAs that come late start copying late (1024
+    // lists of 128 to 2048 rows to 512: 97 us in one launch, 92 in two).
+    copied = units * c <= 4 * sm_count() || (!PROMPT && excess <= FEW);
+    e = per_thread <= 4   ? launch_cluster<4, PROMPT>(a, c, copied, st)
+        : per_thread <= 8 ? launch_cluster<8, PROMPT>(a, c, copied, st)
+                          : launch_cluster<16, PROMPT>(a, c, copied, st);
+  } else {
+    e = a.max_rows > STAGE_ROWS ? launch_select<1024, PROMPT, false>(a, st) : launch_select<1024, PROMPT, true>(a, st);
+  }
+  const int kept = a.max_rows < a.budget ? a.max_rows : a.budget;
+  const int rows = PROMPT ? kept : excess < a.budget ? excess : a.budget;   // to be copied, or moves, per list at most
+  if (e != cudaSuccess || copied || rows == 0) return e;
+  const unsigned gy = units < 32768 ? (unsigned)units : 32768u;
+  const dim3 grid((rows + ROWS_PER_CTA - 1) / ROWS_PER_CTA, gy, (unsigned)((units + gy - 1) / gy));
   e = PROMPT ? launch_pdl(evict_gather_kernel, grid, dim3(256), 0, st, a) : launch_pdl(evict_move_kernel, grid, dim3(256), 0, st, a);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();

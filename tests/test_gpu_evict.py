@@ -336,6 +336,9 @@ def test_evict_prompt_variants():
     run_evict_prompt([100, 40], "bf16", 2, 128, "tail", 32, 2, 2, identity=True, carry=False)
     run_evict_prompt([60000, 50], "bf16", 1, 64, "ties", 9000, 16, 64)       # a list past what shared memory holds
     run_evict_prompt([60000], "bf16", 1, 64, "zeros", 30000, 0, 5)
+    run_evict_prompt([40000, 7], "bf16", 1, 64, "tail", 5000, 16, 64)        # ... past what a cluster holds
+    run_evict_prompt([32768, 32767, 5], "bf16", 1, 64, "ties", 3000, 16, 64)
+    run_evict_prompt([9000, 2000, 100], "f32", 2, 128, "ties", 50, 0, 0)
     run_evict_prompt([10, 3], "bf16", 2, 128, "tail", 2 ** 31 - 1, 2, 2)     # a budget nothing reaches
 
 
@@ -384,6 +387,12 @@ def test_evict_variants():
     run_evict([33, 64, 50], "bf16", 2, 128, "tail", 32, 4, 4, identity=True)
     run_evict([60000, 9], "bf16", 1, 64, "ties", 20000, 16, 64)              # a list past what shared memory holds
     run_evict([60000, 9], "bf16", 1, 64, "tail", 20000, 16, 64, in_place=False)
+    run_evict([40000, 9], "bf16", 1, 64, "odd", 20000, 16, 64)
+    run_evict([32768, 9, 20000], "bf16", 1, 64, "ties", 9000, 16, 64)
+    run_evict([9000, 4100, 100], "f32", 2, 128, "zeros", 4096, 3, 40, in_place=False)
+    for excess in range(1, 10):                                              # few rows too many, some or all behind the budget
+        run_evict([300 + excess, 299, 301], "bf16", 2, 64, "odd", 300, 0, 0, in_place=excess % 2 == 0, seed=excess)
+        run_evict([40 + excess, 39, 41], "f32", 1, 64, "zeros", 40, 20, 20, seed=excess)
     run_evict([100, 20], "bf16", 2, 128, "tail", 2 ** 31 - 1, 4, 4)          # a budget nothing reaches
     run_evict([1025] * 7, "bf16", 3, 128, "tail", 1024, 16, 64)              # a step's worth
 
