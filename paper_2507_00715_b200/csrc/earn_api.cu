@@ -633,7 +633,7 @@ earn_status_t earn_key_weights(const earn_model_t* model, const earn_batch_t* ba
   if (model->n_kv_heads > 65535) return EARN_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < workspace_need(model, batch, 1)) return EARN_ERR_WORKSPACE;
   KeyWeightArgs a{};
-  a.q = q; a.k = k; a.lse = lse; a.weight = weight; a.cu_seqlens = batch->cu_seqlens;
+  a.q = q; a.k = k; a.lse = lse; a.weight = weight; a.cu_seqlens = batch->cu_seqlens; a.cu_seqlens_host = batch->cu_seqlens_host;
   a.batch = batch->batch; a.total = batch->total_tokens; a.max_seqlen = batch->max_seqlen; a.n_obs = n_obs;
   a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
   a.scale = scale_of(model);

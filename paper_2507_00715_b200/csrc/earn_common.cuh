@@ -261,6 +261,7 @@ struct KeyWeightArgs {
   const float* lse;            // [Hq, total]
   float* weight;               // [Hkv, total]
   const int32_t* cu_seqlens;
+  const int32_t* cu_seqlens_host;
   int batch, total, max_seqlen, n_obs, Hq, Hkv, D, dtype;
   float scale;
 };

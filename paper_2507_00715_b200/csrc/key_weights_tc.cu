@@ -52,13 +52,21 @@ struct Cfg {
   static_assert(8 * N_BARS + 16 <= 256 && SMEM_BYTES <= 232448, "shared memory");
 };
 
+// Where the blocks of each sequence start in the list of all blocks, for short windows (every block has about the same work, so
+// they need no sorting) of batches that fit a kernel parameter: no planning kernel, one launch (6.6 -> 4.9 us for one prompt,
+// 71 -> 67 us for 32-row windows of 128 ragged ones).
+constexpr int TABLE_SEQS = 256;
+struct KwTable {
+  int first[TABLE_SEQS + 1];
+};
+
 struct KwParams {
   const float* lse;
   float* weight;
-  const int4* plan;          // {first global row of the block, rows of the sequence from there, block, sequence}
+  const int4* plan;          // {first global row of the block, rows of the sequence from there, block, sequence}, or null: the table
   const int32_t* cu_seqlens;
   int32_t* status;
-  int Hq, Hkv, g, T, n_obs, total, n_items;
+  int batch, Hq, Hkv, g, T, n_obs, total, n_items;
   float scale_log2;
 };
 
@@ -71,14 +79,23 @@ struct Item {
 
 // The planner orders blocks by their number, highest first (for queries that is the longest key range).  Here block t has
 // the more queries the lower it is, so the order is read backwards within the sequence.
-__device__ __forceinline__ Item load_item(const KwParams& p, int i) {
+__device__ __forceinline__ Item load_item(const KwParams& p, const KwTable& table, int i) {
   const int e = i / p.Hkv;
-  const int4 t = __ldg(p.plan + e);
   Item it;
   it.kvh = i - e * p.Hkv;
-  it.lo = __ldg(p.cu_seqlens + t.w);
-  it.len = t.z * (NT * BM) + t.y;
-  it.key0 = ((it.len + NT * BM - 1) / (NT * BM) - 1 - t.z) * (NT * BM);
+  if (p.plan != nullptr) {
+    const int4 t = __ldg(p.plan + e);
+    it.lo = __ldg(p.cu_seqlens + t.w);
+    it.len = t.z * (NT * BM) + t.y;
+    it.key0 = ((it.len + NT * BM - 1) / (NT * BM) - 1 - t.z) * (NT * BM);
+  } else {
+    int b = 0;   // the last sequence whose blocks start at or before e (one without blocks starts where the next one does)
+    for (int step = TABLE_SEQS / 2; step > 0; step >>= 1)
+      if (b + step < p.batch && table.first[b + step] <= e) b += step;
+    it.lo = __ldg(p.cu_seqlens + b);
+    it.len = __ldg(p.cu_seqlens + b + 1) - it.lo;
+    it.key0 = (e - table.first[b]) * (NT * BM);
+  }
   it.first = max(max(it.len - p.n_obs, 0), it.key0);
   it.n_qt = (it.len - it.first + p.T - 1) / p.T;
   return it;
@@ -102,7 +119,8 @@ __device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
 
 template <int HD>
 __global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
-key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, KwParams p) {
+key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                      const __grid_constant__ KwTable table, KwParams p) {
   using C = Cfg<HD>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];   // (swizzled tiles need 1024-byte alignment)
   const uint32_t base = smem_u32(smem_raw);
@@ -161,37 +179,66 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   auto item_at = [&](int k) { return k * n_cta + ((k & 1) ? n_cta - 1 - (int)blockIdx.x : (int)blockIdx.x); };
   pdl_launch_dependents();
   pdl_wait();   // the plan (written by the kernel launched just before this one) and every tensor are read below
+  // Item k of this CTA, for a whole warp: the lanes look 32 items up side by side and hand them out by shuffle.  (A look-up
+  // is a chain of reads of 1000 clocks and more, and a warp stalls on it where it stands: with one an item, 70 us for the
+  // 32-row windows of 128 ragged prompts.)
+  Item mine{};
+  int mine_from = INT32_MIN / 2;
+  auto look_up = [&](int k) {
+    if (k - mine_from >= 32) {
+      mine_from = k;
+      mine = load_item(p, table, min(item_at(k + lane), p.n_items - 1));
+    }
+    const int from = k - mine_from;
+    Item it;
+    it.lo = __shfl_sync(0xffffffffu, mine.lo, from);
+    it.len = __shfl_sync(0xffffffffu, mine.len, from);
+    it.kvh = __shfl_sync(0xffffffffu, mine.kvh, from);
+    it.key0 = __shfl_sync(0xffffffffu, mine.key0, from);
+    it.first = __shfl_sync(0xffffffffu, mine.first, from);
+    it.n_qt = __shfl_sync(0xffffffffu, mine.n_qt, from);
+    return it;
+  };
 
   if (warp == 0) {
-    // ------------------------------------------------------------------ TMA producer
-    if (lane == 0) {
-      int e = 0, n = 0;   // Q tiles and items issued so far
-      bool ok = true;
-      for (int i = item_at(0); i < p.n_items && ok; i = item_at(n)) {
-        const Item it = load_item(p, i);
-        const int kb = n & 1;
-        if (n >= 2 && !mbar_wait_bounded(bar(C::BAR_KFREE + kb), ((n >> 1) - 1) & 1, abort_flag, WAIT_LIMIT)) { ok = false; break; }
+    // ------------------------------------------------------------------ TMA producer (lane 0 issues)
+    const bool leader = lane == 0;
+    auto wait = [&](int b, int parity) {   // warp-uniform result
+      return __all_sync(0xffffffffu, mbar_wait_bounded(bar(b), (uint32_t)parity & 1u, abort_flag, WAIT_LIMIT));
+    };
+    int e = 0, n = 0;   // Q tiles and items issued so far
+    bool ok = true;
+    while (item_at(n) < p.n_items && ok) {
+      const Item it = look_up(n);
+      const int kb = n & 1;
+      if (n >= 2) ok = wait(C::BAR_KFREE + kb, (n >> 1) - 1);
+      if (!ok) break;
+      if (leader) {
         const int tiles = it.key0 + BM < it.len ? NT : 1;   // the second accumulator may lie past the sequence
         mbar_expect_tx(bar(C::BAR_KFULL + kb), tiles * C::TILE);
         for (int x = 0; x < tiles; ++x)
           for (int h = 0; h < HD / 64; ++h)
             tma_load_3d(sK + (kb * NT + x) * C::TILE + h * C::HALF, &map_k, bar(C::BAR_KFULL + kb), h * 64, it.kvh, it.lo + it.key0 + x * BM);
-        ++n;
-        for (int t = 0; t < it.n_qt; ++t, ++e) {
-          const int st = e % C::NSTAGE;
-          if (e >= C::NSTAGE && !mbar_wait_bounded(bar(C::BAR_QFREE + st), ((e / C::NSTAGE) - 1) & 1, abort_flag, WAIT_LIMIT)) { ok = false; break; }
+      }
+      ++n;
+      for (int t = 0; t < it.n_qt; ++t, ++e) {
+        const int st = e % C::NSTAGE;
+        if (e >= C::NSTAGE) ok = wait(C::BAR_QFREE + st, (e / C::NSTAGE) - 1);
+        if (!ok) break;
+        if (leader) {
           mbar_expect_tx(bar(C::BAR_QFULL + st), q_bytes);
           for (int h = 0; h < HD / 64; ++h)
             tma_load_3d(sQ + st * C::TILE + h * C::HALF, &map_q, bar(C::BAR_QFULL + st), h * 64, it.kvh * p.g, it.lo + it.first + t * p.T);
         }
       }
-      if (*abort_flag) {
-        // let the copies already in flight land before the CTA gives its shared memory back
-        int none = 0;
-        for (int f = max(e - C::NSTAGE, 0); f < e; ++f) mbar_wait_bounded(bar(C::BAR_QFULL + f % C::NSTAGE), (f / C::NSTAGE) & 1, &none, WAIT_LIMIT);
-        for (int f = max(n - 2, 0); f < n; ++f) mbar_wait_bounded(bar(C::BAR_KFULL + (f & 1)), (f >> 1) & 1, &none, WAIT_LIMIT);
-      }
     }
+    if (leader && *abort_flag) {
+      // let the copies already in flight land before the CTA gives its shared memory back
+      int none = 0;
+      for (int f = max(e - C::NSTAGE, 0); f < e; ++f) mbar_wait_bounded(bar(C::BAR_QFULL + f % C::NSTAGE), (f / C::NSTAGE) & 1, &none, WAIT_LIMIT);
+      for (int f = max(n - 2, 0); f < n; ++f) mbar_wait_bounded(bar(C::BAR_KFULL + (f & 1)), (f >> 1) & 1, &none, WAIT_LIMIT);
+    }
+    __syncwarp();
   } else if (warp == 2) {
     // ------------------------------------------------------------------ denominators of the columns
     int tok[4];
@@ -202,20 +249,23 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       tok[c] = col < tile_rows ? col / p.g : INT32_MAX / 2;
       at[c] = (int64_t)(col % p.g) * p.total + (col < tile_rows ? col / p.g : 0);
     }
+    auto fetch = [&](float (&v)[4], const Item& it, int t) {
+      const float* src = p.lse + (int64_t)it.kvh * p.g * p.total + it.lo;
+      const int tok0 = it.first + t * p.T;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = tok0 + tok[c] < it.len ? __ldg(src + at[c] + tok0) * -kLog2e : -INFINITY;
+    };
     int e = 0;
     bool ok = true;
-    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
-      const Item it = load_item(p, i);
-      const float* src = p.lse + (int64_t)it.kvh * p.g * p.total + it.lo;
-      auto fetch = [&](float (&v)[4], int t) {
-        const int tok0 = it.first + t * p.T;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = tok0 + tok[c] < it.len ? __ldg(src + at[c] + tok0) * -kLog2e : -INFINITY;
-      };
-      float cur[4], nxt[4];
-      fetch(cur, 0);
+    Item it = look_up(0);
+    float cur[4], nxt[4];
+    if (item_at(0) < p.n_items) fetch(cur, it, 0);
+    for (int n = 0; item_at(n) < p.n_items && ok; ++n) {
+      const Item nxt_it = look_up(n + 1);
       for (int t = 0; t < it.n_qt; ++t, ++e) {
-        if (t + 1 < it.n_qt) fetch(nxt, t + 1);   // (in flight while this tile's slot comes free)
+        // the next tile's denominators, of this item or the next, are in flight while this tile's slot comes free
+        if (t + 1 < it.n_qt) fetch(nxt, it, t + 1);
+        else if (item_at(n + 1) < p.n_items) fetch(nxt, nxt_it, 0);
         const int st = e % C::NSTAGE;
         if (e >= C::NSTAGE &&
             !__all_sync(0xffffffffu, mbar_wait_bounded(bar(C::BAR_LFREE + st), ((e / C::NSTAGE) - 1) & 1, abort_flag, WAIT_LIMIT))) {
@@ -228,6 +278,7 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
         for (int c = 0; c < 4; ++c) cur[c] = nxt[c];
       }
+      it = nxt_it;
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
@@ -240,8 +291,8 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     };
     int e = 0, ns[NT] = {0, 0};
     bool ok = true;
-    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
-      const Item it = load_item(p, i);
+    for (int n = 0; item_at(n) < p.n_items && ok; ++n) {
+      const Item it = look_up(n);
       const int kb = n & 1;
       ok = wait(C::BAR_KFULL + kb, n >> 1);
       for (int t = 0; t < it.n_qt && ok; ++t, ++e) {
@@ -287,8 +338,8 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     for (int q = 0; q < 2; ++q) { tok_lo[q] = (half * 64 + q * 32) / p.g; tok_hi[q] = (half * 64 + q * 32 + 31) / p.g; }
     int e = 0, ns = 0;
     bool ok = true;
-    for (int n = 0, i = item_at(0); i < p.n_items && ok; i = item_at(++n)) {
-      const Item it = load_item(p, i);
+    for (int n = 0; item_at(n) < p.n_items && ok; ++n) {
+      const Item it = look_up(n);
       const int key = it.key0 + x * BM + wq * 32 + lane, key_hi = it.key0 + x * BM + wq * 32 + 31;   // this thread's, the warp's last
       float acc0 = 0.f, acc1 = 0.f;
       for (int t = 0; t < it.n_qt; ++t, ++e) {
@@ -398,19 +449,28 @@ cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int3
   const int g = a.Hq / a.Hkv, T = BC / g;
   CUtensorMap mq, mk;
   if (!tcmap::make_map(&mq, a.q, a.Hq, a.total, T, HD, g) || !tcmap::make_map(&mk, a.k, a.Hkv, a.total, BM, HD)) return cudaErrorInvalidValue;
-  // The whole batch is one group of the plan: sorted by work over all sequences and dealt back and forth the CTAs' loads
-  // come out within 2 % of the mean (8 x 4096 tokens, 8 kv heads), where groups of a few sequences left them 15 to 40 %
-  // apart.  The blocks of a (sequence, head) that run side by side still read its Q tiles through L2 together.
-  cudaError_t e = launch_tile_plan(a.cu_seqlens, a.batch, a.max_seqlen, NT * BM, 0, plan, st);
-  if (e != cudaSuccess) return e;
+  cudaError_t e;
+  KwTable table;
+  const bool by_table = a.batch <= TABLE_SEQS && (int64_t)a.n_obs * g <= 4 * BC;
+  if (by_table) {
+    table.first[0] = 0;
+    for (int i = 0; i < a.batch; ++i)
+      table.first[i + 1] = table.first[i] + (a.cu_seqlens_host[i + 1] - a.cu_seqlens_host[i] + NT * BM - 1) / (NT * BM);
+  } else {
+    // The whole batch is one group of the plan: sorted by work over all sequences and dealt back and forth the CTAs' loads
+    // come out within 2 % of the mean (8 x 4096 tokens, 8 kv heads), where groups of a few sequences left them 15 to 40 %
+    // apart.  The blocks of a (sequence, head) that run side by side still read its Q tiles through L2 together.
+    e = launch_tile_plan(a.cu_seqlens, a.batch, a.max_seqlen, NT * BM, 0, plan, st);
+    if (e != cudaSuccess) return e;
+  }
   KwParams p{};
-  p.lse = a.lse; p.weight = a.weight; p.plan = reinterpret_cast<const int4*>(plan); p.cu_seqlens = a.cu_seqlens; p.status = status;
-  p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = g; p.T = T; p.n_obs = a.n_obs; p.total = a.total;
+  p.lse = a.lse; p.weight = a.weight; p.plan = by_table ? nullptr : reinterpret_cast<const int4*>(plan); p.cu_seqlens = a.cu_seqlens; p.status = status;
+  p.batch = a.batch; p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = g; p.T = T; p.n_obs = a.n_obs; p.total = a.total;
   p.n_items = plan_entries * a.Hkv;
   p.scale_log2 = a.scale * kLog2e;
   e = ensure_dynamic_smem<key_weights_tc_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mk, p);
+  e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mk, table, p);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -13,6 +13,7 @@
 // Small calls: one launch, the chunks of a list in a cluster (below).
 // No atomics: every sum has one order.
 #include <climits>
+#include <type_traits>
 
 #include "decode_tile.cuh"
 #include "sm100_ptx.cuh"
@@ -275,29 +276,32 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ fp32
-// 128 threads per (sequence, kv head, chunk, 16 query rows), tiles of 32 rows in shared memory.  Logits: a lane per row of
-// the tile, a warp per query row (each K element read once per query row); P V: a thread per column.
+// 128 threads per (sequence, kv head, chunk, R query rows), tiles of 32 rows in shared memory, two in turn.  Logits: a lane per
+// row of the tile, a warp per quarter of the columns, so that a K element is read once for all R query rows; the quarters
+// are added through shared memory.  P V: a thread per column (at D = 64 each half of the CTA takes half the tile), a V element
+// read once for all rows.  What bounds it is shared memory: 16 bytes of K per 4 R products.
 constexpr int FT = 32;   // rows per tile
-template <int D>
+template <int D, int R>
 struct F32Smem {
   static constexpr int PITCH = D + 4;   // floats; lanes a row apart hit different banks with 16-byte reads
   float k[2][FT][PITCH], v[2][FT][D];
-  float q[16][D];
-  float s[16][FT];
-  float alpha[16];
+  float q[R][D];
+  float quarter[4][R][FT];
+  float s[R][FT];
+  float alpha[R], m[R], l[R];
 };
 
-template <int D, bool WEIGH>
+template <int D, int R, bool WEIGH>
 __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a) {
-  using S = F32Smem<D>;
+  using S = F32Smem<D, R>;
   extern __shared__ __align__(128) uint8_t smem[];
   S& sh = *reinterpret_cast<S*>(smem);
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int kvh = blockIdx.x, b = blockIdx.z;
-  const int row_tiles = (a.g + 15) / 16;
-  const int split = blockIdx.y / row_tiles, row0 = (blockIdx.y % row_tiles) * 16;
-  const int rows = min(a.g - row0, 16);
+  const int row_tiles = (a.g + R - 1) / R;
+  const int split = blockIdx.y / row_tiles, row0 = (blockIdx.y % row_tiles) * R;
+  const int rows = min(a.g - row0, R);
   const int len = paged_len(a.cache, b);
   const int begin = split * a.chunk, n = min(len - begin, a.chunk);
   if (n <= 0) return;
@@ -307,11 +311,10 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
   const float *kn = reinterpret_cast<const float*>(a.k_new), *vn = reinterpret_cast<const float*>(a.v_new);
   const int newest = kn != nullptr ? len - 1 - begin : -1;
   const int64_t new_off = ((int64_t)b * a.Hkv + kvh) * D;
-  for (int i = tid; i < 16 * D; i += 128)
-    sh.q[i / D][i % D] = i / D < rows ? reinterpret_cast<const float*>(a.q)[((int64_t)b * a.Hq + kvh * a.g + row0) * D + i] : 0.f;
 
   constexpr int CH = D / 4;   // 16-byte pieces of a row
   auto issue_tile = [&](int t) {
+#pragma unroll
     for (int i = tid; i < FT * CH; i += 128) {
       const int r = i / CH, c = (i % CH) * 4, p = t * FT + r;
       bool ok;
@@ -324,14 +327,14 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
     cp_async_commit();
   };
   issue_tile(0);
-  constexpr int HALVES = 128 / D, MY = 16 / HALVES;   // P V: a thread per column; at D = 64 each half of the CTA takes 8 query rows
+  for (int i = tid; i < R * D; i += 128)
+    sh.q[i / D][i % D] = i / D < rows ? reinterpret_cast<const float*>(a.q)[((int64_t)b * a.Hq + kvh * a.g + row0) * D + i] : 0.f;
+  constexpr int HALVES = 128 / D, JN = FT / HALVES;   // rows of the tile a thread takes in P V
   const int col = tid % D, half = tid / D;
-  float acc[MY];
+  float acc[R];
 #pragma unroll
-  for (int r = 0; r < MY; ++r) acc[r] = 0.f;
-  float m[4], l[4];   // rows warp, warp + 4, ..: kept by every lane of the warp
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+  for (int r = 0; r < R; ++r) acc[r] = 0.f;
+  if (tid < R) { sh.m[tid] = -INFINITY; sh.l[tid] = 0.f; }
   float* s_base = WEIGH ? a.scores + ((int64_t)b * a.Hkv + kvh) * a.g * a.score_ld + begin : nullptr;
 
   for (int t = 0; t < n_tiles; ++t) {
@@ -340,49 +343,58 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
     cp_async_wait<1>();
     __syncthreads();
     const int buf = t & 1, p = t * FT + lane;
+    {
+      float x[R];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+      for (int r = 0; r < R; ++r) x[r] = 0.f;
+      const int d0 = warp * (D / 4);
+#pragma unroll
+      for (int d = 0; d < D / 4; d += 4) {
+        const float4 kk = *reinterpret_cast<const float4*>(&sh.k[buf][lane][d0 + d]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float4 qq = *reinterpret_cast<const float4*>(&sh.q[r][d0 + d]);
+          x[r] = fmaf(kk.x, qq.x, x[r]); x[r] = fmaf(kk.y, qq.y, x[r]);
+          x[r] = fmaf(kk.z, qq.z, x[r]); x[r] = fmaf(kk.w, qq.w, x[r]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) sh.quarter[warp][r][lane] = x[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (R + 3) / 4; ++i) {   // softmax: a warp per query row
       const int r = warp + 4 * i;
       if (r < rows) {   // warp-uniform
-        float x = 0.f, y = 0.f;
-#pragma unroll 8
-        for (int d = 0; d < D; d += 4) {
-          const float4 kk = *reinterpret_cast<const float4*>(&sh.k[buf][lane][d]);
-          const float4 qq = *reinterpret_cast<const float4*>(&sh.q[r][d]);
-          x = fmaf(kk.x, qq.x, x); y = fmaf(kk.y, qq.y, y);
-          x = fmaf(kk.z, qq.z, x); y = fmaf(kk.w, qq.w, y);
-        }
-        const float s = p < n ? (x + y) * scale_log2 : -INFINITY;
+        const float dot = (sh.quarter[0][r][lane] + sh.quarter[1][r][lane]) + (sh.quarter[2][r][lane] + sh.quarter[3][r][lane]);
+        const float s = p < n ? dot * scale_log2 : -INFINITY;
         if (WEIGH && p < n) s_base[(int64_t)(row0 + r) * a.score_ld + p] = s;
         float mx = s;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float mn = fmaxf(m[i], mx), mu = mn == -INFINITY ? 0.f : mn;
-        const float al = exp2f(m[i] - mu), e = exp2f(s - mu);
+        const float m = sh.m[r], mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
+        const float al = exp2f(m - mu), e = exp2f(s - mu);
         float sum = e;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        l[i] = l[i] * al + sum;
-        m[i] = mn;
         sh.s[r][lane] = e;
-        if (lane == 0) sh.alpha[r] = al;
+        __syncwarp();
+        if (lane == 0) { sh.alpha[r] = al; sh.m[r] = mn; sh.l[r] = sh.l[r] * al + sum; }
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MY; ++i) {
-      const int r = half * MY + i;
-      if (r < rows) {
-        float x = acc[i] * sh.alpha[r];
-#pragma unroll 8
-        for (int j = 0; j < FT; j += 4) {
+    for (int r = 0; r < R; ++r) acc[r] *= r < rows ? sh.alpha[r] : 0.f;
+#pragma unroll 2
+    for (int j = half * JN; j < (half + 1) * JN; j += 4) {
+      const float v0 = sh.v[buf][j][col], v1 = sh.v[buf][j + 1][col], v2 = sh.v[buf][j + 2][col], v3 = sh.v[buf][j + 3][col];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r < rows) {
           const float4 pp = *reinterpret_cast<const float4*>(&sh.s[r][j]);
-          x = fmaf(pp.x, sh.v[buf][j][col], x);
-          x = fmaf(pp.y, sh.v[buf][j + 1][col], x);
-          x = fmaf(pp.z, sh.v[buf][j + 2][col], x);
-          x = fmaf(pp.w, sh.v[buf][j + 3][col], x);
+          acc[r] = fmaf(pp.x, v0, acc[r]); acc[r] = fmaf(pp.y, v1, acc[r]);
+          acc[r] = fmaf(pp.z, v2, acc[r]); acc[r] = fmaf(pp.w, v3, acc[r]);
         }
-        acc[i] = x;
       }
     }
     __syncthreads();   // the tile and the probabilities have been read
@@ -399,19 +411,20 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
   }
   pdl_launch_dependents();
   const int64_t prow = (((int64_t)b * a.Hkv + kvh) * a.n_splits + split) * a.g + row0;
+  if (tid < rows) {
+    sh.alpha[tid] = sh.l[tid] == 0.f ? 0.f : 1.f / sh.l[tid];   // (0: every logit of the chunk is -inf)
+    a.part_lse[prow + tid] = sh.m[tid] + log2f(sh.l[tid]);
+  }
+  float* other = &sh.v[0][0][0];   // the second half's sums (D = 64)
+  if (HALVES == 2 && half == 1) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = warp + 4 * i;
-    if (r < rows && lane == 0) {
-      sh.alpha[r] = l[i] == 0.f ? 0.f : 1.f / l[i];   // (0: every logit of the chunk is -inf)
-      a.part_lse[prow + r] = m[i] + log2f(l[i]);
-    }
+    for (int r = 0; r < R; ++r) other[r * D + col] = acc[r];
   }
   __syncthreads();
+  if (half == 0) {
 #pragma unroll
-  for (int i = 0; i < MY; ++i) {
-    const int r = half * MY + i;
-    if (r < rows) a.part_o[(prow + r) * D + col] = acc[i] * sh.alpha[r];
+    for (int r = 0; r < R; ++r)
+      if (r < rows) a.part_o[(prow + r) * D + col] = (HALVES == 2 ? acc[r] + other[r * D + col] : acc[r]) * sh.alpha[r];
   }
 }
 
@@ -568,9 +581,16 @@ cudaError_t launch_main(const PagedDecodeArgs& a, cudaStream_t st) {
     e = ensure_dynamic_smem<paged_decode_kernel<D, WEIGH, false>>(smem);
     if (e == cudaSuccess) e = launch_pdl(paged_decode_kernel<D, WEIGH, false>, grid, dim3(32), smem, st, a);
   } else {
-    constexpr int smem = (int)sizeof(F32Smem<D>);
-    e = ensure_dynamic_smem<paged_decode_f32_kernel<D, WEIGH>>(smem);
-    if (e == cudaSuccess) e = launch_pdl(paged_decode_f32_kernel<D, WEIGH>, grid, dim3(128), smem, st, a);
+    // query rows per CTA: four if the group has no more (fewer idle products), else sixteen
+    auto launch = [&](auto rows_tag) {
+      constexpr int R = decltype(rows_tag)::value;
+      constexpr int smem = (int)sizeof(F32Smem<D, R>);
+      cudaError_t err = ensure_dynamic_smem<paged_decode_f32_kernel<D, R, WEIGH>>(smem);
+      if (err == cudaSuccess)
+        err = launch_pdl(paged_decode_f32_kernel<D, R, WEIGH>, dim3(a.Hkv, a.n_splits * ((a.g + R - 1) / R), a.n_seq), dim3(128), smem, st, a);
+      return err;
+    };
+    e = a.g <= 4 ? launch(std::integral_constant<int, 4>{}) : launch(std::integral_constant<int, 16>{});
   }
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
