@@ -440,6 +440,7 @@ __global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n
         if (gone[m] < budget && below == rank) to = gone[m];
       }
     }
+    if (!copy_here && tid == 0) a.n_moves[unit] = 0;   // (the moves are made here all the same)
     // (nobody reads a row below the budget any more: the rows were read ahead of the barriers)
     if (from >= 0) {
       w_out[to] = weight[from];

@@ -160,3 +160,74 @@ class EarnSession:
             shared = int(lens.sum()) if layer < self.split_k else self.R * len(lens)
             total += shared + len(lens) * self.beams * generated
         return total
+
+
+class BudgetedLayers:
+    """The full layers (``l < split_k``) of a session's batch with at most ``budget`` rows per sequence and kv head.
+
+    After the prefill of a layer (with its softmax denominators) ``take_prompt`` weighs the prompt's rows by the last
+    ``n_obs`` queries and copies the budget's worth into pages of its own; the packed K/V may be dropped then.  A decode
+    step is ``begin_step``, ``decode_layer`` for every full layer (the register layers stay with the session), and
+    ``end_step``.  By default the session's prefix and suffix registers always stay and the suffix registers (at least
+    one row) do the weighing.  One beam per sequence.
+    """
+
+    def __init__(self, session: EarnSession, budget: int, n_first: Optional[int] = None, n_last: Optional[int] = None,
+                 n_obs: Optional[int] = None, paged_shuffle_seed: Optional[int] = None):
+        if session.beams != 1:
+            raise ValueError("a budgeted cache holds one beam per sequence")
+        self.session, self.budget = session, budget
+        batch, dev = session.batch, session.device
+        r_head, r_tail = batch.c.n_head_reg, batch.c.n_tail_reg
+        self.policy = B.make_evict(budget, r_head if n_first is None else n_first, r_tail if n_last is None else n_last)
+        self.n_obs = max(1, r_tail) if n_obs is None else n_obs
+        nb = batch.batch
+        lens = np.diff(batch.cu_host)
+        held = int(min(int(lens.max()) + session.max_new if nb else 1, budget + 1))   # rows during a step
+        self.pages_per_seq = max(1, -(-held // B.PAGE_TOKENS))
+        n_pages = max(1, nb * self.pages_per_seq)
+        self.block_table = None
+        if paged_shuffle_seed is not None:
+            perm = np.random.Generator(np.random.Philox(paged_shuffle_seed)).permutation(n_pages)
+            self.block_table = torch.from_numpy(perm.astype(np.int32).reshape(nb, self.pages_per_seq)).to(dev)
+        shape, rows = (n_pages, B.PAGE_TOKENS, session.Hkv, session.D), (nb, session.Hkv, B.PAGE_TOKENS * self.pages_per_seq)
+        full = range(session.split_k)
+        self.k_pages = [torch.zeros(shape, device=dev, dtype=session.dtype) for _ in full]
+        self.v_pages = [torch.zeros(shape, device=dev, dtype=session.dtype) for _ in full]
+        self.weight = [torch.zeros(rows, device=dev, dtype=torch.float32) for _ in full]
+        self.pos = [torch.zeros(rows, device=dev, dtype=torch.int32) for _ in full]
+        self.seq_len = torch.from_numpy(np.minimum(lens, budget).astype(np.int32)).to(dev)
+        self.new_pos = torch.from_numpy((lens - 1).astype(np.int32)).to(dev)
+        self.prompt_weight = torch.empty(session.Hkv, max(batch.c.total_tokens, 1), device=dev, dtype=torch.float32)
+        self.caches = [B.make_paged_cache(self.k_pages[i], self.v_pages[i], self.block_table, self.seq_len, held, self.pages_per_seq)
+                       for i in full]
+        if self.caches:
+            self.workspace = torch.empty(B.earn_paged_workspace_bytes(session.model, nb, self.caches[0]), dtype=torch.uint8, device=dev)
+            B.earn_workspace_init(self.workspace)
+
+    def take_prompt(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor) -> None:
+        """q, k, v of a full layer (packed) and the lse its prefill wrote -> the layer's pages, weights and positions."""
+        ses = self.session
+        B.earn_key_weights(ses.model, ses.batch, layer, self.n_obs, q, k, lse, self.prompt_weight, ses.workspace)
+        B.earn_evict_prompt_kv(ses.model, ses.batch, layer, self.policy, k, v, self.prompt_weight, self.caches[layer],
+                               self.weight[layer], self.pos[layer], self.workspace)
+
+    def begin_step(self) -> None:
+        self.seq_len.add_(1)
+        self.new_pos.add_(1)
+
+    def decode_layer(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The layer's decode step and its return to the budget; O [B, Hq, D]."""
+        o = out if out is not None else torch.empty_like(q)
+        nb, w, p = self.session.batch.batch, self.weight[layer], self.pos[layer]
+        B.earn_paged_decode_attn(self.session.model, nb, layer, q, k_new, v_new, self.caches[layer], o, w, w, self.new_pos, p,
+                                 self.workspace)
+        B.earn_evict_kv(self.session.model, nb, layer, self.policy, self.caches[layer], w, p, w, p, self.workspace)
+        return o
+
+    def end_step(self) -> None:
+        self.seq_len.clamp_(max=self.budget)
+
+    def device_status(self) -> int:
+        return B.earn_device_status(self.workspace)

@@ -13,7 +13,9 @@ import torch
 
 from oracle import earn_oracle as orc
 from paper_2507_00715_b200 import binding as B
-from parity_util import to_np
+from paper_2507_00715_b200 import workloads as wl
+from paper_2507_00715_b200.session import BudgetedLayers
+from parity_util import assert_close, make_session, to_np
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -339,6 +341,7 @@ def test_evict_prompt_variants():
     run_evict_prompt([40000, 7], "bf16", 1, 64, "tail", 5000, 16, 64)        # ... past what a cluster holds
     run_evict_prompt([32768, 32767, 5], "bf16", 1, 64, "ties", 3000, 16, 64)
     run_evict_prompt([9000, 2000, 100], "f32", 2, 128, "ties", 50, 0, 0)
+    run_evict_prompt([21, 40, 19, 20, 28, 0, 300] * 86 + [33], "bf16", 1, 64, "ties", 20, 2, 2)   # more than are resident at once
     run_evict_prompt([10, 3], "bf16", 2, 128, "tail", 2 ** 31 - 1, 2, 2)     # a budget nothing reaches
 
 
@@ -390,6 +393,9 @@ def test_evict_variants():
     run_evict([40000, 9], "bf16", 1, 64, "odd", 20000, 16, 64)
     run_evict([32768, 9, 20000], "bf16", 1, 64, "ties", 9000, 16, 64)
     run_evict([9000, 4100, 100], "f32", 2, 128, "zeros", 4096, 3, 40, in_place=False)
+    # more lists than are resident at once, long and hardly too long ones among them: the moves go to a second kernel
+    run_evict([21, 40, 19, 20, 28, 29, 300] * 86 + [33], "bf16", 1, 64, "ties", 20, 2, 2)
+    run_evict([21, 40, 19, 20, 28, 29, 300] * 86 + [33], "f32", 1, 64, "tail", 20, 2, 2, in_place=False)
     for excess in range(1, 10):                                              # few rows too many, some or all behind the budget
         run_evict([300 + excess, 299, 301], "bf16", 2, 64, "odd", 300, 0, 0, in_place=excess % 2 == 0, seed=excess)
         run_evict([40 + excess, 39, 41], "f32", 1, 64, "zeros", 40, 20, 20, seed=excess)
@@ -525,3 +531,84 @@ def test_two_streams_with_a_workspace_each():
         torch.cuda.synchronize()
         for (o, w), (o1, w1) in zip(got, ones):
             assert torch.equal(o, o1) and torch.equal(w, w1)
+
+
+# ------------------------------------------------------------------------------------------------ the session's form
+def budgeted(w, budget, **kw):
+    ses = make_session(w)
+    b = BudgetedLayers(ses, budget, **kw)
+    return ses, b
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("budget,n_last", [(10 ** 6, None), (64, None), (24, 8)])
+def test_budgeted_layers(dtype, d, budget, n_last):
+    """A model of two full layers through the session: with a budget nothing reaches, every decode output is that of the whole
+    cache; with a small one the outputs are the oracle's over the rows that `pos` names, and no more rows are held."""
+    w = wl.Workload("budget", batch=3, n_layers=2, split_k=2, n_q_heads=4, n_kv_heads=2, head_dim=d, dtype=dtype, prompt_len=0,
+                    lens=(90, 40, 131), r_head=4, r_tail=4, decode_steps=6, seed=51)
+    cu, lens = wl.cu_seqlens(w), wl.seqlens(w)
+    ses, bud = budgeted(w, budget, n_last=n_last, paged_shuffle_seed=3)
+    rows = []      # per layer and sequence: every token's key and value so far
+    for layer in range(2):
+        q, k, v = wl.layer_qkv(w, layer, "cuda")
+        lse = torch.empty(w.n_q_heads, int(cu[-1]), device="cuda")
+        ses.prefill_layer(layer, q, k, v, lse=lse)
+        bud.take_prompt(layer, q, k, v, lse)
+        rows.append([[list(to_np(x)[cu[b]:cu[b + 1]]) for x in (k, v)] for b in range(w.batch)])
+    for step in range(1, w.decode_steps + 1):
+        bud.begin_step()
+        for layer in range(2):
+            before = bud.pos[layer].cpu().numpy()
+            n_before = [min(int(n) + step - 1, budget) for n in lens]
+            q, k, v = wl.decode_qkv(w, layer, step, "cuda")
+            o = bud.decode_layer(layer, q, k, v)
+            if budget >= 10 ** 6:
+                whole = ses.decode_layer(layer, step, q, k, v)
+                assert_close(o, to_np(whole).astype(np.float64), dtype, "whole cache")
+            for b in range(w.batch):
+                for x, new in zip(rows[layer][b], (k, v)):
+                    x.append(to_np(new)[b])
+                ref = np.zeros((w.n_q_heads, d))
+                for h in range(2):
+                    idx = list(before[b, h, :n_before[b]]) + [len(rows[layer][b][0]) - 1]
+                    kk, vv = (np.asarray(x)[idx, h][:, None] for x in rows[layer][b])
+                    ref[2 * h:2 * h + 2] = orc.paged_decode(to_np(q)[b, 2 * h:2 * h + 2], kk, vv)[0]
+                assert_close(o[b], ref, dtype, f"step {step} layer {layer} sequence {b}")
+        bud.end_step()
+        assert bud.seq_len.tolist() == [min(int(n) + step, budget) for n in lens]
+        for layer in range(2):     # the registers and the last rows are there, and no token twice
+            p = bud.pos[layer].cpu().numpy()
+            for b in range(w.batch):
+                m = int(bud.seq_len[b])
+                for h in range(2):
+                    held = set(p[b, h, :m].tolist())
+                    assert len(held) == m and set(range(w.r_head)) <= held
+                    total = int(lens[b]) + step
+                    assert set(range(total - (w.r_tail if n_last is None else n_last), total)) <= held
+    assert bud.device_status() == B.EARN_OK
+    with pytest.raises(ValueError, match="one beam"):
+        BudgetedLayers(make_session(w.replace(beams=2)), 16)
+
+
+def test_binding_refusals_on_the_device():
+    """What the wrappers turn down before the library is called: another type, a strided view, too few elements, host memory."""
+    hq, hkv, d = 4, 2, 128
+    pool = Pool(2, hkv, d, "bf16", 2)
+    cache = pool.cache([5, 9])
+    model = model_of(hq, hkv, d, "bf16")
+    ws = workspace(B.earn_paged_workspace_bytes(model, 2, cache))
+    q = torch.zeros(2, hq, d, device="cuda", dtype=torch.bfloat16)
+    n0 = B.earn_launch_count()
+    for bad in (q.float(), torch.zeros(2, d, hq, device="cuda", dtype=torch.bfloat16).transpose(1, 2), q[:1], q.cpu()):
+        with pytest.raises(ValueError, match="q: "):
+            B.earn_paged_decode_attn(model, 2, 0, bad, None, None, cache, q, workspace=ws)
+    with pytest.raises(ValueError, match="weight_out"):
+        B.earn_paged_decode_attn(model, 2, 0, q, None, None, cache, q, weight_out=torch.zeros(2, hkv, 8, device="cuda"), workspace=ws)
+    with pytest.raises(ValueError, match="fewer than 3"):
+        B.earn_paged_decode_attn(model, 3, 0, q, None, None, cache, q, workspace=ws)
+    with pytest.raises(ValueError, match="cache of"):
+        B.earn_paged_decode_attn(model_of(hq, hkv, 64, "bf16"), 2, 0, q, None, None, cache, q, workspace=ws)
+    with pytest.raises(B.EarnError):
+        B.earn_paged_decode_attn(model, 2, 0, q, None, None, cache, q, workspace=None)
+    assert B.earn_launch_count() == n0
