@@ -31,12 +31,6 @@ struct RowMap {
   }
 };
 
-// attend() and attend2() hand the (masked, unscaled) logits of a tile's fragments to an optional sink; this one drops them.
-struct NoSink {
-  __device__ __forceinline__ void operator()(int, const float (&)[2][4]) const {}
-  __device__ __forceinline__ void operator()(int, const float (&)[4][4]) const {}
-};
-
 // One warp's 16 query rows: Q fragments, running maximum / sum (scaled log2 domain) and the output accumulator.
 // Lane l holds rows l/4 and l/4 + 8, columns 2*(l%4) + {0,1} of every 8-column block.
 template <int D>
@@ -65,9 +59,8 @@ struct RowTile {
   // One tile of KT positions: S = Q K^T, online softmax, O += P V.  ks / vs: shared-memory addresses of the K and V
   // tiles.  When `masked`, visible(column, second_row) says whether position `column` of the tile counts for the
   // lane's first (false) or second (true) row.
-  template <typename Vis, typename Sink = NoSink>
-  __device__ __forceinline__ void attend(uint32_t ks, uint32_t vs, float scale_log2, int lane, bool masked, Vis visible,
-                                         Sink sink = Sink(), int sink_at = 0) {
+  template <typename Vis>
+  __device__ __forceinline__ void attend(uint32_t ks, uint32_t vs, float scale_log2, int lane, bool masked, Vis visible) {
     constexpr int PITCH = Geo<D>::PITCH;
     const int c2 = (lane & 3) * 2, mat = lane >> 3;
     const uint32_t k_lane = (uint32_t)(((mat >> 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat & 1) * 16;
@@ -95,7 +88,6 @@ struct RowTile {
         for (int e = 0; e < 4; ++e)
           if (!visible(n * 8 + c2 + (e & 1), e >= 2)) s[n][e] = -INFINITY;
     }
-    sink(sink_at, s);
     float mx0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
     float mx1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
@@ -138,9 +130,7 @@ struct RowTile {
 
   // Two whole tiles (2 * KT positions, every one visible to every row) in one softmax step: four independent chains
   // of MMAs instead of two, one rescale of the accumulator and one round of quad shuffles per 32 positions.
-  template <typename Sink = NoSink>
-  __device__ __forceinline__ void attend2(uint32_t ksa, uint32_t vsa, uint32_t ksb, uint32_t vsb, float scale_log2, int lane,
-                                          Sink sink = Sink(), int sink_at = 0) {
+  __device__ __forceinline__ void attend2(uint32_t ksa, uint32_t vsa, uint32_t ksb, uint32_t vsb, float scale_log2, int lane) {
     constexpr int PITCH = Geo<D>::PITCH;
     const int mat = lane >> 3;
     const uint32_t k_lane = (uint32_t)(((mat >> 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat & 1) * 16;
@@ -158,7 +148,6 @@ struct RowTile {
       mma_bf16(s[2], qf[kk], c0, c1);
       mma_bf16(s[3], qf[kk], c2_, c3);
     }
-    sink(sink_at, s);
     float mx0 = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), fmaxf(fmaxf(s[2][0], s[2][1]), fmaxf(s[3][0], s[3][1])));
     float mx1 = fmaxf(fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3])), fmaxf(fmaxf(s[2][2], s[2][3]), fmaxf(s[3][2], s[3][3])));
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));

@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "earn_common.cuh"
+#include "paged_cache.cuh"
 
 namespace earn {
 

@@ -13,7 +13,7 @@
 // in shared memory while they fit, and a copying kernel behind it.
 #include <climits>
 
-#include "earn_common.cuh"
+#include "paged_cache.cuh"
 
 namespace earn {
 namespace {

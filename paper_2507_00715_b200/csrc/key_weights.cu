@@ -3,7 +3,7 @@
 // small -- and walks the (query row, head of the group) pairs of the sequence's window in tiles of 64 columns; the logits are
 // register-blocked 8 x 4 (2 x 4) over 256 threads.  Every weight is summed by
 // one CTA in one order.  FMA-bound, with three 16-byte shared-memory reads per 32 products (24 TFLOP/s, 8 whole prompts of 1024 rows at 32/8 heads: 1.46 ms).
-#include "earn_common.cuh"
+#include "paged_cache.cuh"
 
 namespace earn {
 namespace {
@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
   extern __shared__ __align__(16) float dyn[];
   float* ks = dyn;              // [D][KP]: all of the keys' columns, loaded once
   float* qs = dyn + D * KP;     // [TD][QP]
-  __shared__ float lse2[TQ];
+  __shared__ float lse[TQ];
   __shared__ int row_of[TQ];    // query row (position in the sequence) of a column, -1: none
   __shared__ int64_t q_at[TQ];  // element offset of its query
   pdl_wait();
@@ -45,7 +45,6 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
 #pragma unroll
     for (int c = 0; c < 4; ++c) ks[(d + c) * KP + r] = x[c];
   }
-  const float scale_log2 = a.scale * kLog2e;
   const int first = max(len - a.n_obs > 0 ? len - a.n_obs : 0, key0);   // rows in front of key0 see none of these keys
   const int64_t n_cols = (int64_t)(len - first) * g;
   float sum[KM];
@@ -58,7 +57,7 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
       const int row = in ? first + (int)((c0 + tid) / g) : -1, h = kvh * g + (int)((c0 + tid) % g);
       row_of[tid] = row;
       q_at[tid] = in ? ((int64_t)(lo + row) * a.Hq + h) * D : -1;
-      lse2[tid] = in ? a.lse[(int64_t)h * a.total + lo + row] * kLog2e : 0.f;
+      lse[tid] = in ? a.lse[(int64_t)h * a.total + lo + row] : 0.f;
     }
     float s[KM][4] = {};
     for (int d0 = 0; d0 < D; d0 += TD) {
@@ -93,10 +92,10 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int row = row_of[tx * 4 + j];
-      const float d = lse2[tx * 4 + j];
+      const float d = lse[tx * 4 + j];
 #pragma unroll
       for (int i = 0; i < KM; ++i)
-        if (row >= key0 + ty * KM + i) sum[i] += exp2f(fmaf(s[i][j], scale_log2, -d));   // causal; columns that do not exist: row -1
+        if (row >= key0 + ty * KM + i) sum[i] += exp2f(fmaf(s[i][j], a.scale, -d) * kLog2e);   // causal; columns that do not exist: row -1
     }
   }
 #pragma unroll

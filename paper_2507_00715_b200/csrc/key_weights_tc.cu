@@ -22,7 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "earn_common.cuh"
+#include "paged_cache.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_maps.cuh"
 
@@ -376,6 +376,8 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           for (int c = 0; c < 32; c += 4) {
             const float4 l = l4[q * 8 + (c >> 2)];
             float e0, e1, e2, e3;
+            // (subtracting in the natural domain and multiplying by log2 e afterwards: no more exact, 8e-7 either way -- the
+            // matrix unit's truncating sums are the larger part -- and 3 % slower)
             fma2(e0, e1, __uint_as_float(a[c]), __uint_as_float(a[c + 1]), sl2, l.x, l.y);
             fma2(e2, e3, __uint_as_float(a[c + 2]), __uint_as_float(a[c + 3]), sl2, l.z, l.w);
             add2(acc0, acc1, ex2(e0), ex2(e1));   // (a share of the exponentials as polynomials on the FMA pipe: no faster,
@@ -444,11 +446,23 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   }
 }
 
+// packed [total, heads, HD] bf16 as tcmap::make_map describes it, but with boxes of `box_heads` heads
+inline bool make_map(CUtensorMap* map, const void* ptr, int heads, int total, int head_dim, int box_heads, int box_rows) {
+  auto fn = tcmap::encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)total};
+  cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)heads * head_dim * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int HD>
 cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int32_t* status, cudaStream_t st) {
   const int g = a.Hq / a.Hkv, T = BC / g;
   CUtensorMap mq, mk;
-  if (!tcmap::make_map(&mq, a.q, a.Hq, a.total, T, HD, g) || !tcmap::make_map(&mk, a.k, a.Hkv, a.total, BM, HD)) return cudaErrorInvalidValue;
+  if (!make_map(&mq, a.q, a.Hq, a.total, HD, g, T) || !make_map(&mk, a.k, a.Hkv, a.total, HD, 1, BM)) return cudaErrorInvalidValue;
   cudaError_t e;
   KwTable table;
   const bool by_table = a.batch <= TABLE_SEQS && (int64_t)a.n_obs * g <= 4 * BC;

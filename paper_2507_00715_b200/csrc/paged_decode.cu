@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "decode_tile.cuh"
+#include "paged_cache.cuh"
 #include "sm100_ptx.cuh"
 
 namespace earn {
@@ -23,6 +24,160 @@ namespace {
 using namespace dec;
 
 constexpr int STAGES = 4;
+
+// One warp's 16 query rows against tiles of 16 or 32 positions, as RowTile, with the logits of every tile handed on:
+// sink(at, fragments) receives the (masked, unscaled) logits of the 8-column blocks that start at tile `at`.
+template <int D>
+struct PagedTile : RowTile<D> {
+  using Base = RowTile<D>;
+  using Base::KSTEPS;
+  using Base::NTILES;
+  using Base::l0;
+  using Base::l1;
+  using Base::m0;
+  using Base::m1;
+  using Base::o;
+  using Base::qf;
+
+  // One tile of KT positions: S = Q K^T, online softmax, O += P V.  ks / vs: shared-memory addresses of the K and V
+  // tiles.  When `masked`, visible(column, second_row) says whether position `column` of the tile counts for the
+  // lane's first (false) or second (true) row.
+  template <typename Vis, typename Sink>
+  __device__ __forceinline__ void attend(uint32_t ks, uint32_t vs, float scale_log2, int lane, bool masked, Vis visible,
+                                         Sink sink, int at) {
+    constexpr int PITCH = Geo<D>::PITCH;
+    const int c2 = (lane & 3) * 2, mat = lane >> 3;
+    const uint32_t k_lane = (uint32_t)(((mat >> 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat & 1) * 16;
+    const uint32_t v_lane = (uint32_t)(((mat & 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat >> 1) * 16;
+    // two accumulator sets per 8-column block (even / odd k-steps) halve the chain of dependent MMAs
+    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, s2[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; kk += 2) {
+      uint32_t b0, b1, b2, b3, c0, c1, c2_, c3;
+      ldsm_x4(ks + k_lane + kk * 32, b0, b1, b2, b3);
+      ldsm_x4(ks + k_lane + (kk + 1) * 32, c0, c1, c2_, c3);
+      mma_bf16(s[0], qf[kk], b0, b1);
+      mma_bf16(s[1], qf[kk], b2, b3);
+      mma_bf16(s2[0], qf[kk + 1], c0, c1);
+      mma_bf16(s2[1], qf[kk + 1], c2_, c3);
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[n][e] += s2[n][e];
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!visible(n * 8 + c2 + (e & 1), e >= 2)) s[n][e] = -INFINITY;
+    }
+    sink(at, s);
+    float mx0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+    float mx1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
+    const float mn0 = fmaxf(m0, mx0 * scale_log2), mn1 = fmaxf(m1, mx1 * scale_log2);
+    const float mu0 = (mn0 == -INFINITY) ? 0.f : mn0, mu1 = (mn1 == -INFINITY) ? 0.f : mn1;
+    const float al0 = ex2(m0 - mu0), al1 = ex2(m1 - mu1);
+    const bool grew = (mn0 != m0) || (mn1 != m1);
+    m0 = mn0;
+    m1 = mn1;
+    uint32_t pf[4];
+    {
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float p0 = ex2(fmaf(s[n][0], scale_log2, -mu0)), p1 = ex2(fmaf(s[n][1], scale_log2, -mu0));
+        const float p2 = ex2(fmaf(s[n][2], scale_log2, -mu1)), p3 = ex2(fmaf(s[n][3], scale_log2, -mu1));
+        sum0 += p0 + p1;
+        sum1 += p2 + p3;
+        pf[n * 2] = pack2(p0, p1);
+        pf[n * 2 + 1] = pack2(p2, p3);
+      }
+      l0 = l0 * al0 + sum0;   // per-lane partial sums; reduced over the quad by finish()
+      l1 = l1 * al1 + sum1;
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int n = 0; n < NTILES; ++n) { o[n][0] *= al0; o[n][1] *= al0; o[n][2] *= al1; o[n][3] *= al1; }
+    }
+#pragma unroll
+    for (int nn = 0; nn < NTILES / 2; ++nn) {
+      uint32_t b0, b1, b2, b3;
+      ldsm_x4_t(vs + v_lane + nn * 32, b0, b1, b2, b3);
+      mma_bf16(o[2 * nn], pf, b0, b1);
+      mma_bf16(o[2 * nn + 1], pf, b2, b3);
+    }
+  }
+
+  // Two whole tiles (2 * KT positions, every one visible to every row) in one softmax step: four independent chains
+  // of MMAs instead of two, one rescale of the accumulator and one round of quad shuffles per 32 positions.
+  template <typename Sink>
+  __device__ __forceinline__ void attend2(uint32_t ksa, uint32_t vsa, uint32_t ksb, uint32_t vsb, float scale_log2, int lane,
+                                          Sink sink, int at) {
+    constexpr int PITCH = Geo<D>::PITCH;
+    const int mat = lane >> 3;
+    const uint32_t k_lane = (uint32_t)(((mat >> 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat & 1) * 16;
+    const uint32_t v_lane = (uint32_t)(((mat & 1) << 3) + (lane & 7)) * PITCH + (uint32_t)(mat >> 1) * 16;
+    float s[4][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; ++kk) {
+      uint32_t b0, b1, b2, b3, c0, c1, c2_, c3;
+      ldsm_x4(ksa + k_lane + kk * 32, b0, b1, b2, b3);
+      ldsm_x4(ksb + k_lane + kk * 32, c0, c1, c2_, c3);
+      mma_bf16(s[0], qf[kk], b0, b1);
+      mma_bf16(s[1], qf[kk], b2, b3);
+      mma_bf16(s[2], qf[kk], c0, c1);
+      mma_bf16(s[3], qf[kk], c2_, c3);
+    }
+    sink(at, s);
+    float mx0 = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), fmaxf(fmaxf(s[2][0], s[2][1]), fmaxf(s[3][0], s[3][1])));
+    float mx1 = fmaxf(fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3])), fmaxf(fmaxf(s[2][2], s[2][3]), fmaxf(s[3][2], s[3][3])));
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
+    const float mn0 = fmaxf(m0, mx0 * scale_log2), mn1 = fmaxf(m1, mx1 * scale_log2);   // finite: every position is visible
+    const float al0 = ex2(m0 - mn0), al1 = ex2(m1 - mn1);
+    const bool grew = (mn0 != m0) || (mn1 != m1);
+    m0 = mn0;
+    m1 = mn1;
+    uint32_t pf[2][4];
+    {
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float p0 = ex2(fmaf(s[n][0], scale_log2, -mn0)), p1 = ex2(fmaf(s[n][1], scale_log2, -mn0));
+        const float p2 = ex2(fmaf(s[n][2], scale_log2, -mn1)), p3 = ex2(fmaf(s[n][3], scale_log2, -mn1));
+        sum0 += p0 + p1;
+        sum1 += p2 + p3;
+        pf[n >> 1][(n & 1) * 2] = pack2(p0, p1);
+        pf[n >> 1][(n & 1) * 2 + 1] = pack2(p2, p3);
+      }
+      l0 = l0 * al0 + sum0;
+      l1 = l1 * al1 + sum1;
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int n = 0; n < NTILES; ++n) { o[n][0] *= al0; o[n][1] *= al0; o[n][2] *= al1; o[n][3] *= al1; }
+    }
+#pragma unroll
+    for (int nn = 0; nn < NTILES / 2; ++nn) {
+      uint32_t b0, b1, b2, b3, c0, c1, c2_, c3;
+      ldsm_x4_t(vsa + v_lane + nn * 32, b0, b1, b2, b3);
+      ldsm_x4_t(vsb + v_lane + nn * 32, c0, c1, c2_, c3);
+      mma_bf16(o[2 * nn], pf[0], b0, b1);
+      mma_bf16(o[2 * nn + 1], pf[0], b2, b3);
+      mma_bf16(o[2 * nn], pf[1], c0, c1);
+      mma_bf16(o[2 * nn + 1], pf[1], c2_, c3);
+    }
+  }
+};
 
 // four rows' weights: out[0..3] = before + w for the rows j + i < n; row `fresh` (the appended one, or outside) starts from zero
 __device__ __forceinline__ void add_weights(float* out, const float4& before, int j, int n, int fresh, const float (&w)[4]) {
@@ -135,7 +290,7 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
     if (s < n_tiles) issue_tile(s);
     cp_async_commit();
   }
-  RowTile<D> t;
+  PagedTile<D> t;
   t.init(reinterpret_cast<const bf16*>(a.q), rm, lane);
 
   // logits of tile `tile` (8-column blocks 0 .. NB - 1 from its first position on) -> scores, this lane's two rows

@@ -1,5 +1,5 @@
 // Host-side TMA tensor maps shared by the tensor-core attention kernels: packed [total, H, 128] bf16 tensors, box =
-// 64 columns x `box_heads` heads (one, unless said otherwise) x `box_rows` tokens, 128-byte swizzle (a 128 x 128 tile arrives as two 64-column halves).
+// 64 columns x 1 head x `box_rows` tokens, 128-byte swizzle (a 128 x 128 tile arrives as two 64-column halves).
 #pragma once
 #include <cudaTypedefs.h>
 
@@ -20,12 +20,12 @@ inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-inline bool make_map(CUtensorMap* map, const void* ptr, int heads, int total, int box_rows, int head_dim = 128, int box_heads = 1) {
+inline bool make_map(CUtensorMap* map, const void* ptr, int heads, int total, int box_rows, int head_dim = 128) {
   auto fn = encode_fn();
   if (fn == nullptr) return false;
   cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)total};
   cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)heads * head_dim * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
