@@ -584,11 +584,17 @@ __global__ void __launch_bounds__(128) paged_decode_f32_kernel(PagedDecodeArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// The first ceil(g / 4) blocks of a (sequence, kv head) take four output rows each, two warps to a row: the partials, weighted
-// by 2^(their LSE - LSE of all).  The blocks behind them take JOIN_KEYS rows of the list each: their weights.  What a block
+// The first blocks of a (sequence, kv head) take ROWS output rows each, the warps shared out to them: the partials, weighted
+// by 2^(their LSE - LSE of all).  The blocks behind them take KEYS rows of the list each: their weights.  Four rows and 2048
+// keys a block, so that the blocks of a batch make one wave; one row and 1024 keys where the lists are few (and cut into many
+// chunks: one list of 16384 rows, 8 kv heads: 30 us with the wide blocks).  What a block
 // reads does not depend on the length (only what it uses does), so the denominators, partials and logits are all asked for
 // at once: one round trip to L2 instead of the chain length -> denominators -> partials, and few enough blocks for one wave.
-constexpr int JOIN_THREADS = 256, JOIN_ROWS = 4, JOIN_KEYS = 8 * JOIN_THREADS, JOIN_AHEAD = 4, JOIN_MAX_G = 1024;
+constexpr int JOIN_THREADS = 256, JOIN_AHEAD = 4, JOIN_MAX_G = 1024;
+template <bool FEW>
+struct Join {
+  static constexpr int ROWS = FEW ? 1 : 4, KEYS = (FEW ? 4 : 8) * JOIN_THREADS;
+};
 
 // log2-domain denominator of query row r over `live` splits, by one warp; x0, x1: the lane's splits lane and lane + 32
 __device__ __forceinline__ float join_lse(const float* lse, int g, int r, int live, int lane, float x0, float x1) {
@@ -606,8 +612,9 @@ __device__ __forceinline__ float join_lse(const float* lse, int g, int r, int li
   return mu + log2f(sum);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool FEW>
 __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArgs a) {
+  constexpr int JOIN_ROWS = Join<FEW>::ROWS, JOIN_KEYS = Join<FEW>::KEYS, HALVES = JOIN_KEYS / (4 * JOIN_THREADS), WPR = JOIN_THREADS / 32 / JOIN_ROWS;
   __shared__ float lse_all[JOIN_MAX_G];
   __shared__ float4 part[JOIN_THREADS];
   pdl_wait();
@@ -618,9 +625,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
   const float* lse = a.part_lse + unit * a.n_splits * g;
   const int o_blocks = (g + JOIN_ROWS - 1) / JOIN_ROWS;
   if ((int)blockIdx.x < o_blocks) {
-    constexpr int V4 = D / 4, SUB = 32 / V4, STEP = 2 * SUB, AHEAD = 4;   // float4 per row; splits a warp, a row's two warps take at once
-    const int r = (int)blockIdx.x * JOIN_ROWS + warp / 2;
-    const int first = (warp & 1) * SUB + lane / V4;
+    constexpr int V4 = D / 4, SUB = 32 / V4, STEP = WPR * SUB, AHEAD = 4;   // float4 per row; splits a warp, a row's warps take at once
+    const int r = (int)blockIdx.x * JOIN_ROWS + warp / WPR;
+    const int first = warp % WPR * SUB + lane / V4;
     const float4* po = reinterpret_cast<const float4*>(a.part_o) + (unit * a.n_splits * g + r) * V4 + lane % V4;
     const bool in = r < g;
     float4 y[AHEAD];
@@ -649,7 +656,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
     }
     part[tid] = acc;
     __syncthreads();
-    if (in && (warp & 1) == 0 && lane < V4) {
+    if (in && warp % WPR == 0 && lane < V4) {
       float o[4] = {0.f, 0.f, 0.f, 0.f};   // (a sequence without rows: zeros)
 #pragma unroll
       for (int k = 0; k < STEP; ++k) {
@@ -665,19 +672,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
   // ---- weights
   const int key0 = ((int)blockIdx.x - o_blocks) * JOIN_KEYS + tid * 4;
   const float* sc = a.scores + unit * g * a.score_ld + key0;
-  float4 x[2][JOIN_AHEAD];
+  float4 x[HALVES][JOIN_AHEAD];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < HALVES; ++h)
 #pragma unroll
     for (int r = 0; r < JOIN_AHEAD; ++r)
-      if (r < g && key0 + h * (JOIN_KEYS / 2) < a.score_ld)
-        x[h][r] = *reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (JOIN_KEYS / 2));   // (columns past the list are not used)
+      if (r < g && key0 + h * (4 * JOIN_THREADS) < a.score_ld)
+        x[h][r] = *reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (4 * JOIN_THREADS));   // (columns past the list are not used)
   const int64_t row0 = unit * EARN_PAGE_TOKENS * a.cache.pages_per_seq;
-  float4 in[2];
+  float4 in[HALVES];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < HALVES; ++h) {
     in[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.weight && key0 + h * (JOIN_KEYS / 2) < a.score_ld) in[h] = *reinterpret_cast<const float4*>(a.weight + row0 + key0 + h * (JOIN_KEYS / 2));
+    if (a.weight && key0 + h * (4 * JOIN_THREADS) < a.score_ld) in[h] = *reinterpret_cast<const float4*>(a.weight + row0 + key0 + h * (4 * JOIN_THREADS));
   }
   const int len = paged_len(a.cache, b), live = (len + a.chunk - 1) / a.chunk;
   for (int r = warp; r < g; r += JOIN_THREADS / 32) {
@@ -688,8 +695,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
   __syncthreads();
   const int fresh = a.k_new != nullptr ? len - 1 : -1;   // the appended row starts from zero
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int j = key0 + h * (JOIN_KEYS / 2);
+  for (int h = 0; h < HALVES; ++h) {
+    const int j = key0 + h * (4 * JOIN_THREADS);
     if (j >= len) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](const float4& y, float d) { w[0] += ex2(y.x - d); w[1] += ex2(y.y - d); w[2] += ex2(y.z - d); w[3] += ex2(y.w - d); };
@@ -698,7 +705,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) paged_join_kernel(PagedDecodeArg
       if (r < g) add(x[h][r], lse_all[r]);
 #pragma unroll 4
     for (int r = JOIN_AHEAD; r < g; ++r)
-      add(*reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (JOIN_KEYS / 2)), lse_all[r]);
+      add(*reinterpret_cast<const float4*>(sc + (int64_t)r * a.score_ld + h * (4 * JOIN_THREADS)), lse_all[r]);
     add_weights(a.weight_out + row0 + j, in[h], j, len, fresh, w);
   }
 }
@@ -756,9 +763,14 @@ cudaError_t launch_d(const PagedDecodeArgs& a, cudaStream_t st) {
   if (a.cluster > 0) return a.weight_out ? launch_cluster<D, true>(a, st) : launch_cluster<D, false>(a, st);
   cudaError_t e = a.weight_out ? launch_main<D, true>(a, st) : launch_main<D, false>(a, st);
   if (e != cudaSuccess) return e;
-  const dim3 grid((a.g + JOIN_ROWS - 1) / JOIN_ROWS + (a.weight_out ? (a.cache.max_len + JOIN_KEYS - 1) / JOIN_KEYS : 0), a.Hkv, a.n_seq);
-  e = a.dtype == EARN_BF16 ? launch_pdl(paged_join_kernel<bf16, D>, grid, dim3(JOIN_THREADS), 0, st, a)
-                           : launch_pdl(paged_join_kernel<float, D>, grid, dim3(JOIN_THREADS), 0, st, a);
+  auto join = [&](auto few_tag) {
+    constexpr bool FEW = decltype(few_tag)::value;
+    constexpr int ROWS = Join<FEW>::ROWS, KEYS = Join<FEW>::KEYS;
+    const dim3 grid((a.g + ROWS - 1) / ROWS + (a.weight_out ? (a.cache.max_len + KEYS - 1) / KEYS : 0), a.Hkv, a.n_seq);
+    return a.dtype == EARN_BF16 ? launch_pdl(paged_join_kernel<bf16, D, FEW>, grid, dim3(JOIN_THREADS), 0, st, a)
+                                : launch_pdl(paged_join_kernel<float, D, FEW>, grid, dim3(JOIN_THREADS), 0, st, a);
+  };
+  e = (int64_t)a.n_seq * a.Hkv * a.g <= 2 * sm_count() ? join(std::true_type{}) : join(std::false_type{});
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -780,11 +792,12 @@ PagedPlan plan_paged_decode(int n_seq, int n_kv_heads, int g, int max_len, int d
     p.chunk = ((max_len + KT - 1) / KT + c - 1) / c * KT;
     return p;
   }
-  // about three chunks per warp slot (six one-warp CTAs an SM), so that uneven lists even out; a chunk of at least 32 rows
-  int64_t c = (units * max_len + 18 * sms - 1) / (18 * sms);
+  // One chunk per warp slot (six one-warp CTAs an SM) while that leaves it at most 256 rows; otherwise about three chunks per
+  // slot, so that uneven lists even out, of 160 to 512 rows.
+  int64_t c = (units * max_len + 6 * sms - 1) / (6 * sms);
+  if (c > kPagedMaxChunk / 2) c = c / 3 < 160 ? 160 : c / 3;
   c = (c + 31) / 32 * 32;
-  if (c < 32) c = 32;
-  if (c > kPagedMaxChunk) c = kPagedMaxChunk;
+  c = c < 32 ? 32 : c > kPagedMaxChunk ? kPagedMaxChunk : c;
   p.chunk = (int)c;
   p.n_splits = (int)((max_len + c - 1) / c);
   return p;
