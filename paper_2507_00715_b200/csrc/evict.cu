@@ -12,6 +12,7 @@
 // Lists of up to 32768 rows take one launch (evict_cluster_kernel), longer ones a selecting kernel of one CTA per list, keys
 // in shared memory while they fit, and a copying kernel behind it.
 #include <climits>
+#include <type_traits>
 
 #include "paged_cache.cuh"
 
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
   }
 }
 
-// ---- lists of at most 32768 rows: one launch.  A cluster of C CTAs of 256 threads owns a (sequence, kv head); every key is in
+// ---- lists of at most 32768 rows: one launch.  A cluster of C CTAs owns a (sequence, kv head); every key is in
 // a register (CTA r holds the r-th stretch of the list, a warp a stretch of that, row j0 + 32 i + lane), read once.
 // Four digits of 8 bits: each CTA counts a digit's 256 bins in its shared memory (a histogram of its own per digit, cleared
 // once; four copies of the first digit's, where every row counts and most fall into a few bins), the counts of the cluster
@@ -234,11 +235,11 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
 // of the moves (in place), without a second launch: while one list is still being searched, others are being copied.
 // In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one instead, by a minimum
 // over the CTA each.
-// Measured (8 kv heads, bf16, D = 128): 8 prompts of 12000 to 16384 rows to 2048 in 40 us, of which the copies are 20 at 6.7 TB/s
-// and the search with its exchanges 8 (fetching the rows that a first digit had settled into L2 meanwhile: 43 us); 64 lists of
-// 8192 rows halved in 40 us; 512 lists of 1025 rows to 1024 in 5.5 us (20 us with 11-bit digits and full scans over the
+// Measured (8 kv heads, bf16, D = 128): 8 prompts of 12000 to 16384 rows to 2048 in 37 us, of which the copies are 20 at 6.7 TB/s
+// and the search with its exchanges 7 (fetching the rows that a first digit had settled into L2 meanwhile: 3 us more); 64 lists of
+// 8192 rows halved in 38 us; 512 lists of 1025 rows to 1024 in 5.5 us (20 us with 11-bit digits and full scans over the
 // CTA, 17 with a search bit by bit).
-constexpr int NT = 256, NW = NT / 32, MAX_CLUSTER = 8, MAX_IPT = 16;
+constexpr int MAX_CLUSTER = 8, MAX_IPT = 16;
 constexpr int FEW = 8;           // rows too many that are taken out one by one
 // rows of a list a CTA of a cluster is worth (prompt form: 8 x 8 prompts of 2048 rows 34.1 us with 1024 rows each, 24.7 with 512,
 // 23.5 with 256; in place, where the moves are fewer: 19.1, 17.3 and 20.4)
@@ -262,8 +263,9 @@ __device__ __forceinline__ int peer_int(const int* p, int rank) {
   return x;
 }
 
-template <int IPT>
+template <int NT, int IPT>
 struct ClusterShared {
+  static constexpr int NW = NT / 32;
   int hist[4][256], more[3][256];   // digit d; copies of the first digit's (d = 3)
   int sum[256];                     // the digit's bins over the cluster
   int2 ranks[2][NW];
@@ -276,6 +278,7 @@ struct ClusterShared {
 };
 
 // sum over the warps in front of this one, CTAs of lower rank included (x, y), and over all of them, of one pair per warp
+template <int NW>
 __device__ __forceinline__ int2 rank_base(int2 mine, int2* slots, int2* cta_total, int rank, int n_cta, int2& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (lane == 0) slots[warp] = mine;
@@ -295,9 +298,11 @@ __device__ __forceinline__ int2 rank_base(int2 mine, int2* slots, int2* cta_tota
   return base;
 }
 
-template <int IPT, bool PROMPT>
-__global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n_cta, bool copy_here) {
-  __shared__ ClusterShared<IPT> sh;
+// NT threads a CTA, 1024 of them on an SM
+template <int NT, int IPT, bool PROMPT>
+__global__ void __launch_bounds__(NT, 1024 / NT) evict_cluster_kernel(EvictArgs a, int n_cta, bool copy_here) {
+  constexpr int NW = NT / 32;
+  __shared__ ClusterShared<NT, IPT> sh;
   pdl_wait();   // everything below reads or writes global memory
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -468,18 +473,18 @@ __global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n
     __syncthreads();
     int count = 0;
     if (n_cta > 1) {
-      if (d == 3) {
+      if (d == 3 && tid < 256) {
         sh.hist[3][tid] += sh.more[0][tid] + sh.more[1][tid] + sh.more[2][tid];
       }
       cluster_sync();
 #pragma unroll
       for (int r = 0; r < MAX_CLUSTER; ++r)
-        if (r < n_cta) count += peer_int(&sh.hist[d][tid], r);
-    } else {
+        if (r < n_cta && tid < 256) count += peer_int(&sh.hist[d][tid], r);
+    } else if (tid < 256) {
       count = sh.hist[d][tid];
       if (d == 3) count += sh.more[0][tid] + sh.more[1][tid] + sh.more[2][tid];
     }
-    sh.sum[tid] = count;
+    if (tid < 256) sh.sum[tid] = count;
     __syncthreads();
     if (warp == 0) {
       // lane l owns bins 255 - 8 l .. 248 - 8 l; the bins of the lanes below it hold larger digits
@@ -515,7 +520,7 @@ __global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n
     int eq = 0;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) eq += __popc(__ballot_sync(0xffffffffu, u[i] == T));
-    int seen = rank_base(make_int2(eq, 0), sh.ranks[0], &sh.cta_total[0], rank, n_cta, total).x;
+    int seen = rank_base<NW>(make_int2(eq, 0), sh.ranks[0], &sh.cta_total[0], rank, n_cta, total).x;
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
       const uint32_t eqs = __ballot_sync(0xffffffffu, u[i] == T);
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(NT, 4) evict_cluster_kernel(EvictArgs a, int n
     cx += __popc(__ballot_sync(0xffffffffu, is_x(i)));
     if (!PROMPT) cy += __popc(__ballot_sync(0xffffffffu, is_y(i)));
   }
-  const int2 base = rank_base(make_int2(cx, cy), sh.ranks[1], &sh.cta_total[1], rank, n_cta, total);
+  const int2 base = rank_base<NW>(make_int2(cx, cy), sh.ranks[1], &sh.cta_total[1], rank, n_cta, total);
   int rx = base.x, ry = base.y;
   int32_t* from = PROMPT ? nullptr : a.moves + (int64_t)unit * 2 * a.list;
   int32_t* to = PROMPT ? nullptr : from + a.list;
@@ -664,7 +669,7 @@ cudaError_t launch_select(const EvictArgs& a, cudaStream_t st) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <int IPT, bool PROMPT>
+template <int NT, int IPT, bool PROMPT>
 cudaError_t launch_cluster(const EvictArgs& a, int n_cta, bool copy_here, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)a.n_seq * a.Hkv * n_cta);
@@ -678,7 +683,7 @@ cudaError_t launch_cluster(const EvictArgs& a, int n_cta, bool copy_here, cudaSt
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = n_cta > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_cluster_kernel<IPT, PROMPT>, a, n_cta, copy_here);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, evict_cluster_kernel<NT, IPT, PROMPT>, a, n_cta, copy_here);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -689,20 +694,30 @@ cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
   const int excess = a.max_rows > a.budget ? a.max_rows - a.budget : 0;   // rows that go, at most
   bool copied = false;
   cudaError_t e;
-  if (a.max_rows <= MAX_CLUSTER * NT * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
+  // Threads a CTA.  More of them on a list mean fewer CTAs to a cluster and less waiting for one another (8 prompts of 12000 to
+  // 16384 rows 37.2 us with 512, 39.6 with 256); a short list, or one that loses a few rows only, is done sooner by 256
+  // (5.6 us against 8.3 for 512 lists of 1025 rows), and more lists than 512-thread CTAs are resident with them.
+  constexpr int WIDE = 512, NARROW = 256;
+  if (a.max_rows <= MAX_CLUSTER * NARROW * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
     // CTAs per list: one if only a few rows go, otherwise as many as leave them ROWS_EACH (_PROMPT) rows while the grid
-    // stays within what is resident at once (four CTAs an SM)
+    // stays within what is resident at once
     int c = 1;
-    while (c < MAX_CLUSTER && (a.max_rows > c * NT * MAX_IPT ||
-                               ((PROMPT || excess > FEW) && a.max_rows >= 2 * c * (PROMPT ? ROWS_EACH_PROMPT : ROWS_EACH) && units * 2 * c <= 4 * sm_count())))
+    while (c < MAX_CLUSTER && (a.max_rows > c * (c > 1 ? WIDE : NARROW) * MAX_IPT ||
+                               ((PROMPT || excess > FEW) && a.max_rows >= 2 * c * (PROMPT ? ROWS_EACH_PROMPT : ROWS_EACH) &&
+                                units * 2 * c <= 1024 / WIDE * sm_count())))
       c *= 2;
-    const int per_thread = (a.max_rows + c * NT - 1) / (c * NT);
+    const bool wide = c > 1 || ((PROMPT || excess > FEW) && a.max_rows > 4 * NARROW && units <= 1024 / WIDE * sm_count());
+    const int nt = wide ? WIDE : NARROW, per_thread = (a.max_rows + c * nt - 1) / (c * nt);
     // A grid of more than one wave leaves the copies to a kernel of their own: CTAs that come late start copying late (1024
     // lists of 128 to 2048 rows to 512: 97 us in one launch, 92 in two).
-    copied = units * c <= 4 * sm_count() || (!PROMPT && excess <= FEW);
-    e = per_thread <= 4   ? launch_cluster<4, PROMPT>(a, c, copied, st)
-        : per_thread <= 8 ? launch_cluster<8, PROMPT>(a, c, copied, st)
-                          : launch_cluster<16, PROMPT>(a, c, copied, st);
+    copied = units * c <= 1024 / nt * sm_count() || (!PROMPT && excess <= FEW);
+    auto launch = [&](auto nt_tag) {
+      constexpr int NT = decltype(nt_tag)::value;
+      return per_thread <= 4   ? launch_cluster<NT, 4, PROMPT>(a, c, copied, st)
+             : per_thread <= 8 ? launch_cluster<NT, 8, PROMPT>(a, c, copied, st)
+                               : launch_cluster<NT, 16, PROMPT>(a, c, copied, st);
+    };
+    e = wide ? launch(std::integral_constant<int, WIDE>{}) : launch(std::integral_constant<int, NARROW>{});
   } else {
     e = a.max_rows > STAGE_ROWS ? launch_select<1024, PROMPT, false>(a, st) : launch_select<1024, PROMPT, true>(a, st);
   }
