@@ -283,7 +283,7 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     const bool leader = lane == 0;
-    const uint32_t idesc = idesc_bf16_f32(BM, (tile_rows + 31) / 32 * 32, 0, 0);   // K (K-major) x Q^T (K-major); whole 32-column chunks
+    constexpr uint32_t idesc = idesc_bf16_f32(BM, BC, 0, 0);   // K (K-major) x Q^T (K-major); all columns, also those that no token fills
     constexpr uint32_t desc_hi = smem_desc_hi_sw128(1024);
     const uint32_t k_lo = smem_desc_lo(sK, 16), q_lo = smem_desc_lo(sQ, 16);
     auto wait = [&](int b, int parity) {   // warp-uniform result

@@ -90,6 +90,17 @@ def test_key_weights_ignore_what_is_outside_the_window(d):
     run_key_weights([130, 40], 4, 2, d, "f32", 20, seed=4, garbage=True)
 
 
+@pytest.mark.parametrize("hq,d", [(48, 128), (70, 128), (43, 64)])
+def test_key_weights_columns_that_no_product_fills(hq, d):
+    """Groups whose tiles leave whole accumulator columns unused, after a call that left NaN in tensor memory."""
+    cu = np.asarray([0, 4096], np.int32)
+    q = torch.full((4096, 40, 128), float("nan"), device="cuda", dtype=torch.bfloat16)
+    model, batch = model_of(40, 40, 128, "bf16"), B.Batch(cu, 0, 0)
+    ws = workspace(B.earn_workspace_bytes(model, batch, 1))
+    B.earn_prefill_attn(model, batch, 0, q, q, q, torch.empty_like(q), None, ws)
+    run_key_weights([300, 140], hq, 1, d, "bf16", 12, seed=hq)
+
+
 def test_key_weights_other_scale():
     run_key_weights([200, 131], 4, 2, 128, "bf16", 50, seed=5, scale=0.25)
 
