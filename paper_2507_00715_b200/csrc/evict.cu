@@ -9,8 +9,8 @@
 //   prompt into row m of the pages;
 //   step form: the i-th free row below the budget and the i-th kept row behind it form a move; sources and destinations are
 //   disjoint, so the moves run in any order.
-// Lists of up to 32768 rows take one launch (evict_cluster_kernel), longer ones a selecting kernel of one CTA per list, keys
-// in shared memory while they fit, and a copying kernel behind it.
+// Lists of up to 65536 rows take one launch (evict_cluster_kernel), longer ones a selecting kernel of one CTA per list and a
+// copying kernel behind it.
 #include <climits>
 #include <type_traits>
 
@@ -20,7 +20,6 @@ namespace earn {
 namespace {
 
 constexpr int DIGIT_BINS = 2048;
-constexpr int STAGE_ROWS = 48 * 1024;   // keys held in shared memory (192 KB); longer lists are read again from L2
 
 // monotone key of a weight: a larger key is a larger weight; -0 counts as 0 and NaN as -inf
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -80,9 +79,12 @@ __device__ __forceinline__ void move_row(const EvictArgs& a, int b, int kvh, int
   }
 }
 
-template <int NT, bool PROMPT, bool STAGED>
-__global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
-  extern __shared__ uint32_t staged[];
+// ---- lists of any length: one CTA per list, the keys read again from L2 for every step
+constexpr int SELECT_THREADS = 1024;
+
+template <bool PROMPT>
+__global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(EvictArgs a) {
+  constexpr int NT = SELECT_THREADS;
   __shared__ SelectShared sh;
   pdl_wait();   // everything below reads or writes global memory
   pdl_launch_dependents();
@@ -117,15 +119,10 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
     __syncthreads();
     last = sh.last;
   }
-  auto key_of = [&](int j) -> uint32_t {
+  auto key = [&](int j) -> uint32_t {
     const int64_t p = PROMPT ? j : pos[j];
     return (p < a.n_first || p > (int64_t)last - a.n_last) ? KEY_PROTECTED : weight_key(weight[j]);
   };
-  if (STAGED) {
-    for (int j = tid; j < n; j += NT) staged[j] = key_of(j);
-    __syncthreads();
-  }
-  auto key = [&](int j) -> uint32_t { return STAGED ? staged[j] : key_of(j); };
   // ---- the budget-th largest key
   uint32_t prefix = 0, mask = 0;
   int want = budget;   // how many of the keys that agree with the prefix stay
@@ -226,7 +223,7 @@ __global__ void __launch_bounds__(NT) evict_select_kernel(EvictArgs a) {
   }
 }
 
-// ---- lists of at most 32768 rows: one launch.  A cluster of C CTAs owns a (sequence, kv head); every key is in
+// ---- lists of at most 65536 rows: one launch.  A cluster of C CTAs owns a (sequence, kv head); every key is in
 // a register (CTA r holds the r-th stretch of the list, a warp a stretch of that, row j0 + 32 i + lane), read once.
 // Four digits of 8 bits: each CTA counts a digit's 256 bins in its shared memory (a histogram of its own per digit, cleared
 // once; four copies of the first digit's, where every row counts and most fall into a few bins), the counts of the cluster
@@ -657,14 +654,9 @@ __global__ void __launch_bounds__(256) evict_gather_kernel(EvictArgs a) {
   }
 }
 
-template <int THREADS, bool PROMPT, bool STAGED>
+template <bool PROMPT>
 cudaError_t launch_select(const EvictArgs& a, cudaStream_t st) {
-  const int smem = STAGED ? (a.max_rows + 3) / 4 * 16 : 0;
-  if (STAGED) {
-    const cudaError_t e = ensure_dynamic_smem<evict_select_kernel<THREADS, PROMPT, STAGED>>(STAGE_ROWS * 4);
-    if (e != cudaSuccess) return e;
-  }
-  const cudaError_t e = launch_pdl(evict_select_kernel<THREADS, PROMPT, STAGED>, dim3((unsigned)a.n_seq * a.Hkv), dim3(THREADS), smem, st, a);
+  const cudaError_t e = launch_pdl(evict_select_kernel<PROMPT>, dim3((unsigned)a.n_seq * a.Hkv), dim3(SELECT_THREADS), 0, st, a);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -698,7 +690,7 @@ cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
   // 16384 rows 37.2 us with 512, 39.6 with 256); a short list, or one that loses a few rows only, is done sooner by 256
   // (5.6 us against 8.3 for 512 lists of 1025 rows), and more lists than 512-thread CTAs are resident with them.
   constexpr int WIDE = 512, NARROW = 256;
-  if (a.max_rows <= MAX_CLUSTER * NARROW * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
+  if (a.max_rows <= MAX_CLUSTER * WIDE * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
     // CTAs per list: one if only a few rows go, otherwise as many as leave them ROWS_EACH (_PROMPT) rows while the grid
     // stays within what is resident at once
     int c = 1;
@@ -719,7 +711,7 @@ cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
     };
     e = wide ? launch(std::integral_constant<int, WIDE>{}) : launch(std::integral_constant<int, NARROW>{});
   } else {
-    e = a.max_rows > STAGE_ROWS ? launch_select<1024, PROMPT, false>(a, st) : launch_select<1024, PROMPT, true>(a, st);
+    e = launch_select<PROMPT>(a, st);
   }
   const int kept = a.max_rows < a.budget ? a.max_rows : a.budget;
   const int rows = PROMPT ? kept : excess < a.budget ? excess : a.budget;   // to be copied, or moves, per list at most

@@ -90,6 +90,13 @@ def test_key_weights_ignore_what_is_outside_the_window(d):
     run_key_weights([130, 40], 4, 2, d, "f32", 20, seed=4, garbage=True)
 
 
+def test_key_weights_many_sequences():
+    """Batches past what the block table of the short windows holds (256 sequences), and just at it; empty ones at either end."""
+    run_key_weights([0, 0] + [(11 * i) % 40 for i in range(252)] + [0, 0], 4, 2, 64, "bf16", 3, seed=8)
+    run_key_weights([0] + [(11 * i) % 40 for i in range(300)] + [0], 4, 2, 64, "bf16", 3, seed=9)
+    run_key_weights([(131 * i) % 400 for i in range(20)], 6, 2, 128, "bf16", 400, seed=10)
+
+
 @pytest.mark.parametrize("hq,d", [(48, 128), (70, 128), (43, 64)])
 def test_key_weights_columns_that_no_product_fills(hq, d):
     """Groups whose tiles leave whole accumulator columns unused, after a call that left NaN in tensor memory."""
@@ -203,6 +210,13 @@ def test_decode_lengths(lens):
 
 def test_decode_many_sequences():
     run_decode([(37 * i) % 300 for i in range(300)], 4, 1, 128, "bf16", seed=5)
+    run_decode([(7 * i) % 20 for i in range(2500)], 1, 1, 64, "bf16", seed=6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_many_heads(dtype):
+    run_decode([40, 3, 0], 1024, 1, 64, dtype, seed=7)        # the largest group
+    run_decode([33, 700], 128, 64, 64, dtype, seed=8)
 
 
 def test_decode_length_past_the_bound_counts_as_the_bound():
@@ -347,9 +361,11 @@ def run_evict_prompt(lens, dtype, hkv, d, kind, budget, n_first, n_last, identit
 
 def test_evict_prompt_variants():
     run_evict_prompt([100, 40], "bf16", 2, 128, "tail", 32, 2, 2, identity=True, carry=False)
-    run_evict_prompt([60000, 50], "bf16", 1, 64, "ties", 9000, 16, 64)       # a list past what shared memory holds
+    run_evict_prompt([60000, 50], "bf16", 1, 64, "ties", 9000, 16, 64)
     run_evict_prompt([60000], "bf16", 1, 64, "zeros", 30000, 0, 5)
-    run_evict_prompt([40000, 7], "bf16", 1, 64, "tail", 5000, 16, 64)        # ... past what a cluster holds
+    run_evict_prompt([70000, 7], "bf16", 1, 64, "ties", 5000, 16, 64)        # a list past what a cluster holds
+    run_evict_prompt([66000], "bf16", 1, 64, "odd", 300, 16, 64)
+    run_evict_prompt([65536, 65535, 7], "bf16", 1, 64, "tail", 5000, 16, 64)
     run_evict_prompt([32768, 32767, 5], "bf16", 1, 64, "ties", 3000, 16, 64)
     run_evict_prompt([9000, 2000, 100], "f32", 2, 128, "ties", 50, 0, 0)
     run_evict_prompt([21, 40, 19, 20, 28, 0, 300] * 86 + [33], "bf16", 1, 64, "ties", 20, 2, 2)   # more than are resident at once
@@ -399,7 +415,10 @@ def test_evict(dtype, hkv, d, kind, budget, n_first, n_last):
 
 def test_evict_variants():
     run_evict([33, 64, 50], "bf16", 2, 128, "tail", 32, 4, 4, identity=True)
-    run_evict([60000, 9], "bf16", 1, 64, "ties", 20000, 16, 64)              # a list past what shared memory holds
+    run_evict([60000, 9], "bf16", 1, 64, "ties", 20000, 16, 64)
+    run_evict([70000, 9, 66000], "bf16", 1, 64, "ties", 20000, 16, 64)       # a list past what a cluster holds
+    run_evict([70000, 9], "bf16", 1, 64, "odd", 40000, 16, 64, in_place=False)
+    run_evict([65536], "bf16", 1, 64, "tail", 65535, 16, 64)
     run_evict([60000, 9], "bf16", 1, 64, "tail", 20000, 16, 64, in_place=False)
     run_evict([40000, 9], "bf16", 1, 64, "odd", 20000, 16, 64)
     run_evict([32768, 9, 20000], "bf16", 1, 64, "ties", 9000, 16, 64)
@@ -512,6 +531,50 @@ def test_prompt_then_steps_at_the_budget(graph):
                 assert np.allclose(got_w[b, h, :m], st["w"], rtol=1e-4, atol=1e-6)
     assert pool.seq_len.tolist() == [min(n + steps, budget) for n in lens]
     assert B.earn_device_status(pws) == B.EARN_OK
+
+
+def test_mixed_outputs_and_a_decode_that_adds_in_place_by_graph():
+    """Weights in place and positions elsewhere (and the other way round) in one eviction; a captured decode replayed on changed
+    inputs, lengths among them, beside an eager call with a workspace of its own on another stream."""
+    for w_here in (True, False):
+        hkv, d, n = 2, 64, 40
+        pool, twin = Pool(2, hkv, d, "bf16", 3), Pool(2, hkv, d, "bf16", 3)
+        model, policy = model_of(hkv, hkv, d, "bf16"), B.make_evict(20, 2, 3)
+        w = torch.rand(2, hkv, pool.cap, generator=gen(1), device="cuda")
+        pos = torch.arange(pool.cap, dtype=torch.int32, device="cuda").expand(2, hkv, pool.cap).contiguous()
+        outs = []
+        for p, wo, po in ((pool, w.clone(), pos.clone()), (twin, torch.zeros_like(w), torch.zeros_like(pos))):
+            cache = p.cache([n, 33])
+            ws = workspace(B.earn_paged_workspace_bytes(model, 2, cache))
+            wi, pi = w.clone(), pos.clone()
+            if p is pool:
+                wo, po = (wi, po) if w_here else (wo, pi)
+            B.earn_evict_kv(model, 2, 0, policy, cache, wi, pi, wo, po, ws)
+            outs.append((wo[:, :, :20], po[:, :, :20], p.k, p.v))
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+    hq, hkv, d = 8, 2, 128
+    model, pool = model_of(hq, hkv, d, "bf16"), Pool(3, hkv, d, "bf16", 60)
+    cache = pool.cache([900, 5, 60], 960)
+    ws, ws2 = (workspace(B.earn_paged_workspace_bytes(model, 3, cache)) for _ in range(2))
+    q = torch.randn(3, hq, d, generator=gen(2), device="cuda").to(torch.bfloat16)
+    o, o2 = torch.empty_like(q), torch.empty_like(q)
+    w, w2 = (torch.zeros(3, hkv, pool.cap, device="cuda") for _ in range(2))
+    B.earn_paged_decode_attn(model, 3, 0, q, None, None, cache, o, w, w, None, None, ws)
+    w.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.earn_paged_decode_attn(model, 3, 0, q, None, None, cache, o, w, w, None, None, ws)
+    side = torch.cuda.Stream()
+    for lens in ([900, 5, 60], [17, 960, 0], [1, 1, 959]):
+        pool.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        q.copy_(torch.randn(q.shape, generator=gen(sum(lens)), device="cuda"))
+        side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        with torch.cuda.stream(side):
+            B.earn_paged_decode_attn(model, 3, 0, q, None, None, cache, o2, w2, w2, None, None, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(o, o2) and torch.equal(w, w2)
 
 
 def test_two_streams_with_a_workspace_each():
