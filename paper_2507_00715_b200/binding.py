@@ -312,24 +312,30 @@ def earn_train_attn_bwd(model, batch: Batch, layer, n_target, q, k, v, o, lse, d
 _TORCH_DTYPE = {EARN_F32: torch.float32, EARN_BF16: torch.bfloat16}
 
 
-def _tensor(t, what: str, dtype: torch.dtype, numel: int, device: int) -> Optional[int]:
-    """Address of a dense tensor of `dtype` on CUDA device `device` with at least `numel` elements (None stays None)."""
-    if t is None:
-        return None
+# A call is a launch or two of a few microseconds, so what stands in front of it counts: the checks are one condition per
+# tensor, and absent tensors and the workspace are passed without any.
+def _tensor(t, what: str, dtype: torch.dtype, numel: int, device: int) -> int:
+    """Address of a dense tensor of `dtype` on CUDA device `device` with at least `numel` elements."""
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.numel() >= numel and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        raise ValueError(f"{what}: {type(t).__name__}, expected a tensor") from None
     if t.dtype is not dtype:
         raise ValueError(f"{what}: {t.dtype}, expected {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: not contiguous")
     if t.numel() < numel:
         raise ValueError(f"{what}: {t.numel()} elements, expected at least {numel}")
-    if t.get_device() != device:
-        raise ValueError(f"{what}: on {t.device}, expected the current CUDA device ({device})")
-    return t.data_ptr()
+    raise ValueError(f"{what}: on {t.device}, expected the current CUDA device ({device})")
 
 
 def _stream_of(device: int) -> Optional[int]:
     """torch's current stream on `device` (the raw handle; building a torch.cuda.Stream costs a few microseconds a call)."""
     return torch._C._cuda_getCurrentRawStream(device) or None
+
+
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def make_evict(budget: int, n_first: int = 0, n_last: int = 0) -> EarnEvict:
@@ -353,8 +359,8 @@ def make_paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: 
         raise ValueError("pages_per_seq is needed without a block table")
     dev = torch.cuda.current_device()
     cache = EarnPagedCache(_tensor(k_pages, "k_pages", k_pages.dtype, 0, dev), _tensor(v_pages, "v_pages", v_pages.dtype, 0, dev),
-                           _tensor(block_table, "block_table", torch.int32, 0, dev), pages_per_seq, k_pages.shape[0],
-                           _tensor(seq_len, "seq_len", torch.int32, 0, dev),
+                           None if block_table is None else _tensor(block_table, "block_table", torch.int32, 0, dev), pages_per_seq,
+                           k_pages.shape[0], None if seq_len is None else _tensor(seq_len, "seq_len", torch.int32, 0, dev),
                            PAGE_TOKENS * pages_per_seq if max_len is None else max_len)
     # what the calls check against the model, the number of sequences and the current device
     cache.kind = (k_pages.dtype, k_pages.shape[2], k_pages.shape[3])
@@ -380,9 +386,9 @@ def earn_paged_workspace_bytes(model: EarnModel, n_seq: int, cache: EarnPagedCac
 
 def earn_key_weights(model: EarnModel, batch: Batch, layer: int, n_obs: int, q, k, lse, weight, workspace) -> None:
     """q [total, Hq, D], k [total, Hkv, D], lse fp32 [Hq, total] (earn_prefill_attn) -> weight fp32 [Hkv, total]."""
-    n, dt, dev = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], torch.cuda.current_device()
+    n, dt, dev = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], _current_device()
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
-    p, size = _ws(workspace)
+    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _check(lib().earn_key_weights(model, batch.c, layer, n_obs, _tensor(q, "q", dt, n * hq * d, dev),
                                   _tensor(k, "k", dt, n * hkv * d, dev), _tensor(lse, "lse", torch.float32, n * hq, dev),
                                   _tensor(weight, "weight", torch.float32, n * hkv, dev), p, size, _stream_of(dev)),
@@ -393,14 +399,14 @@ def earn_evict_prompt_kv(model: EarnModel, batch: Batch, layer: int, policy: Ear
                          weight_out, pos_out, workspace) -> None:
     """k, v [total, Hkv, D], weight fp32 [Hkv, total] -> the pages, weight_out fp32 (or None) and pos_out int32
     [B, Hkv, 16 * pages_per_seq].  Sequence b then holds min(L_b, budget) rows: put that into seq_len."""
-    n, n_seq, dt, dev = batch.c.total_tokens, batch.c.batch, _TORCH_DTYPE[model.dtype], torch.cuda.current_device()
+    n, n_seq, dt, dev = batch.c.total_tokens, batch.c.batch, _TORCH_DTYPE[model.dtype], _current_device()
     hkv, d = model.n_kv_heads, model.head_dim
     rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
-    p, size = _ws(workspace)
+    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _check(lib().earn_evict_prompt_kv(model, batch.c, layer, policy, _tensor(k, "k", dt, n * hkv * d, dev),
                                       _tensor(v, "v", dt, n * hkv * d, dev),
                                       _tensor(weight, "weight", torch.float32, n * hkv, dev), cache,
-                                      _tensor(weight_out, "weight_out", torch.float32, rows, dev),
+                                      None if weight_out is None else _tensor(weight_out, "weight_out", torch.float32, rows, dev),
                                       _tensor(pos_out, "pos_out", torch.int32, rows, dev), p, size, _stream_of(dev)),
            "earn_evict_prompt_kv")
 
@@ -409,25 +415,28 @@ def earn_paged_decode_attn(model: EarnModel, n_seq: int, layer: int, q, k_new, v
                            weight_out=None, new_pos=None, pos=None, workspace=None) -> None:
     """q, o [n_seq, Hq, D], k_new, v_new [n_seq, Hkv, D] (or None), weight, weight_out fp32 and pos int32
     [n_seq, Hkv, 16 * pages_per_seq] (or None), new_pos int32 [n_seq]; weight_out may be weight."""
-    dt, dev, f32, i32 = _TORCH_DTYPE[model.dtype], torch.cuda.current_device(), torch.float32, torch.int32
+    dt, dev, f32, i32 = _TORCH_DTYPE[model.dtype], _current_device(), torch.float32, torch.int32
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
     rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
     nq, nk = n_seq * hq * d, n_seq * hkv * d
-    p, size = _ws(workspace)
-    _check(lib().earn_paged_decode_attn(model, n_seq, layer, _tensor(q, "q", dt, nq, dev), _tensor(k_new, "k_new", dt, nk, dev),
-                                        _tensor(v_new, "v_new", dt, nk, dev), cache, _tensor(o, "o", dt, nq, dev),
-                                        _tensor(weight, "weight", f32, rows, dev), _tensor(weight_out, "weight_out", f32, rows, dev),
-                                        _tensor(new_pos, "new_pos", i32, n_seq, dev), _tensor(pos, "pos", i32, rows, dev),
-                                        p, size, _stream_of(dev)), "earn_paged_decode_attn")
+    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _check(lib().earn_paged_decode_attn(model, n_seq, layer, _tensor(q, "q", dt, nq, dev),
+                                        None if k_new is None else _tensor(k_new, "k_new", dt, nk, dev),
+                                        None if v_new is None else _tensor(v_new, "v_new", dt, nk, dev), cache,
+                                        _tensor(o, "o", dt, nq, dev),
+                                        None if weight is None else _tensor(weight, "weight", f32, rows, dev),
+                                        None if weight_out is None else _tensor(weight_out, "weight_out", f32, rows, dev),
+                                        None if new_pos is None else _tensor(new_pos, "new_pos", i32, n_seq, dev),
+                                        None if pos is None else _tensor(pos, "pos", i32, rows, dev), p, size, _stream_of(dev)), "earn_paged_decode_attn")
 
 
 def earn_evict_kv(model: EarnModel, n_seq: int, layer: int, policy: EarnEvict, cache: EarnPagedCache, weight, pos, weight_out,
                   pos_out, workspace) -> None:
     """weight fp32 and pos int32 [n_seq, Hkv, 16 * pages_per_seq]; weight_out / pos_out may be the same tensors.  Sequence b
     then holds min(seq_len[b], budget) rows: put that into seq_len."""
-    dt, dev, hkv, d = _TORCH_DTYPE[model.dtype], torch.cuda.current_device(), model.n_kv_heads, model.head_dim
+    dt, dev, hkv, d = _TORCH_DTYPE[model.dtype], _current_device(), model.n_kv_heads, model.head_dim
     n = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
-    p, size = _ws(workspace)
+    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _check(lib().earn_evict_kv(model, n_seq, layer, policy, cache, _tensor(weight, "weight", torch.float32, n, dev),
                                _tensor(pos, "pos", torch.int32, n, dev), _tensor(weight_out, "weight_out", torch.float32, n, dev),
                                _tensor(pos_out, "pos_out", torch.int32, n, dev), p, size, _stream_of(dev)), "earn_evict_kv")

@@ -133,7 +133,8 @@ def test_the_binding_turns_down_what_the_library_cannot_see():
         B._tensor(x, "q", torch.bfloat16, 33, 0)
     with pytest.raises(ValueError, match="expected the current CUDA device"):
         B._tensor(x, "q", torch.bfloat16, 32, 0)
-    assert B._tensor(None, "q", torch.float32, 1, 0) is None
+    with pytest.raises(ValueError, match="q: NoneType"):
+        B._tensor(None, "q", torch.bfloat16, 32, 0)
     with pytest.raises(ValueError, match="n_pages"):
         B.make_paged_cache(torch.zeros(2, 8, 2, 64), torch.zeros(2, 8, 2, 64), pages_per_seq=1)
     with pytest.raises(ValueError, match="pages_per_seq"):
