@@ -233,8 +233,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(EvictArgs 
 // In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one instead, by a minimum
 // over the CTA each.
 // Measured (8 kv heads, bf16, D = 128): 8 prompts of 12000 to 16384 rows to 2048 in 37 us, of which the copies are 20 at 6.7 TB/s
-// and the search with its exchanges 7 (fetching the rows that a first digit had settled into L2 meanwhile: 3 us more); 64 lists of
-// 8192 rows halved in 38 us; 512 lists of 1025 rows to 1024 in 5.5 us (20 us with 11-bit digits and full scans over the
+// and the exchanges of the search 7 (fetching the rows that a first digit had settled into L2 meanwhile: 3 us more); 64 lists of
+// 8192 rows halved in 38 us; 512 lists of 1025 rows to 1024 in 5.9 us (20 us with 11-bit digits and full scans over the
 // CTA, 17 with a search bit by bit).
 constexpr int MAX_CLUSTER = 8, MAX_IPT = 16;
 constexpr int FEW = 8;           // rows too many that are taken out one by one

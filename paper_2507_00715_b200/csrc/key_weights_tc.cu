@@ -119,8 +119,8 @@ __device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
 
 template <int HD>
 __global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
-key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                      const __grid_constant__ KwTable table, KwParams p) {
+key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_pad,
+                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ KwTable table, KwParams p) {
   using C = Cfg<HD>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];   // (swizzled tiles need 1024-byte alignment)
   const uint32_t base = smem_u32(smem_raw);
@@ -132,8 +132,7 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   float* s_lse = reinterpret_cast<float*>(gen + C::OFF_LSE);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile_rows = p.T * p.g;                        // columns a TMA box fills
-  const uint32_t q_bytes = (uint32_t)tile_rows * HD * 2;
+  const int tile_rows = p.T * p.g;                        // columns that belong to a token
   if (threadIdx.x == 0) {
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar(C::BAR_KFULL + s), 1);
@@ -159,13 +158,6 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
   }
-  // The rows of a Q tile that no box fills (128 is not a multiple of g) stay zero: a logit of 0 against a denominator of
-  // +inf, where leftover bits could be a NaN.
-  for (int i = threadIdx.x; i < C::NSTAGE * (HD / 64) * (BC - tile_rows) * 8; i += C::THREADS) {
-    const int piece = i & 7, r = tile_rows + (i >> 3) % (BC - tile_rows), blk = (i >> 3) / (BC - tile_rows);
-    st_shared_v4(sQ + blk * C::HALF + (uint32_t)r * 128 + piece * 16, 0u, 0u, 0u, 0u);
-  }
-  fence_async_smem();
   if (warp == 1) {
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
     tmem_relinquish();
@@ -226,9 +218,17 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         if (e >= C::NSTAGE) ok = wait(C::BAR_QFREE + st, (e / C::NSTAGE) - 1);
         if (!ok) break;
         if (leader) {
-          mbar_expect_tx(bar(C::BAR_QFULL + st), q_bytes);
+          mbar_expect_tx(bar(C::BAR_QFULL + st), C::TILE);
           for (int h = 0; h < HD / 64; ++h)
             tma_load_3d(sQ + st * C::TILE + h * C::HALF, &map_q, bar(C::BAR_QFULL + st), h * 64, it.kvh * p.g, it.lo + it.first + t * p.T);
+          // The columns left over (128 is not a multiple of g) take rows of the tile's last token once more, against a
+          // denominator of +inf.  Any key that sees them sees that token, so they add a 0 unless it adds a NaN or an
+          // infinity itself; a row of zeros would turn an infinite key, whose weight may be 0, into a NaN.
+          if (tile_rows < BC) {
+            const int last = it.lo + min(it.first + (t + 1) * p.T, it.len) - 1;
+            for (int h = 0; h < HD / 64; ++h)
+              tma_load_3d(sQ + st * C::TILE + h * C::HALF + tile_rows * 128, &map_pad, bar(C::BAR_QFULL + st), h * 64, it.kvh * p.g, last);
+          }
         }
       }
     }
@@ -463,6 +463,8 @@ cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int3
   const int g = a.Hq / a.Hkv, T = BC / g;
   CUtensorMap mq, mk;
   if (!make_map(&mq, a.q, a.Hq, a.total, HD, g, T) || !make_map(&mk, a.k, a.Hkv, a.total, HD, 1, BM)) return cudaErrorInvalidValue;
+  CUtensorMap mpad = mq;   // (BC - T g < g heads of one token)
+  if (T * g < BC && !make_map(&mpad, a.q, a.Hq, a.total, HD, BC - T * g, 1)) return cudaErrorInvalidValue;
   cudaError_t e;
   KwTable table;
   const bool by_table = a.batch <= TABLE_SEQS && (int64_t)a.n_obs * g <= 4 * BC;
@@ -484,7 +486,7 @@ cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int3
   p.scale_log2 = a.scale * kLog2e;
   e = ensure_dynamic_smem<key_weights_tc_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mk, table, p);
+  e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mpad, mk, table, p);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

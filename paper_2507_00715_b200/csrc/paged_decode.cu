@@ -12,6 +12,7 @@
 // instead of a second kernel cost 66 us there: one warp is too few for the logits.
 // Small calls: one launch, the chunks of a list in a cluster (below).
 // No atomics: every sum has one order.
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -80,8 +81,7 @@ struct PagedTile : RowTile<D> {
     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
     const float mn0 = fmaxf(m0, mx0 * scale_log2), mn1 = fmaxf(m1, mx1 * scale_log2);
-    const float mu0 = (mn0 == -INFINITY) ? 0.f : mn0, mu1 = (mn1 == -INFINITY) ? 0.f : mn1;
-    const float al0 = ex2(m0 - mu0), al1 = ex2(m1 - mu1);
+    const float al0 = ex2(m0 - mn0), al1 = ex2(m1 - mn1);
     const bool grew = (mn0 != m0) || (mn1 != m1);
     m0 = mn0;
     m1 = mn1;
@@ -90,8 +90,8 @@ struct PagedTile : RowTile<D> {
       float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        const float p0 = ex2(fmaf(s[n][0], scale_log2, -mu0)), p1 = ex2(fmaf(s[n][1], scale_log2, -mu0));
-        const float p2 = ex2(fmaf(s[n][2], scale_log2, -mu1)), p3 = ex2(fmaf(s[n][3], scale_log2, -mu1));
+        const float p0 = ex2(fmaf(s[n][0], scale_log2, -mn0)), p1 = ex2(fmaf(s[n][1], scale_log2, -mn0));
+        const float p2 = ex2(fmaf(s[n][2], scale_log2, -mn1)), p3 = ex2(fmaf(s[n][3], scale_log2, -mn1));
         sum0 += p0 + p1;
         sum1 += p2 + p3;
         pf[n * 2] = pack2(p0, p1);
@@ -142,7 +142,7 @@ struct PagedTile : RowTile<D> {
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 2));
     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 1));
     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, 2));
-    const float mn0 = fmaxf(m0, mx0 * scale_log2), mn1 = fmaxf(m1, mx1 * scale_log2);   // finite: every position is visible
+    const float mn0 = fmaxf(m0, mx0 * scale_log2), mn1 = fmaxf(m1, mx1 * scale_log2);
     const float al0 = ex2(m0 - mn0), al1 = ex2(m1 - mn1);
     const bool grew = (mn0 != m0) || (mn1 != m1);
     m0 = mn0;
@@ -292,6 +292,7 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
   }
   PagedTile<D> t;
   t.init(reinterpret_cast<const bf16*>(a.q), rm, lane);
+  t.m0 = t.m1 = -FLT_MAX;   // (a finite floor: rows whose logits are all -inf so far subtract to 2^-inf, not to NaN)
 
   // logits of tile `tile` (8-column blocks 0 .. NB - 1 from its first position on) -> scores, this lane's two rows
   const int q0 = row0 + (lane >> 2), q1 = q0 + 8, c2 = (lane & 3) * 2;
@@ -367,16 +368,15 @@ __global__ void __launch_bounds__(32) paged_decode_kernel(PagedDecodeArgs a) {
         m[k] = k < a.cluster ? peer_ld(peer_smem(at, k)) : -INFINITY;
         mx = fmaxf(mx, m[k]);
       }
-      const float mu = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
       for (int k = 0; k < kMaxCluster; ++k) {
-        m[k] = ex2(m[k] - mu);
+        m[k] = ex2(m[k] - mx);
         if (k < a.cluster) sum += m[k] * peer_ld(peer_smem(at + 64, k));
       }
       const float inv = len > 0 ? 1.f / sum : 0.f;   // (a sequence without rows: zeros)
 #pragma unroll
       for (int k = 0; k < kMaxCluster; ++k) s_wt[k * 16 + lane] = m[k] * inv;
-      s_lse[lane] = mu + log2f(sum);
+      s_lse[lane] = mx + log2f(sum);
     }
     __syncwarp();
     constexpr int V4 = D / 4;

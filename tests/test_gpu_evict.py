@@ -108,6 +108,34 @@ def test_key_weights_columns_that_no_product_fills(hq, d):
     run_key_weights([300, 140], hq, 1, d, "bf16", 12, seed=hq)
 
 
+@pytest.mark.parametrize("hq,hkv,d,n_obs", [(8, 2, 128, 400), (7, 1, 128, 400), (7, 1, 64, 20), (48, 1, 128, 30), (100, 1, 128, 9)])
+def test_key_weights_of_keys_that_overflow(hq, hkv, d, n_obs):
+    """Keys whose logit is -inf under every query have a weight of 0, whatever columns the group leaves unused; a -inf logit is
+    one of the inputs' own (an infinite channel against a positive query), so the others' tolerance is that of finite keys."""
+    lens = [300, 140]
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    g = gen(hq)
+    q = torch.randn(int(cu[-1]), hq, d, generator=g, device="cuda").to(torch.bfloat16)
+    k = torch.randn(int(cu[-1]), hkv, d, generator=g, device="cuda").to(torch.bfloat16)
+    q[..., 0] = 0.5
+    finite = to_np(k)
+    dead = torch.arange(int(cu[-1]), device="cuda") % 3 == 1
+    dead[:cu[1] - 100] |= torch.arange(int(cu[1]) - 100, device="cuda") >= 64    # a long stretch of them, too
+    k[dead, :, 0] = float("-inf")
+    qn, kn = to_np(q), to_np(k)
+    _, lse64 = orc.causal_attention(qn, kn, np.zeros_like(kn), cu)
+    lse = torch.from_numpy(lse64.astype(np.float32)).cuda()
+    w = torch.full((hkv, int(cu[-1])), 7.0, device="cuda")
+    model, batch = model_of(hq, hkv, d, "bf16"), B.Batch(cu, 0, 0)
+    ws = workspace(B.earn_workspace_bytes(model, batch, 1))
+    B.earn_key_weights(model, batch, 0, n_obs, q, k, lse, w, ws)
+    ref = orc.key_weights(qn, kn, lse.cpu().numpy(), cu, n_obs)
+    tol = delta_of(qn, finite, 1.0 / np.sqrt(d), np.abs(lse64).max()) + n_obs * (hq // hkv) * 2.0 ** -24 + 2.0 ** -23
+    got = w.double().cpu().numpy()
+    assert (got[:, dead.cpu().numpy()] == 0).all()
+    assert (np.abs(got - ref) <= tol * ref + 1e-37).all()
+
+
 def test_key_weights_other_scale():
     run_key_weights([200, 131], 4, 2, 128, "bf16", 50, seed=5, scale=0.25)
 
@@ -279,6 +307,39 @@ def test_decode_masked_places_may_hold_anything():
             outs.append((o, w))
         for o, w in outs[1:]:
             assert torch.equal(o, outs[0][0]) and torch.equal(w, outs[0][1])
+
+
+@pytest.mark.parametrize("n", [100, 1500, 5000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_keys_that_overflow(dtype, n):
+    """Whole tiles of rows with a logit of -inf, the first ones among them, get no weight and change no output."""
+    hq, hkv, d = 8, 2, 128
+    pool = Pool(1, hkv, d, dtype, -(-n // 16), seed=3)
+    cache = pool.cache([n])
+    g = gen(3)
+    q = torch.randn(1, hq, d, generator=g, device="cuda").to(DT[dtype])
+    q[..., 0] = 0.5
+    live = pool.rows(pool.k, 0).clone()
+    dead = torch.zeros(pool.cap, dtype=torch.bool, device="cuda")
+    dead[:n // 3] = True
+    dead[n // 2::2] = True
+    k = live.clone()
+    k[dead, :, 0] = float("-inf")
+    pool.k[pool.pages(0)] = k.reshape(-1, 16, hkv, d)
+    o = torch.empty_like(q)
+    w = torch.empty(1, hkv, pool.cap, device="cuda")
+    model = model_of(hq, hkv, d, dtype)
+    ws = workspace(B.earn_paged_workspace_bytes(model, 1, cache), fill=0xff)
+    B.earn_paged_decode_attn(model, 1, 0, q, None, None, cache, o, None, w, None, None, ws)
+    qn, ks, vs, gone = to_np(q[0]), to_np(live[:n]), to_np(pool.rows(pool.v, 0)[:n]), dead[:n].cpu().numpy()
+    ref, step = orc.paged_decode(qn, ks[~gone], vs[~gone])
+    dl = 2 * delta_of(qn, ks, 1.0 / np.sqrt(d), 0.0) + n * 2.0 ** -23
+    rnd = 2.0 ** -8 if dtype == "bf16" else 0.0
+    av = np.stack([orc.attention_scores(qn[a], ks[~gone][:, a // 4]) @ np.abs(vs[~gone][:, a // 4]) for a in range(hq)])
+    got, wn = o[0].double().cpu().numpy(), w[0, :, :n].double().cpu().numpy()
+    assert (np.abs(got - ref) <= (dl + rnd) * av + max(rnd, 2.0 ** -23) * np.abs(ref) + 1e-37).all()
+    assert (wn[:, gone] == 0).all()
+    assert (np.abs(wn[:, ~gone] - step) <= (dl + 4 * 2.0 ** -24) * step + 1e-37).all()
 
 
 def test_decode_offsets_past_32_bits():
@@ -663,6 +724,25 @@ def test_budgeted_layers(dtype, d, budget, n_last):
     assert bud.device_status() == B.EARN_OK
     with pytest.raises(ValueError, match="one beam"):
         BudgetedLayers(make_session(w.replace(beams=2)), 16)
+
+
+def test_budgeted_layers_refuse_steps_without_room():
+    """Below the budget a session has room for max_new tokens; at the budget there is no end; without full layers nothing to do."""
+    w = wl.Workload("budget", batch=2, n_layers=2, split_k=1, n_q_heads=4, n_kv_heads=2, head_dim=64, dtype="bf16", prompt_len=0,
+                    lens=(20, 9), r_head=2, r_tail=2, decode_steps=3, seed=1)
+    _, wide = budgeted(w, 100)
+    _, tight = budgeted(w, 16)
+    for _ in range(3):
+        wide.begin_step()
+    with pytest.raises(ValueError, match="no room"):
+        wide.begin_step()
+    assert wide.seq_len.tolist() == [23, 12]
+    for _ in range(9):
+        tight.begin_step()
+        tight.end_step()
+    assert tight.seq_len.tolist() == [16, 16]
+    _, none = budgeted(w.replace(split_k=0), 16)
+    assert none.device_status() == B.EARN_OK
 
 
 def test_binding_refusals_on_the_device():
