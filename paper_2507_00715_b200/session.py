@@ -168,7 +168,8 @@ class BudgetedLayers:
     After the prefill of a layer (with its softmax denominators) ``take_prompt`` weighs the prompt's rows by the last
     ``n_obs`` queries and copies the budget's worth into pages of its own; the packed K/V may be dropped then.  A decode
     step is ``begin_step``, ``decode_layer`` for every full layer (the register layers stay with the session), and
-    ``end_step``.  By default the session's prefix and suffix registers always stay and the suffix registers (at least
+    ``end_step``.  While the rows stay below the budget there is room for the session's ``max_new`` tokens, as in its own
+    cache; at the budget there is no end.  By default the session's prefix and suffix registers always stay and the suffix registers (at least
     one row) do the weighing.  One beam per sequence.
     """
 
@@ -183,7 +184,9 @@ class BudgetedLayers:
         self.n_obs = max(1, r_tail) if n_obs is None else n_obs
         nb = batch.batch
         lens = np.diff(batch.cu_host)
-        held = int(min(int(lens.max()) + session.max_new if nb else 1, budget + 1))   # rows during a step
+        longest = int(lens.max()) if nb else 0
+        held = max(1, min(longest + session.max_new, budget + 1))   # rows during a step
+        self.steps_left = session.max_new if held <= budget else None
         self.pages_per_seq = max(1, -(-held // B.PAGE_TOKENS))
         n_pages = max(1, nb * self.pages_per_seq)
         self.block_table = None
@@ -213,6 +216,10 @@ class BudgetedLayers:
                                self.weight[layer], self.pos[layer], self.workspace)
 
     def begin_step(self) -> None:
+        if self.steps_left is not None:
+            if self.steps_left == 0:
+                raise ValueError(f"a session of max_new = {self.session.max_new} has no room for another token")
+            self.steps_left -= 1
         self.seq_len.add_(1)
         self.new_pos.add_(1)
 
@@ -230,4 +237,4 @@ class BudgetedLayers:
         self.seq_len.clamp_(max=self.budget)
 
     def device_status(self) -> int:
-        return B.earn_device_status(self.workspace)
+        return B.earn_device_status(self.workspace) if self.caches else B.EARN_OK
