@@ -360,6 +360,9 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         // columns [c_lo, c_lo + width) of this half are visible to this key: tokens at or after it, tokens of the sequence
         const int c_lo = max(key - tok0, 0) * p.g - half * 64;
         const uint32_t width = (uint32_t)max(toks * p.g - half * 64 - c_lo, 0);
+        // A tile's terms are summed by themselves first: a chain over all of a long window's terms rounds each of them at the
+        // size of the whole sum (4096 tokens, groups of 4: 1.0e-6 off, and 5.6e-7 this way; 8192, groups of 8: 1.7e-6, 5.4e-7).
+        float sum0 = 0.f, sum1 = 0.f;
         const float4* l4 = reinterpret_cast<const float4*>(s_lse + st * BC + half * 64);
         uint32_t a[32];
         auto load = [&](int q) {
@@ -380,8 +383,8 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             // matrix unit's truncating sums are the larger part -- and 3 % slower)
             fma2(e0, e1, __uint_as_float(a[c]), __uint_as_float(a[c + 1]), sl2, l.x, l.y);
             fma2(e2, e3, __uint_as_float(a[c + 2]), __uint_as_float(a[c + 3]), sl2, l.z, l.w);
-            add2(acc0, acc1, ex2(e0), ex2(e1));   // (a share of the exponentials as polynomials on the FMA pipe: no faster,
-            add2(acc0, acc1, ex2(e2), ex2(e3));   // 620 us with none, 643 with a quarter, 729 with half at 8 x 4096 tokens)
+            add2(sum0, sum1, ex2(e0), ex2(e1));   // (a share of the exponentials as polynomials on the FMA pipe: no faster,
+            add2(sum0, sum1, ex2(e2), ex2(e3));   // 620 us with none, 643 with a quarter, 729 with half at 8 x 4096 tokens)
           }
         };
         // The interior takes straight-line code of its own: with a test per chunk in between, 641 us instead of 620.
@@ -409,12 +412,13 @@ key_weights_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const float v = ex2(fmaf(__uint_as_float(a[c + k]), sl2, ll[k]));
-                acc0 += (uint32_t)(q * 32 + c + k - c_lo) < width ? v : 0.f;
+                sum0 += (uint32_t)(q * 32 + c + k - c_lo) < width ? v : 0.f;
               }
             }
           }
           release();
         }
+        add2(acc0, acc1, sum0, sum1);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::BAR_LFREE + st));
       }
