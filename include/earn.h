@@ -307,11 +307,14 @@ typedef struct {
 
 /* What stays when a sequence holds more than `budget` rows: the rows of the first n_first tokens and of the last n_last
  * tokens, and of the others those with the largest weight (equal weights: the lower row number; NaN counts as -inf).
- * n_first + n_last <= budget. */
+ * n_first + n_last <= budget.  The last tokens are the newest, generated ones included: n_last covers the suffix registers
+ * at the prompt only.  Rows that are to stay at any length, the suffix registers above all, get a weight of +inf in front
+ * of earn_evict_prompt_kv; every step leaves it +inf.  (n_first + n_last + the rows of such a weight <= budget: the first and
+ * last tokens go before them.) */
 typedef struct {
   int32_t budget;  /* >= 1 rows per sequence and kv head */
   int32_t n_first; /* >= 0; at least the prefix registers, as a rule */
-  int32_t n_last;  /* >= 0; at least the suffix registers, as a rule */
+  int32_t n_last;  /* >= 0; at least the suffix registers for the prompt's eviction, as a rule */
 } earn_evict_t;
 
 /* Bytes of scratch that cover the three calls on a paged cache for n_seq sequences (256 for a malformed request).  Host

@@ -169,8 +169,14 @@ class BudgetedLayers:
     ``n_obs`` queries and copies the budget's worth into pages of its own; the packed K/V may be dropped then.  A decode
     step is ``begin_step``, ``decode_layer`` for every full layer (the register layers stay with the session), and
     ``end_step``.  While the rows stay below the budget there is room for the session's ``max_new`` tokens, as in its own
-    cache; at the budget there is no end.  By default the session's prefix and suffix registers always stay and the suffix registers (at least
-    one row) do the weighing.  One beam per sequence.
+    cache; at the budget there is no end.  By default the suffix registers (at least one row) do the weighing.  One beam
+    per sequence.
+
+    The policy's last tokens are the newest ones, generated ones included, so it lets go of the suffix registers as the
+    sequence grows.  They stay all the same: those among the prompt's last ``n_last`` rows (all of them by default) enter
+    the cache with a weight of +inf, which no step changes.  ``n_first`` is the number of prefix registers by default;
+    ``n_last`` that of suffix registers, or as many as the budget holds beside the registers.  A budget too small for the
+    first rows, the suffix registers and the last rows together is refused.
     """
 
     def __init__(self, session: EarnSession, budget: int, n_first: Optional[int] = None, n_last: Optional[int] = None,
@@ -180,10 +186,18 @@ class BudgetedLayers:
         self.session, self.budget = session, budget
         batch, dev = session.batch, session.device
         r_head, r_tail = batch.c.n_head_reg, batch.c.n_tail_reg
-        self.policy = B.make_evict(budget, r_head if n_first is None else n_first, r_tail if n_last is None else n_last)
+        n_first = r_head if n_first is None else n_first
+        pinned = r_tail if n_last is None else min(r_tail, max(n_last, 0))   # suffix registers that stay for good
+        if n_last is None:
+            n_last = max(0, min(r_tail, budget - n_first - pinned))
+        if n_first + pinned + n_last > budget:
+            raise ValueError(f"a budget of {budget} rows does not hold {n_first} first rows, {pinned} suffix registers and "
+                             f"{n_last} last rows")
+        self.policy = B.make_evict(budget, n_first, n_last)
         self.n_obs = max(1, r_tail) if n_obs is None else n_obs
         nb = batch.batch
         lens = np.diff(batch.cu_host)
+        self.pinned_rows = torch.from_numpy((batch.cu_host[1:, None] - np.arange(1, pinned + 1)).reshape(-1).astype(np.int64)).to(dev)
         longest = int(lens.max()) if nb else 0
         held = max(1, min(longest + session.max_new, budget + 1))   # rows during a step
         self.steps_left = session.max_new if held <= budget else None
@@ -212,6 +226,8 @@ class BudgetedLayers:
         """q, k, v of a full layer (packed) and the lse its prefill wrote -> the layer's pages, weights and positions."""
         ses = self.session
         B.earn_key_weights(ses.model, ses.batch, layer, self.n_obs, q, k, lse, self.prompt_weight, ses.workspace)
+        if self.pinned_rows.numel():
+            self.prompt_weight.index_fill_(1, self.pinned_rows, float("inf"))
         B.earn_evict_prompt_kv(ses.model, ses.batch, layer, self.policy, k, v, self.prompt_weight, self.caches[layer],
                                self.weight[layer], self.pos[layer], self.workspace)
 

@@ -1,0 +1,30 @@
+"""Host side of the budgeted layers: what a budget has to hold."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_00715_b200 import binding as B
+from paper_2507_00715_b200.session import BudgetedLayers, EarnSession
+from test_abi_host import lib  # noqa: F401  (the fixture builds the library)
+
+
+@pytest.fixture
+def session(lib, monkeypatch):  # noqa: F811
+    """Two full layers and a register layer, four registers at either end, in host memory (no call reaches a device)."""
+    monkeypatch.setattr(B, "earn_workspace_init", lambda workspace: None)
+    monkeypatch.setattr(B, "make_paged_cache", lambda *a: a)
+    monkeypatch.setattr(B, "earn_paged_workspace_bytes", lambda *a: 256)
+    cu = np.concatenate([[0], np.cumsum([30, 9, 50])])
+    return EarnSession(3, 2, 4, 2, 64, torch.float32, cu, 4, 4, max_new=6, device="cpu")
+
+
+def test_a_budget_holds_the_registers_and_the_last_rows(session):
+    for budget, n_last, policy, pinned in ((24, None, (24, 4, 4), 4), (10, None, (10, 4, 2), 4), (8, None, (8, 4, 0), 4),
+                                           (16, 8, (16, 4, 8), 4), (20, 2, (20, 4, 2), 2), (20, 0, (20, 4, 0), 0)):
+        bud = BudgetedLayers(session, budget, n_last=n_last)
+        assert (bud.policy.budget, bud.policy.n_first, bud.policy.n_last) == policy
+        want = sorted(e - i for e in (30, 39, 89) for i in range(1, pinned + 1))
+        assert sorted(bud.pinned_rows.tolist()) == want
+    for kw in (dict(budget=7), dict(budget=15, n_last=8), dict(budget=9, n_first=2, n_last=4)):
+        with pytest.raises(ValueError, match="does not hold"):
+            BudgetedLayers(session, **kw)
