@@ -487,10 +487,11 @@ cudaError_t launch_hd(const KeyWeightArgs& a, int plan_entries, void* plan, int3
   p.lse = a.lse; p.weight = a.weight; p.plan = by_table ? nullptr : reinterpret_cast<const int4*>(plan); p.cu_seqlens = a.cu_seqlens; p.status = status;
   p.batch = a.batch; p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = g; p.T = T; p.n_obs = a.n_obs; p.total = a.total;
   p.n_items = plan_entries * a.Hkv;
-  // The matrix unit truncates where it adds, so a logit comes out 7e-10 D of itself short on average (measured on N(0, 1) inputs,
-  // D = 64 and 128); the factor makes up for that as far as its own rounding allows.  With the denominators' product in two
-  // parts the weights are off by 1.6e-7 instead of 5.6e-7 at 8 x 4096 tokens, 1.2e-7 instead of 5.9e-7 for ragged windows.
-  p.scale_log2 = (float)((double)a.scale * 1.4426950408889634 * (1.0 + 7e-10 * HD));
+  // The same product, rounded the same way, as the prefill's: what its rounding and the truncating sums of the matrix unit add
+  // to a logit is in the prefill's denominators too (D = 128), and cancels: 4096 tokens, groups of 4, logits of a standard deviation
+  // of 1: 2.0e-7 off with those denominators, 1.8e-7 with exact ones; of 4: 1.9e-7 and 1.3e-6.  (A scale with the truncation's
+  // mean on N(0, 1) inputs made up for does better with exact denominators, 2.5e-7 at 4, and 1.4e-6 with the prefill's.)
+  p.scale_log2 = a.scale * kLog2e;
   e = ensure_dynamic_smem<key_weights_tc_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
   if (e != cudaSuccess) return e;
   e = launch_pdl(key_weights_tc_kernel<HD>, dim3(std::min(p.n_items, sm_count())), dim3(Cfg<HD>::THREADS), Cfg<HD>::SMEM_BYTES, st, mq, mpad, mk, table, p);
