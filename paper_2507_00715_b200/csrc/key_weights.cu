@@ -2,7 +2,7 @@
 // the tensor-core kernel does not take.  A CTA owns 128 keys of one (sequence, kv head) -- 32 where that leaves the grid
 // small -- and walks the (query row, head of the group) pairs of the sequence's window in tiles of 64 columns; the logits are
 // register-blocked 8 x 4 (2 x 4) over 256 threads.  Every weight is summed by
-// one CTA in one order.  FMA-bound, with three 16-byte shared-memory reads per 32 products (24 TFLOP/s, 8 whole prompts of 1024 rows at 32/8 heads: 1.46 ms).
+// one CTA in one order.  FMA-bound, with three 16-byte shared-memory reads per 32 products (23 TFLOP/s, 8 whole prompts of 1024 rows at 32/8 heads: 1.47 ms).
 #include "paged_cache.cuh"
 
 namespace earn {
@@ -47,9 +47,13 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
   }
   const int first = max(len - a.n_obs > 0 ? len - a.n_obs : 0, key0);   // rows in front of key0 see none of these keys
   const int64_t n_cols = (int64_t)(len - first) * g;
-  float sum[KM];
+  // A thread's terms of a tile are summed by themselves, tiles in sixteens, and those into the key's sum: a chain over all
+  // of a long window's terms rounds each of them at the size of the whole sum (8192 rows, groups of 8: 4096 terms a thread).
+  // (Selects at the end of the loop: with a branch for the sixteenth tile the small form's loop takes a sixth longer.)
+  float sum[KM], sum16[KM];
 #pragma unroll
-  for (int i = 0; i < KM; ++i) sum[i] = 0.f;
+  for (int i = 0; i < KM; ++i) sum[i] = sum16[i] = 0.f;
+  int tile = 0;
   for (int64_t c0 = 0; c0 < n_cols; c0 += TQ) {
     __syncthreads();   // the last tile's columns have been used
     if (tid < TQ) {
@@ -89,17 +93,29 @@ __global__ void __launch_bounds__(256) key_weights_simt_kernel(KeyWeightArgs a) 
           for (int j = 0; j < 4; ++j) s[i][j] = fmaf(kv[i], qv[j], s[i][j]);
       }
     }
+    float sum1[KM];
+#pragma unroll
+    for (int i = 0; i < KM; ++i) sum1[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int row = row_of[tx * 4 + j];
       const float d = lse[tx * 4 + j];
 #pragma unroll
       for (int i = 0; i < KM; ++i)
-        if (row >= key0 + ty * KM + i) sum[i] += exp2f(fmaf(s[i][j], a.scale, -d) * kLog2e);   // causal; columns that do not exist: row -1
+        if (row >= key0 + ty * KM + i) sum1[i] += exp2f(fmaf(s[i][j], a.scale, -d) * kLog2e);   // causal; columns that do not exist: row -1
+    }
+#pragma unroll
+    for (int i = 0; i < KM; ++i) sum16[i] += sum1[i];
+    const bool full = (++tile & 15) == 0;
+#pragma unroll
+    for (int i = 0; i < KM; ++i) {
+      sum[i] += full ? sum16[i] : 0.f;
+      sum16[i] = full ? 0.f : sum16[i];
     }
   }
 #pragma unroll
   for (int i = 0; i < KM; ++i) {
+    sum[i] += sum16[i];
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
     if (tx == 0 && key0 + ty * KM + i < len) a.weight[(int64_t)kvh * a.total + lo + key0 + ty * KM + i] = sum[i];

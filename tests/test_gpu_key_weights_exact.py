@@ -73,3 +73,24 @@ def test_every_query_hands_out_one_under_the_prefills_denominators(scale, n_obs)
     w = call(q, k, None, scale, "bf16", n_obs)
     got = w.double().sum(1) / (n_obs * (hq // hkv)) - 1.0
     assert float(got.abs().max()) <= 3 * 2.0 ** -22 + 2.0 ** -23, got.tolist()
+
+
+@pytest.mark.parametrize("dtype,depth", [("f32", 2 + 16 + 64 + 4), ("bf16", 32 + 512 + 4)])
+def test_small_terms_of_a_long_window_are_not_lost(dtype, depth):
+    """The first eight queries give 1 each, 8184 others 2^-22.5 each (zero queries, denominators to match), under eight heads: a
+    sum that took them one by one would lose every one of the small ones, 1.7e-4 of the weight.  A sum of positive terms is off
+    by at most 2^-24 per addition that a term goes through.  fp32: 64 columns of a tile, four of them a thread's (2 additions),
+    16 tiles, 64 sixteens of tiles, 16 threads (4).  bf16: half of a tile's 64 columns, 512 tiles, and the four parts of a key's sum."""
+    n, g, d = 8192, 8, 64
+    q, k = inputs(n, g, 1, d, dtype, 0.0, seed=1)
+    lse = torch.full((g, n), 22.5 * np.log(2.0), device="cuda")
+    lse[:, :8] = 0.0
+    w = call(q, k, lse, 0.0, dtype, n)
+    seen = torch.arange(n, 0, -1, device="cuda").double()             # queries that see key j
+    large = (8.0 - torch.arange(n, device="cuda").double()).clamp_(min=0.0)
+    ref = g * (large + (seen - large) * torch.exp(-lse[0, -1].double()))
+    err = ((w[0].double() - ref).abs() / ref)
+    # a small term itself: 22.5 (two roundings, log2 e) and the exponential unit
+    tol = torch.full_like(ref, depth * 2.0 ** -24 + 22.5 * 3 * 2.0 ** -24 + 2.0 ** -22)
+    tol[:8] = depth * 2.0 ** -24 + 2.0 ** -22
+    assert bool((err <= tol).all()), (float(err[:8].max()), float(err.max()))
