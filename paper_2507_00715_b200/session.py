@@ -253,4 +253,7 @@ class BudgetedLayers:
         self.seq_len.clamp_(max=self.budget)
 
     def device_status(self) -> int:
-        return B.earn_device_status(self.workspace) if self.caches else B.EARN_OK
+        """The first error in the status words of the session's workspace, into which the weighing of the prompt's rows reports
+        (after one of those the rows kept may be the wrong ones), and of the workspace of the pages."""
+        status = self.session.device_status()
+        return status if status != B.EARN_OK or not self.caches else B.earn_device_status(self.workspace)

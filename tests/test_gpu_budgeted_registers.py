@@ -60,3 +60,15 @@ def test_registers_stay(dtype, d, budget, n_last, kept, recent):
                     for at, x in zip(held, weight[b, h, :m]):
                         assert np.isposinf(x) if n - kept <= at < n else np.isfinite(x)
     assert bud.device_status() == B.EARN_OK
+
+
+def test_a_wait_that_ran_out_in_the_sessions_workspace_is_reported():
+    w = wl.Workload("status", batch=1, n_layers=1, split_k=1, n_q_heads=4, n_kv_heads=2, head_dim=64, dtype="bf16", prompt_len=0,
+                    lens=(20,), r_head=2, r_tail=2, decode_steps=1, seed=1)
+    ses = make_session(w)
+    bud = BudgetedLayers(ses, 16)
+    assert bud.device_status() == B.EARN_OK
+    B.earn_selftest_wait_timeout(ses.workspace, 1000)      # a bounded wait on a barrier that nothing completes, in place of the kernel's
+    assert bud.device_status() == B.EARN_ERR_TIMEOUT
+    B.earn_workspace_init(ses.workspace)
+    assert bud.device_status() == B.EARN_OK

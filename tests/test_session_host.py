@@ -28,3 +28,17 @@ def test_a_budget_holds_the_registers_and_the_last_rows(session):
     for kw in (dict(budget=7), dict(budget=15, n_last=8), dict(budget=9, n_first=2, n_last=4)):
         with pytest.raises(ValueError, match="does not hold"):
             BudgetedLayers(session, **kw)
+
+
+def test_a_timeout_of_the_prompts_weighing_reaches_the_budgeted_layers(session, monkeypatch):
+    """earn_key_weights reports into the workspace it is given, which is the session's."""
+    bud = BudgetedLayers(session, 24)
+    given = []
+    for name in ("earn_key_weights", "earn_evict_prompt_kv"):
+        monkeypatch.setattr(B, name, lambda *a, name=name: given.append((name, a[-1])))
+    bud.take_prompt(0, None, None, None, None)
+    word = torch.zeros(1, dtype=torch.int32)
+    monkeypatch.setattr(B, "earn_device_status", lambda ws: int(word) if ws is dict(given)["earn_key_weights"] else B.EARN_OK)
+    assert bud.device_status() == B.EARN_OK
+    word.fill_(B.EARN_ERR_TIMEOUT)
+    assert bud.device_status() == B.EARN_ERR_TIMEOUT
