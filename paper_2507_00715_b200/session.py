@@ -43,6 +43,7 @@ class EarnSession:
         self.v_shared: List[Optional[torch.Tensor]] = [None] * n_layers
         self.k_full: List[Optional[torch.Tensor]] = [None] * n_layers
         self.v_full: List[Optional[torch.Tensor]] = [None] * n_layers
+        self.released = set()   # full layers whose packed K/V another cache has taken over
         self.k_priv, self.v_priv = [], []
         # the private (generated-token) segment: flat slabs, or pages behind a scattered table (one table for all layers)
         self.priv_table, self.priv_pages_per_beam, self.n_priv_pages = None, 0, 0
@@ -76,6 +77,17 @@ class EarnSession:
                             self.reg_idx, self.priv_table, self.priv_pages_per_beam, self.n_priv_pages)
 
     # ---- prefill
+    def release_prompt(self, layer: int) -> None:
+        """Lets go of the packed K/V of a layer < k that ``prefill_layer`` was given (a BudgetedLayers holds its rows from then
+        on).  decode_layer refuses the layer until it is prefilled again."""
+        if not 0 <= layer < self.split_k:
+            raise ValueError(f"layer {layer} is not a full layer")
+        for kv in (self.k_full, self.v_full):
+            if kv[layer] is not None and kv[layer].is_cuda:
+                kv[layer].record_stream(torch.cuda.current_stream(kv[layer].device))   # (what is enqueued here still reads it)
+            kv[layer] = None
+        self.released.add(layer)
+
     def prefill_layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                       q_reg: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -85,6 +97,7 @@ class EarnSession:
             o = out if out is not None else torch.empty_like(q)
             B.earn_prefill_attn(self.model, self.batch, layer, q, k, v, o, lse, self.workspace)
             self.k_full[layer], self.v_full[layer] = k, v
+            self.released.discard(layer)
             return o
         nb = self.batch.batch
         if q_reg is None:
@@ -144,6 +157,8 @@ class EarnSession:
 
     def decode_layer(self, layer: int, step: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if layer in self.released:
+            raise ValueError(f"layer {layer}: the prompt's keys and values were released")
         o = out if out is not None else torch.empty_like(q)
         B.earn_decode_attn(self.model, self.batch, layer, step, q, k_new, v_new, self.cache(layer), o,
                            self.k_full[layer], self.v_full[layer], self.workspace)
@@ -152,11 +167,14 @@ class EarnSession:
     def device_status(self) -> int:
         return B.earn_device_status(self.workspace)
 
-    # ---- accounting (Eq. 9 on the actual buffers): KV entries per kv head held after `generated` steps
+    # ---- accounting (Eq. 9 on the actual buffers): KV entries per kv head held after `generated` steps (a released layer's
+    # rows are in another cache, which counts them)
     def kv_entries(self, generated: int) -> int:
         lens = np.diff(self.batch.cu_host)
         total = 0
         for layer in range(self.n_layers):
+            if layer in self.released:
+                continue
             shared = int(lens.sum()) if layer < self.split_k else self.R * len(lens)
             total += shared + len(lens) * self.beams * generated
         return total
@@ -166,7 +184,8 @@ class BudgetedLayers:
     """The full layers (``l < split_k``) of a session's batch with at most ``budget`` rows per sequence and kv head.
 
     After the prefill of a layer (with its softmax denominators) ``take_prompt`` weighs the prompt's rows by the last
-    ``n_obs`` queries and copies the budget's worth into pages of its own; the packed K/V may be dropped then.  A decode
+    ``n_obs`` queries and copies the budget's worth into pages of its own.  The session keeps the packed K/V that its prefill
+    was given all the same, unless ``take_prompt`` is told to ``release`` them (its own decode of the layer needs them).  A decode
     step is ``begin_step``, ``decode_layer`` for every full layer (the register layers stay with the session), and
     ``end_step``.  While the rows stay below the budget there is room for the session's ``max_new`` tokens, as in its own
     cache; at the budget there is no end.  By default the suffix registers (at least one row) do the weighing.  One beam
@@ -222,14 +241,18 @@ class BudgetedLayers:
             self.workspace = torch.empty(B.earn_paged_workspace_bytes(session.model, nb, self.caches[0]), dtype=torch.uint8, device=dev)
             B.earn_workspace_init(self.workspace)
 
-    def take_prompt(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor) -> None:
-        """q, k, v of a full layer (packed) and the lse its prefill wrote -> the layer's pages, weights and positions."""
+    def take_prompt(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor,
+                    release: bool = False) -> None:
+        """q, k, v of a full layer (packed) and the lse its prefill wrote -> the layer's pages, weights and positions.
+        release: the session lets go of the packed K/V, which are freed once the caller drops them too."""
         ses = self.session
         B.earn_key_weights(ses.model, ses.batch, layer, self.n_obs, q, k, lse, self.prompt_weight, ses.workspace)
         if self.pinned_rows.numel():
             self.prompt_weight.index_fill_(1, self.pinned_rows, float("inf"))
         B.earn_evict_prompt_kv(ses.model, ses.batch, layer, self.policy, k, v, self.prompt_weight, self.caches[layer],
                                self.weight[layer], self.pos[layer], self.workspace)
+        if release:
+            ses.release_prompt(layer)
 
     def begin_step(self) -> None:
         if self.steps_left is not None:
@@ -251,6 +274,18 @@ class BudgetedLayers:
 
     def end_step(self) -> None:
         self.seq_len.clamp_(max=self.budget)
+
+    def kv_entries(self, generated: int) -> int:
+        """KV entries per kv head that the session and the budgeted layers hold after `generated` steps of the layers: the rows
+        within the budget, the register layers' rows, and the packed prompts that were not released."""
+        ses, lens = self.session, np.diff(self.session.batch.cu_host)
+        total = 0
+        for layer in range(ses.n_layers):
+            if layer < ses.split_k:
+                total += int(np.minimum(lens + generated, self.budget).sum()) + (0 if layer in ses.released else int(lens.sum()))
+            else:
+                total += (ses.R + generated) * len(lens)
+        return total
 
     def device_status(self) -> int:
         """The first error in the status words of the session's workspace, into which the weighing of the prompt's rows reports

@@ -72,3 +72,31 @@ def test_a_wait_that_ran_out_in_the_sessions_workspace_is_reported():
     assert bud.device_status() == B.EARN_ERR_TIMEOUT
     B.earn_workspace_init(ses.workspace)
     assert bud.device_status() == B.EARN_OK
+
+
+def test_steps_after_the_packed_prompt_is_gone():
+    """Released layers free the packed K/V and decode as unreleased ones do."""
+    w = wl.Workload("release", batch=2, n_layers=1, split_k=1, n_q_heads=8, n_kv_heads=8, head_dim=128, dtype="bf16", prompt_len=0,
+                    lens=(900, 1200), r_head=4, r_tail=4, decode_steps=3, seed=5)
+    total, outs = int(wl.cu_seqlens(w)[-1]), []
+    for release in (False, True):
+        ses = make_session(w)
+        bud = BudgetedLayers(ses, 64)
+        q, k, v = wl.layer_qkv(w, 0, "cuda")
+        lse = torch.empty(w.n_q_heads, total, device="cuda")
+        ses.prefill_layer(0, q, k, v, lse=lse)
+        bud.take_prompt(0, q, k, v, lse, release=release)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        del k, v
+        freed = before - torch.cuda.memory_allocated()
+        assert freed == (2 * total * 8 * 128 * 2 if release else 0)
+        junk = torch.full((2 * total, 8, 128), float("nan"), device="cuda", dtype=torch.bfloat16)
+        out = []
+        for step in range(1, 4):
+            bud.begin_step()
+            out.append(bud.decode_layer(0, *wl.decode_qkv(w, 0, step, "cuda")))
+            bud.end_step()
+        outs.append(torch.stack(out))
+        del junk
+    assert torch.equal(*outs)

@@ -1,4 +1,7 @@
-"""Host side of the budgeted layers: what a budget has to hold."""
+"""Host side of the budgeted layers: what a budget has to hold, whose status is reported, what a released prompt leaves."""
+import gc
+import weakref
+
 import numpy as np
 import pytest
 import torch
@@ -42,3 +45,33 @@ def test_a_timeout_of_the_prompts_weighing_reaches_the_budgeted_layers(session, 
     assert bud.device_status() == B.EARN_OK
     word.fill_(B.EARN_ERR_TIMEOUT)
     assert bud.device_status() == B.EARN_ERR_TIMEOUT
+
+
+def test_the_session_lets_go_of_a_released_prompt(session, monkeypatch):
+    """The packed K/V of a full layer are referenced by nobody but the caller after a released take_prompt, the layer's own
+    decode is refused, and the accounting follows."""
+    for name in ("earn_prefill_attn", "earn_key_weights", "earn_evict_prompt_kv", "earn_decode_attn"):
+        monkeypatch.setattr(B, name, lambda *a: None)
+    bud = BudgetedLayers(session, 24)
+    q, lens = torch.zeros(89, 4, 64), (30, 9, 50)
+    kept, held = [], sum(min(n + 2, 24) for n in lens)
+    for layer in range(2):
+        k, v = torch.zeros(89, 2, 64), torch.zeros(89, 2, 64)
+        kept += [weakref.ref(k), weakref.ref(v)]
+        session.prefill_layer(layer, q, k, v)
+        bud.take_prompt(layer, q, k, v, None, release=layer == 1)
+    del k, v
+    gc.collect()
+    assert [r() is None for r in kept] == [False, False, True, True]
+    registers = (8 + 2) * 3
+    assert session.kv_entries(2) == 89 + 2 * 3 + registers
+    assert bud.kv_entries(2) == 2 * held + 89 + registers
+    for layer in (-1, 2):
+        with pytest.raises(ValueError, match="not a full layer"):
+            session.release_prompt(layer)
+    session.decode_layer(0, 1, q[:3], None, None)
+    with pytest.raises(ValueError, match="released"):
+        session.decode_layer(1, 1, q[:3], None, None)
+    session.prefill_layer(1, q, torch.zeros(89, 2, 64), torch.zeros(89, 2, 64))
+    session.decode_layer(1, 1, q[:3], None, None)
+    assert session.kv_entries(2) == 2 * (89 + 2 * 3) + registers
