@@ -161,6 +161,9 @@ class Batch:
                  cu_seqlens_dev: Optional[torch.Tensor] = None):
         self.cu_host = np.ascontiguousarray(cu_seqlens_host, dtype=np.int32)
         self.cu_dev = cu_seqlens_dev if cu_seqlens_dev is not None else torch.from_numpy(self.cu_host).to(device)
+        if self.cu_dev.dtype != torch.int32 or not self.cu_dev.is_contiguous() or self.cu_dev.numel() < len(self.cu_host):
+            raise ValueError(f"cu_seqlens: {self.cu_dev.dtype} of {tuple(self.cu_dev.shape)}, expected {len(self.cu_host)} dense int32")
+        self.device = self.cu_dev.get_device()
         n = len(self.cu_host) - 1
         lens = np.diff(self.cu_host) if n > 0 else np.zeros(0, dtype=np.int32)
         self.c = EarnBatch(n, int(self.cu_host[-1]) if n >= 0 and len(self.cu_host) else 0,
@@ -313,7 +316,7 @@ _TORCH_DTYPE = {EARN_F32: torch.float32, EARN_BF16: torch.bfloat16}
 
 
 # A call is a launch or two of a few microseconds, so what stands in front of it counts: the checks are one condition per
-# tensor, and absent tensors and the workspace are passed without any.
+# tensor, and absent tensors are passed without any.
 def _tensor(t, what: str, dtype: torch.dtype, numel: int, device: int) -> int:
     """Address of a dense tensor of `dtype` on CUDA device `device` with at least `numel` elements."""
     try:
@@ -328,6 +331,19 @@ def _tensor(t, what: str, dtype: torch.dtype, numel: int, device: int) -> int:
     if t.numel() < numel:
         raise ValueError(f"{what}: {t.numel()} elements, expected at least {numel}")
     raise ValueError(f"{what}: on {t.device}, expected the current CUDA device ({device})")
+
+
+def _wrong_device(device: int, current: int):
+    raise ValueError(f"cu_seqlens: on CUDA device {device} (-1: in host memory), expected the current one ({current})")
+
+
+def _scratch(t, device: int):
+    """Address and bytes of a workspace on CUDA device `device` (None is left for the library to refuse)."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"workspace: on {t.device}, expected a contiguous tensor on the current CUDA device ({device})")
+    return t.data_ptr(), t.nbytes
 
 
 def _stream_of(device: int) -> Optional[int]:
@@ -388,7 +404,9 @@ def earn_key_weights(model: EarnModel, batch: Batch, layer: int, n_obs: int, q, 
     """q [total, Hq, D], k [total, Hkv, D], lse fp32 [Hq, total] (earn_prefill_attn) -> weight fp32 [Hkv, total]."""
     n, dt, dev = batch.c.total_tokens, _TORCH_DTYPE[model.dtype], _current_device()
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
-    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    p, size = _scratch(workspace, dev)
+    if batch.device != dev:
+        _wrong_device(batch.device, dev)
     _check(lib().earn_key_weights(model, batch.c, layer, n_obs, _tensor(q, "q", dt, n * hq * d, dev),
                                   _tensor(k, "k", dt, n * hkv * d, dev), _tensor(lse, "lse", torch.float32, n * hq, dev),
                                   _tensor(weight, "weight", torch.float32, n * hkv, dev), p, size, _stream_of(dev)),
@@ -402,7 +420,9 @@ def earn_evict_prompt_kv(model: EarnModel, batch: Batch, layer: int, policy: Ear
     n, n_seq, dt, dev = batch.c.total_tokens, batch.c.batch, _TORCH_DTYPE[model.dtype], _current_device()
     hkv, d = model.n_kv_heads, model.head_dim
     rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
-    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    p, size = _scratch(workspace, dev)
+    if batch.device != dev:
+        _wrong_device(batch.device, dev)
     _check(lib().earn_evict_prompt_kv(model, batch.c, layer, policy, _tensor(k, "k", dt, n * hkv * d, dev),
                                       _tensor(v, "v", dt, n * hkv * d, dev),
                                       _tensor(weight, "weight", torch.float32, n * hkv, dev), cache,
@@ -419,7 +439,7 @@ def earn_paged_decode_attn(model: EarnModel, n_seq: int, layer: int, q, k_new, v
     hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
     rows = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
     nq, nk = n_seq * hq * d, n_seq * hkv * d
-    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    p, size = _scratch(workspace, dev)
     _check(lib().earn_paged_decode_attn(model, n_seq, layer, _tensor(q, "q", dt, nq, dev),
                                         None if k_new is None else _tensor(k_new, "k_new", dt, nk, dev),
                                         None if v_new is None else _tensor(v_new, "v_new", dt, nk, dev), cache,
@@ -436,7 +456,7 @@ def earn_evict_kv(model: EarnModel, n_seq: int, layer: int, policy: EarnEvict, c
     then holds min(seq_len[b], budget) rows: put that into seq_len."""
     dt, dev, hkv, d = _TORCH_DTYPE[model.dtype], _current_device(), model.n_kv_heads, model.head_dim
     n = n_seq * hkv * _check_cache(model, n_seq, cache, dt, hkv, d, dev)
-    p, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    p, size = _scratch(workspace, dev)
     _check(lib().earn_evict_kv(model, n_seq, layer, policy, cache, _tensor(weight, "weight", torch.float32, n, dev),
                                _tensor(pos, "pos", torch.int32, n, dev), _tensor(weight_out, "weight_out", torch.float32, n, dev),
                                _tensor(pos_out, "pos_out", torch.int32, n, dev), p, size, _stream_of(dev)), "earn_evict_kv")

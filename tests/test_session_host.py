@@ -75,3 +75,48 @@ def test_the_session_lets_go_of_a_released_prompt(session, monkeypatch):
     session.prefill_layer(1, q, torch.zeros(89, 2, 64), torch.zeros(89, 2, 64))
     session.decode_layer(1, 1, q[:3], None, None)
     assert session.kv_entries(2) == 2 * (89 + 2 * 3) + registers
+
+
+def test_the_binding_turns_down_workspaces_and_prompt_offsets_it_must_not_pass(monkeypatch):
+    """A workspace in host memory, one that is not dense, and offsets of another type never reach the library.  (Host tensors
+    stand in for device tensors: their device number is -1.)"""
+    called = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: called.append(name) or B.EARN_OK
+
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(B, "_stream_of", lambda device: None)
+    model, batch = B.make_model(1, 1, 2, 1, 64, "f32"), B.Batch(np.asarray([0, 3, 5]), 0, 0, device="cpu")
+    cache = B.EarnPagedCache(0, 0, None, 1, 2, 0, 16)
+    cache.kind, cache.n_seq, cache.device = (torch.float32, 1, 64), 2, -1
+    f32, i32 = torch.zeros(2048), torch.zeros(64, dtype=torch.int32)
+
+    def calls(ws):
+        yield lambda: B.earn_key_weights(model, batch, 0, 4, f32, f32, f32, f32, ws)
+        yield lambda: B.earn_evict_prompt_kv(model, batch, 0, B.make_evict(4), f32, f32, f32, cache, f32, i32, ws)
+        yield lambda: B.earn_paged_decode_attn(model, 2, 0, f32, None, None, cache, f32, workspace=ws)
+        yield lambda: B.earn_evict_kv(model, 2, 0, B.make_evict(4), cache, f32, i32, f32, i32, ws)
+
+    dense = torch.zeros(512, dtype=torch.uint8)
+    monkeypatch.setattr(B, "_current_device", lambda: -1)
+    for call in calls(dense):
+        call()
+    assert len(called) == 4
+    for call in calls(torch.zeros(2, dtype=torch.uint8).expand(256, 2)):
+        with pytest.raises(ValueError, match="workspace"):
+            call()
+    for bad in (batch.cu_dev.long(), batch.cu_dev[:2], torch.zeros(3, 2, dtype=torch.int32)[:, 0]):
+        with pytest.raises(ValueError, match="cu_seqlens"):
+            B.Batch(batch.cu_host, 0, 0, cu_seqlens_dev=bad)
+    batch.device = 0
+    for call in list(calls(dense))[:2]:
+        with pytest.raises(ValueError, match="cu_seqlens"):
+            call()
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    cache.device = 0
+    for call in calls(dense):
+        with pytest.raises(ValueError, match="workspace: on cpu"):
+            call()
+    assert len(called) == 4
