@@ -291,8 +291,8 @@ earn_status_t earn_beam_topk(int32_t batch, int32_t beams, int32_t n_live, int32
 /* Paged K/V cache of one layer.  Row j of sequence b is slot j % 16 of page block_table[b * pages_per_seq + j / 16].
  * No page is named twice (table entries past the page of the last row do not count).  An entry outside [0, n_pages) reads
  * a wrong page, never outside the cache; a row that would be written there is dropped.  The per-row arrays that go with it
- * (weight, pos) are [B, Hkv, 16 * pages_per_seq]; rows at or past a sequence's length are neither read nor written in any
- * of them. */
+ * (weight, pos) are [B, Hkv, 16 * pages_per_seq]; rows at or past a sequence's length are not written in any of them, and
+ * what they hold is not used (earn_paged_decode_attn may read a weight there). */
 typedef struct {
   void* k_pages;              /* device [n_pages, 16, Hkv, D] */
   void* v_pages;              /* device, same shape */

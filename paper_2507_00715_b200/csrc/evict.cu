@@ -9,8 +9,9 @@
 //   prompt into row m of the pages;
 //   step form: the i-th free row below the budget and the i-th kept row behind it form a move; sources and destinations are
 //   disjoint, so the moves run in any order.
-// Lists of up to 65536 rows take one launch (evict_cluster_kernel), longer ones a selecting kernel of one CTA per list and a
-// copying kernel behind it.
+// Lists of up to 65536 rows are selected by clusters (evict_cluster_kernel), which also copy unless the lists are more than
+// one wave of them; longer lists by a kernel of one CTA each.  Where the selecting launch does not copy, a second one does.
+// Times in this file are of calls replayed from a graph.
 #include <climits>
 #include <type_traits>
 
@@ -223,18 +224,18 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(EvictArgs 
   }
 }
 
-// ---- lists of at most 65536 rows: one launch.  A cluster of C CTAs owns a (sequence, kv head); every key is in
+// ---- lists of at most 65536 rows.  A cluster of C CTAs owns a (sequence, kv head); every key is in
 // a register (CTA r holds the r-th stretch of the list, a warp a stretch of that, row j0 + 32 i + lane), read once.
 // Four digits of 8 bits: each CTA counts a digit's 256 bins in its shared memory (a histogram of its own per digit, cleared
 // once; four copies of the first digit's, where every row counts and most fall into a few bins), the counts of the cluster
 // are added through distributed shared memory, and the search ends with the first digit whose bin stays whole.  Ranks come
 // from one count per warp and one per CTA.  The CTAs then copy the rows they have found themselves (prompt form) or a share
-// of the moves (in place), without a second launch: while one list is still being searched, others are being copied.
-// In place, a list that is only a few rows too long -- a step's worth -- has them taken out one by one instead, by a minimum
-// over the CTA each.
+// of the moves (in place), without a second launch where all lists are resident at once.
+// In place, a list of at most 4096 rows (one CTA) that is only a few rows too long -- a step's worth -- has them taken out one by
+// one instead, by a minimum over the CTA each; a longer list goes through the digits whatever it loses.
 // Measured (8 kv heads, bf16, D = 128): 8 prompts of 12000 to 16384 rows to 2048 in 37 us, of which the copies are 20 at 6.7 TB/s
 // and the exchanges of the search 7 (fetching the rows that a first digit had settled into L2 meanwhile: 3 us more); 64 lists of
-// 8192 rows halved in 38 us; 512 lists of 1025 rows to 1024 in 5.9 us (20 us with 11-bit digits and full scans over the
+// 8192 rows halved in 38 us; 512 lists of 1025 rows to 1024 in 5.7 us (20 us with 11-bit digits and full scans over the
 // CTA, 17 with a search bit by bit).
 constexpr int MAX_CLUSTER = 8, MAX_IPT = 16;
 constexpr int FEW = 8;           // rows too many that are taken out one by one
@@ -691,8 +692,8 @@ cudaError_t launch_form(const EvictArgs& a, cudaStream_t st) {
   // (5.6 us against 8.3 for 512 lists of 1025 rows), and more lists than 512-thread CTAs are resident with them.
   constexpr int WIDE = 512, NARROW = 256;
   if (a.max_rows <= MAX_CLUSTER * WIDE * MAX_IPT && units * MAX_CLUSTER <= INT_MAX) {
-    // CTAs per list: one if only a few rows go, otherwise as many as leave them ROWS_EACH (_PROMPT) rows while the grid
-    // stays within what is resident at once
+    // CTAs per list: one if only a few rows go and a CTA's registers hold the list (4096 rows), otherwise as many as leave
+    // them ROWS_EACH (_PROMPT) rows while the grid stays within what is resident at once
     int c = 1;
     while (c < MAX_CLUSTER && (a.max_rows > c * (c > 1 ? WIDE : NARROW) * MAX_IPT ||
                                ((PROMPT || excess > FEW) && a.max_rows >= 2 * c * (PROMPT ? ROWS_EACH_PROMPT : ROWS_EACH) &&

@@ -1,15 +1,17 @@
 // One new token per sequence over the paged cache of a full layer (Eq. 4: append K_t, V_t, then attend over K_{1:t}), with
 // the attention weight every row received added to its accumulated weight.
 //
-// HBM-bound: K and V of every row are read once.  The key list of a (sequence, kv head) is cut into chunks; a warp takes
+// HBM-bound: K and V of every row are read once for every 16 query heads of a kv head.  The key list of a (sequence, kv head) is cut into chunks; a warp takes
 // one chunk under 16 query rows (the group's heads), page by page -- a page is a tile of 16 positions -- through a ring
 // of cp.async stages, and leaves a normalised partial with its log2-domain softmax denominator.  A second kernel joins
 // the partials.  The weight of a row needs the denominator of the whole list, so the first kernel also leaves the scaled
-// logits (4 bytes per query head and row beside the 4 D bytes of K and V: 6 % at a group of 8 and D = 128, written and read
-// while they are in L2), and the second kernel turns them into weights: sum over the heads of 2^(logit - LSE).
-// 32/8 heads of 128, with weights: 166 us over 8 lists of 20000 to 32768 rows (5.5 TB/s, 0.85 of a copy; the first kernel
+// logits (4 bytes per query head and row beside the 4 D bytes of K and V: 6 % at a group of 8 and D = 128; where a call's
+// logits outgrow L2 beside its K and V they go through DRAM, 35 MB written and 52 MB read over 8 lists of 20000 to 32768 rows
+// in a cold-cache profile), and the second kernel turns them into weights: sum over the heads of 2^(logit - LSE).
+// 32/8 heads of 128, with weights: 168 us over 8 lists of 20000 to 32768 rows (5.4 TB/s, 0.84 of a copy; the first kernel
 // alone 151 us), 51 us over 64 of 700 to 1044 (44 us alone).  The last warp of a (sequence, kv head) joining by itself
 // instead of a second kernel cost 66 us there: one warp is too few for the logits.
+// (Times in this file are of calls replayed from a graph; issued one by one the two above take 173 and 52 us.)
 // Small calls: one launch, the chunks of a list in a cluster (below).
 // No atomics: every sum has one order.
 #include <cfloat>
@@ -28,6 +30,10 @@ constexpr int STAGES = 4;
 
 // One warp's 16 query rows against tiles of 16 or 32 positions, as RowTile, with the logits of every tile handed on:
 // sink(at, fragments) receives the (masked, unscaled) logits of the 8-column blocks that start at tile `at`.
+// The probabilities are rounded to bf16 in front of V, as in the other decode kernels: the output is off by 1.93e-3 of itself
+// (root of the mean square, 64 lists of 700 to 1044 rows) where the output's own rounding is 1.66e-3.  Two bf16 numbers
+// per probability and twice the products with V would leave that alone, for 1 to 8 % more time (64 lists 51.0 -> 52.6 us, one 5.7
+// -> 6.1, group of 7 33.6 -> 35.6).
 template <int D>
 struct PagedTile : RowTile<D> {
   using Base = RowTile<D>;

@@ -188,8 +188,8 @@ class BudgetedLayers:
     was given all the same, unless ``take_prompt`` is told to ``release`` them (its own decode of the layer needs them).  A decode
     step is ``begin_step``, ``decode_layer`` for every full layer (the register layers stay with the session), and
     ``end_step``.  While the rows stay below the budget there is room for the session's ``max_new`` tokens, as in its own
-    cache; at the budget there is no end.  By default the suffix registers (at least one row) do the weighing.  One beam
-    per sequence.
+    cache (``begin_step`` counts them on the host, so a captured step is replayed at the budget only); at the budget there is no
+    end.  By default the suffix registers (at least one row) do the weighing.  One beam per sequence.
 
     The policy's last tokens are the newest ones, generated ones included, so it lets go of the suffix registers as the
     sequence grows.  They stay all the same: those among the prompt's last ``n_last`` rows (all of them by default) enter
