@@ -194,8 +194,8 @@ class BudgetedLayers:
     The policy's last tokens are the newest ones, generated ones included, so it lets go of the suffix registers as the
     sequence grows.  They stay all the same: those among the prompt's last ``n_last`` rows (all of them by default) enter
     the cache with a weight of +inf, which no step changes.  ``n_first`` is the number of prefix registers by default;
-    ``n_last`` that of suffix registers, or as many as the budget holds beside the registers.  A budget too small for the
-    first rows, the suffix registers and the last rows together is refused.
+    ``n_last`` that of suffix registers, or as many as the budget holds beside the registers.  A budget that the
+    sequences reach and that is too small for the first rows, the suffix registers and the last rows together is refused.
     """
 
     def __init__(self, session: EarnSession, budget: int, n_first: Optional[int] = None, n_last: Optional[int] = None,
@@ -209,9 +209,6 @@ class BudgetedLayers:
         pinned = r_tail if n_last is None else min(r_tail, max(n_last, 0))   # suffix registers that stay for good
         if n_last is None:
             n_last = max(0, min(r_tail, budget - n_first - pinned))
-        if n_first + pinned + n_last > budget:
-            raise ValueError(f"a budget of {budget} rows does not hold {n_first} first rows, {pinned} suffix registers and "
-                             f"{n_last} last rows")
         self.policy = B.make_evict(budget, n_first, n_last)
         self.n_obs = max(1, r_tail) if n_obs is None else n_obs
         nb = batch.batch
@@ -220,6 +217,9 @@ class BudgetedLayers:
         longest = int(lens.max()) if nb else 0
         held = max(1, min(longest + session.max_new, budget + 1))   # rows during a step
         self.steps_left = session.max_new if held <= budget else None
+        if held > budget and n_first + pinned + n_last > budget:
+            raise ValueError(f"a budget of {budget} rows does not hold {n_first} first rows, {pinned} suffix registers and "
+                             f"{n_last} last rows")
         self.pages_per_seq = max(1, -(-held // B.PAGE_TOKENS))
         n_pages = max(1, nb * self.pages_per_seq)
         self.block_table = None

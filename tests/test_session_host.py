@@ -31,6 +31,7 @@ def test_a_budget_holds_the_registers_and_the_last_rows(session):
     for kw in (dict(budget=7), dict(budget=15, n_last=8), dict(budget=9, n_first=2, n_last=4)):
         with pytest.raises(ValueError, match="does not hold"):
             BudgetedLayers(session, **kw)
+    BudgetedLayers(session, 56, n_last=52)   # (nothing reaches it: 50 rows and six steps)
 
 
 def test_a_timeout_of_the_prompts_weighing_reaches_the_budgeted_layers(session, monkeypatch):
