@@ -371,6 +371,111 @@ earn_status_t earn_evict_kv(const earn_model_t* model, int32_t n_seq, int32_t la
                             const earn_paged_cache_t* cache, const float* weight, const int32_t* pos, float* weight_out,
                             int32_t* pos_out, void* workspace, size_t workspace_bytes, earn_stream_t stream);
 
+/* ---- A step of several new tokens per sequence ----------------------------------------------------------------------
+ * The paged cache above grows by one token per sequence and call.  With the three calls below a step brings every sequence to
+ * a length of its own: by a chunk of a prompt, by the items a history has gained, by drafted tokens to verify, by the single
+ * token of a decode, all in one batch; or back to a shorter length, or to none (not part of the paper's method; it is the
+ * serving side of the full layers):
+ *
+ *   earn_page_tables (once per step) -> per layer l < k: earn_rope_append -> earn_paged_chunk_attn
+ *
+ * The new tokens of a step are packed back to back in the order of the sequences, as prompts are in earn_batch_t, but their
+ * offsets are on the device only: cu_new[n_seq + 1].  n_tokens is what the packed tensors have room for; rows from
+ * cu_new[n_seq] on are padding.  A step may so be captured into a CUDA graph once and replayed with other lengths. */
+
+/* Pages of all sequences, and which of them are free.  One pool serves every layer: page p of a layer's k_pages / v_pages
+ * belongs to whom page p of the pool belongs to. */
+typedef struct {
+  int32_t* block_table; /* device [n_seq, pages_per_seq]: entries below ceil(held / 16) are live */
+  int32_t pages_per_seq;
+  int32_t n_pages;
+  const int32_t* held;  /* device [n_seq]: rows held */
+  int32_t* free_pages;  /* device [n_pages], a stack: entries below *n_free are the free pages */
+  const int32_t* n_free; /* device [1] */
+} earn_page_pool_t;
+
+/* What a step's other calls need to know, written by earn_page_tables. */
+typedef struct {
+  int32_t n_tokens;   /* room for new tokens */
+  int32_t* cu_new;    /* device [n_seq + 1]: first new token of every sequence, and their number */
+  int32_t* seq_len;   /* device [n_seq]: rows with the new ones; 0: refused (earn_paged_cache_t.seq_len of the step) */
+  int32_t* positions; /* device [n_tokens], 16-byte aligned: row number of every new token, -1: takes no part */
+  int32_t* slots;     /* device [n_tokens], 16-byte aligned: 16 * page + slot of that row, -1: takes no part */
+  int32_t* n_refused; /* device [1]: sequences that stay as they were */
+} earn_step_t;
+
+/* Block tables and slots of a step.  Sequence b holds h = held[b] rows and is to hold t = max(target[b], 0):
+ *   t < h : its pages from ceil(t / 16) on are given back, in order of b and then of the table: they go on top of the stack;
+ *   t > h : its t - h new tokens follow those of the sequences before it in the packed batch, and it takes the pages
+ *           ceil(h / 16) .. ceil(t / 16) - 1 from the top of the stack (pages given back by this call included), in order.
+ * A sequence that grows is refused, as a whole, when its tokens end past n_tokens, when t exceeds 16 * pages_per_seq, or when
+ * the pages that it and the sequences before it want (refused ones included: nobody is overtaken) are not there.  A refused
+ * sequence keeps its rows; its tokens stay in the packed batch with position and slot -1, and its seq_len is 0.
+ * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
+ * must not overlap it).  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
+ * or above the new height hold nothing.
+ * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter.
+ * Errors: n_seq < 0, n_tokens < 0, n_pages < 1, pages_per_seq < 1, NULL or misaligned arrays -> INVALID_ARG; n_seq > 16384,
+ * row or slot numbers beyond 2^31 - 32 -> UNSUPPORTED; workspace -> WORKSPACE. */
+size_t earn_page_tables_workspace_bytes(int32_t n_seq);
+earn_status_t earn_page_tables(int32_t n_seq, const int32_t* target, const earn_page_pool_t* pool, const earn_step_t* step,
+                               int32_t* held_out, int32_t* n_free_out, void* workspace, size_t workspace_bytes,
+                               earn_stream_t stream);
+
+/* Rotary positions.  The first rot_dim elements of a head are pairs (i, i + rot_dim/2), or (2i, 2i + 1) interleaved; pair i of
+ * a token at position p is turned by p * freq[i] and scaled by the amplitude:
+ *   y_a = A (x_a cos - x_b sin),   y_b = A (x_a sin + x_b cos);
+ * the other elements are copied.  Scalings for long contexts are other frequencies, and an amplitude. */
+typedef struct {
+  int32_t rot_dim;     /* even, 0 .. head_dim (0: nothing turns) */
+  int32_t interleaved;
+  float amplitude;     /* 0 => 1 */
+  const double* freq;  /* device fp64 [rot_dim / 2]: radians per position */
+} earn_rope_t;
+
+/* Q and K turned by their tokens' positions, dense: q_out device [n_tokens, Hq, D], k_out [n_tokens, Hkv, D].  q and k hold a
+ * token's heads one after the other and a token every q_stride / k_stride ELEMENTS (at least a token's heads, a multiple of
+ * 16 bytes), so they may be parts of a projection's output; q_out may be q and k_out k where those are dense (no other
+ * overlap).  q and q_out, or k and k_out, may both be NULL.  positions: device int32 [n_tokens]; a token whose position is
+ * negative takes no part: its rows are left as they are.
+ * inverse = 0: the rotation.  inverse = 1: its transpose (sin negated, same amplitude): the gradient of the inputs from the
+ * gradient of the outputs.  Angles are formed and reduced in 64 bits, sine, cosine and the turn are fp32, one rounding.
+ * Errors: n_tokens < 0, a rot_dim that is odd, negative or larger than head_dim, NULL or misaligned tensors, a bad stride ->
+ * INVALID_ARG. */
+earn_status_t earn_rope(const earn_model_t* model, const earn_rope_t* rope, int32_t n_tokens, const int32_t* positions,
+                        const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
+                        int32_t inverse, earn_stream_t stream);
+
+/* The same rotation with the rows of K, turned, and of V, as they are, stored at their slots (16 * page + slot; the step's)
+ * of the paged cache of a layer l < k; Q, turned, goes to q_out (q and q_out may both be NULL).  A slot outside the cache
+ * drops the token's K and V rows.  No slot is named twice.  Of the cache only the pages are used.  Without a turn
+ * (rot_dim = 0, freq NULL) the call appends rows that come turned already.
+ * Errors: as earn_rope, layer outside [0, k), a malformed cache -> INVALID_ARG; 16 * n_pages beyond 2^31 - 1 -> UNSUPPORTED. */
+earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const earn_rope_t* rope, int32_t n_tokens,
+                               const int32_t* positions, const int32_t* slots, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, void* q_out, const earn_paged_cache_t* cache,
+                               earn_stream_t stream);
+
+/* Causal attention of every sequence's new tokens over its rows in the paged cache of a layer l < k, the new ones (stored
+ * before) included: new token i of the n of sequence b is row p = seq_len[b] - n + i and sees rows 0 .. p,
+ *   o = sum_{j <= p} softmax_j( q . k_j * scale ) v_j .
+ * q, o: device [n_tokens, Hq, D]; lse_or_null: device fp32 [Hq, n_tokens], natural-log softmax denominators.  A token that
+ * sees nothing (its sequence has seq_len 0, or fewer rows than new tokens; every logit -inf): o = 0, lse = -inf.  Rows of q
+ * past cu_new[n_seq] are not read, those of o and lse are left as they were.  Rows at or past seq_len are not used, whatever
+ * they hold; every row of a sequence below seq_len is to hold finite values (a row that some new token sees meets the earlier
+ * ones with a weight of zero).  cu_new: device [n_seq + 1], increasing; offsets past n_tokens count as n_tokens.  No weights
+ * are accumulated (earn_paged_decode_attn does that for a single token).
+ * Logits, softmax and sums in fp32; with bf16 the probabilities are rounded to bf16 in front of the product with V only.
+ * Lists are cut at places that depend on the lengths only, and joined in the order of the keys: equal calls, equal results.
+ * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init.
+ * Errors: layer outside [0, k), n_seq < 0, n_tokens < 0, a malformed cache, NULL or misaligned tensors -> INVALID_ARG;
+ * n_seq > 65535 -> UNSUPPORTED; workspace -> WORKSPACE. */
+size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
+                                        const earn_paged_cache_t* cache);
+earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, int32_t n_tokens,
+                                    const int32_t* cu_new, const void* q, const earn_paged_cache_t* cache, void* o,
+                                    float* lse_or_null, void* workspace, size_t workspace_bytes, earn_stream_t stream);
+
 /* Number of kernels this library has launched in this process so far (host counter, all streams). */
 uint64_t earn_launch_count(void);
 

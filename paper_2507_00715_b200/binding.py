@@ -57,6 +57,20 @@ class EarnEvict(C.Structure):
     _fields_ = [("budget", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32)]
 
 
+class EarnPagePool(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("held", C.c_void_p),
+                ("free_pages", C.c_void_p), ("n_free", C.c_void_p)]
+
+
+class EarnStep(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("cu_new", C.c_void_p), ("seq_len", C.c_void_p), ("positions", C.c_void_p),
+                ("slots", C.c_void_p), ("n_refused", C.c_void_p)]
+
+
+class EarnRope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_float), ("freq", C.c_void_p)]
+
+
 SYMBOLS = {
     "earn_workspace_bytes": (C.c_size_t, [C.POINTER(EarnModel), C.POINTER(EarnBatch), C.c_int32]),
     "earn_workspace_init": (C.c_int, [C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -101,6 +115,17 @@ SYMBOLS = {
                                          C.c_void_p, C.c_size_t, C.c_void_p]),
     "earn_evict_kv": (C.c_int, [C.POINTER(EarnModel), C.c_int32, C.c_int32, C.POINTER(EarnEvict), C.POINTER(EarnPagedCache),
                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "earn_page_tables_workspace_bytes": (C.c_size_t, [C.c_int32]),
+    "earn_page_tables": (C.c_int, [C.c_int32, C.c_void_p, C.POINTER(EarnPagePool), C.POINTER(EarnStep), C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_size_t, C.c_void_p]),
+    "earn_rope": (C.c_int, [C.POINTER(EarnModel), C.POINTER(EarnRope), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                            C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "earn_rope_append": (C.c_int, [C.POINTER(EarnModel), C.c_int32, C.POINTER(EarnRope), C.c_int32, C.c_void_p, C.c_void_p,
+                                   C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                   C.POINTER(EarnPagedCache), C.c_void_p]),
+    "earn_paged_chunk_workspace_bytes": (C.c_size_t, [C.POINTER(EarnModel), C.c_int32, C.c_int32, C.POINTER(EarnPagedCache)]),
+    "earn_paged_chunk_attn": (C.c_int, [C.POINTER(EarnModel), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                        C.POINTER(EarnPagedCache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "earn_launch_count": (C.c_uint64, []),
     "earn_status_string": (C.c_char_p, [C.c_int]),
     "earn_version": (C.c_int32, []),
@@ -460,3 +485,123 @@ def earn_evict_kv(model: EarnModel, n_seq: int, layer: int, policy: EarnEvict, c
     _check(lib().earn_evict_kv(model, n_seq, layer, policy, cache, _tensor(weight, "weight", torch.float32, n, dev),
                                _tensor(pos, "pos", torch.int32, n, dev), _tensor(weight_out, "weight_out", torch.float32, n, dev),
                                _tensor(pos_out, "pos_out", torch.int32, n, dev), p, size, _stream_of(dev)), "earn_evict_kv")
+
+
+# ---- steps of several new tokens per sequence (same checks as above)
+def make_page_pool(block_table: torch.Tensor, held: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor) -> EarnPagePool:
+    """block_table int32 [n_seq, pages_per_seq], held int32 [n_seq], free_pages int32 [n_pages], n_free int32 [1].  The caller
+    keeps the tensors alive."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected [n_seq, pages_per_seq]")
+    dev, i32, n_seq = torch.cuda.current_device(), torch.int32, block_table.shape[0]
+    pool = EarnPagePool(_tensor(block_table, "block_table", i32, 0, dev), block_table.shape[1], free_pages.numel(),
+                        _tensor(held, "held", i32, n_seq, dev), _tensor(free_pages, "free_pages", i32, 1, dev),
+                        _tensor(n_free, "n_free", i32, 1, dev))
+    pool.n_seq, pool.device = n_seq, dev
+    return pool
+
+
+def make_step(cu_new: torch.Tensor, seq_len: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+              n_refused: torch.Tensor) -> EarnStep:
+    """cu_new int32 [n_seq + 1], seq_len int32 [n_seq], positions, slots int32 [n_tokens], n_refused int32 [1].  The caller
+    keeps the tensors alive."""
+    dev, i32, n = torch.cuda.current_device(), torch.int32, positions.numel()
+    step = EarnStep(n, _tensor(cu_new, "cu_new", i32, 1, dev), _tensor(seq_len, "seq_len", i32, 0, dev),
+                    _tensor(positions, "positions", i32, n, dev), _tensor(slots, "slots", i32, n, dev),
+                    _tensor(n_refused, "n_refused", i32, 1, dev))
+    step.n_seq, step.device = min(cu_new.numel() - 1, seq_len.numel()), dev
+    return step
+
+
+def earn_page_tables_workspace_bytes(n_seq: int) -> int:
+    return lib().earn_page_tables_workspace_bytes(n_seq)
+
+
+def earn_page_tables(n_seq: int, target, pool: EarnPagePool, step: EarnStep, held_out, n_free_out, workspace) -> None:
+    """target int32 [n_seq] -> the pool's tables and stack, the step's arrays, held_out int32 [n_seq] (may be the pool's held)
+    and n_free_out int32 [1] (may be its n_free)."""
+    dev, i32 = _current_device(), torch.int32
+    if pool.n_seq < n_seq or step.n_seq < n_seq:
+        raise ValueError(f"the pool or the step holds fewer than {n_seq} sequences")
+    if pool.device != dev or step.device != dev:
+        raise ValueError(f"pool on CUDA device {pool.device}, step on {step.device}, expected the current one ({dev})")
+    p, size = _scratch(workspace, dev)
+    _check(lib().earn_page_tables(n_seq, _tensor(target, "target", i32, n_seq, dev), pool, step,
+                                  _tensor(held_out, "held_out", i32, n_seq, dev), _tensor(n_free_out, "n_free_out", i32, 1, dev),
+                                  p, size, _stream_of(dev)), "earn_page_tables")
+
+
+def make_rope(freq: Optional[torch.Tensor], interleaved: bool = False, amplitude: float = 1.0) -> EarnRope:
+    """freq: fp64 [rot_dim / 2] on the current device, radians per position (rope.frequencies), kept alive by the caller;
+    None: nothing turns."""
+    dev = torch.cuda.current_device()
+    n = 0 if freq is None else freq.numel()
+    rope = EarnRope(2 * n, int(interleaved), amplitude, None if n == 0 else _tensor(freq, "freq", torch.float64, n, dev))
+    rope.device = dev
+    return rope
+
+
+def _rows(t, what: str, dtype: torch.dtype, n: int, heads: int, d: int, device: int):
+    """Address and token stride (elements) of [>= n, heads, d] rows whose heads are dense."""
+    if t is None:
+        return None, 0
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{what}: {tuple(shape)}, expected at least [{n}, {heads}, {d}]")
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != d) or (shape[0] > 1 and stride[0] < heads * d):
+        raise ValueError(f"{what}: strides {stride}, expected a token's heads one after the other")
+    if t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on the current CUDA device ({device})")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
+
+
+def earn_rope(model: EarnModel, rope: EarnRope, n_tokens: int, positions, q, k, q_out, k_out, inverse: bool = False) -> None:
+    """q [n, Hq, D] and k [n, Hkv, D] (a token's heads dense, tokens at any stride; either may be None) -> q_out, k_out dense."""
+    dt, dev = _TORCH_DTYPE[model.dtype], _current_device()
+    hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
+    if rope.device != dev:
+        raise ValueError(f"rope on CUDA device {rope.device}, expected the current one ({dev})")
+    qp, qs = _rows(q, "q", dt, n_tokens, hq, d, dev)
+    kp, ks = _rows(k, "k", dt, n_tokens, hkv, d, dev)
+    _check(lib().earn_rope(model, rope, n_tokens, _tensor(positions, "positions", torch.int32, n_tokens, dev), qp, qs, kp, ks,
+                           None if q_out is None else _tensor(q_out, "q_out", dt, n_tokens * hq * d, dev),
+                           None if k_out is None else _tensor(k_out, "k_out", dt, n_tokens * hkv * d, dev), int(inverse),
+                           _stream_of(dev)), "earn_rope")
+
+
+def earn_rope_append(model: EarnModel, layer: int, rope: EarnRope, n_tokens: int, positions, slots, q, k, v, q_out,
+                     cache: EarnPagedCache) -> None:
+    """q [n, Hq, D] (or None), k, v [n, Hkv, D] (a token's heads dense, tokens at any stride) -> q_out dense and the pages;
+    positions, slots int32 [n] (earn_page_tables)."""
+    dt, dev, i32 = _TORCH_DTYPE[model.dtype], _current_device(), torch.int32
+    hq, hkv, d = model.n_q_heads, model.n_kv_heads, model.head_dim
+    if rope.device != dev:
+        raise ValueError(f"rope on CUDA device {rope.device}, expected the current one ({dev})")
+    _check_cache(model, 0, cache, dt, hkv, d, dev)
+    qp, qs = _rows(q, "q", dt, n_tokens, hq, d, dev)
+    kp, ks = _rows(k, "k", dt, n_tokens, hkv, d, dev)
+    vp, vs = _rows(v, "v", dt, n_tokens, hkv, d, dev)
+    _check(lib().earn_rope_append(model, layer, rope, n_tokens, _tensor(positions, "positions", i32, n_tokens, dev),
+                                  _tensor(slots, "slots", i32, n_tokens, dev), qp, qs, kp, ks, vp, vs,
+                                  None if q_out is None else _tensor(q_out, "q_out", dt, n_tokens * hq * d, dev), cache,
+                                  _stream_of(dev)), "earn_rope_append")
+
+
+def earn_paged_chunk_workspace_bytes(model: EarnModel, n_seq: int, n_tokens: int, cache: EarnPagedCache) -> int:
+    return lib().earn_paged_chunk_workspace_bytes(C.byref(model), n_seq, n_tokens, C.byref(cache))
+
+
+def earn_paged_chunk_attn(model: EarnModel, n_seq: int, layer: int, n_tokens: int, cu_new, q, cache: EarnPagedCache, o, lse=None,
+                          workspace=None) -> None:
+    """q, o [n_tokens, Hq, D], cu_new int32 [n_seq + 1], lse fp32 [Hq, n_tokens] or None; the cache's seq_len counts the new
+    rows, which are in its pages."""
+    dt, dev = _TORCH_DTYPE[model.dtype], _current_device()
+    hq, d = model.n_q_heads, model.head_dim
+    _check_cache(model, n_seq, cache, dt, model.n_kv_heads, d, dev)
+    nq = n_tokens * hq * d
+    p, size = _scratch(workspace, dev)
+    _check(lib().earn_paged_chunk_attn(model, n_seq, layer, n_tokens, _tensor(cu_new, "cu_new", torch.int32, n_seq + 1, dev),
+                                       _tensor(q, "q", dt, nq, dev), cache, _tensor(o, "o", dt, nq, dev),
+                                       None if lse is None else _tensor(lse, "lse", torch.float32, n_tokens * hq, dev), p, size,
+                                       _stream_of(dev)), "earn_paged_chunk_attn")

@@ -4,6 +4,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "chunk_step.cuh"
 #include "earn_common.cuh"
 #include "paged_cache.cuh"
 
@@ -247,6 +248,42 @@ static PagedLayout paged_layout(const earn_model_t* m, int32_t n_seq, const earn
   l.moves = l.n_moves + round_up(units * 4, 256);
   const size_t evict_end = l.moves + round_up(units * 2 * (size_t)l.list * 4, 256);
   l.total = decode_end > evict_end ? decode_end : evict_end;
+  return l;
+}
+
+// ---- steps of several new tokens: shared checks
+static earn_status_t check_rope(const earn_model_t* m, const earn_rope_t* r, int32_t n_tokens) {
+  if (r == nullptr || n_tokens < 0 || r->rot_dim < 0 || r->rot_dim > m->head_dim || r->rot_dim % 2 != 0) return EARN_ERR_INVALID_ARG;
+  if (!(r->amplitude >= 0.f) || (r->rot_dim > 0 && (r->freq == nullptr || (reinterpret_cast<uintptr_t>(r->freq) & 7u) != 0)))
+    return EARN_ERR_INVALID_ARG;
+  return EARN_OK;
+}
+// rows of `heads` heads, a token every `stride` elements
+static bool bad_rows(const earn_model_t* m, const void* p, int64_t stride, int heads) {
+  return !aligned16(p) || stride < (int64_t)heads * m->head_dim || stride > (INT64_MAX >> 4) / INT32_MAX ||
+         stride * (int64_t)elem_size(m) % 16 != 0;
+}
+static RopeArgs rope_args(const earn_model_t* m, const earn_rope_t* r, int32_t n_tokens, const int32_t* positions) {
+  RopeArgs a{};
+  a.positions = positions; a.freq = r->freq; a.n_tokens = n_tokens;
+  a.Hq = m->n_q_heads; a.Hkv = m->n_kv_heads; a.D = m->head_dim; a.dtype = m->dtype;
+  a.rot = r->rot_dim; a.interleaved = r->interleaved != 0;
+  a.amplitude = r->amplitude > 0.f ? r->amplitude : 1.f; a.sign = 1.f;
+  return a;
+}
+// Workspace of the chunk attention: status block, tickets, the parts' sums and references, the parts.
+struct ChunkLayout {
+  size_t tickets, part_ml, part_o, total;
+  ChunkPlan plan;
+};
+static ChunkLayout chunk_layout(const earn_model_t* m, int32_t n_seq, int32_t n_tokens, const earn_paged_cache_t* c) {
+  ChunkLayout l{};
+  l.plan = plan_chunk_attn(n_seq, m->n_q_heads, m->n_kv_heads, m->head_dim, m->dtype, n_tokens, c->max_len);
+  const size_t tiles = (size_t)l.plan.grid * l.plan.tiles, rows = 2 * tiles * l.plan.rows;
+  l.tickets = kStatusBytes;
+  l.part_ml = l.tickets + round_up(tiles * 4, 256);
+  l.part_o = l.part_ml + round_up(rows * 8, 256);
+  l.total = l.part_o + rows * (size_t)m->head_dim * 4;
   return l;
 }
 
@@ -750,6 +787,129 @@ earn_status_t earn_evict_kv(const earn_model_t* model, int32_t n_seq, int32_t la
   a.budget = policy->budget; a.n_first = policy->n_first; a.n_last = policy->n_last;
   note_call(stream, CALL_UNKNOWN);
   return launch_evict(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+size_t earn_page_tables_workspace_bytes(int32_t n_seq) {
+  (void)n_seq;
+  return kStatusBytes + 256;
+}
+
+earn_status_t earn_page_tables(int32_t n_seq, const int32_t* target, const earn_page_pool_t* pool, const earn_step_t* step,
+                               int32_t* held_out, int32_t* n_free_out, void* workspace, size_t workspace_bytes,
+                               earn_stream_t stream) {
+  if (pool == nullptr || step == nullptr || n_seq < 0 || step->n_tokens < 0) return EARN_ERR_INVALID_ARG;
+  if (pool->pages_per_seq < 1 || pool->n_pages < 1) return EARN_ERR_INVALID_ARG;
+  if (n_seq > kPageTablesMaxSeqs || pool->pages_per_seq > INT32_MAX / EARN_PAGE_TOKENS - 1 ||
+      pool->n_pages > INT32_MAX / EARN_PAGE_TOKENS - 1 || step->n_tokens > INT32_MAX - (1 << 24))
+    return EARN_ERR_UNSUPPORTED;   // row and slot numbers are 32-bit
+  if (n_seq == 0) return EARN_OK;
+  if (!target || !pool->block_table || !pool->held || !pool->free_pages || !pool->n_free || !held_out || !n_free_out ||
+      !step->cu_new || !step->seq_len || !step->n_refused || (step->n_tokens > 0 && (!step->positions || !step->slots)))
+    return EARN_ERR_INVALID_ARG;
+  if (!aligned4(target) || !aligned4(pool->block_table) || !aligned4(pool->held) || !aligned4(pool->free_pages) ||
+      !aligned4(pool->n_free) || !aligned4(held_out) || !aligned4(n_free_out) || !aligned4(step->cu_new) ||
+      !aligned4(step->seq_len) || !aligned4(step->n_refused) || !aligned16(step->positions) || !aligned16(step->slots))
+    return EARN_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < earn_page_tables_workspace_bytes(n_seq))
+    return EARN_ERR_WORKSPACE;
+  PageTableArgs a{};
+  a.target = target; a.held = pool->held; a.held_out = held_out; a.block_table = pool->block_table;
+  a.free_pages = pool->free_pages; a.n_free = pool->n_free; a.n_free_out = n_free_out;
+  a.cu_new = step->cu_new; a.seq_len = step->seq_len; a.positions = step->positions; a.slots = step->slots;
+  a.n_refused = step->n_refused;
+  a.ticket = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + kStatusBytes);
+  a.n_seq = n_seq; a.n_tokens = step->n_tokens; a.pages_per_seq = pool->pages_per_seq; a.n_pages = pool->n_pages;
+  note_call(stream, CALL_UNKNOWN);
+  return launch_page_tables(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+earn_status_t earn_rope(const earn_model_t* model, const earn_rope_t* rope, int32_t n_tokens, const int32_t* positions,
+                        const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
+                        int32_t inverse, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  s = check_rope(model, rope, n_tokens);
+  if (s != EARN_OK) return s;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return EARN_ERR_INVALID_ARG;
+  if (n_tokens == 0 || (q == nullptr && k == nullptr)) return EARN_OK;
+  if (!positions || !aligned4(positions) || !aligned16(q_out) || !aligned16(k_out)) return EARN_ERR_INVALID_ARG;
+  if ((q != nullptr && bad_rows(model, q, q_stride, model->n_q_heads)) || (k != nullptr && bad_rows(model, k, k_stride, model->n_kv_heads)))
+    return EARN_ERR_INVALID_ARG;
+  RopeArgs a = rope_args(model, rope, n_tokens, positions);
+  const int64_t es = (int64_t)elem_size(model);
+  a.q = reinterpret_cast<const char*>(q); a.q_stride = q_stride * es; a.q_out = reinterpret_cast<char*>(q_out);
+  a.k = reinterpret_cast<const char*>(k); a.k_stride = k_stride * es; a.k_out = reinterpret_cast<char*>(k_out);
+  if (inverse) a.sign = -1.f;
+  note_call(stream, CALL_UNKNOWN);
+  return launch_rope(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const earn_rope_t* rope, int32_t n_tokens,
+                               const int32_t* positions, const int32_t* slots, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, void* q_out, const earn_paged_cache_t* cache,
+                               earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  if (layer < 0 || layer >= model->split_k) return EARN_ERR_INVALID_ARG;
+  s = check_rope(model, rope, n_tokens);
+  if (s != EARN_OK) return s;
+  s = check_paged(cache, 0, false);
+  if (s != EARN_OK) return s;
+  if (cache->n_pages > INT32_MAX / EARN_PAGE_TOKENS) return EARN_ERR_UNSUPPORTED;   // slot numbers are 32-bit
+  if ((q == nullptr) != (q_out == nullptr)) return EARN_ERR_INVALID_ARG;
+  if (n_tokens == 0) return EARN_OK;
+  if (!positions || !slots || !k || !v || !aligned4(positions) || !aligned4(slots) || !aligned16(q_out)) return EARN_ERR_INVALID_ARG;
+  if ((q != nullptr && bad_rows(model, q, q_stride, model->n_q_heads)) || bad_rows(model, k, k_stride, model->n_kv_heads) ||
+      bad_rows(model, v, v_stride, model->n_kv_heads))
+    return EARN_ERR_INVALID_ARG;
+  RopeArgs a = rope_args(model, rope, n_tokens, positions);
+  const int64_t es = (int64_t)elem_size(model);
+  a.q = reinterpret_cast<const char*>(q); a.q_stride = q_stride * es; a.q_out = reinterpret_cast<char*>(q_out);
+  a.k = reinterpret_cast<const char*>(k); a.k_stride = k_stride * es;
+  a.v = reinterpret_cast<const char*>(v); a.v_stride = v_stride * es;
+  a.slots = slots;
+  a.cache = paged_rows(cache);
+  note_call(stream, CALL_UNKNOWN);
+  return launch_rope(a, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+}
+
+size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
+                                        const earn_paged_cache_t* cache) {
+  if (check_model(model) != EARN_OK || n_seq < 0 || n_seq > 65535 || n_tokens < 0 || check_paged(cache, n_seq, false) != EARN_OK)
+    return kStatusBytes;
+  return chunk_layout(model, n_seq, n_tokens, cache).total;
+}
+
+earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, int32_t n_tokens,
+                                    const int32_t* cu_new, const void* q, const earn_paged_cache_t* cache, void* o,
+                                    float* lse_or_null, void* workspace, size_t workspace_bytes, earn_stream_t stream) {
+  earn_status_t s = check_model(model);
+  if (s != EARN_OK) return s;
+  if (n_seq < 0 || n_tokens < 0 || layer < 0 || layer >= model->split_k) return EARN_ERR_INVALID_ARG;
+  if (n_seq > 65535) return EARN_ERR_UNSUPPORTED;
+  s = check_paged(cache, n_seq, true);
+  if (s != EARN_OK) return s;
+  if (n_seq == 0 || n_tokens == 0) return EARN_OK;
+  if (!cu_new || !q || !o || !aligned4(cu_new) || !aligned16(q) || !aligned16(o) || !aligned4(lse_or_null)) return EARN_ERR_INVALID_ARG;
+  const ChunkLayout l = chunk_layout(model, n_seq, n_tokens, cache);
+  if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < l.total) return EARN_ERR_WORKSPACE;
+  char* ws = reinterpret_cast<char*>(workspace);
+  ChunkArgs a{};
+  a.q = q; a.o = o; a.lse = lse_or_null; a.cache = paged_rows(cache);
+  a.sched.cu_new = cu_new; a.sched.seq_len = cache->seq_len;
+  a.sched.n_seq = n_seq; a.sched.n_tokens = n_tokens; a.sched.max_len = cache->max_len;
+  a.sched.heads = model->n_kv_heads * l.plan.blocks;
+  a.sched.item_tok = l.plan.tile_tok * l.plan.tiles; a.sched.key_tile = l.plan.keys;
+  a.sched.grid = l.plan.grid; a.sched.min_share = l.plan.min_share;
+  a.tickets = reinterpret_cast<int32_t*>(ws + l.tickets);
+  a.part_ml = reinterpret_cast<float2*>(ws + l.part_ml);
+  a.part_o = reinterpret_cast<float4*>(ws + l.part_o);
+  a.status = reinterpret_cast<int32_t*>(ws);
+  a.Hq = model->n_q_heads; a.Hkv = model->n_kv_heads; a.D = model->head_dim; a.dtype = model->dtype;
+  a.g = model->n_q_heads / model->n_kv_heads; a.block_heads = l.plan.block_heads; a.blocks = l.plan.blocks;
+  a.scale = scale_of(model);
+  note_call(stream, CALL_UNKNOWN);
+  return launch_chunk_simt(a, l.plan, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }
 
 }  // extern "C"
