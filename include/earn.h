@@ -469,7 +469,7 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  * Lists are cut at places that depend on the lengths only, and joined in the order of the keys: equal calls, equal results.
  * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init.
  * Errors: layer outside [0, k), n_seq < 0, n_tokens < 0, a malformed cache, NULL or misaligned tensors -> INVALID_ARG;
- * n_seq > 65535 -> UNSUPPORTED; workspace -> WORKSPACE. */
+ * n_seq > 65535, 16 * n_pages beyond 2^31 - 1 -> UNSUPPORTED; workspace -> WORKSPACE. */
 size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
                                         const earn_paged_cache_t* cache);
 earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, int32_t n_tokens,

@@ -185,11 +185,11 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   }
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
   constexpr int RT = 64, bytes = smem_floats<D, RT>() * 4;
-  cudaError_t e = ensure_dynamic_smem<chunk_simt_kernel<T, D, RT>>(bytes);
-  if (e == cudaSuccess) e = launch_pdl(chunk_simt_kernel<T, D, RT>, dim3(a.sched.grid), dim3(THREADS), bytes, st, a);
+  cudaError_t e = ensure_dynamic_smem<chunk_simt_kernel<float, D, RT>>(bytes);
+  if (e == cudaSuccess) e = launch_pdl(chunk_simt_kernel<float, D, RT>, dim3(a.sched.grid), dim3(THREADS), bytes, st, a);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -198,22 +198,22 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
 
 ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int dtype, int n_tokens, int max_len) {
   ChunkPlan p{};
-  p.rows = 64; p.tiles = 1; p.keys = KT; p.min_share = 1;
+  const bool tc = dtype == EARN_BF16;
+  p.rows = tc ? 128 : 64;
+  p.tiles = tc ? 2 : 1;
+  p.keys = tc ? 128 : KT;
+  p.min_share = tc ? 2 : 1;
   const int g = n_q_heads / n_kv_heads;
   p.blocks = (g + p.rows - 1) / p.rows;
   p.block_heads = (g + p.blocks - 1) / p.blocks;
   p.tile_tok = p.rows / p.block_heads;
   // no more CTAs than there can be units
-  const int64_t items = (int64_t)n_tokens / p.tile_tok + std::min(n_seq, n_tokens);
+  const int64_t items = (int64_t)n_tokens / (p.tile_tok * p.tiles) + std::min(n_seq, n_tokens);
   const int64_t units = items * n_kv_heads * p.blocks * ((max_len + p.keys - 1) / p.keys);
-  p.grid = (int)std::min<int64_t>(sm_count() * (D == 64 ? 3 : 2), std::max<int64_t>(units, 1));
+  p.grid = (int)std::min<int64_t>(sm_count() * (tc ? 1 : D == 64 ? 3 : 2), std::max<int64_t>(units, 1));
   return p;
 }
 
-cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st) {
-  (void)p;
-  if (a.dtype == EARN_F32) return a.D == 64 ? launch<float, 64>(a, st) : launch<float, 128>(a, st);
-  return a.D == 64 ? launch<__nv_bfloat16, 64>(a, st) : launch<__nv_bfloat16, 128>(a, st);
-}
+cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st) { return a.D == 64 ? launch<64>(a, st) : launch<128>(a, st); }
 
 }  // namespace earn

@@ -51,7 +51,8 @@ struct ChunkPlan {
   int rows, tiles, keys, block_heads, blocks, tile_tok, grid, min_share;
 };
 ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int dtype, int n_tokens, int max_len);
-cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);
+cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st);                      // fp32
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);    // bf16
 
 // Softmax denominator of a row, natural log: once per row, so the logarithm is taken in 64 bits (the fast 32-bit one is off by
 // a few 1e-7, which is all of what fp32 callers see).  A row that sees nothing: -inf.

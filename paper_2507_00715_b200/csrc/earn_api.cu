@@ -889,6 +889,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   if (n_seq > 65535) return EARN_ERR_UNSUPPORTED;
   s = check_paged(cache, n_seq, true);
   if (s != EARN_OK) return s;
+  if (cache->n_pages > INT32_MAX / EARN_PAGE_TOKENS) return EARN_ERR_UNSUPPORTED;   // the copy engine's row numbers are 32-bit
   if (n_seq == 0 || n_tokens == 0) return EARN_OK;
   if (!cu_new || !q || !o || !aligned4(cu_new) || !aligned16(q) || !aligned16(o) || !aligned4(lse_or_null)) return EARN_ERR_INVALID_ARG;
   const ChunkLayout l = chunk_layout(model, n_seq, n_tokens, cache);
@@ -909,7 +910,8 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   a.g = model->n_q_heads / model->n_kv_heads; a.block_heads = l.plan.block_heads; a.blocks = l.plan.blocks;
   a.scale = scale_of(model);
   note_call(stream, CALL_UNKNOWN);
-  return launch_chunk_simt(a, l.plan, (cudaStream_t)stream) == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
+  const cudaError_t e = a.dtype == EARN_BF16 ? launch_chunk_tc(a, l.plan, (cudaStream_t)stream) : launch_chunk_simt(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }
 
 }  // extern "C"
