@@ -84,6 +84,7 @@ struct ChunkWalk {
   int64_t total, tol;  // units in all; a cut closer than this to an item's edge is moved there
   int shares;          // shares the line is cut into
   int b, h, m, off;    // where pos is: unit `off` of item m under head block h of sequence b
+  int longest;         // most new tokens of a sequence
 };
 
 __host__ __device__ inline int64_t chunk_cut(const ChunkWalk& w, int c) { return (int64_t)c * w.total / w.shares; }
@@ -135,13 +136,15 @@ __host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, int64_t st
 }
 
 #ifdef __CUDACC__
-// This CTA's share of the line; every thread of the CTA calls it (`scratch`: shared memory for 40 64-bit words).
+// This CTA's share of the line; every thread of the CTA calls it (`scratch`: shared memory for 64 64-bit words).
 __device__ inline ChunkWalk chunk_share(const ChunkSched& s, int64_t* scratch) {
   const int t = threadIdx.x, threads = blockDim.x, lane = t & 31, warp = t >> 5;
   const int per = (s.n_seq + threads - 1) / threads, b0 = min(t * per, s.n_seq), b1 = min(b0 + per, s.n_seq);
   int64_t mine = 0;
+  int longest = 0;
   for (int b = b0; b < b1; ++b) {
     const ChunkSeq q = chunk_seq(s, b);
+    longest = max(longest, q.n);
     if (q.n > 0) mine += s.heads * chunk_units_before(s, q, chunk_items(s, q));
   }
   int64_t incl = mine;
@@ -150,14 +153,17 @@ __device__ inline ChunkWalk chunk_share(const ChunkSched& s, int64_t* scratch) {
     const int64_t v = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += v;
   }
-  if (lane == 31) scratch[warp] = incl;
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 31) { scratch[warp] = incl; scratch[32 + warp] = longest; }
   __syncthreads();
   int64_t before = incl - mine, total = 0;
   for (int w = 0; w < threads / 32; ++w) {
     if (w < warp) before += scratch[w];
     total += scratch[w];
+    longest = max(longest, (int)scratch[32 + w]);
   }
   ChunkWalk w{};
+  w.longest = longest;
   w.total = total;
   const int64_t shares = (total + s.min_share - 1) / s.min_share;
   w.shares = (int)(shares < s.grid ? (shares > 0 ? shares : 1) : s.grid);

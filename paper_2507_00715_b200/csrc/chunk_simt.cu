@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   float* Ks = Qs + RT * D;   // float4 c of row r lies at c ^ (r & 7): sixteen rows are read at once
   float* Vs = Ks + KT * D;
   float* Ps = Vs + KT * D;
-  __shared__ int64_t scratch[40];
+  __shared__ int64_t scratch[64];
   __shared__ int last_part;
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
   const ChunkSched& s = a.sched;
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
         __threadfence();
       }
       __syncthreads();
-      if (last_part) chunk_join<T, D, RT, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads);
+      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads);
     }
     w.pos += stop - w.off;
     if (stop == units) chunk_next(s, w, q);

@@ -38,7 +38,7 @@ struct ChunkArgs {
   float* lse;                  // [Hq, n_tokens] or null
   PagedSource cache;
   ChunkSched sched;
-  float4* part_o;              // [2 * grid][row tiles][D / 4][rows]
+  float4* part_o;              // [2 * grid][row tiles][D / 4][rows], or [rows][D / 4]
   float2* part_ml;             // [2 * grid][row tiles][rows]: reference of the exponentials, their sum
   int32_t* tickets;            // [grid][row tiles], zero between calls
   int32_t* status;
@@ -64,14 +64,15 @@ __device__ __forceinline__ float chunk_lse(float ref, float sum) {
 
 // Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows: element (row, four
 // columns) by element, `threads` threads of which this is number t.  The parts are added in their order along the keys, so
-// the result does not depend on which of them came last.  LOG2: references are in the log2 domain, else natural.
-template <typename T, int D, int ROWS, bool LOG2>
+// the result does not depend on which of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR:
+// a part is [rows][D], else [D / 4][rows][4].
+template <typename T, int D, int ROWS, bool LOG2, bool ROW_MAJOR>
 __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t, int threads,
                                            int tok0, int n_tok, int head0, int n_heads) {
   constexpr int C4 = D / 4, AHEAD = 8;
   const int used = n_tok * a.block_heads;   // rows of the tile that hold a token
   for (int i = t; i < used * C4; i += threads) {
-    const int row = i % used, c4 = i / used, tok = row / a.block_heads, head = row - tok * a.block_heads;
+    const int row = ROW_MAJOR ? i / C4 : i % used, c4 = ROW_MAJOR ? i % C4 : i / used, tok = row / a.block_heads, head = row - tok * a.block_heads;
     if (head >= n_heads) continue;
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -83,7 +84,7 @@ __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts&
         if (p0 + p >= parts.parts) { ml[p] = make_float2(-INFINITY, 0.f); v[p] = make_float4(0.f, 0.f, 0.f, 0.f); continue; }
         const int64_t slot = (int64_t)(2 * (parts.first + p0 + p) + (p0 + p == 0 ? 1 : 0)) * tiles + x;
         ml[p] = __ldcg(a.part_ml + slot * ROWS + row);
-        v[p] = __ldcg(a.part_o + (slot * C4 + c4) * ROWS + row);
+        v[p] = __ldcg(a.part_o + (ROW_MAJOR ? (slot * ROWS + row) * C4 + c4 : (slot * C4 + c4) * ROWS + row));
       }
       float mx = m;
 #pragma unroll

@@ -1,20 +1,30 @@
 // Causal attention of every sequence's new tokens over its paged list, on the Blackwell tensor cores (bf16, fp32 logits,
 // softmax and accumulation).
 //
-// A CTA (one per SM) walks its share of the work line (chunk_sched.cuh).  A row tile is 128 rows (token, query head) of one kv
-// head, so that a kv head's K and V tiles of 128 keys (8 pages) serve all its query heads at once.  An item of more than one
-// row tile runs two of them against the same K/V tiles; an item of at most one (a decoded token, a short chunk) runs its even
-// and odd key tiles as two streams that meet in the end, so that both softmax warpgroups have work and the copies never pause.
+// A CTA (one per SM) walks its share of the work line (chunk_sched.cuh) with K and V tiles of 128 keys (8 pages), each read once
+// for all query heads of a kv head.  An item's rows are (token, query head); how many there are picks its form:
 //
-//   warp 0    TMA: the pages of the K and V tiles -> shared memory (128-byte swizzle), 16 rows x 64 columns a copy, a ring that
-//             runs on across items
-//   warp 2    TMA: the Q tiles of the next item, as soon as the last S of the current item has read them
-//   warp 3    rows behind the last key in the last page of an item: zeroed in V (a weight of zero does not undo a NaN)
-//   warp 1    tcgen05.mma: S_x = Q K^T into tensor memory, O_x += P_x V with P_x read from tensor memory
-//   warps 4.. one softmax warpgroup per stream x, one row per thread; the row's reference maximum is that of its first 32 visible
-//             keys and raised only when a tile's sum of exponentials exceeds 2^8 (exact after the division by the row's sum)
+//   PAIR   more than 128 rows: two row tiles of 128 against the same K/V tiles
+//   ROWS   up to 128 rows: one row tile, even and odd key tiles as two streams that meet in the end
+//   COLS   where no item of the call has more than 32 rows (decoded tokens, drafts): the same two streams transposed,
+//          S^T = K Q^T and O^T = V^T P^T, so that all threads have a key each instead of a few threads a row each
 //
-// An item that is cut leaves fp32 parts; the CTA that finishes last joins them (chunk_join).  Every mbarrier wait is bounded:
+//   warp 0      TMA: the pages of the K and V tiles -> shared memory (128-byte swizzle), 16 rows x 64 columns a copy, a ring that
+//               runs on across items
+//   warp 1      what there is to do, a few parts ahead; TMA: the Q tiles of the next item, as soon as the last S of the current
+//               one has read them; and the rows behind the last key in the last page of an item, zeroed in V (a weight of zero
+//               does not undo a NaN)
+//   warps 2, 3  tcgen05.mma, one warp per stream (row tile, or half of the key tiles): S into tensor memory, O += P V with P read
+//               from tensor memory (COLS: shared memory).  What a warp waits for and how long it takes to issue is hidden behind
+//               the other's products: one warp for both was 1.4 times slower on long lists
+//   warps 4..   one softmax warpgroup per stream x
+//
+// PAIR and ROWS: one row per thread, a key tile in two halves of 64 with an accumulator each, so that a warpgroup works on one
+// half while the tensor core multiplies the other (P V of a half, then the next tile's S over it: P lies over S).  The row's
+// reference maximum is that of its first 32 visible keys and raised only when a half's sum of exponentials exceeds 2^8 (exact
+// after the division by the row's sum).  COLS: one key per thread, references common to the warpgroup, raised likewise.
+//
+// An item that is cut leaves fp32 parts; the CTA that finishes last joins them (chunk_join), once it has nothing else to do.  Every mbarrier wait is bounded:
 // when one runs out the CTA raises its abort flag, writes EARN_ERR_TIMEOUT to the status word, waits for what it has in flight,
 // frees its TMEM and returns.
 #include <algorithm>
@@ -37,28 +47,38 @@ struct Cfg {
   static constexpr int NHALF = HD / 64;
   static constexpr int NSTAGE = HD == 128 ? 4 : 8;
   static constexpr int OFF_Q = 0, OFF_RING = OFF_Q + 2 * TILE, OFF_OUT = OFF_RING + NSTAGE * TILE;
-  static constexpr int OFF_ML = OFF_OUT + 8 * 4096, OFF_BAR = OFF_ML + 128 * 8;
-  static constexpr int SMEM_BYTES = OFF_BAR + 768 + 1024;       // + alignment slack
+  static constexpr int OFF_ML = OFF_OUT + 8 * 4096, OFF_REF = OFF_ML + 128 * 8, OFF_PART = OFF_REF + 2 * 32 * 4, OFF_BAR = OFF_PART + 4 * 64;
+  static constexpr int SMEM_BYTES = OFF_BAR + 512 + 1024;       // + alignment slack
   static constexpr int THREADS = 384;
-  static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 2, O = P + 2,
-                       OM = O + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, N_BARS = DRAIN + 1;
-  static_assert(8 * N_BARS + 16 + 320 <= 768, "barrier block");
+  static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 4, O = P + 4,
+                       D = O + 2, OM = D + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2, PARTFREE = PARTFULL + 4,
+                       GROUP = PARTFREE + 4, N_BARS = GROUP + 2, OFF_VOTE = 8 * N_BARS + 32;
+  static_assert(OFF_VOTE + 32 <= 512, "barrier block");
 };
 
-// One item's share of this CTA.
-struct Part {
+enum Form { PAIR, ROWS, COLS };
+constexpr int MAX_COLS = 32;   // rows of an item in the transposed form
+
+// One item's share of this CTA, as warp 1 hands it to the others (16 words in shared memory).
+struct alignas(16) Part {
   int b, kvh, head0, n_heads;   // sequence, kv head, first query head, query heads
   int tok0, tok_in, n_tok;      // first token in the batch and in the chunk, tokens
   int base, keys;               // rows in front of the chunk; keys that the item's last token sees
-  int u0, n;                    // key tiles u0 .. u0 + n - 1
-  bool two;                     // two row tiles; else two streams of key tiles
-  bool last;                    // the item's last key tile is among them
+  int u0, n;                    // key tiles u0 .. u0 + n - 1; n = 0: no more parts
+  int form;
+  int n_rows;                   // rows of the first row tile
+  int last;                     // the item's last key tile is among them
+  int first, parts;             // CTAs first .. first + parts - 1 hold one part each
 };
-__device__ __forceinline__ Part part_of(const ChunkArgs& a, const ChunkWalk& w, const ChunkSeq& q, int tile_tok) {
+static_assert(sizeof(Part) == 64, "four 16-byte words");
+
+// The CTA's parts one after the other.
+__device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols) {
   const ChunkSched& s = a.sched;
-  Part p;
+  Part p{};
+  if (w.pos >= w.end) return p;
   p.b = w.b;
-  p.kvh = w.h / a.blocks;
+  p.kvh = a.blocks > 1 ? w.h / a.blocks : w.h;
   p.head0 = p.kvh * a.g + (w.h - p.kvh * a.blocks) * a.block_heads;
   p.n_heads = min(a.block_heads, (p.kvh + 1) * a.g - p.head0);
   p.tok_in = w.m * s.item_tok;
@@ -69,21 +89,26 @@ __device__ __forceinline__ Part part_of(const ChunkArgs& a, const ChunkWalk& w, 
   const int units = chunk_units(s, q, w.m);
   p.u0 = w.off;
   p.n = (int)min((int64_t)(units - w.off), w.end - w.pos);
-  p.two = p.n_tok > tile_tok;
+  p.n_rows = min(p.n_tok, tile_tok) * a.block_heads;
+  p.form = cols ? COLS : p.n_tok > tile_tok ? PAIR : ROWS;
   p.last = w.off + p.n == units;
+  p.parts = 1;
+  if (w.off > 0 || !p.last) {
+    const ChunkParts parts = chunk_parts(w, w.pos - w.off, units);
+    p.first = parts.first;
+    p.parts = parts.parts;
+  }
+  w.pos += p.n;
+  if (p.last) chunk_next(s, w, q);
+  else w.off += p.n;
   return p;
 }
-__device__ __forceinline__ void part_next(const ChunkArgs& a, ChunkWalk& w, ChunkSeq& q, const Part& p) {
-  w.pos += p.n;
-  if (p.last) chunk_next(a.sched, w, q);
-  else w.off += p.n;
-}
-// Ring entries of a part, 2 n of them.  Two row tiles: K0 V0 K1 V1 ..; two streams: K0 K1 V0 K2 V1 K3 .. V(n-1), as they are
-// consumed (a stream's next S follows its P V).
-__device__ __forceinline__ int entry_k(const Part& p, int j) { return p.two ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int entry_v(const Part& p, int j) { return p.two ? 2 * j + 1 : j == p.n - 1 ? 2 * p.n - 1 : 2 * j + 2; }
+// Ring entries of a part, 2 n of them.  PAIR: K0 V0 K1 V1 ..; two streams: K0 K1 V0 K2 V1 K3 .. V(n-1), as they are consumed (a
+// stream's next S follows its P V).
+__device__ __forceinline__ int entry_k(const Part& p, int j) { return p.form == PAIR ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int entry_v(const Part& p, int j) { return p.form == PAIR ? 2 * j + 1 : j == p.n - 1 ? 2 * p.n - 1 : 2 * j + 2; }
 __device__ __forceinline__ void entry_at(const Part& p, int i, bool& is_v, int& j) {
-  if (p.two) { is_v = i & 1; j = i >> 1; return; }
+  if (p.form == PAIR) { is_v = i & 1; j = i >> 1; return; }
   if (i & 1) { j = (i + 1) >> 1; is_v = j >= p.n; if (is_v) j = p.n - 1; return; }
   is_v = i > 0;
   j = is_v ? (i >> 1) - 1 : 0;
@@ -95,10 +120,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c) {   // d = a * b + c
-  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %4};\n\tmov.b64 rc, {%5, %5};\n\t"
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c0, float c1) {   // d = a * b + c
+  asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %4};\n\tmov.b64 rc, {%5, %6};\n\t"
       "fma.rn.ftz.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c0), "f"(c1));
 }
 __device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {   // d += a
   asm("{\n\t.reg .b64 ra, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rd, {%0, %1};\n\tadd.rn.ftz.f32x2 rd, rd, ra;\n\t"
@@ -111,18 +136,329 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst_smem, const CUtensorMap
       ::"r"(dst_smem), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
-__device__ __forceinline__ void group_sync(int x) { asm volatile("bar.sync %0, 128;" ::"r"(x + 1) : "memory"); }
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {   // 32 lanes x 16 columns, waited for
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// v[c] of all lanes combined; the result for column `lane % N` is returned
+template <int N, class Op>
+__device__ __forceinline__ float across_lanes(float (&v)[N], int lane, Op op) {
+#pragma unroll
+  for (int d = N / 2; d > 0; d >>= 1) {
+#pragma unroll
+    for (int i = 0; i < d; ++i) {
+      const float give = (lane & d) ? v[i] : v[i + d], keep = (lane & d) ? v[i + d] : v[i];
+      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, d));
+    }
+  }
+  if (N == 16) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
+  return v[0];
+}
+constexpr float NO_REF = 3.0e38f;   // added to a logit that has no reference yet: 2^(that) is inf unless the logit is -inf
+
+// The warp's arrival: what its lanes did before is visible to who waits.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+  __syncwarp();
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar) : "memory");
+}
+// Warp-wide bounded wait, the same answer in every lane.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, (uint32_t)parity & 1u, abort_flag, WAIT_LIMIT)) != 0;
+}
+// The four warps of a softmax warpgroup wait for one another, on an mbarrier: a named barrier would wait for good for a warp
+// that has given up.  False: a wait ran out.
+struct Group {
+  uint32_t bar, votes;   // votes: four words, that of phase n is n & 3
+  volatile int* abort_flag;
+  int n;
+  __device__ __forceinline__ bool sync() {
+    warp_arrive(bar);
+    return warp_wait(bar, n++, abort_flag);
+  }
+  __device__ __forceinline__ bool any(bool mine, bool& result) {
+    const uint32_t at = votes + 4u * (uint32_t)(n & 3);
+    if (__any_sync(0xffffffffu, mine)) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(1u) : "memory");
+    const bool ok = sync();
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    result = v != 0;
+    // (this word's next phase is four on; the others have read it before they get there, and it is cleared in between)
+    return ok;
+  }
+  __device__ __forceinline__ void clear() {   // by the first warp, after each phase: the word of the phase after the next
+    asm volatile("st.shared.u32 [%0], %1;" ::"r"(votes + 4u * (uint32_t)((n + 1) & 3)), "r"(0u) : "memory");
+  }
+};
 __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
 
+// The same instructions as in sm100_ptx.cuh, issued by one elected lane of a converged warp, so that the descriptors stay
+// warp-uniform arithmetic (a branch on the lane around them cost 1.1 times the time on long lists).
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+               "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
 struct TcArgs {
   ChunkArgs a;
   int tile_tok, q_box_tok;   // tokens of a row tile; tokens that a copy of Q brings
   float scale_log2;
 };
+
+// What a warpgroup has left of items that are cut: at most its first part and its last.
+struct Cut {
+  int n;
+  Part part[2];
+};
+// Its parts are written: joins those of which it was the last to finish.  (All 128 threads; x: stream, rows: row tile.)
+template <int HD, bool ROW_MAJOR>
+__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Cut& cut, int tile_tok, int x, int t, volatile int* flag, Group& group) {
+  if (cut.n == 0) return;
+  __threadfence();
+  if (!group.sync()) return;
+#pragma unroll 1
+  for (int i = 0; i < cut.n; ++i) {
+    const Part& p = cut.part[i];
+    if (t == 0) {
+      const int32_t at = p.first * 2 + x;
+      const bool is_last = atomicAdd(a.tickets + at, 1) == p.parts - 1;
+      if (is_last) a.tickets[at] = 0;   // for the next call
+      flag[x] = is_last;
+      __threadfence();
+    }
+    if (!group.sync()) return;
+    if (flag[x] != 0) {
+      const int my_tok = p.form == PAIR ? x * tile_tok : 0;
+      ChunkParts parts;
+      parts.first = p.first;
+      parts.parts = p.parts;
+      chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 128, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads);
+    }
+    if (!group.sync()) return;   // (the flag has been read)
+  }
+}
+__device__ __forceinline__ int64_t part_slot(const Part& p, int x) {
+  return (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == p.first ? 1 : 0)) * 2 + x;
+}
+
+// Phases that a stream has consumed: S of either half of a key tile, O_x, D_x, merges.
+struct Phases {
+  int s[2], o, d, ml;
+  bool pending;   // stream 1: stream 0 may still be reading what the last merge needs
+};
+
+// Stream x of a part of at most NC rows, transposed: thread = key, column = row.  Sums stay with the threads until the part ends;
+// the references (negated, log2 domain) are shared.  Returns false when a wait ran out.
+template <int HD, int NC>
+__device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& ta, const Part& p, int x, uint32_t tmem, uint32_t base,
+                                             uint32_t bars, volatile int* abort_flag, Phases& n, Group& group) {
+  using C = Cfg<HD>;
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
+  const uint32_t lane0 = (uint32_t)(warp * 32) << 16, t_s = tmem + lane0 + x * 128, t_o = tmem + lane0 + (2 + x) * 128;
+  const uint32_t slab = base + C::OFF_OUT + (uint32_t)x * (4 * 4096);   // P^T [key][row], 128 bytes a key
+  const uint32_t refs = base + C::OFF_REF + (uint32_t)x * 128, ml1 = base + C::OFF_ML;
+  const float sl2 = ta.scale_log2;
+  auto wait = [&](int i, int parity) { return warp_wait(bars + 8u * (uint32_t)i, parity, abort_flag); };
+  auto sync = [&]() {
+    const bool ok = group.sync();
+    if (warp == 0) group.clear();
+    return ok;
+  };
+  auto ld = [](uint32_t at) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; };
+  auto st = [](uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); };
+  auto ld2 = [](uint32_t at) { float2 v; asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory"); return v; };
+  auto st2 = [](uint32_t at, float u, float v) { asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(u), "f"(v) : "memory"); };
+  const int first_seen = p.base + p.tok_in + 1;   // keys that the first token sees
+  float l[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) l[c] = 0.f;
+  for (int j = x; j < p.n; j += 2) {
+    if (!wait(C::S + 2 * x, n.s[0]++)) return false;
+    tc_fence_after();
+    const bool first = j < 2, interior = (p.u0 + j + 1) * BN <= first_seen;
+    const int at = (p.u0 + j) * BN + key;
+    // the tile's logits in the log2 domain, without a reference; what the row does not see is -inf
+    auto logits = [&](uint32_t (&s)[NC]) {
+      if constexpr (NC == 32) { tmem_ld_32x32(t_s, s); tmem_wait_ld(s); }
+      else tmem_ld_32x16(t_s, s);
+      if (!interior) {
+        int tok = 0, head = 0;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (at >= first_seen + tok) s[c] = 0xff800000u;
+          if (++head == a.block_heads) { head = 0; ++tok; }
+        }
+      }
+    };
+    // references from the tile's own maxima, where the old ones (none in front of the first tile) do not hold: shared by way of
+    // the slab, whose last reader, the stream's last product with V, is done
+    auto raise = [&]() {
+      uint32_t s[NC];
+      float v[NC];
+      logits(s);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) v[c] = __uint_as_float(s[c]) * sl2;
+      const float mine = across_lanes<NC>(v, lane, [](float u, float t) { return fmaxf(u, t); });
+      if (lane < NC) st(slab + (uint32_t)(warp * NC + lane) * 4, mine);
+      if (!sync()) return false;
+      if (warp == 0 && lane < NC) {
+        const float top = fmaxf(fmaxf(ld(slab + lane * 4), ld(slab + (NC + lane) * 4)), fmaxf(ld(slab + (2 * NC + lane) * 4), ld(slab + (3 * NC + lane) * 4)));
+        const float old = first ? NO_REF : ld(refs + lane * 4);
+        // (rows that hold nothing get -inf: their weights are 0, or NaN, and go nowhere)
+        const float fresh = lane >= p.n_rows ? -INFINITY : top == -INFINITY ? old : old == NO_REF ? -top : top + old > 8.f ? -top : old;
+        st(slab + (uint32_t)(4 * NC + lane) * 4, old == NO_REF ? 0.f : lane >= p.n_rows ? 1.f : ex2(fresh - old));
+        st(refs + lane * 4, fresh);
+      }
+      return sync();
+    };
+    if (first && !raise()) return false;
+    uint32_t pk[NC / 2];
+    float e[NC];
+#pragma unroll 1
+    for (int attempt = 0;; ++attempt) {
+      uint32_t s[NC];
+      logits(s);
+      float top = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; c += 2) {
+        const float2 r = ld2(refs + c * 4);
+        fma2(e[c], e[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), sl2, r.x, r.y);
+        e[c] = ex2(e[c]);
+        e[c + 1] = ex2(e[c + 1]);
+        top = max3(top, e[c], e[c + 1]);
+        pk[c >> 1] = pack_bf16(e[c], e[c + 1]);
+      }
+      if (first || attempt > 0) break;   // (the references are this tile's)
+      bool grown;
+      if (!group.any(top > 256.f, grown)) return false;
+      if (warp == 0) group.clear();
+      if (!grown) break;
+      if (!raise()) return false;
+      // what has been accumulated, to the new references: O^T is quiescent (S was issued behind the stream's last product)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) l[c] *= ld(slab + (uint32_t)(4 * NC + c) * 4);
+      if constexpr (NC == 32) {
+        tmem_ld_32x32(t_o, s);
+        tmem_wait_ld(s);
+      } else {
+        tmem_ld_32x16(t_o, s);
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) * ld(slab + (uint32_t)(4 * NC + c) * 4));
+      if constexpr (NC == 32) tmem_st_32x32(t_o, s);
+      else tmem_st_32x16(t_o, s);
+      tmem_wait_st();
+      if (!sync()) return false;   // (the slab is P's again)
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) l[c] += e[c];
+#pragma unroll
+    for (int ch = 0; ch < NC / 8; ++ch)
+      st_shared_v4(slab + (uint32_t)key * 128 + (uint32_t)((ch ^ (key & 7)) << 4), pk[ch * 4], pk[ch * 4 + 1], pk[ch * 4 + 2], pk[ch * 4 + 3]);
+    fence_async_smem();
+    if (n.pending) {
+      n.pending = false;
+      if (!wait(C::MERGED, n.ml - 1)) return false;
+    }
+    tc_fence_before();
+    warp_arrive(bars + 8u * (C::P + 2 * x));
+  }
+  // ---- end of the part
+  const bool merge = p.n > 1;
+  const float sum = across_lanes<NC>(l, lane, [](float u, float t) { return u + t; });
+  if (merge && x == 1) {
+    if (lane < NC) st2(ml1 + (uint32_t)(warp * NC + lane) * 8, ld(refs + lane * 4), sum);
+    tc_fence_before();
+    warp_arrive(bars + 8u * C::ML);
+    ++n.ml;
+    n.pending = true;
+    return true;
+  }
+  if (!wait(C::O + x, n.o++)) return false;
+  if (merge && !(wait(C::OM, n.ml) && wait(C::ML, n.ml))) return false;
+  tc_fence_after();
+  if (merge) ++n.ml;
+  const bool whole = p.parts == 1;
+  const int64_t slot = part_slot(p, x);
+  if (lane < NC) st(slab + (uint32_t)(warp * NC + lane) * 4, sum);
+  if (!sync()) return false;
+  if (warp == 0 && lane < NC) {
+    const float neg0 = ld(refs + lane * 4);
+    float l0 = (ld(slab + lane * 4) + ld(slab + (NC + lane) * 4)) + (ld(slab + (2 * NC + lane) * 4) + ld(slab + (3 * NC + lane) * 4));
+    float m = neg0 == NO_REF ? -INFINITY : -neg0, w0 = 1.f, w1 = 0.f;
+    if (merge) {
+      const float2 o0 = ld2(ml1 + lane * 8), o1 = ld2(ml1 + (NC + lane) * 8), o2 = ld2(ml1 + (2 * NC + lane) * 8), o3 = ld2(ml1 + (3 * NC + lane) * 8);
+      const float m1 = o0.x == NO_REF ? -INFINITY : -o0.x, mx = fmaxf(m, m1), ref = mx == -INFINITY ? 0.f : mx;
+      w0 = ex2(m - ref);
+      w1 = ex2(m1 - ref);
+      l0 = l0 * w0 + ((o0.y + o1.y) + (o2.y + o3.y)) * w1;
+      m = mx;
+    }
+    const float inv = !whole ? 1.f : l0 == 0.f ? 0.f : __frcp_rn(l0);
+    st2(slab + 1024 + lane * 8, w0 * inv, w1 * inv);
+    st(slab + 2048 + lane * 4, l0);
+    const int tok = lane / a.block_heads, head = lane - tok * a.block_heads;
+    if (lane < p.n_rows && head < p.n_heads) {
+      if (!whole) a.part_ml[slot * BM + lane] = make_float2(m, l0);
+      else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + p.tok0 + tok] = chunk_lse<true>(m, l0);
+    }
+  }
+  if (!sync()) return false;
+  if (key < HD) {   // (whole warps) lane = element of the head
+    uint32_t s0[NC], s1[NC];
+    if constexpr (NC == 32) { tmem_ld_32x32(t_o, s0); tmem_wait_ld(s0); }
+    else tmem_ld_32x16(t_o, s0);
+    if (merge) {
+      if constexpr (NC == 32) { tmem_ld_32x32(t_o + 128, s1); tmem_wait_ld(s1); }
+      else tmem_ld_32x16(t_o + 128, s1);
+    }
+    int tok = 0, head = 0;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (c < p.n_rows) {
+        const float2 f = ld2(slab + 1024 + c * 8);
+        float y = __uint_as_float(s0[c]) * f.x;
+        if (merge) y += __uint_as_float(s1[c]) * f.y;
+        if (ld(slab + 2048 + c * 4) == 0.f) y = 0.f;   // (nothing visible: O holds nothing)
+        if (head < p.n_heads) {
+          if (whole) reinterpret_cast<__nv_bfloat16*>(a.o)[((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + key] = __float2bfloat16(y);
+          else reinterpret_cast<float*>(a.part_o)[(slot * BM + c) * HD + key] = y;
+        }
+        if (++head == a.block_heads) { head = 0; ++tok; }
+      }
+    }
+  }
+  tc_fence_before();
+  if (merge) warp_arrive(bars + 8u * C::MERGED);
+  return sync();   // (the slab's numbers have been read)
+}
 
 template <int HD>
 __global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
@@ -138,34 +474,45 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_BAR + 8 * C::N_BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 8);
-  int* last_part = reinterpret_cast<int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 12);   // [2], behind the flag
+  volatile int* last_part = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 12);   // [2], behind the flag
   float2* ml1 = reinterpret_cast<float2*>(gen + C::OFF_ML);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NSTAGE; ++i) {
       mbar_init(bar(C::FULL + i), 1);
-      mbar_init(bar(C::EMPTY + i), 2);   // the tensor core's reads, and warp 3
+      mbar_init(bar(C::EMPTY + i), 3);   // both streams, warp 1
       mbar_init(bar(C::FIX + i), 1);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(bar(C::QFULL + x), 1);
-      mbar_init(bar(C::QFREE + x), 1);
-      mbar_init(bar(C::S + x), 1);
-      mbar_init(bar(C::P + x), 128);
+      mbar_init(bar(C::QFREE + x), 2 - x);   // both streams see the first Q tile, the second one only stream 1
       mbar_init(bar(C::O + x), 1);
+      mbar_init(bar(C::D + x), 1);
+    }
+    for (int i = 0; i < 4; ++i) {   // stream, half of the key tile
+      mbar_init(bar(C::S + i), 1);
+      mbar_init(bar(C::P + i), 4);   // (one lane a warp: 128 arrivals took as long as a quarter of the tile's exponentials)
     }
     mbar_init(bar(C::OM), 1);
-    mbar_init(bar(C::ML), 128);
-    mbar_init(bar(C::MERGED), 128);
+    mbar_init(bar(C::ML), 4);
+    mbar_init(bar(C::MERGED), 4);
     mbar_init(bar(C::DRAIN), 1);
+    mbar_init(bar(C::DRAIN + 1), 1);
+    mbar_init(bar(C::GROUP), 4);
+    mbar_init(bar(C::GROUP + 1), 4);
+    for (int i = 0; i < 8; ++i) reinterpret_cast<uint32_t*>(gen + C::OFF_BAR + C::OFF_VOTE)[i] = 0;
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar(C::PARTFULL + i), 1);
+      mbar_init(bar(C::PARTFREE + i), 11);   // warps 0, 2, 3 and the softmax warps
+    }
     *abort_flag = 0;
     fence_barrier_init();
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
   }
-  if (warp == 1) {
+  if (warp == 2) {
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
     tmem_relinquish();
   }
@@ -175,20 +522,32 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   const uint32_t tmem = *tmem_slot;   // S_x (and P_x over it) at x * 128, O_x at (2 + x) * 128
   pdl_launch_dependents();
   pdl_wait();
-  ChunkWalk w = chunk_share(a.sched, reinterpret_cast<int64_t*>(gen + C::OFF_BAR + 8 * C::N_BARS + 32));
-  ChunkSeq q{};
-  if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
-  auto wait = [&](int i, int parity) {   // warp-uniform result
-    return __all_sync(0xffffffffu, mbar_wait_bounded(bar(i), (uint32_t)parity & 1u, abort_flag, WAIT_LIMIT));
+  ChunkWalk w = chunk_share(a.sched, reinterpret_cast<int64_t*>(gen));
+  const bool cols = w.longest * a.block_heads <= MAX_COLS;
+  fence_async_smem();   // (the copies that come next land where the shares' scratch was)
+  __syncthreads();
+  auto wait = [&](int i, int parity) { return warp_wait(bar(i), parity, abort_flag); };
+
+  // Part k of this CTA, from warp 1; false: no more of them, or a wait ran out.
+  auto get_part = [&](int k, Part& p) {
+    const int at = k & 3;
+    if (!wait(C::PARTFULL + at, k >> 2)) return false;
+    const int4* from = reinterpret_cast<const int4*>(gen + C::OFF_PART + at * 64);
+    int4* to = reinterpret_cast<int4*>(&p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = from[i];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(C::PARTFREE + at));
+    return p.n > 0;
   };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer: K/V ring
     const int pg = lane & 7, half = lane >> 3;   // lane's page of the tile and 64-column block of it
-    int e = 0;   // ring entries issued so far, over all items
+    int e = 0;   // ring entries issued so far, over all parts
     bool ok = true;
-    while (w.pos < w.end && ok) {
-      const Part p = part_of(a, w, q, ta.tile_tok);
+    Part p;
+    for (int k = 0; ok && get_part(k, p); ++k) {
       const int n_pages = (p.keys + EARN_PAGE_TOKENS - 1) / EARN_PAGE_TOKENS;
       for (int i = 0; i < 2 * p.n; ++i, ++e) {
         bool is_v;
@@ -205,7 +564,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           tma_load_3d(sRing + st * C::TILE + half * C::HALF + pg * (EARN_PAGE_TOKENS * 128), is_v ? &map_v : &map_k, bar(C::FULL + st),
                       half * 64, p.kvh, page * EARN_PAGE_TOKENS);
       }
-      part_next(a, w, q, p);
     }
     if (*abort_flag) {
       // let the copies already in flight land before the CTA gives its shared memory back
@@ -213,39 +571,43 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       for (int f = max(e - C::NSTAGE, 0); f < e; ++f)
         mbar_wait_bounded(bar(C::FULL + f % C::NSTAGE), (f / C::NSTAGE) & 1, &none, WAIT_LIMIT);
     }
-  } else if (warp == 2) {
-    // ------------------------------------------------------------------ TMA producer: Q tiles
-    if (lane == 0) {
-      int n[2] = {0, 0};   // tiles loaded so far
-      bool ok = true;
-      const uint32_t bytes = (uint32_t)(ta.q_box_tok * a.block_heads) * (HD * 2);
-      while (w.pos < w.end && ok) {
-        const Part p = part_of(a, w, q, ta.tile_tok);
-        for (int x = 0; x < (p.two ? 2 : 1); ++x) {
-          if (n[x] > 0 && !mbar_wait_bounded(bar(C::QFREE + x), (n[x] - 1) & 1, abort_flag, WAIT_LIMIT)) { ok = false; break; }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ parts; TMA producer: Q tiles; rows of V behind the last key
+    ChunkSeq q{};
+    if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
+    int e = 0, n_q[2] = {0, 0}, made = 0;   // ring entries passed, Q tiles loaded, parts handed out so far
+    bool ok = true, more = true;
+    const uint32_t bytes = (uint32_t)(ta.q_box_tok * a.block_heads) * (HD * 2);
+    for (int k = 0; ok; ++k) {
+      while (more && made <= k + 2) {   // two parts ahead of the one whose Q is loaded (four places: this warp reads its own there)
+        const int at = made & 3;
+        if (made >= 4 && !wait(C::PARTFREE + at, (made >> 2) - 1)) { ok = false; break; }
+        const Part fresh = next_part(a, w, q, ta.tile_tok, cols);
+        more = fresh.n > 0;
+        if (lane < 4) reinterpret_cast<int4*>(gen + C::OFF_PART + at * 64)[lane] = lane == 0 ? make_int4(fresh.b, fresh.kvh, fresh.head0, fresh.n_heads)
+                          : lane == 1 ? make_int4(fresh.tok0, fresh.tok_in, fresh.n_tok, fresh.base)
+                          : lane == 2 ? make_int4(fresh.keys, fresh.u0, fresh.n, fresh.form) : make_int4(fresh.n_rows, fresh.last, fresh.first, fresh.parts);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::PARTFULL + at));
+        ++made;
+      }
+      if (!ok) break;
+      const Part p = *reinterpret_cast<const Part*>(gen + C::OFF_PART + (k & 3) * 64);
+      if (p.n == 0) break;
+      for (int x = 0; x < (p.form == PAIR ? 2 : 1); ++x) {
+        if (n_q[x] > 0 && !wait(C::QFREE + x, n_q[x] - 1)) { ok = false; break; }
+        if (lane == 0) {
           mbar_expect_tx(bar(C::QFULL + x), bytes);
           for (int h = 0; h < C::NHALF; ++h)
             tma_load_4d(sQ + x * C::TILE + h * C::HALF, &map_q, bar(C::QFULL + x), h * 64, p.head0 - p.kvh * a.g, p.kvh,
                         p.tok0 + x * ta.tile_tok);
-          ++n[x];
         }
-        part_next(a, w, q, p);
+        ++n_q[x];
       }
-      if (*abort_flag) {
-        int none = 0;
-        for (int x = 0; x < 2; ++x)
-          if (n[x] > 0) mbar_wait_bounded(bar(C::QFULL + x), (n[x] - 1) & 1, &none, WAIT_LIMIT);
-      }
-    }
-  } else if (warp == 3) {
-    // ------------------------------------------------------------------ rows of V behind the last key
-    int e = 0;
-    bool ok = true;
-    while (w.pos < w.end && ok) {
-      const Part p = part_of(a, w, q, ta.tile_tok);
-      for (int i = 0; i < 2 * p.n; ++i, ++e) {
+      for (int i = 0; i < 2 * p.n && ok; ++i, ++e) {
         const int st = e % C::NSTAGE;
-        if (!wait(C::FULL + st, e / C::NSTAGE)) { ok = false; break; }
+        ok = wait(C::FULL + st, e / C::NSTAGE);
+        if (!ok) break;
         const int over = p.keys % EARN_PAGE_TOKENS;
         if (p.last && i == 2 * p.n - 1 && over != 0) {   // (the last entry of a part is its last V tile)
           const int row0 = p.keys % BN, rows = EARN_PAGE_TOKENS - over;
@@ -259,264 +621,335 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
         if (lane == 0) mbar_arrive(bar(C::EMPTY + st));
       }
-      part_next(a, w, q, p);
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (the warp runs the loop, lane 0 issues)
-    const bool leader = lane == 0;
-    constexpr uint32_t idesc_s = idesc_bf16_f32(BM, BN, 0, 0);   // Q (K-major) x K^T (K-major)
-    constexpr uint32_t idesc_o = idesc_bf16_f32(BM, HD, 0, 1);   // P (TMEM) x V (MN-major)
+    if (*abort_flag) {
+      int none = 0;
+      for (int x = 0; x < 2; ++x)
+        if (n_q[x] > 0) mbar_wait_bounded(bar(C::QFULL + x), (n_q[x] - 1) & 1, &none, WAIT_LIMIT);
+    }
+  } else if (warp < 4) {
+    // ------------------------------------------------------------------ MMA issuer of stream x
+    const int x = warp - 2;
+    constexpr uint32_t idesc_s = idesc_bf16_f32(BM, BN / 2, 0, 0);   // Q (K-major) x half a K tile^T (K-major)
+    constexpr uint32_t idesc_o = idesc_bf16_f32(BM, HD, 0, 1);       // P (TMEM) x V (MN-major)
     constexpr uint32_t desc_hi = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sRing, 16), v_lo = smem_desc_lo(sRing, C::HALF);
-    auto wait_full = [&](int e) { return wait(C::FULL + e % C::NSTAGE, e / C::NSTAGE); };
-    // S_x = Q_y K^T with the K tile of ring entry e; free_k: nobody else reads the tile
-    auto issue_s = [&](int x, int y, int e, bool free_k) {
-      const uint32_t a0 = q_lo + y * (C::TILE >> 4), b0 = k_lo + (e % C::NSTAGE) * (C::TILE >> 4);
-      if (leader) {
+    const uint32_t p_lo = smem_desc_lo(base + C::OFF_OUT + x * (4 * 4096), 16);
+    const uint32_t t_s = tmem + x * 128, t_o = tmem + (2 + x) * 128;
+    auto free_entry = [&](int e) { mma_commit(bar(C::EMPTY + e % C::NSTAGE)); };
+    // S of half b of a row tile: Q_y times keys 64 b .. of the K tile of ring entry e
+    auto issue_s = [&](int b, int y, int e) {
+      const uint32_t a0 = q_lo + y * (C::TILE >> 4), b0 = k_lo + ((e % C::NSTAGE) * C::TILE + b * (64 * 128) >> 4);
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t off = ((kk >> 2) * C::HALF + (kk & 3) * 32) >> 4;
-          umma_ss_lohi(tmem + x * 128, a0 + off, desc_hi, b0 + off, desc_hi, idesc_s, kk > 0);
-        }
-        umma_commit(bar(C::S + x));
-        if (free_k) umma_commit(bar(C::EMPTY + e % C::NSTAGE));
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        const uint32_t off = ((kk >> 2) * C::HALF + (kk & 3) * 32) >> 4;
+        mma_ss(t_s + b * 64, a0 + off, b0 + off, desc_hi, idesc_s, kk > 0);
+      }
+      mma_commit(bar(C::S + 2 * x + b));
+    };
+    // O (+)= P V over the pages that half b of the tile has
+    auto issue_pv = [&](int b, int e, int pages, bool first) {
+      const uint32_t b0 = v_lo + ((e % C::NSTAGE) * C::TILE + b * (64 * 128) >> 4);
+      const uint32_t more = first ? 0u : 1u;
+      if (pages >= 4 * b + 4) {   // (without a test per product: the tests cost as much as the products)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) mma_ts(t_o, t_s + b * 64 + kk * 8, b0 + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 ? 1u : more);
+      } else {
+#pragma unroll 1
+        for (int kk = 0; 4 * b + kk < pages; ++kk) mma_ts(t_o, t_s + b * 64 + kk * 8, b0 + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 ? 1u : more);
       }
     };
-    // O_x (+)= P_x V over the pages that the tile has
-    auto issue_pv = [&](int x, int e, int pages, bool first, bool free_v) {
-      const uint32_t b0 = v_lo + (e % C::NSTAGE) * (C::TILE >> 4);
-      if (leader) {
-        if (pages >= 8) {
+    // COLS: S^T = K Q^T, and O^T (+)= V^T P^T with P^T [key][row] in shared memory.  (head_dim 64: O^T has 64 rows more than V has
+    // columns; what they are computed from lies within the ring or behind it, and nobody reads them.)
+    auto issue_st = [&](int e, uint32_t idesc) {
+      const uint32_t a0 = k_lo + (e % C::NSTAGE) * (C::TILE >> 4);
 #pragma unroll
-          for (int kk = 0; kk < BN / 16; ++kk)
-            umma_ts_lohi(tmem + (2 + x) * 128, tmem + x * 128 + kk * 8, b0 + kk * (2048 >> 4), desc_hi, idesc_o, (!first || kk > 0) ? 1u : 0u);
-        } else {
-          for (int kk = 0; kk < pages; ++kk)
-            umma_ts_lohi(tmem + (2 + x) * 128, tmem + x * 128 + kk * 8, b0 + kk * (2048 >> 4), desc_hi, idesc_o, (!first || kk > 0) ? 1u : 0u);
-        }
-        if (free_v) umma_commit(bar(C::EMPTY + e % C::NSTAGE));
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        const uint32_t off = ((kk >> 2) * C::HALF + (kk & 3) * 32) >> 4;
+        mma_ss(t_s, a0 + off, q_lo + off, desc_hi, idesc, kk > 0);
       }
+      mma_commit(bar(C::S + 2 * x));
+      free_entry(e);
     };
-    int eb = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};   // ring entry of the part's K_0; phases consumed so far
-    uint32_t fix_phase = 0;                    // a bit per ring stage: warp 3 may be several items ahead, but not on one stage
+    auto issue_vp = [&](int e, int pages, bool first, uint32_t idesc) {
+      const uint32_t a0 = v_lo + (e % C::NSTAGE) * (C::TILE >> 4);
+#pragma unroll 1
+      for (int kk = 0; kk < pages; ++kk) mma_ss(t_o, a0 + kk * (2048 >> 4), p_lo + kk * (2048 >> 4), desc_hi, idesc, (!first || kk > 0) ? 1u : 0u);
+      free_entry(e);
+    };
+    int eb = 0, n_q = 0, n_q0 = 0;   // ring entry of the part's K_0; parts with a second Q tile, and all
+    int filled = 0;                  // ring entries waited for
+    uint32_t p_phase = 0;            // a bit per P barrier
+    uint32_t fix_phase = 0;          // a bit per ring stage: warp 1 may be several items ahead, but not on one stage
+    auto wait_p = [&](int b) {
+      const bool done = wait(C::P + 2 * x + b, p_phase >> b);
+      p_phase ^= 1u << b;
+      return done;
+    };
     bool ok = true;
-    while (w.pos < w.end && ok) {
-      const Part p = part_of(a, w, q, ta.tile_tok);
+    Part p;
+    for (int k = 0; ok && get_part(k, p); ++k) {
       const int n = p.n, n_pages = (p.keys + EARN_PAGE_TOKENS - 1) / EARN_PAGE_TOKENS;
-      // first S of both streams (the part before this one has its P V's in the queue already)
-      ok = wait(C::QFULL, n_q[0]) && wait_full(eb);
-      ++n_q[0];
+      const int stride = p.form == PAIR ? 1 : 2, y = p.form == PAIR ? x : 0, j0 = p.form == PAIR ? 0 : x;
+      const bool fixed = p.last && p.keys % EARN_PAGE_TOKENS != 0;   // the last V tile is one that warp 1 works on
+      const int fix_st = (eb + 2 * n - 1) % C::NSTAGE;
+      // Every entry is waited for, the other stream's too (and handed on at once): a barrier's parity tells the phase only to
+      // those who leave none out.
+      auto wait_full = [&](int e) {
+        for (; filled <= e; ++filled) {
+          const int st = filled % C::NSTAGE;
+          if (!wait(C::FULL + st, filled / C::NSTAGE)) return false;
+          bool is_v;
+          int j;
+          entry_at(p, filled - eb, is_v, j);
+          if (p.form != PAIR && (j & 1) != x && lane == 0) mbar_arrive(bar(C::EMPTY + st));
+        }
+        return true;
+      };
+      ok = wait(C::QFULL, n_q0);
+      if (ok && (y == 1 || j0 >= n) && lane == 0) mbar_arrive(bar(C::QFREE));   // (seen, but not read)
+      if (ok && y == 1) ok = wait(C::QFULL + 1, n_q);
       if (!ok) break;
-      tc_fence_after();
-      issue_s(0, 0, eb, !p.two);
-      if (p.two) {
-        ok = wait(C::QFULL + 1, n_q[1]);
-        ++n_q[1];
+      if (j0 < n) {
+        ok = wait_full(eb + entry_k(p, j0));
         if (!ok) break;
         tc_fence_after();
-        issue_s(1, 1, eb, true);
-        if (leader && n == 1) { umma_commit(bar(C::QFREE)); umma_commit(bar(C::QFREE + 1)); }
-      } else {
-        if (n > 1) {
-          ok = wait_full(eb + 1);
-          if (!ok) break;
-          tc_fence_after();
-          issue_s(1, 0, eb + 1, true);
-        }
-        if (leader && n <= 2) umma_commit(bar(C::QFREE));
-      }
-      for (int j = 0; j < n && ok; ++j) {
-        const int ev = eb + entry_v(p, j), pages = min(n_pages - (p.u0 + j) * 8, 8);
-        const int step = p.two ? 1 : 2;                                    // tiles between two S of a stream
-        const int ek = j + step < n ? eb + entry_k(p, j + step) : -1;
-        for (int y = 0; y < (p.two ? 2 : 1) && ok; ++y) {
-          const int x = p.two ? y : j & 1;
-          ok = wait(C::P + x, n_p[x]);   // P_x written, S_x consumed
-          ++n_p[x];
-          if (ok && y == 0) {
-            ok = wait_full(ev);
-            if (ok && p.last && j == n - 1 && p.keys % EARN_PAGE_TOKENS != 0) {
-              const int st = ev % C::NSTAGE;
-              ok = wait(C::FIX + st, fix_phase >> st);
-              fix_phase ^= 1u << st;
+        auto wait_v = [&](int j) { return wait_full(eb + entry_v(p, j)) && (!fixed || j + 1 < n || wait(C::FIX + fix_st, fix_phase >> fix_st)); };
+        auto pages_of = [&](int j) { return min(n_pages - (p.u0 + j) * 8, 8); };
+        auto free_q = [&]() { mma_commit(bar(C::QFREE + y)); };   // the stream's last S has been issued
+        if (p.form != COLS) {
+          issue_s(0, y, eb + entry_k(p, j0));
+          issue_s(1, y, eb + entry_k(p, j0));
+          free_entry(eb + entry_k(p, j0));
+          if (j0 + stride >= n) free_q();
+          for (int j = j0; j < n && ok; j += stride) {
+            const int ev = eb + entry_v(p, j), ek = eb + entry_k(p, j + stride), pages = pages_of(j);
+            const bool more = j + stride < n;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              ok = wait_p(b) && (b > 0 || wait_v(j));   // P written, S consumed
+              if (!ok) break;
+              tc_fence_after();
+              issue_pv(b, ev, pages, j == j0 && b == 0);
+              if (b == 1) free_entry(ev);
+              if (more) {
+                if (b == 0) ok = wait_full(ek);
+                if (!ok) break;
+                tc_fence_after();
+                issue_s(b, y, ek);
+                if (b == 1) {
+                  free_entry(ek);
+                  if (j + 2 * stride >= n) free_q();
+                }
+              } else if (b == 0) {
+                mma_commit(bar(C::D + x));   // this P V is done (see the softmax)
+              }
             }
           }
-          if (!ok) break;
-          tc_fence_after();
-          issue_pv(x, ev, pages, j < step, !p.two || y == 1);
-          if (ek >= 0) {
-            if (y == 0) ok = wait_full(ek);
+        } else {
+          const uint32_t idesc_st = idesc_bf16_f32(BM, p.n_rows <= 16 ? 16 : 32, 0, 0);   // K (K-major) x Q^T (K-major)
+          const uint32_t idesc_ot = idesc_bf16_f32(BM, p.n_rows <= 16 ? 16 : 32, 1, 1);   // V^T (MN-major) x P^T (MN-major)
+          issue_st(eb + entry_k(p, j0), idesc_st);
+          if (j0 + 2 >= n) free_q();
+          for (int j = j0; j < n && ok; j += 2) {
+            const int ek = eb + entry_k(p, j + 2);
+            ok = wait_p(0) && wait_v(j);
             if (!ok) break;
             tc_fence_after();
-            issue_s(x, p.two ? x : 0, ek, !p.two || y == 1);
-            if (leader && j + step == n - 1) umma_commit(bar(C::QFREE + (p.two ? x : 0)));
-          } else if (leader && p.two) {
-            umma_commit(bar(C::O + x));
+            issue_vp(eb + entry_v(p, j), pages_of(j), j == j0, idesc_ot);
+            if (j + 2 < n) {
+              ok = wait_full(ek);
+              if (!ok) break;
+              tc_fence_after();
+              issue_st(ek, idesc_st);
+              if (j + 4 >= n) free_q();
+            }
           }
         }
+        if (ok) mma_commit(bar(p.form == PAIR || x == 0 ? C::O + x : C::OM));
       }
-      if (ok && !p.two && leader) {
-        umma_commit(bar(C::O));
-        if (n > 1) umma_commit(bar(C::OM));
-      }
+      ok = ok && wait_full(eb + 2 * n - 1);
+      ++n_q0;
+      if (p.form == PAIR) ++n_q;
+      if (fixed) fix_phase ^= 1u << fix_st;
       eb += 2 * n;
-      part_next(a, w, q, p);
     }
-    if (leader && *abort_flag) {
+    if (*abort_flag) {
       int none = 0;
-      umma_commit(bar(C::DRAIN));   // everything this thread issued has retired once this fires
-      mbar_wait_bounded(bar(C::DRAIN), 0, &none, WAIT_LIMIT);
+      mma_commit(bar(C::DRAIN + x));   // everything this warp issued has retired once this fires
+      mbar_wait_bounded(bar(C::DRAIN + x), 0, &none, WAIT_LIMIT);
     }
     __syncwarp();
   } else {
-    // ------------------------------------------------------------------ softmax warpgroup x, one row per thread
+    // ------------------------------------------------------------------ softmax warpgroup x
     const int x = (warp - 4) >> 2;
     const int wq = warp & 3;            // a warp may only touch TMEM lanes 32*(warp % 4) ..
-    const int row = wq * 32 + lane, tok = row / a.block_heads, head = row - tok * a.block_heads;
+    const int row = wq * 32 + lane;
     const uint32_t lane0 = (uint32_t)(wq * 32) << 16;
     const uint32_t t_s = tmem + lane0 + x * 128, t_o = tmem + lane0 + (2 + x) * 128;
     const float sl2 = ta.scale_log2;
-    int n_s = 0, n_o = 0, n_ml = 0;   // phases consumed: S_x, O_x, merges
-    bool pending = false;             // stream 1: stream 0 may still be reading what the last merge needs
+    Phases n{};
+    const int per_head = 65536 / a.block_heads + 1;   // row * per_head >> 16 = row / block_heads for rows below 128
+    const int tok = row * per_head >> 16, head = row - tok * a.block_heads;
+    // before P of a stream is handed over: O_1 and the numbers of the last merge are this stream's again
+    auto settle = [&]() {
+      if (!n.pending) return true;
+      n.pending = false;
+      return wait(C::MERGED, n.ml - 1);
+    };
+    Cut cut;
+    cut.n = 0;
+    Group group{bar(C::GROUP + x), bars + C::OFF_VOTE + 16u * (uint32_t)x, abort_flag, 0};
     bool ok = true;
-    while (w.pos < w.end && ok) {
-      const Part p = part_of(a, w, q, ta.tile_tok);
-      if (!p.two && x >= p.n) { part_next(a, w, q, p); continue; }   // a part of one key tile leaves stream 1 out
-      const int my_tok = p.two ? x * ta.tile_tok : 0;                // first token of this stream's row tile within the item
-      const int n_tok = min(ta.tile_tok, p.n_tok - my_tok);
+    Part p;
+    if (cols) {
+      for (int k = 0; ok && get_part(k, p); ++k) {
+        if (x >= p.n) continue;   // a part of one key tile leaves stream 1 out
+        ok = w.longest * a.block_heads <= 16 ? softmax_cols<HD, 16>(a, ta, p, x, tmem, base, bars, abort_flag, n, group)
+                                             : softmax_cols<HD, 32>(a, ta, p, x, tmem, base, bars, abort_flag, n, group);
+        if (x == 0 && p.parts > 1) cut.part[cut.n++] = p;
+      }
+      if (ok) join_cuts<HD, true>(a, cut, ta.tile_tok, x, row, last_part, group);
+    } else
+    for (int k = 0; ok && get_part(k, p); ++k) {
+      if (p.form != PAIR && x >= p.n) continue;   // a part of one key tile leaves stream 1 out
+      const bool merge = p.form != PAIR && p.n > 1;
+      const int stride = p.form == PAIR ? 1 : 2, my_tok = p.form == PAIR ? x * ta.tile_tok : 0;   // first token of the row tile
+      const int n_tok = min(ta.tile_tok, p.n_tok - my_tok), tok0 = p.tok0 + my_tok;
+      const uint32_t stage = base + C::OFF_OUT + (uint32_t)(warp - 4) * 4096;
       const bool valid = tok < n_tok && head < p.n_heads;
       const int seen = p.base + p.tok_in + my_tok + tok + 1;         // keys that the row sees
       const bool any_row = wq * 32 < n_tok * a.block_heads;          // this warp has a row
+      const int seen_least = __reduce_min_sync(0xffffffffu, valid ? seen : INT32_MAX), seen_most = __reduce_max_sync(0xffffffffu, valid ? seen : 0);
       float m_ref = -INFINITY, l0 = 0.f, l1 = 0.f;                   // -inf: no reference yet
-      for (int j = p.two ? 0 : x; j < p.n; j += p.two ? 1 : 2, ++n_s) {
-        ok = wait(C::S + x, n_s);
-        if (!ok) break;
-        tc_fence_after();
-        const bool first = j < (p.two ? 1 : 2);
-        if (any_row) {
-          // columns visible to the row (all of them to rows that hold nothing: their values go nowhere)
-          const int vis = valid ? min(max(seen - (p.u0 + j) * BN, 0), BN) : BN;
-          const bool interior = __all_sync(0xffffffffu, vis == BN);
-          const int n_chunks = (__reduce_max_sync(0xffffffffu, valid ? vis : 0) + 31) >> 5;   // 32-column chunks with a visible key
-          uint32_t ra[32], rb[32], pk[4][16];
-          // row maximum of the visible part of S_x(j), scaled into the log2 domain (a pass of its own over TMEM)
-          auto row_max_all = [&]() {
-            float mx = -INFINITY;
-            for (int c0 = 0; c0 < n_chunks; ++c0) {
-              tmem_ld_32x32(t_s + c0 * 32, ra);
+      for (int j = p.form == PAIR ? 0 : x; j < p.n && ok; j += stride) {
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          ok = wait(C::S + 2 * x + b, b == 0 ? n.s[0]++ : n.s[1]++);
+          if (!ok) break;
+          tc_fence_after();
+          const bool first = j < stride && b == 0;
+          const uint32_t t_sb = t_s + b * 64;
+          if (any_row) {
+            // columns visible to the row (all of them to rows that hold nothing: their values go nowhere)
+            const int key0 = (p.u0 + j) * BN + b * 64, vis = valid ? min(max(seen - key0, 0), 64) : 64;
+            const bool interior = seen_least >= key0 + 64;
+            const int n_chunks = seen_most > key0 + 32 ? 2 : seen_most > key0 ? 1 : 0;   // 32-column chunks with a visible key
+            uint32_t ra[32], rb[32], pk[2][16];
+            // P = 2^(S * scale - m_ref) as bf16 pairs (kept in registers until the reference is known to hold) and their row
+            // sum, in one pass.  If the sum exceeds 2^8 some logit may have outgrown the reference, or there is none yet: then
+            // find the half's own maximum, raise the reference, rescale what has been accumulated, and redo the pass (S is
+            // intact: nothing has been written over it).
+            float ls0, ls1;
+#pragma unroll 1
+            for (int attempt = 0;; ++attempt) {
+              ls0 = ls1 = 0.f;
+              tmem_ld_32x32(t_sb, ra);
               tmem_wait_ld(ra);
+              if (first && attempt == 0) {
+                float mx = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-              for (int c = 0; c < 32; ++c) mx = fmaxf(mx, c0 * 32 + c < vis ? __uint_as_float(ra[c]) : -INFINITY);
-            }
-            return mx * sl2;
-          };
-          // P = 2^(S * scale - m_ref) as bf16 pairs (kept in registers until the reference is known to hold) and their row
-          // sum, in one pass.  If the sum exceeds 2^8 some logit may have outgrown the reference, and if there is none yet the
-          // first 32 columns had no finite logit: then find the tile's own maximum, raise the reference, rescale what has been
-          // accumulated, and redo the pass (S_x is intact: nothing has been written over it).
-          float ls0, ls1;
-#pragma unroll 1
-          for (int attempt = 0;; ++attempt) {
-            ls0 = ls1 = 0.f;
-            tmem_ld_32x32(t_s, ra);
-            tmem_wait_ld(ra);
-            if (first && attempt == 0) {
-              float mx = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                mx = max3(mx, c < vis ? __uint_as_float(ra[c]) : -INFINITY, c + 1 < vis ? __uint_as_float(ra[c + 1]) : -INFINITY);
-                m1 = max3(m1, c + 2 < vis ? __uint_as_float(ra[c + 2]) : -INFINITY, c + 3 < vis ? __uint_as_float(ra[c + 3]) : -INFINITY);
-              }
-              m_ref = fmaxf(mx, m1) * sl2;
-            }
-            const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
-            // an interior tile takes a copy of the loop without a test per chunk: one block of straight-line code
-            auto chunks = [&](auto interior_tag) {
-              constexpr bool INTERIOR = decltype(interior_tag)::value;
-#pragma unroll
-              for (int c0 = 0; c0 < 4; ++c0) {
-                if (INTERIOR || c0 < n_chunks) {
-                  uint32_t(&cur)[32] = (c0 & 1) ? rb : ra;
-                  uint32_t(&nxt)[32] = (c0 & 1) ? ra : rb;
-                  if (c0 + 1 < 4 && (INTERIOR || c0 + 1 < n_chunks)) tmem_ld_32x32(t_s + (c0 + 1) * 32, nxt);
-                  if (!INTERIOR) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                      if (c0 * 32 + c >= vis) cur[c] = 0xff800000u;   // -inf
-                  }
-#pragma unroll
-                  for (int c = 0; c < 32; c += 2) {
-                    float e0, e1;
-                    fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, neg_m);
-                    e0 = ex2(e0);
-                    e1 = ex2(e1);
-                    add2(ls0, ls1, e0, e1);
-                    pk[c0][c >> 1] = pack_bf16(e0, e1);
-                  }
-                  if (c0 + 1 < 4 && (INTERIOR || c0 + 1 < n_chunks)) tmem_wait_ld(nxt);
-                } else {
-#pragma unroll
-                  for (int c = 0; c < 16; ++c) pk[c0][c] = 0u;
+                for (int c = 0; c < 32; c += 4) {
+                  mx = max3(mx, c < vis ? __uint_as_float(ra[c]) : -INFINITY, c + 1 < vis ? __uint_as_float(ra[c + 1]) : -INFINITY);
+                  m1 = max3(m1, c + 2 < vis ? __uint_as_float(ra[c + 2]) : -INFINITY, c + 3 < vis ? __uint_as_float(ra[c + 3]) : -INFINITY);
                 }
+                m_ref = fmaxf(mx, m1) * sl2;
               }
-            };
-            if (interior) chunks(std::true_type{});
-            else chunks(std::false_type{});
-            const bool grow = valid && (!(ls0 + ls1 <= 256.f) || (m_ref == -INFINITY && vis > 0));
-            if (attempt > 0 || !__any_sync(0xffffffffu, grow)) break;
-            // S_x(j) was issued after the stream's last P V, so the commit that signalled it covers that too: O_x is quiescent.
-            // The whole warp repeats the pass, but only the rows that asked for it take a new reference: a row's result
-            // depends on its own logits alone, whatever its neighbours in the tile do.
-            const float mx_all = row_max_all();
-            const float mxs = grow ? mx_all : m_ref;
-            const float alpha = mxs > m_ref ? ex2(m_ref - mxs) : 1.f;
-            m_ref = fmaxf(m_ref, mxs);
-            l0 *= alpha;
-            l1 *= alpha;
-            if (!first) {
-#pragma unroll 1
-              for (int c0 = 0; c0 < HD / 32; ++c0) {
-                tmem_ld_32x32(t_o + c0 * 32, ra);
+              const float neg_m = m_ref == -INFINITY ? NO_REF : -m_ref;
+              // an interior half takes a copy of the code without a test per chunk: one block of straight-line code
+              auto chunks = [&](auto interior_tag) {
+                constexpr bool INTERIOR = decltype(interior_tag)::value;
+#pragma unroll
+                for (int c0 = 0; c0 < 2; ++c0) {
+                  if (INTERIOR || c0 < n_chunks) {
+                    uint32_t(&cur)[32] = c0 ? rb : ra;
+                    if (c0 == 0 && (INTERIOR || n_chunks > 1)) tmem_ld_32x32(t_sb + 32, rb);
+                    if (!INTERIOR) {
+#pragma unroll
+                      for (int c = 0; c < 32; ++c)
+                        if (c0 * 32 + c >= vis) cur[c] = 0xff800000u;   // -inf
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                      float e0, e1;
+                      fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, neg_m, neg_m);
+                      e0 = ex2(e0);
+                      e1 = ex2(e1);
+                      add2(ls0, ls1, e0, e1);
+                      pk[c0][c >> 1] = pack_bf16(e0, e1);
+                    }
+                    if (c0 == 0 && (INTERIOR || n_chunks > 1)) tmem_wait_ld(rb);
+                  } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) pk[c0][c] = 0u;
+                  }
+                }
+              };
+              if (interior) chunks(std::true_type{});
+              else chunks(std::false_type{});
+              const bool grow = valid && !(ls0 + ls1 <= 256.f);
+              if (attempt > 0 || !__any_sync(0xffffffffu, grow)) break;
+              float mx = -INFINITY;
+              for (int c0 = 0; c0 < n_chunks; ++c0) {
+                tmem_ld_32x32(t_sb + c0 * 32, ra);
                 tmem_wait_ld(ra);
 #pragma unroll
-                for (int c = 0; c < 32; ++c) ra[c] = __float_as_uint(__uint_as_float(ra[c]) * alpha);
-                tmem_st_32x32(t_o + c0 * 32, ra);
+                for (int c = 0; c < 32; ++c) mx = fmaxf(mx, c0 * 32 + c < vis ? __uint_as_float(ra[c]) : -INFINITY);
+              }
+              // The whole warp repeats the pass, but only the rows that asked for it take a new reference: a row's result
+              // depends on its own logits alone, whatever its neighbours in the tile do.
+              const float mxs = grow ? mx * sl2 : m_ref;
+              const float alpha = mxs > m_ref ? ex2(m_ref - mxs) : 1.f;
+              m_ref = fmaxf(m_ref, mxs);
+              l0 *= alpha;
+              l1 *= alpha;
+              if (!first) {
+                // The stream's last P V (the other half's) may be running.  What follows it in the tensor core's queue is the
+                // next S over that half, or, behind the last tile's first half, the commit to D.
+                ok = b == 1 && j + stride >= p.n ? wait(C::D + x, n.d) : wait(C::S + 2 * x + 1 - b, b == 0 ? n.s[1] : n.s[0]);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c0 = 0; c0 < HD / 32; ++c0) {
+                  tmem_ld_32x32(t_o + c0 * 32, ra);
+                  tmem_wait_ld(ra);
+#pragma unroll
+                  for (int c = 0; c < 32; ++c) ra[c] = __float_as_uint(__uint_as_float(ra[c]) * alpha);
+                  tmem_st_32x32(t_o + c0 * 32, ra);
+                }
               }
             }
+            if (!ok) break;
+            l0 += ls0;
+            l1 += ls1;
+            tmem_st_32x16(t_sb, pk[0]);
+            tmem_st_32x16(t_sb + 16, pk[1]);
+            tmem_wait_st();
           }
-          l0 += ls0;
-          l1 += ls1;
-#pragma unroll
-          for (int c0 = 0; c0 < 4; ++c0) tmem_st_32x16(t_s + c0 * 16, pk[c0]);
-          tmem_wait_st();
-        }
-        if (pending) {   // O_1 and the numbers of the last merge are this stream's again
-          ok = wait(C::MERGED, n_ml - 1);
-          pending = false;
+          ok = settle();
           if (!ok) break;
+          tc_fence_before();
+          warp_arrive(bar(C::P + 2 * x + b));
         }
-        tc_fence_before();
-        mbar_arrive(bar(C::P + x));
       }
+      if (ok) ok = wait(C::D + x, n.d++);
       if (!ok) break;
       // ---- end of the part
       float l = l0 + l1, w0 = 1.f, w1 = 0.f;
-      const bool merge = !p.two && p.n > 1;
       if (merge && x == 1) {
         ml1[row] = make_float2(m_ref, l);
         tc_fence_before();
-        mbar_arrive(bar(C::ML));
-        ++n_ml;
-        pending = true;
-        part_next(a, w, q, p);
+        warp_arrive(bar(C::ML));
+        ++n.ml;
+        n.pending = true;
         continue;
       }
-      ok = wait(C::O + x, n_o++);
-      if (ok && merge) ok = wait(C::OM, n_ml) && wait(C::ML, n_ml);
+      ok = wait(C::O + x, n.o++);
+      if (ok && merge) ok = wait(C::OM, n.ml) && wait(C::ML, n.ml);
       if (!ok) break;
       tc_fence_after();
       if (merge) {
-        ++n_ml;
+        ++n.ml;
         const float2 other = ml1[row];
         const float mx = fmaxf(m_ref, other.x), ref = mx == -INFINITY ? 0.f : mx;
         w0 = ex2(m_ref - ref);
@@ -524,15 +957,11 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         l = l * w0 + other.y * w1;
         m_ref = mx;
       }
-      const int64_t start = w.pos - w.off;
-      const ChunkParts parts = chunk_parts(w, start, chunk_units(a.sched, q, w.m));
-      const bool whole = parts.parts == 1;
+      const bool whole = p.parts == 1;
       const float inv = !whole ? 1.f : l == 0.f ? 0.f : __frcp_rn(l);
       w0 *= inv;
       w1 *= inv;
-      const int tok0 = p.tok0 + my_tok;
-      const int64_t slot = (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == parts.first ? 1 : 0)) * 2 + x;
-      const uint32_t stage = base + C::OFF_OUT + (uint32_t)(warp - 4) * 4096;
+      const int64_t slot = part_slot(p, x);
       if (any_row) {
         uint32_t ra[32];
 #pragma unroll
@@ -565,7 +994,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
               __syncwarp();
 #pragma unroll 4
               for (int i = 0; i < 8; ++i) {
-                const int r = i * 4 + (lane >> 3), gr = wq * 32 + r, t = gr / a.block_heads, h = gr - t * a.block_heads;
+                const int r = i * 4 + (lane >> 3), gr = wq * 32 + r, t = gr * per_head >> 16, h = gr - t * a.block_heads;
                 if (t < n_tok && h < p.n_heads) {
                   const uint4 v = ld_shared_v4(stage + (uint32_t)r * 128 + (uint32_t)(((lane & 7) ^ (r & 7)) << 4));
                   *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.o) + ((int64_t)(tok0 + t) * a.Hq + p.head0 + h) * HD +
@@ -585,30 +1014,16 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (valid && !whole) a.part_ml[slot * BM + row] = make_float2(m_ref, l);
       }
       tc_fence_before();   // the next P V over O_x is issued after this warp's next arrive on P_x
-      if (merge) mbar_arrive(bar(C::MERGED));
-      if (!whole) {
-        __threadfence();
-        group_sync(x);
-        if (row == 0) {
-          const int32_t at = parts.first * 2 + x;
-          const bool is_last = atomicAdd(a.tickets + at, 1) == parts.parts - 1;
-          if (is_last) a.tickets[at] = 0;   // for the next call
-          last_part[x] = is_last;
-          __threadfence();
-        }
-        group_sync(x);
-        if (last_part[x])
-          chunk_join<__nv_bfloat16, HD, BM, true>(a, parts, 2, x, row, 128, tok0, n_tok, p.head0, p.n_heads);
-        group_sync(x);   // (the flag has been read)
-      }
-      part_next(a, w, q, p);
+      if (merge) warp_arrive(bar(C::MERGED));
+      if (!whole) cut.part[cut.n++] = p;
     }
+    if (ok && !cols) join_cuts<HD, false>(a, cut, ta.tile_tok, x, row, last_part, group);
   }
 
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(a.status, (int32_t)EARN_ERR_TIMEOUT);
-  if (warp == 1) {
+  if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
