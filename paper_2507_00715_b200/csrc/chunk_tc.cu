@@ -17,12 +17,15 @@
 //   warps 2, 3  tcgen05.mma, one warp per stream (row tile, or half of the key tiles): S into tensor memory, O += P V with P read
 //               from tensor memory (COLS: shared memory).  What a warp waits for and how long it takes to issue is hidden behind
 //               the other's products: one warp for both was 1.4 times slower on long lists
-//   warps 4..   one softmax warpgroup per stream x
+//   warps 4..   softmax, two warpgroups per stream
 //
-// PAIR and ROWS: one row per thread, a key tile in two halves of 64 with an accumulator each, so that a warpgroup works on one
-// half while the tensor core multiplies the other (P V of a half, then the next tile's S over it: P lies over S).  The row's
-// reference maximum is that of its first 32 visible keys and raised only when a half's sum of exponentials exceeds 2^8 (exact
-// after the division by the row's sum).  COLS: one key per thread, references common to the warpgroup, raised likewise.
+// PAIR and ROWS: a key tile is taken in two halves of 64 keys, each with an accumulator and a warpgroup of its own, one row per
+// thread, so that the tensor core has the other halves to multiply while one is in the exponentials (P lies over S: the next S
+// of a half follows its P V).  The reference of a row's exponentials is its largest logit among its first 32 visible keys, and
+// stays: fp32 and bf16 hold 2^127, so a row needs another one only if a logit exceeds that by 44 nats or more.  If the sums tell
+// that one did (or that the first keys had no finite logit), the CTA takes all its parts again, each twice: for the rows' maxima,
+// and with them.  (A test per half and a rescaling of O in place, with one warpgroup per row tile, took 1.4 times as long.)
+// COLS: one key per thread, 16 rows per warpgroup, references common to the warpgroup and raised tile by tile.
 //
 // An item that is cut leaves fp32 parts; the CTA that finishes last joins them (chunk_join), once it has nothing else to do.  Every mbarrier wait is bounded:
 // when one runs out the CTA raises its abort flag, writes EARN_ERR_TIMEOUT to the status word, waits for what it has in flight,
@@ -46,26 +49,38 @@ struct Cfg {
   static constexpr int TILE = 128 * HD * 2, HALF = 128 * 128;   // bytes of a tile, and of its 64-column blocks
   static constexpr int NHALF = HD / 64;
   static constexpr int NSTAGE = HD == 128 ? 4 : 8;
-  static constexpr int OFF_Q = 0, OFF_RING = OFF_Q + 2 * TILE, OFF_OUT = OFF_RING + NSTAGE * TILE;
-  static constexpr int OFF_ML = OFF_OUT + 8 * 4096, OFF_REF = OFF_ML + 128 * 8, OFF_PART = OFF_REF + 2 * 32 * 4, OFF_BAR = OFF_PART + 4 * 64;
-  static constexpr int SMEM_BYTES = OFF_BAR + 512 + 1024;       // + alignment slack
-  static constexpr int THREADS = 384;
+  static constexpr int OFF_Q = 0, OFF_RING = OFF_Q + 2 * TILE, RING_END = OFF_RING + NSTAGE * TILE;
+  static constexpr int OFF_PT = HD == 128 ? OFF_Q + TILE : RING_END;                   // COLS: P^T of either stream (no second Q tile then)
+  static constexpr int OFF_REF = HD == 128 ? RING_END : OFF_PT + 2 * 16384;            // references [stream][row]
+  static constexpr int OFF_SUM = OFF_REF + 2 * 128 * 4;                                // sums [parity][stream][half][row]
+  static constexpr int OFF_MAX = OFF_SUM + 2 * 2 * 2 * 128 * 4;                        // maxima [stream][half][row]
+  static constexpr int OFF_RED = OFF_MAX + 2 * 2 * 128 * 4, RED = 1024;                // COLS: a warpgroup's scratch
+  static constexpr int OFF_SUM1 = OFF_RED + 4 * RED;                                    // stream 1's sums [half][row] for a merge
+  static constexpr int OFF_CUT = OFF_SUM1 + 2 * 128 * 4;                               // parts of items that are cut [stream][2]
+  static constexpr int OFF_PART = OFF_CUT + 4 * 64, OFF_BAR = OFF_PART + 4 * 64;
+  static constexpr int THREADS = 32 * 20;
   static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 4, O = P + 4,
-                       D = O + 2, OM = D + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2, PARTFREE = PARTFULL + 4,
-                       GROUP = PARTFREE + 4, N_BARS = GROUP + 2, OFF_VOTE = 8 * N_BARS + 32;
-  static_assert(OFF_VOTE + 32 <= 512, "barrier block");
+                       OM = O + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2,
+                       PARTFREE = PARTFULL + 4, GROUP = PARTFREE + 4, REFS = GROUP + 4, SUMS = REFS + 2, DONE = SUMS + 2,
+                       N_BARS = DONE + 1, OFF_VOTE = 8 * N_BARS + 32;
+  static constexpr int SMEM_BYTES = OFF_BAR + (OFF_VOTE + 64 + 127) / 128 * 128 + 1024;   // + alignment slack
+  static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of an SM");
 };
 
 enum Form { PAIR, ROWS, COLS };
+enum Pass { FAST, MAXIMA, EXACT };
+constexpr float SUM_LIMIT = 1.8446744e19f;   // 2^64: sums up to here leave O's below 2^64 |v|
 constexpr int MAX_COLS = 32;   // rows of an item in the transposed form
 
 // One item's share of this CTA, as warp 1 hands it to the others (16 words in shared memory).
 struct alignas(16) Part {
+  __device__ __forceinline__ int pass() const { return kind >> 2; }
+  __device__ __forceinline__ int form() const { return kind & 3; }
   int b, kvh, head0, n_heads;   // sequence, kv head, first query head, query heads
   int tok0, tok_in, n_tok;      // first token in the batch and in the chunk, tokens
   int base, keys;               // rows in front of the chunk; keys that the item's last token sees
-  int u0, n;                    // key tiles u0 .. u0 + n - 1; n = 0: no more parts
-  int form;
+  int u0, n;                    // key tiles u0 .. u0 + n - 1; n = 0: all parts have been handed out, n < 0: that was it
+  int kind;                     // form, pass
   int n_rows;                   // rows of the first row tile
   int last;                     // the item's last key tile is among them
   int first, parts;             // CTAs first .. first + parts - 1 hold one part each
@@ -73,7 +88,7 @@ struct alignas(16) Part {
 static_assert(sizeof(Part) == 64, "four 16-byte words");
 
 // The CTA's parts one after the other.
-__device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols) {
+__device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols, int pass) {
   const ChunkSched& s = a.sched;
   Part p{};
   if (w.pos >= w.end) return p;
@@ -90,7 +105,7 @@ __device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, Chun
   p.u0 = w.off;
   p.n = (int)min((int64_t)(units - w.off), w.end - w.pos);
   p.n_rows = min(p.n_tok, tile_tok) * a.block_heads;
-  p.form = cols ? COLS : p.n_tok > tile_tok ? PAIR : ROWS;
+  p.kind = (cols ? COLS : p.n_tok > tile_tok ? PAIR : ROWS) + 4 * pass;
   p.last = w.off + p.n == units;
   p.parts = 1;
   if (w.off > 0 || !p.last) {
@@ -105,10 +120,10 @@ __device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, Chun
 }
 // Ring entries of a part, 2 n of them.  PAIR: K0 V0 K1 V1 ..; two streams: K0 K1 V0 K2 V1 K3 .. V(n-1), as they are consumed (a
 // stream's next S follows its P V).
-__device__ __forceinline__ int entry_k(const Part& p, int j) { return p.form == PAIR ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int entry_v(const Part& p, int j) { return p.form == PAIR ? 2 * j + 1 : j == p.n - 1 ? 2 * p.n - 1 : 2 * j + 2; }
+__device__ __forceinline__ int entry_k(const Part& p, int j) { return p.form() == PAIR ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int entry_v(const Part& p, int j) { return p.form() == PAIR ? 2 * j + 1 : j == p.n - 1 ? 2 * p.n - 1 : 2 * j + 2; }
 __device__ __forceinline__ void entry_at(const Part& p, int i, bool& is_v, int& j) {
-  if (p.form == PAIR) { is_v = i & 1; j = i >> 1; return; }
+  if (p.form() == PAIR) { is_v = i & 1; j = i >> 1; return; }
   if (i & 1) { j = (i + 1) >> 1; is_v = j >= p.n; if (is_v) j = p.n - 1; return; }
   is_v = i > 0;
   j = is_v ? (i >> 1) - 1 : 0;
@@ -136,14 +151,30 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst_smem, const CUtensorMap
       ::"r"(dst_smem), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
-__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {   // 32 lanes x 16 columns, waited for
+__device__ __forceinline__ void tmem_ld_16(uint32_t taddr, uint32_t (&r)[16]) {   // 32 lanes x 16 columns, to be waited for
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
         "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_wait_16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
+  tmem_ld_16(taddr, r);
+  tmem_wait_16(r);
+}
+__device__ __forceinline__ void tmem_st_8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 // v[c] of all lanes combined; the result for column `lane % N` is returned
 template <int N, class Op>
@@ -194,12 +225,6 @@ struct Group {
     asm volatile("st.shared.u32 [%0], %1;" ::"r"(votes + 4u * (uint32_t)((n + 1) & 3)), "r"(0u) : "memory");
   }
 };
-__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-
 // The same instructions as in sm100_ptx.cuh, issued by one elected lane of a converged warp, so that the descriptors stay
 // warp-uniform arithmetic (a branch on the lane around them cost 1.1 times the time on long lists).
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
@@ -226,36 +251,42 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
                "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void st_global_32b(void* at, const uint32_t (&v)[8]) {   // 32-byte aligned
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ float lds(uint32_t at) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; }
+__device__ __forceinline__ void sts(uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
+__device__ __forceinline__ float2 lds2(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts2(uint32_t at, float u, float v) { asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(u), "f"(v) : "memory"); }
+
 struct TcArgs {
   ChunkArgs a;
   int tile_tok, q_box_tok;   // tokens of a row tile; tokens that a copy of Q brings
   float scale_log2;
 };
 
-// What a warpgroup has left of items that are cut: at most its first part and its last.
-struct Cut {
-  int n;
-  Part part[2];
-};
-// Its parts are written: joins those of which it was the last to finish.  (All 128 threads; x: stream, rows: row tile.)
+// The CTA's n parts of items that are cut (at most its first part and its last) are written: joins those of which it was the last
+// to finish.  (All 128 threads; x: row tile.)
 template <int HD, bool ROW_MAJOR>
-__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Cut& cut, int tile_tok, int x, int t, volatile int* flag, Group& group) {
-  if (cut.n == 0) return;
-  __threadfence();
-  if (!group.sync()) return;
+__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, Group& group) {
 #pragma unroll 1
-  for (int i = 0; i < cut.n; ++i) {
-    const Part& p = cut.part[i];
+  for (int i = 0; i < n; ++i) {
+    const Part p = cuts[i];
     if (t == 0) {
       const int32_t at = p.first * 2 + x;
       const bool is_last = atomicAdd(a.tickets + at, 1) == p.parts - 1;
       if (is_last) a.tickets[at] = 0;   // for the next call
-      flag[x] = is_last;
+      *flag = is_last;
       __threadfence();
     }
     if (!group.sync()) return;
-    if (flag[x] != 0) {
-      const int my_tok = p.form == PAIR ? x * tile_tok : 0;
+    if (*flag != 0) {
+      const int my_tok = p.form() == PAIR ? x * tile_tok : 0;
       ChunkParts parts;
       parts.first = p.first;
       parts.parts = p.parts;
@@ -268,48 +299,50 @@ __device__ __forceinline__ int64_t part_slot(const Part& p, int x) {
   return (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == p.first ? 1 : 0)) * 2 + x;
 }
 
-// Phases that a stream has consumed: S of either half of a key tile, O_x, D_x, merges.
+// Phases that a warpgroup has consumed: S, O, references, sums, merges of the streams.
 struct Phases {
-  int s[2], o, d, ml;
+  int s, o, ref, sum, ml;
   bool pending;   // stream 1: stream 0 may still be reading what the last merge needs
 };
 
-// Stream x of a part of at most NC rows, transposed: thread = key, column = row.  Sums stay with the threads until the part ends;
-// the references (negated, log2 domain) are shared.  Returns false when a wait ran out.
-template <int HD, int NC>
-__device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& ta, const Part& p, int x, uint32_t tmem, uint32_t base,
+// Rows 16 h .. 16 h + 15 of stream x of a transposed part: thread = key, column = row.  Sums stay with the threads until the part
+// ends; the references (negated, log2 domain) are shared by the warpgroup.  Returns false when a wait ran out.
+template <int HD>
+__device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, float sl2, const Part& p, int x, int h, bool wide, uint32_t tmem, uint32_t base,
                                              uint32_t bars, volatile int* abort_flag, Phases& n, Group& group) {
   using C = Cfg<HD>;
+  constexpr int NC = 16;
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
-  const uint32_t lane0 = (uint32_t)(warp * 32) << 16, t_s = tmem + lane0 + x * 128, t_o = tmem + lane0 + (2 + x) * 128;
-  const uint32_t slab = base + C::OFF_OUT + (uint32_t)x * (4 * 4096);   // P^T [key][row], 128 bytes a key
-  const uint32_t refs = base + C::OFF_REF + (uint32_t)x * 128, ml1 = base + C::OFF_ML;
-  const float sl2 = ta.scale_log2;
+  const uint32_t lane0 = (uint32_t)(warp * 32) << 16, t_s = tmem + lane0 + x * 128 + h * NC, t_o = tmem + lane0 + (2 + x) * 128 + h * NC;
+  const uint32_t pt = base + C::OFF_PT + (uint32_t)x * 16384 + (uint32_t)key * 128;   // P^T [key][row], 128 bytes a key
+  // scratch: 4 x 16 numbers of the warps, 16 factors, 16 references, 16 pairs, and the same of the other stream's end
+  const uint32_t red = base + C::OFF_RED + (uint32_t)(2 * x + h) * C::RED, scale = red + 256, refs = red + 320, fac = red + 384, ends = red + 512;
+  const uint32_t ends1 = base + C::OFF_RED + (uint32_t)(2 + h) * C::RED + 512;
+  const int row0 = h * NC, rows = min(p.n_rows - row0, NC);
   auto wait = [&](int i, int parity) { return warp_wait(bars + 8u * (uint32_t)i, parity, abort_flag); };
   auto sync = [&]() {
     const bool ok = group.sync();
     if (warp == 0) group.clear();
     return ok;
   };
-  auto ld = [](uint32_t at) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; };
-  auto st = [](uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); };
-  auto ld2 = [](uint32_t at) { float2 v; asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory"); return v; };
-  auto st2 = [](uint32_t at, float u, float v) { asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(u), "f"(v) : "memory"); };
+  if (n.pending) {   // the other stream may be reading this one's scratch and accumulator
+    n.pending = false;
+    if (!wait(C::MERGED, n.ml - 1)) return false;
+  }
   const int first_seen = p.base + p.tok_in + 1;   // keys that the first token sees
   float l[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) l[c] = 0.f;
   for (int j = x; j < p.n; j += 2) {
-    if (!wait(C::S + 2 * x, n.s[0]++)) return false;
+    if (!wait(C::S + 2 * x + h, n.s++)) return false;
     tc_fence_after();
     const bool first = j < 2, interior = (p.u0 + j + 1) * BN <= first_seen;
     const int at = (p.u0 + j) * BN + key;
-    // the tile's logits in the log2 domain, without a reference; what the row does not see is -inf
+    // the tile's logits; what the row does not see is -inf
     auto logits = [&](uint32_t (&s)[NC]) {
-      if constexpr (NC == 32) { tmem_ld_32x32(t_s, s); tmem_wait_ld(s); }
-      else tmem_ld_32x16(t_s, s);
+      tmem_ld_32x16(t_s, s);
       if (!interior) {
-        int tok = 0, head = 0;
+        int tok = row0 / a.block_heads, head = row0 - tok * a.block_heads;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if (at >= first_seen + tok) s[c] = 0xff800000u;
@@ -317,8 +350,7 @@ __device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& t
         }
       }
     };
-    // references from the tile's own maxima, where the old ones (none in front of the first tile) do not hold: shared by way of
-    // the slab, whose last reader, the stream's last product with V, is done
+    // references from the tile's own maxima, where the old ones (none in front of the first tile) do not hold
     auto raise = [&]() {
       uint32_t s[NC];
       float v[NC];
@@ -326,15 +358,15 @@ __device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& t
 #pragma unroll
       for (int c = 0; c < NC; ++c) v[c] = __uint_as_float(s[c]) * sl2;
       const float mine = across_lanes<NC>(v, lane, [](float u, float t) { return fmaxf(u, t); });
-      if (lane < NC) st(slab + (uint32_t)(warp * NC + lane) * 4, mine);
+      if (lane < NC) sts(red + (uint32_t)(warp * NC + lane) * 4, mine);
       if (!sync()) return false;
       if (warp == 0 && lane < NC) {
-        const float top = fmaxf(fmaxf(ld(slab + lane * 4), ld(slab + (NC + lane) * 4)), fmaxf(ld(slab + (2 * NC + lane) * 4), ld(slab + (3 * NC + lane) * 4)));
-        const float old = first ? NO_REF : ld(refs + lane * 4);
+        const float top = fmaxf(fmaxf(lds(red + lane * 4), lds(red + (NC + lane) * 4)), fmaxf(lds(red + (2 * NC + lane) * 4), lds(red + (3 * NC + lane) * 4)));
+        const float old = first ? NO_REF : lds(refs + lane * 4);
         // (rows that hold nothing get -inf: their weights are 0, or NaN, and go nowhere)
-        const float fresh = lane >= p.n_rows ? -INFINITY : top == -INFINITY ? old : old == NO_REF ? -top : top + old > 8.f ? -top : old;
-        st(slab + (uint32_t)(4 * NC + lane) * 4, old == NO_REF ? 0.f : lane >= p.n_rows ? 1.f : ex2(fresh - old));
-        st(refs + lane * 4, fresh);
+        const float fresh = lane >= rows ? -INFINITY : top == -INFINITY ? old : old == NO_REF ? -top : top + old > 8.f ? -top : old;
+        sts(scale + lane * 4, old == NO_REF ? 0.f : lane >= rows ? 1.f : ex2(fresh - old));
+        sts(refs + lane * 4, fresh);
       }
       return sync();
     };
@@ -348,7 +380,7 @@ __device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& t
       float top = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; c += 2) {
-        const float2 r = ld2(refs + c * 4);
+        const float2 r = lds2(refs + c * 4);
         fma2(e[c], e[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), sl2, r.x, r.y);
         e[c] = ex2(e[c]);
         e[c + 1] = ex2(e[c + 1]);
@@ -362,41 +394,33 @@ __device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& t
       if (!grown) break;
       if (!raise()) return false;
       // what has been accumulated, to the new references: O^T is quiescent (S was issued behind the stream's last product)
+      tmem_ld_32x16(t_o, s);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) l[c] *= ld(slab + (uint32_t)(4 * NC + c) * 4);
-      if constexpr (NC == 32) {
-        tmem_ld_32x32(t_o, s);
-        tmem_wait_ld(s);
-      } else {
-        tmem_ld_32x16(t_o, s);
+      for (int c = 0; c < NC; ++c) {
+        const float f = lds(scale + c * 4);
+        l[c] *= f;
+        s[c] = __float_as_uint(__uint_as_float(s[c]) * f);
       }
-#pragma unroll
-      for (int c = 0; c < NC; ++c) s[c] = __float_as_uint(__uint_as_float(s[c]) * ld(slab + (uint32_t)(4 * NC + c) * 4));
-      if constexpr (NC == 32) tmem_st_32x32(t_o, s);
-      else tmem_st_32x16(t_o, s);
+      tmem_st_32x16(t_o, s);
       tmem_wait_st();
-      if (!sync()) return false;   // (the slab is P's again)
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) l[c] += e[c];
 #pragma unroll
     for (int ch = 0; ch < NC / 8; ++ch)
-      st_shared_v4(slab + (uint32_t)key * 128 + (uint32_t)((ch ^ (key & 7)) << 4), pk[ch * 4], pk[ch * 4 + 1], pk[ch * 4 + 2], pk[ch * 4 + 3]);
+      st_shared_v4(pt + (uint32_t)(((2 * h + ch) ^ (key & 7)) << 4), pk[ch * 4], pk[ch * 4 + 1], pk[ch * 4 + 2], pk[ch * 4 + 3]);
     fence_async_smem();
-    if (n.pending) {
-      n.pending = false;
-      if (!wait(C::MERGED, n.ml - 1)) return false;
-    }
     tc_fence_before();
-    warp_arrive(bars + 8u * (C::P + 2 * x));
+    warp_arrive(bars + 8u * (C::P + 2 * x + h));
   }
-  // ---- end of the part
+  // ---- end of the part: the warps' sums, and stream 1's references, meet in stream 0's first warp
   const bool merge = p.n > 1;
   const float sum = across_lanes<NC>(l, lane, [](float u, float t) { return u + t; });
+  if (lane < NC) sts2(ends + (uint32_t)(warp * NC + lane) * 8, lds(refs + lane * 4), sum);
   if (merge && x == 1) {
-    if (lane < NC) st2(ml1 + (uint32_t)(warp * NC + lane) * 8, ld(refs + lane * 4), sum);
     tc_fence_before();
     warp_arrive(bars + 8u * C::ML);
+    if (!wide) warp_arrive(bars + 8u * C::ML);   // (in the place of the second warpgroup)
     ++n.ml;
     n.pending = true;
     return true;
@@ -407,57 +431,59 @@ __device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, const TcArgs& t
   if (merge) ++n.ml;
   const bool whole = p.parts == 1;
   const int64_t slot = part_slot(p, x);
-  if (lane < NC) st(slab + (uint32_t)(warp * NC + lane) * 4, sum);
   if (!sync()) return false;
   if (warp == 0 && lane < NC) {
-    const float neg0 = ld(refs + lane * 4);
-    float l0 = (ld(slab + lane * 4) + ld(slab + (NC + lane) * 4)) + (ld(slab + (2 * NC + lane) * 4) + ld(slab + (3 * NC + lane) * 4));
-    float m = neg0 == NO_REF ? -INFINITY : -neg0, w0 = 1.f, w1 = 0.f;
+    auto end_of = [&](uint32_t from, float& m, float& sum_of) {
+      const float2 v0 = lds2(from + lane * 8), v1 = lds2(from + (NC + lane) * 8), v2 = lds2(from + (2 * NC + lane) * 8), v3 = lds2(from + (3 * NC + lane) * 8);
+      m = v0.x == NO_REF ? -INFINITY : -v0.x;
+      sum_of = (v0.y + v1.y) + (v2.y + v3.y);
+    };
+    float m, l0, w0 = 1.f, w1 = 0.f;
+    end_of(ends, m, l0);
     if (merge) {
-      const float2 o0 = ld2(ml1 + lane * 8), o1 = ld2(ml1 + (NC + lane) * 8), o2 = ld2(ml1 + (2 * NC + lane) * 8), o3 = ld2(ml1 + (3 * NC + lane) * 8);
-      const float m1 = o0.x == NO_REF ? -INFINITY : -o0.x, mx = fmaxf(m, m1), ref = mx == -INFINITY ? 0.f : mx;
+      float m1, l1;
+      end_of(ends1, m1, l1);
+      const float mx = fmaxf(m, m1), ref = mx == -INFINITY ? 0.f : mx;
       w0 = ex2(m - ref);
       w1 = ex2(m1 - ref);
-      l0 = l0 * w0 + ((o0.y + o1.y) + (o2.y + o3.y)) * w1;
+      l0 = l0 * w0 + l1 * w1;
       m = mx;
     }
     const float inv = !whole ? 1.f : l0 == 0.f ? 0.f : __frcp_rn(l0);
-    st2(slab + 1024 + lane * 8, w0 * inv, w1 * inv);
-    st(slab + 2048 + lane * 4, l0);
-    const int tok = lane / a.block_heads, head = lane - tok * a.block_heads;
-    if (lane < p.n_rows && head < p.n_heads) {
-      if (!whole) a.part_ml[slot * BM + lane] = make_float2(m, l0);
+    sts2(fac + lane * 8, l0 == 0.f ? -1.f : w0 * inv, w1 * inv);   // (-1: nothing visible, O holds nothing)
+    const int row = row0 + lane, tok = row / a.block_heads, head = row - tok * a.block_heads;
+    if (lane < rows && head < p.n_heads) {
+      if (!whole) a.part_ml[slot * BM + row] = make_float2(m, l0);
       else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + p.tok0 + tok] = chunk_lse<true>(m, l0);
     }
   }
   if (!sync()) return false;
   if (key < HD) {   // (whole warps) lane = element of the head
     uint32_t s0[NC], s1[NC];
-    if constexpr (NC == 32) { tmem_ld_32x32(t_o, s0); tmem_wait_ld(s0); }
-    else tmem_ld_32x16(t_o, s0);
-    if (merge) {
-      if constexpr (NC == 32) { tmem_ld_32x32(t_o + 128, s1); tmem_wait_ld(s1); }
-      else tmem_ld_32x16(t_o + 128, s1);
-    }
-    int tok = 0, head = 0;
+    tmem_ld_32x16(t_o, s0);
+    if (merge) tmem_ld_32x16(t_o + 128, s1);
+    int tok = row0 / a.block_heads, head = row0 - tok * a.block_heads;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      if (c < p.n_rows) {
-        const float2 f = ld2(slab + 1024 + c * 8);
+      if (c < rows) {
+        const float2 f = lds2(fac + c * 8);
         float y = __uint_as_float(s0[c]) * f.x;
         if (merge) y += __uint_as_float(s1[c]) * f.y;
-        if (ld(slab + 2048 + c * 4) == 0.f) y = 0.f;   // (nothing visible: O holds nothing)
+        if (f.x < 0.f) y = 0.f;
         if (head < p.n_heads) {
           if (whole) reinterpret_cast<__nv_bfloat16*>(a.o)[((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + key] = __float2bfloat16(y);
-          else reinterpret_cast<float*>(a.part_o)[(slot * BM + c) * HD + key] = y;
+          else reinterpret_cast<float*>(a.part_o)[(slot * BM + row0 + c) * HD + key] = y;
         }
         if (++head == a.block_heads) { head = 0; ++tok; }
       }
     }
   }
   tc_fence_before();
-  if (merge) warp_arrive(bars + 8u * C::MERGED);
-  return sync();   // (the slab's numbers have been read)
+  if (merge) {
+    warp_arrive(bars + 8u * C::MERGED);
+    if (!wide) warp_arrive(bars + 8u * C::MERGED);
+  }
+  return sync();   // (the scratch's numbers have been read)
 }
 
 template <int HD>
@@ -474,8 +500,8 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_BAR + 8 * C::N_BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 8);
-  volatile int* last_part = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 12);   // [2], behind the flag
-  float2* ml1 = reinterpret_cast<float2*>(gen + C::OFF_ML);
+  volatile int* redo = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 12);       // a sum left the range: all parts again
+  volatile int* last_part = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 16);  // [2]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -488,25 +514,27 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       mbar_init(bar(C::QFULL + x), 1);
       mbar_init(bar(C::QFREE + x), 2 - x);   // both streams see the first Q tile, the second one only stream 1
       mbar_init(bar(C::O + x), 1);
-      mbar_init(bar(C::D + x), 1);
+      mbar_init(bar(C::REFS + x), 4);
+      mbar_init(bar(C::SUMS + x), 8);
     }
     for (int i = 0; i < 4; ++i) {   // stream, half of the key tile
       mbar_init(bar(C::S + i), 1);
       mbar_init(bar(C::P + i), 4);   // (one lane a warp: 128 arrivals took as long as a quarter of the tile's exponentials)
     }
     mbar_init(bar(C::OM), 1);
-    mbar_init(bar(C::ML), 4);
-    mbar_init(bar(C::MERGED), 4);
+    mbar_init(bar(C::ML), 8);
+    mbar_init(bar(C::MERGED), 8);
+    mbar_init(bar(C::DONE), 16);
     mbar_init(bar(C::DRAIN), 1);
     mbar_init(bar(C::DRAIN + 1), 1);
-    mbar_init(bar(C::GROUP), 4);
-    mbar_init(bar(C::GROUP + 1), 4);
-    for (int i = 0; i < 8; ++i) reinterpret_cast<uint32_t*>(gen + C::OFF_BAR + C::OFF_VOTE)[i] = 0;
+    for (int i = 0; i < 4; ++i) mbar_init(bar(C::GROUP + i), 4);
+    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(gen + C::OFF_BAR + C::OFF_VOTE)[i] = 0;
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(C::PARTFULL + i), 1);
-      mbar_init(bar(C::PARTFREE + i), 11);   // warps 0, 2, 3 and the softmax warps
+      mbar_init(bar(C::PARTFREE + i), 19);   // warps 0, 2, 3 and the softmax warps
     }
     *abort_flag = 0;
+    *redo = 0;
     fence_barrier_init();
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
@@ -523,12 +551,12 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   pdl_launch_dependents();
   pdl_wait();
   ChunkWalk w = chunk_share(a.sched, reinterpret_cast<int64_t*>(gen));
-  const bool cols = w.longest * a.block_heads <= MAX_COLS;
+  const bool cols = w.longest * a.block_heads <= MAX_COLS, wide = w.longest * a.block_heads > 16;   // (wide: two warpgroups a stream)
   fence_async_smem();   // (the copies that come next land where the shares' scratch was)
   __syncthreads();
   auto wait = [&](int i, int parity) { return warp_wait(bar(i), parity, abort_flag); };
 
-  // Part k of this CTA, from warp 1; false: no more of them, or a wait ran out.
+  // Part k of this CTA, from warp 1; false: that was it, or a wait ran out.
   auto get_part = [&](int k, Part& p) {
     const int at = k & 3;
     if (!wait(C::PARTFULL + at, k >> 2)) return false;
@@ -538,7 +566,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     for (int i = 0; i < 4; ++i) to[i] = from[i];
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(C::PARTFREE + at));
-    return p.n > 0;
+    return p.n >= 0;
   };
 
   if (warp == 0) {
@@ -573,28 +601,53 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ parts; TMA producer: Q tiles; rows of V behind the last key
+    const ChunkWalk begin = w;
     ChunkSeq q{};
     if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
     int e = 0, n_q[2] = {0, 0}, made = 0;   // ring entries passed, Q tiles loaded, parts handed out so far
     bool ok = true, more = true;
+    int pass = FAST;
+    Part again{};   // EXACT: the part whose maxima were just asked for
     const uint32_t bytes = (uint32_t)(ta.q_box_tok * a.block_heads) * (HD * 2);
     for (int k = 0; ok; ++k) {
       while (more && made <= k + 2) {   // two parts ahead of the one whose Q is loaded (four places: this warp reads its own there)
         const int at = made & 3;
         if (made >= 4 && !wait(C::PARTFREE + at, (made >> 2) - 1)) { ok = false; break; }
-        const Part fresh = next_part(a, w, q, ta.tile_tok, cols);
-        more = fresh.n > 0;
+        Part fresh{};
+        if (pass == EXACT && again.n > 0) {
+          fresh = again;
+          fresh.kind += 4 * (EXACT - MAXIMA);
+          again.n = 0;
+        } else if (w.pos < w.end) {
+          fresh = next_part(a, w, q, ta.tile_tok, cols, pass == FAST ? FAST : MAXIMA);
+          if (pass == EXACT) again = fresh;
+        } else if (cols || pass == EXACT) {
+          fresh.n = -1;
+          more = false;
+        } else {
+          more = false;   // n = 0: this warp goes on once it has come to it
+        }
         if (lane < 4) reinterpret_cast<int4*>(gen + C::OFF_PART + at * 64)[lane] = lane == 0 ? make_int4(fresh.b, fresh.kvh, fresh.head0, fresh.n_heads)
                           : lane == 1 ? make_int4(fresh.tok0, fresh.tok_in, fresh.n_tok, fresh.base)
-                          : lane == 2 ? make_int4(fresh.keys, fresh.u0, fresh.n, fresh.form) : make_int4(fresh.n_rows, fresh.last, fresh.first, fresh.parts);
+                          : lane == 2 ? make_int4(fresh.keys, fresh.u0, fresh.n, fresh.kind) : make_int4(fresh.n_rows, fresh.last, fresh.first, fresh.parts);
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::PARTFULL + at));
         ++made;
       }
       if (!ok) break;
       const Part p = *reinterpret_cast<const Part*>(gen + C::OFF_PART + (k & 3) * 64);
-      if (p.n == 0) break;
-      for (int x = 0; x < (p.form == PAIR ? 2 : 1); ++x) {
+      if (p.n < 0) break;
+      if (p.n == 0) {   // every softmax warp has come to the end of its parts: do they have to be taken again?
+        ok = wait(C::DONE, 0);
+        pass = EXACT;
+        if (*redo != 0) {
+          w = begin;
+          if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
+        }
+        more = true;
+        continue;
+      }
+      for (int x = 0; x < (p.form() == PAIR ? 2 : 1); ++x) {
         if (n_q[x] > 0 && !wait(C::QFREE + x, n_q[x] - 1)) { ok = false; break; }
         if (lane == 0) {
           mbar_expect_tx(bar(C::QFULL + x), bytes);
@@ -634,7 +687,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     constexpr uint32_t idesc_o = idesc_bf16_f32(BM, HD, 0, 1);       // P (TMEM) x V (MN-major)
     constexpr uint32_t desc_hi = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sRing, 16), v_lo = smem_desc_lo(sRing, C::HALF);
-    const uint32_t p_lo = smem_desc_lo(base + C::OFF_OUT + x * (4 * 4096), 16);
+    const uint32_t p_lo = smem_desc_lo(base + C::OFF_PT + x * 16384, 16);
     const uint32_t t_s = tmem + x * 128, t_o = tmem + (2 + x) * 128;
     auto free_entry = [&](int e) { mma_commit(bar(C::EMPTY + e % C::NSTAGE)); };
     // S of half b of a row tile: Q_y times keys 64 b .. of the K tile of ring entry e
@@ -669,6 +722,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         mma_ss(t_s, a0 + off, q_lo + off, desc_hi, idesc, kk > 0);
       }
       mma_commit(bar(C::S + 2 * x));
+      if (wide) mma_commit(bar(C::S + 2 * x + 1));
       free_entry(e);
     };
     auto issue_vp = [&](int e, int pages, bool first, uint32_t idesc) {
@@ -689,8 +743,9 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     bool ok = true;
     Part p;
     for (int k = 0; ok && get_part(k, p); ++k) {
+      if (p.n == 0) continue;
       const int n = p.n, n_pages = (p.keys + EARN_PAGE_TOKENS - 1) / EARN_PAGE_TOKENS;
-      const int stride = p.form == PAIR ? 1 : 2, y = p.form == PAIR ? x : 0, j0 = p.form == PAIR ? 0 : x;
+      const int stride = p.form() == PAIR ? 1 : 2, y = p.form() == PAIR ? x : 0, j0 = p.form() == PAIR ? 0 : x;
       const bool fixed = p.last && p.keys % EARN_PAGE_TOKENS != 0;   // the last V tile is one that warp 1 works on
       const int fix_st = (eb + 2 * n - 1) % C::NSTAGE;
       // Every entry is waited for, the other stream's too (and handed on at once): a barrier's parity tells the phase only to
@@ -702,7 +757,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           bool is_v;
           int j;
           entry_at(p, filled - eb, is_v, j);
-          if (p.form != PAIR && (j & 1) != x && lane == 0) mbar_arrive(bar(C::EMPTY + st));
+          if (p.form() != PAIR && (j & 1) != x && lane == 0) mbar_arrive(bar(C::EMPTY + st));
         }
         return true;
       };
@@ -717,7 +772,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         auto wait_v = [&](int j) { return wait_full(eb + entry_v(p, j)) && (!fixed || j + 1 < n || wait(C::FIX + fix_st, fix_phase >> fix_st)); };
         auto pages_of = [&](int j) { return min(n_pages - (p.u0 + j) * 8, 8); };
         auto free_q = [&]() { mma_commit(bar(C::QFREE + y)); };   // the stream's last S has been issued
-        if (p.form != COLS) {
+        if (p.form() != COLS) {
           issue_s(0, y, eb + entry_k(p, j0));
           issue_s(1, y, eb + entry_k(p, j0));
           free_entry(eb + entry_k(p, j0));
@@ -741,19 +796,17 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                   free_entry(ek);
                   if (j + 2 * stride >= n) free_q();
                 }
-              } else if (b == 0) {
-                mma_commit(bar(C::D + x));   // this P V is done (see the softmax)
               }
             }
           }
         } else {
-          const uint32_t idesc_st = idesc_bf16_f32(BM, p.n_rows <= 16 ? 16 : 32, 0, 0);   // K (K-major) x Q^T (K-major)
-          const uint32_t idesc_ot = idesc_bf16_f32(BM, p.n_rows <= 16 ? 16 : 32, 1, 1);   // V^T (MN-major) x P^T (MN-major)
+          const uint32_t idesc_st = idesc_bf16_f32(BM, wide ? 32 : 16, 0, 0);   // K (K-major) x Q^T (K-major)
+          const uint32_t idesc_ot = idesc_bf16_f32(BM, wide ? 32 : 16, 1, 1);   // V^T (MN-major) x P^T (MN-major)
           issue_st(eb + entry_k(p, j0), idesc_st);
           if (j0 + 2 >= n) free_q();
           for (int j = j0; j < n && ok; j += 2) {
             const int ek = eb + entry_k(p, j + 2);
-            ok = wait_p(0) && wait_v(j);
+            ok = wait_p(0) && (!wide || wait_p(1)) && wait_v(j);
             if (!ok) break;
             tc_fence_after();
             issue_vp(eb + entry_v(p, j), pages_of(j), j == j0, idesc_ot);
@@ -766,11 +819,11 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             }
           }
         }
-        if (ok) mma_commit(bar(p.form == PAIR || x == 0 ? C::O + x : C::OM));
+        if (ok) mma_commit(bar(p.form() == PAIR || x == 0 ? C::O + x : C::OM));
       }
       ok = ok && wait_full(eb + 2 * n - 1);
       ++n_q0;
-      if (p.form == PAIR) ++n_q;
+      if (p.form() == PAIR) ++n_q;
       if (fixed) fix_phase ^= 1u << fix_st;
       eb += 2 * n;
     }
@@ -781,243 +834,227 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
     __syncwarp();
   } else {
-    // ------------------------------------------------------------------ softmax warpgroup x
-    const int x = (warp - 4) >> 2;
+    // ------------------------------------------------------------------ softmax: stream x, half b of its key tiles (COLS: of its rows)
+    const int x = (warp - 4) >> 3, b = ((warp - 4) >> 2) & 1;
     const int wq = warp & 3;            // a warp may only touch TMEM lanes 32*(warp % 4) ..
     const int row = wq * 32 + lane;
-    const uint32_t lane0 = (uint32_t)(wq * 32) << 16;
-    const uint32_t t_s = tmem + lane0 + x * 128, t_o = tmem + lane0 + (2 + x) * 128;
     const float sl2 = ta.scale_log2;
     Phases n{};
-    const int per_head = 65536 / a.block_heads + 1;   // row * per_head >> 16 = row / block_heads for rows below 128
-    const int tok = row * per_head >> 16, head = row - tok * a.block_heads;
-    // before P of a stream is handed over: O_1 and the numbers of the last merge are this stream's again
-    auto settle = [&]() {
-      if (!n.pending) return true;
-      n.pending = false;
-      return wait(C::MERGED, n.ml - 1);
-    };
-    Cut cut;
-    cut.n = 0;
-    Group group{bar(C::GROUP + x), bars + C::OFF_VOTE + 16u * (uint32_t)x, abort_flag, 0};
-    bool ok = true;
+    Part* cuts = reinterpret_cast<Part*>(gen + C::OFF_CUT + x * 128);   // (written by the first half's threads)
+    int n_cuts = 0;
+    Group group{bar(C::GROUP + 2 * x + b), bars + C::OFF_VOTE + 16u * (uint32_t)(2 * x + b), abort_flag, 0};
+    bool ok = true, again = false;
     Part p;
     if (cols) {
       for (int k = 0; ok && get_part(k, p); ++k) {
-        if (x >= p.n) continue;   // a part of one key tile leaves stream 1 out
-        ok = w.longest * a.block_heads <= 16 ? softmax_cols<HD, 16>(a, ta, p, x, tmem, base, bars, abort_flag, n, group)
-                                             : softmax_cols<HD, 32>(a, ta, p, x, tmem, base, bars, abort_flag, n, group);
-        if (x == 0 && p.parts > 1) cut.part[cut.n++] = p;
+        if (x >= p.n || (b == 1 && !wide)) continue;   // no key tile for stream 1, or no row for the second warpgroup
+        ok = softmax_cols<HD>(a, sl2, p, x, b, wide, tmem, base, bars, abort_flag, n, group);
+        if (x == 0 && p.parts > 1) {
+          if (b == 0 && row == 0) cuts[n_cuts] = p;
+          ++n_cuts;
+        }
       }
-      if (ok) join_cuts<HD, true>(a, cut, ta.tile_tok, x, row, last_part, group);
-    } else
-    for (int k = 0; ok && get_part(k, p); ++k) {
-      if (p.form != PAIR && x >= p.n) continue;   // a part of one key tile leaves stream 1 out
-      const bool merge = p.form != PAIR && p.n > 1;
-      const int stride = p.form == PAIR ? 1 : 2, my_tok = p.form == PAIR ? x * ta.tile_tok : 0;   // first token of the row tile
-      const int n_tok = min(ta.tile_tok, p.n_tok - my_tok), tok0 = p.tok0 + my_tok;
-      const uint32_t stage = base + C::OFF_OUT + (uint32_t)(warp - 4) * 4096;
-      const bool valid = tok < n_tok && head < p.n_heads;
-      const int seen = p.base + p.tok_in + my_tok + tok + 1;         // keys that the row sees
-      const bool any_row = wq * 32 < n_tok * a.block_heads;          // this warp has a row
-      const int seen_least = __reduce_min_sync(0xffffffffu, valid ? seen : INT32_MAX), seen_most = __reduce_max_sync(0xffffffffu, valid ? seen : 0);
-      float m_ref = -INFINITY, l0 = 0.f, l1 = 0.f;                   // -inf: no reference yet
-      for (int j = p.form == PAIR ? 0 : x; j < p.n && ok; j += stride) {
-#pragma unroll 1
-        for (int b = 0; b < 2; ++b) {
-          ok = wait(C::S + 2 * x + b, b == 0 ? n.s[0]++ : n.s[1]++);
+    } else {
+      const int per_head = 65536 / a.block_heads + 1;   // row * per_head >> 16 = row / block_heads for rows below 128
+      const int tok = row * per_head >> 16, head = row - tok * a.block_heads;
+      const uint32_t lane0 = (uint32_t)(wq * 32) << 16;
+      const uint32_t t_s = tmem + lane0 + x * 128 + b * 64, t_o = tmem + lane0 + (2 + x) * 128 + b * (HD / 2);
+      const uint32_t refs = base + C::OFF_REF + (uint32_t)row * 4, sums = base + C::OFF_SUM + (uint32_t)row * 4, maxima = base + C::OFF_MAX + (uint32_t)row * 4, sums1 = base + C::OFF_SUM1 + (uint32_t)row * 4;
+      for (int k = 0; ok && get_part(k, p); ++k) {
+        if (p.n == 0) {   // the end of a pass
+          warp_arrive(bar(C::DONE));
+          again = true;
+          continue;
+        }
+        if (again) {      // all parts once more
+          n_cuts = 0;
+          again = false;
+        }
+        const bool pair = p.form() == PAIR, merge = !pair && p.n > 1;
+        if (!pair && x >= p.n) continue;   // a part of one key tile leaves stream 1 out
+        if (n.pending) {                   // stream 0 has read what the last merge needs
+          n.pending = false;
+          ok = wait(C::MERGED, n.ml - 1);
+          if (!ok) break;
+        }
+        const int stride = pair ? 1 : 2, my_tok = pair ? x * ta.tile_tok : 0, pass = p.pass();
+        const int n_tok = min(ta.tile_tok, p.n_tok - my_tok);
+        const bool valid = tok < n_tok && head < p.n_heads;
+        const int seen = p.base + p.tok_in + my_tok + tok + 1;         // keys that the row sees
+        const bool any_row = wq * 32 < n_tok * a.block_heads;          // this warp has a row
+        const int seen_least = __reduce_min_sync(0xffffffffu, valid ? seen : INT32_MAX), seen_most = __reduce_max_sync(0xffffffffu, valid ? seen : 0);
+        float neg_m = NO_REF, l0 = 0.f, l1 = 0.f, top = -INFINITY;
+        const int j0 = pair ? 0 : x;
+        for (int j = j0; j < p.n; j += stride) {
+          ok = wait(C::S + 2 * x + b, n.s++);
           if (!ok) break;
           tc_fence_after();
-          const bool first = j < stride && b == 0;
-          const uint32_t t_sb = t_s + b * 64;
-          if (any_row) {
-            // columns visible to the row (all of them to rows that hold nothing: their values go nowhere)
-            const int key0 = (p.u0 + j) * BN + b * 64, vis = valid ? min(max(seen - key0, 0), 64) : 64;
-            const bool interior = seen_least >= key0 + 64;
-            const int n_chunks = seen_most > key0 + 32 ? 2 : seen_most > key0 ? 1 : 0;   // 32-column chunks with a visible key
-            uint32_t ra[32], rb[32], pk[2][16];
-            // P = 2^(S * scale - m_ref) as bf16 pairs (kept in registers until the reference is known to hold) and their row
-            // sum, in one pass.  If the sum exceeds 2^8 some logit may have outgrown the reference, or there is none yet: then
-            // find the half's own maximum, raise the reference, rescale what has been accumulated, and redo the pass (S is
-            // intact: nothing has been written over it).
-            float ls0, ls1;
-#pragma unroll 1
-            for (int attempt = 0;; ++attempt) {
-              ls0 = ls1 = 0.f;
-              tmem_ld_32x32(t_sb, ra);
-              tmem_wait_ld(ra);
-              if (first && attempt == 0) {
-                float mx = -INFINITY, m1 = -INFINITY;
+          const int key0 = (p.u0 + j) * BN + b * 64;
+          // columns visible to the row (all of them to rows that hold nothing: their values go nowhere)
+          const int vis = valid ? min(max(seen - key0, 0), 64) : 64;
+          if (j == j0) {   // the row's reference: from the first half's first 32 columns, or the maxima of the pass before
+            if (b == 0) {
+              if (pass == EXACT) {
+                neg_m = -fmaxf(lds(maxima + x * 1024), lds(maxima + x * 1024 + 512));
+              } else if (any_row) {
+                float mx = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                  mx = max3(mx, c < vis ? __uint_as_float(ra[c]) : -INFINITY, c + 1 < vis ? __uint_as_float(ra[c + 1]) : -INFINITY);
-                  m1 = max3(m1, c + 2 < vis ? __uint_as_float(ra[c + 2]) : -INFINITY, c + 3 < vis ? __uint_as_float(ra[c + 3]) : -INFINITY);
+                for (int c0 = 0; c0 < 32; c0 += 16) {
+                  uint32_t s[16];
+                  tmem_ld_32x16(t_s + c0, s);
+#pragma unroll
+                  for (int c = 0; c < 16; c += 2)
+                    mx = max3(mx, c0 + c < vis ? __uint_as_float(s[c]) : -INFINITY, c0 + c + 1 < vis ? __uint_as_float(s[c + 1]) : -INFINITY);
                 }
-                m_ref = fmaxf(mx, m1) * sl2;
+                neg_m = -mx * sl2;
               }
-              const float neg_m = m_ref == -INFINITY ? NO_REF : -m_ref;
-              // an interior half takes a copy of the code without a test per chunk: one block of straight-line code
-              auto chunks = [&](auto interior_tag) {
-                constexpr bool INTERIOR = decltype(interior_tag)::value;
-#pragma unroll
-                for (int c0 = 0; c0 < 2; ++c0) {
-                  if (INTERIOR || c0 < n_chunks) {
-                    uint32_t(&cur)[32] = c0 ? rb : ra;
-                    if (c0 == 0 && (INTERIOR || n_chunks > 1)) tmem_ld_32x32(t_sb + 32, rb);
-                    if (!INTERIOR) {
-#pragma unroll
-                      for (int c = 0; c < 32; ++c)
-                        if (c0 * 32 + c >= vis) cur[c] = 0xff800000u;   // -inf
-                    }
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                      float e0, e1;
-                      fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, neg_m, neg_m);
-                      e0 = ex2(e0);
-                      e1 = ex2(e1);
-                      add2(ls0, ls1, e0, e1);
-                      pk[c0][c >> 1] = pack_bf16(e0, e1);
-                    }
-                    if (c0 == 0 && (INTERIOR || n_chunks > 1)) tmem_wait_ld(rb);
-                  } else {
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) pk[c0][c] = 0u;
-                  }
-                }
-              };
-              if (interior) chunks(std::true_type{});
-              else chunks(std::false_type{});
-              const bool grow = valid && !(ls0 + ls1 <= 256.f);
-              if (attempt > 0 || !__any_sync(0xffffffffu, grow)) break;
-              float mx = -INFINITY;
-              for (int c0 = 0; c0 < n_chunks; ++c0) {
-                tmem_ld_32x32(t_sb + c0 * 32, ra);
-                tmem_wait_ld(ra);
-#pragma unroll
-                for (int c = 0; c < 32; ++c) mx = fmaxf(mx, c0 * 32 + c < vis ? __uint_as_float(ra[c]) : -INFINITY);
-              }
-              // The whole warp repeats the pass, but only the rows that asked for it take a new reference: a row's result
-              // depends on its own logits alone, whatever its neighbours in the tile do.
-              const float mxs = grow ? mx * sl2 : m_ref;
-              const float alpha = mxs > m_ref ? ex2(m_ref - mxs) : 1.f;
-              m_ref = fmaxf(m_ref, mxs);
-              l0 *= alpha;
-              l1 *= alpha;
-              if (!first) {
-                // The stream's last P V (the other half's) may be running.  What follows it in the tensor core's queue is the
-                // next S over that half, or, behind the last tile's first half, the commit to D.
-                ok = b == 1 && j + stride >= p.n ? wait(C::D + x, n.d) : wait(C::S + 2 * x + 1 - b, b == 0 ? n.s[1] : n.s[0]);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int c0 = 0; c0 < HD / 32; ++c0) {
-                  tmem_ld_32x32(t_o + c0 * 32, ra);
-                  tmem_wait_ld(ra);
-#pragma unroll
-                  for (int c = 0; c < 32; ++c) ra[c] = __float_as_uint(__uint_as_float(ra[c]) * alpha);
-                  tmem_st_32x32(t_o + c0 * 32, ra);
-                }
-              }
+              if (neg_m == INFINITY) neg_m = NO_REF;   // (no finite logit)
+              sts(refs + x * 512, neg_m);
+              warp_arrive(bar(C::REFS + x));
+            } else {
+              ok = wait(C::REFS + x, n.ref++);
+              if (!ok) break;
+              neg_m = lds(refs + x * 512);
             }
-            if (!ok) break;
-            l0 += ls0;
-            l1 += ls1;
-            tmem_st_32x16(t_sb, pk[0]);
-            tmem_st_32x16(t_sb + 16, pk[1]);
-            tmem_wait_st();
           }
-          ok = settle();
-          if (!ok) break;
+          if (any_row) {
+            // P = 2^(S * scale - reference) as bf16 pairs over the first columns of S, and the row's sum, 16 columns at a time.  A
+            // half that all rows see whole takes a copy without a test per column.
+            auto half = [&](auto interior) {
+              uint32_t s[2][16];
+              tmem_ld_16(t_s, s[0]);
+              tmem_wait_16(s[0]);
+#pragma unroll
+              for (int c0 = 0; c0 < 4; ++c0) {
+                uint32_t(&cur)[16] = s[c0 & 1];
+                if (c0 < 3) tmem_ld_16(t_s + (c0 + 1) * 16, s[(c0 + 1) & 1]);
+                if (!decltype(interior)::value) {
+#pragma unroll
+                  for (int c = 0; c < 16; ++c)
+                    if (c0 * 16 + c >= vis) cur[c] = 0xff800000u;   // -inf
+                }
+                uint32_t pk[8];
+#pragma unroll
+                for (int c = 0; c < 16; c += 2) {
+                  float e0, e1;
+                  fma2(e0, e1, __uint_as_float(cur[c]), __uint_as_float(cur[c + 1]), sl2, neg_m, neg_m);
+                  e0 = ex2(e0);
+                  e1 = ex2(e1);
+                  add2(l0, l1, e0, e1);
+                  pk[c >> 1] = pack_bf16(e0, e1);
+                }
+                if (c0 < 3) tmem_wait_16(s[(c0 + 1) & 1]);
+                tmem_st_8(t_s + c0 * 8, pk);
+              }
+              tmem_wait_st();
+            };
+            if (pass == MAXIMA) {
+#pragma unroll 1
+              for (int c0 = 0; c0 < 64; c0 += 16) {
+                uint32_t s[16];
+                tmem_ld_32x16(t_s + c0, s);
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                  if (c0 + c < vis) top = fmaxf(top, __uint_as_float(s[c]));
+              }
+            } else if (seen_least >= key0 + 64) {
+              half(std::true_type{});
+            } else {
+              half(std::false_type{});
+            }
+          }
           tc_fence_before();
           warp_arrive(bar(C::P + 2 * x + b));
         }
-      }
-      if (ok) ok = wait(C::D + x, n.d++);
-      if (!ok) break;
-      // ---- end of the part
-      float l = l0 + l1, w0 = 1.f, w1 = 0.f;
-      if (merge && x == 1) {
-        ml1[row] = make_float2(m_ref, l);
-        tc_fence_before();
-        warp_arrive(bar(C::ML));
-        ++n.ml;
-        n.pending = true;
-        continue;
-      }
-      ok = wait(C::O + x, n.o++);
-      if (ok && merge) ok = wait(C::OM, n.ml) && wait(C::ML, n.ml);
-      if (!ok) break;
-      tc_fence_after();
-      if (merge) {
-        ++n.ml;
-        const float2 other = ml1[row];
-        const float mx = fmaxf(m_ref, other.x), ref = mx == -INFINITY ? 0.f : mx;
-        w0 = ex2(m_ref - ref);
-        w1 = ex2(other.x - ref);
-        l = l * w0 + other.y * w1;
-        m_ref = mx;
-      }
-      const bool whole = p.parts == 1;
-      const float inv = !whole ? 1.f : l == 0.f ? 0.f : __frcp_rn(l);
-      w0 *= inv;
-      w1 *= inv;
-      const int64_t slot = part_slot(p, x);
-      if (any_row) {
-        uint32_t ra[32];
+        if (!ok) break;
+        // ---- end of the part: the halves' sums meet, and the streams'
+        const uint32_t mine = merge && x == 1 ? sums1 : sums + (uint32_t)(((n.sum & 1) * 2 + x) * 1024);
+        sts(mine + b * 512, l0 + l1);
+        if (pass == MAXIMA) sts(maxima + x * 1024 + b * 512, top * sl2);
+        if (merge && x == 1) {
+          tc_fence_before();
+          warp_arrive(bar(C::ML));
+          ++n.ml;
+          n.pending = true;
+          continue;
+        }
+        warp_arrive(bar(C::SUMS + x));
+        ok = wait(C::SUMS + x, n.sum++) && wait(C::O + x, n.o++);
+        if (ok && merge) ok = wait(C::OM, n.ml) && wait(C::ML, n.ml);
+        if (!ok) break;
+        tc_fence_after();
+        float l = lds(mine) + lds(mine + 512), m_ref = neg_m == NO_REF ? -INFINITY : -neg_m, w0 = 1.f, w1 = 0.f;
+        bool fits = l <= SUM_LIMIT;
+        if (merge) {
+          ++n.ml;
+          const float other = lds(sums1) + lds(sums1 + 512), neg1 = lds(refs + 512), m1 = neg1 == NO_REF ? -INFINITY : -neg1;
+          fits = fits && other <= SUM_LIMIT;
+          const float mx = fmaxf(m_ref, m1), ref = mx == -INFINITY ? 0.f : mx;
+          w0 = ex2(m_ref - ref);
+          w1 = ex2(m1 - ref);
+          l = l * w0 + other * w1;
+          m_ref = mx;
+        }
+        if (pass == FAST && valid && !fits) *redo = 1;
+        const bool whole = p.parts == 1;
+        if (any_row && pass != MAXIMA) {
+          const float inv = !whole ? 1.f : l == 0.f ? 0.f : __frcp_rn(l);
+          w0 *= inv;
+          w1 *= inv;
+          const int64_t slot = part_slot(p, x);
+          const int at_tok = p.tok0 + my_tok + tok;
+          __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(a.o) + ((int64_t)at_tok * a.Hq + p.head0 + head) * HD + b * (HD / 2);
+          const bool by32 = (reinterpret_cast<uintptr_t>(a.o) & 31) == 0;
 #pragma unroll
-        for (int c0 = 0; c0 < HD / 32; ++c0) {
-          tmem_ld_32x32(t_o + c0 * 32, ra);
-          tmem_wait_ld(ra);
-          float y[32];
+          for (int c0 = 0; c0 < HD / 32; ++c0) {   // this half's columns of O, 16 at a time
+            uint32_t s0[16], s1[16];
+            float y[16];
+            tmem_ld_32x16(t_o + c0 * 16, s0);
+            if (merge) tmem_ld_32x16(t_o + 128 + c0 * 16, s1);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) y[c] = __uint_as_float(ra[c]) * w0;
-          if (merge) {
-            tmem_ld_32x32(t_o + 128 + c0 * 32, ra);
-            tmem_wait_ld(ra);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) y[c] += __uint_as_float(ra[c]) * w1;
-          }
-          if (l == 0.f) {   // (nothing visible: O holds nothing)
-#pragma unroll
-            for (int c = 0; c < 32; ++c) y[c] = 0.f;
-          }
-          if (whole) {
-            // 64 columns of the warp's 32 rows are staged (16-byte chunk c of row r at chunk c ^ (r % 8) of its line) and
-            // written by eight lanes a row
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int ch = (c0 & 1) * 4 + c;
-              st_shared_v4(stage + (uint32_t)lane * 128 + (uint32_t)((ch ^ (lane & 7)) << 4), pack_bf16(y[c * 8], y[c * 8 + 1]),
-                           pack_bf16(y[c * 8 + 2], y[c * 8 + 3]), pack_bf16(y[c * 8 + 4], y[c * 8 + 5]), pack_bf16(y[c * 8 + 6], y[c * 8 + 7]));
+            for (int c = 0; c < 16; ++c) {
+              y[c] = __uint_as_float(s0[c]) * w0;
+              if (merge) y[c] += __uint_as_float(s1[c]) * w1;
+              if (l == 0.f) y[c] = 0.f;   // (nothing visible: O holds nothing)
             }
-            if (c0 & 1) {
-              __syncwarp();
-#pragma unroll 4
-              for (int i = 0; i < 8; ++i) {
-                const int r = i * 4 + (lane >> 3), gr = wq * 32 + r, t = gr * per_head >> 16, h = gr - t * a.block_heads;
-                if (t < n_tok && h < p.n_heads) {
-                  const uint4 v = ld_shared_v4(stage + (uint32_t)r * 128 + (uint32_t)(((lane & 7) ^ (r & 7)) << 4));
-                  *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.o) + ((int64_t)(tok0 + t) * a.Hq + p.head0 + h) * HD +
-                                            (c0 >> 1) * 64 + (lane & 7) * 8) = v;
-                }
+            if (valid && whole) {
+              uint32_t v[8];
+#pragma unroll
+              for (int c = 0; c < 8; ++c) v[c] = pack_bf16(y[2 * c], y[2 * c + 1]);
+              if (by32) {
+                st_global_32b(o + c0 * 16, v);
+              } else {
+                *reinterpret_cast<uint4*>(o + c0 * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint4*>(o + c0 * 16 + 8) = make_uint4(v[4], v[5], v[6], v[7]);
               }
-              __syncwarp();
-            }
-          } else if (valid) {
+            } else if (valid) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-              a.part_o[(slot * (HD / 4) + c0 * 8 + c) * BM + row] = make_float4(y[c * 4], y[c * 4 + 1], y[c * 4 + 2], y[c * 4 + 3]);
+              for (int c = 0; c < 4; ++c)
+                a.part_o[(slot * (HD / 4) + b * (HD / 8) + c0 * 4 + c) * BM + row] = make_float4(y[c * 4], y[c * 4 + 1], y[c * 4 + 2], y[c * 4 + 3]);
+            }
+          }
+          if (b == 0 && valid) {
+            if (!whole) a.part_ml[slot * BM + row] = make_float2(m_ref, l);
+            else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + at_tok] = chunk_lse<true>(m_ref, l);
           }
         }
-        if (valid && whole && a.lse != nullptr)
-          a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<true>(m_ref, l);
-        if (valid && !whole) a.part_ml[slot * BM + row] = make_float2(m_ref, l);
+        tc_fence_before();   // the next P V over O_x is issued after both halves' next arrivals on P
+        if (merge) warp_arrive(bar(C::MERGED));
+        if (!whole && pass != MAXIMA) {
+          if (b == 0 && row == 0) cuts[n_cuts] = p;
+          ++n_cuts;
+        }
       }
-      tc_fence_before();   // the next P V over O_x is issued after this warp's next arrive on P_x
-      if (merge) warp_arrive(bar(C::MERGED));
-      if (!whole) cut.part[cut.n++] = p;
     }
-    if (ok && !cols) join_cuts<HD, false>(a, cut, ta.tile_tok, x, row, last_part, group);
+    // ---- items that are cut: both halves have written their columns (COLS: rows) of the parts
+    if (ok && *abort_flag == 0) {
+      __threadfence();
+      warp_arrive(bar(C::SUMS + x));
+      if (wait(C::SUMS + x, n.sum) && b == 0) {
+        if (cols) join_cuts<HD, true>(a, cuts, n_cuts, ta.tile_tok, x, row, last_part + x, group);
+        else join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, row, last_part + x, group);
+      }
+    }
   }
 
   tc_fence_before();

@@ -360,6 +360,21 @@ def test_chunk_logits_far_apart(dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [[300, 1, 40], [7, 1, 3]])
+def test_chunk_logits_beyond_any_reference(dtype, new):
+    """Keys whose logits exceed those in front of them by hundreds: late in the list, early in it, and in one list of several."""
+    c = Chunk(new, [900, 300, 290], 4, 2, 128, dtype, seed=9)
+    c.q[..., 0] = 4.0
+    for b, far in ((0, (500, 640, 641)), (2, (40, 288))):
+        row = torch.tensor(far, device="cuda")
+        at = c.table[b].long()[row // PAGE] * PAGE + row % PAGE
+        c.k.view(-1, 2, 128)[at, :, 0] = torch.linspace(500.0, 900.0, len(far), device="cuda").to(c.k.dtype)[:, None]
+    first = c.call().check().o.clone()
+    c.o.fill_(7)
+    assert torch.equal(c.call().o, first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_chunk_dead_keys(dtype):
     """Keys whose logits are -inf weigh nothing, long stretches of them at the start and whole lists included."""
     c = Chunk([6, 2, 140], [300, 40, 200], 8, 2, 128, dtype, seed=5)
