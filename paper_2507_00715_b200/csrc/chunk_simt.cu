@@ -21,13 +21,14 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   float* Ks = Qs + RT * D;   // float4 c of row r lies at c ^ (r & 7): sixteen rows are read at once
   float* Vs = Ks + KT * D;
   float* Ps = Vs + KT * D;
-  __shared__ int64_t scratch[64];
+  __shared__ alignas(16) int64_t scratch[96];
   __shared__ int last_part;
+  __shared__ float2 weights[RT];
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-  const ChunkSched& s = a.sched;
+  ChunkSched s = a.sched;
   pdl_launch_dependents();
   pdl_wait();
-  ChunkWalk w = chunk_share(s, scratch);
+  ChunkWalk w = chunk_share(s, scratch, nullptr);
   if (w.pos >= w.end) return;
   ChunkSeq q = chunk_seq(s, w.b);
   while (w.pos < w.end) {
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
         __threadfence();
       }
       __syncthreads();
-      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads);
+      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads, weights, [] { __syncthreads(); return true; });
     }
     w.pos += stop - w.off;
     if (stop == units) chunk_next(s, w, q);

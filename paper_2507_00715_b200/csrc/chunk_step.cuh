@@ -62,50 +62,65 @@ __device__ __forceinline__ float chunk_lse(float ref, float sum) {
   return (float)((LOG2 ? (double)ref * 0.69314718055994530942 : (double)ref) + log((double)sum));
 }
 
-// Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows: element (row, four
-// columns) by element, `threads` threads of which this is number t.  The parts are added in their order along the keys, so
-// the result does not depend on which of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR:
-// a part is [rows][D], else [D / 4][rows][4].
-template <typename T, int D, int ROWS, bool LOG2, bool ROW_MAJOR>
+// Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows, by `threads` threads of
+// which this is number t: first a row's reference and denominator (into `rows`, shared memory for ROWS pairs), then four columns
+// of a row at a time.  The parts are added in their order along the keys, so the result does not depend on which of them came
+// last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else [D / 4][rows][4].  sync():
+// barrier of the threads, false if it gave up.
+template <typename T, int D, int ROWS, bool LOG2, bool ROW_MAJOR, class Sync>
 __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t, int threads,
-                                           int tok0, int n_tok, int head0, int n_heads) {
-  constexpr int C4 = D / 4, AHEAD = 8;
-  const int used = n_tok * a.block_heads;   // rows of the tile that hold a token
-  for (int i = t; i < used * C4; i += threads) {
-    const int row = ROW_MAJOR ? i / C4 : i % used, c4 = ROW_MAJOR ? i % C4 : i / used, tok = row / a.block_heads, head = row - tok * a.block_heads;
-    if (head >= n_heads) continue;
+                                           int tok0, int n_tok, int head0, int n_heads, float2* rows, Sync sync) {
+  constexpr int C4 = D / 4;
+  const int used = n_tok * a.block_heads, n = parts.parts;   // rows of the tile that hold a token
+  auto slot = [&](int p) { return (int64_t)(2 * (parts.first + p) + (p == 0 ? 1 : 0)) * tiles + x; };
+  auto weight = [&](float from, float ref) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
+  for (int row = t; row < used; row += threads) {
+    const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+    if (head >= n_heads) { rows[row] = make_float2(0.f, -1.f); continue; }
     float m = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = 0; p0 < parts.parts; p0 += AHEAD) {
-      float2 ml[AHEAD];
-      float4 v[AHEAD];
-#pragma unroll
-      for (int p = 0; p < AHEAD; ++p) {
-        if (p0 + p >= parts.parts) { ml[p] = make_float2(-INFINITY, 0.f); v[p] = make_float4(0.f, 0.f, 0.f, 0.f); continue; }
-        const int64_t slot = (int64_t)(2 * (parts.first + p0 + p) + (p0 + p == 0 ? 1 : 0)) * tiles + x;
-        ml[p] = __ldcg(a.part_ml + slot * ROWS + row);
-        v[p] = __ldcg(a.part_o + (ROW_MAJOR ? (slot * ROWS + row) * C4 + c4 : (slot * C4 + c4) * ROWS + row));
-      }
-      float mx = m;
-#pragma unroll
-      for (int p = 0; p < AHEAD; ++p) mx = fmaxf(mx, ml[p].x);
-      const float ref = mx == -INFINITY ? 0.f : mx;   // (nothing seen so far: every weight below is 2^-inf = 0)
-      auto weight = [&](float from) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
-      const float keep = weight(m);
-      l *= keep; acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
-#pragma unroll
-      for (int p = 0; p < AHEAD; ++p) {
-        const float w = weight(ml[p].x);
-        l += ml[p].y * w;
-        acc.x += v[p].x * w; acc.y += v[p].y * w; acc.z += v[p].z * w; acc.w += v[p].w * w;
-      }
-      m = mx;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) m = fmaxf(m, __ldcg(a.part_ml + slot(p) * ROWS + row).x);
+    const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen: every weight is 2^-inf = 0)
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float2 ml = __ldcg(a.part_ml + slot(p) * ROWS + row);
+      l += ml.y * weight(ml.x, ref);
     }
-    const float inv = l == 0.f ? 0.f : __frcp_rn(l);
-    const float y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-    Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D + c4 * 4, y);
-    if (c4 == 0 && a.lse != nullptr)
-      a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+    rows[row] = make_float2(ref, l == 0.f ? 0.f : __frcp_rn(l));
+    if (a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+  }
+  if (!sync()) return;
+  constexpr int BATCH = 4;   // elements of a thread, or parts, in flight
+  const int all = ROW_MAJOR ? used * C4 : ROWS * C4;
+  for (int i0 = t; i0 < all; i0 += BATCH * threads) {
+    float4 acc[BATCH];
+    float2 of[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS;
+      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      of[k] = i < all && row < used ? rows[row] : make_float2(0.f, -1.f);
+    }
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const int64_t from = slot(p);
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS, c4 = ROW_MAJOR ? i % C4 : i / ROWS;
+        if (of[k].y < 0.f) continue;
+        const float w = weight(__ldcg(a.part_ml + from * ROWS + row).x, of[k].x);
+        const float4 v = __ldcg(a.part_o + (ROW_MAJOR ? (from * ROWS + row) * C4 + c4 : (from * C4 + c4) * ROWS + row));
+        acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS, c4 = ROW_MAJOR ? i % C4 : i / ROWS;
+      if (of[k].y < 0.f) continue;
+      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+      const float y[4] = {acc[k].x * of[k].y, acc[k].y * of[k].y, acc[k].z * of[k].y, acc[k].w * of[k].y};
+      Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D + c4 * 4, y);
+    }
   }
 }
 

@@ -21,7 +21,8 @@
 //
 // PAIR and ROWS: a key tile is taken in two halves of 64 keys, each with an accumulator and a warpgroup of its own, one row per
 // thread, so that the tensor core has the other halves to multiply while one is in the exponentials (P lies over S: the next S
-// of a half follows its P V).  The reference of a row's exponentials is its largest logit among its first 32 visible keys, and
+// of a half follows its P V).  With whole tiles a product of 128 x 128 costs the tensor core less (the halves read Q twice), but
+// it waits more: 1152 us instead of 920 for 4096 new tokens over 12000 rows, 32/8 heads.  The reference of a row's exponentials is its largest logit among its first 32 visible keys, and
 // stays: fp32 and bf16 hold 2^127, so a row needs another one only if a logit exceeds that by 44 nats or more.  If the sums tell
 // that one did (or that the first keys had no finite logit), the CTA takes all its parts again, each twice: for the rows' maxima,
 // and with them.  (A test per half and a rescaling of O in place, with one warpgroup per row tile, took 1.4 times as long.)
@@ -57,12 +58,13 @@ struct Cfg {
   static constexpr int OFF_RED = OFF_MAX + 2 * 2 * 128 * 4, RED = 1024;                // COLS: a warpgroup's scratch
   static constexpr int OFF_SUM1 = OFF_RED + 4 * RED;                                    // stream 1's sums [half][row] for a merge
   static constexpr int OFF_CUT = OFF_SUM1 + 2 * 128 * 4;                               // parts of items that are cut [stream][2]
-  static constexpr int OFF_PART = OFF_CUT + 4 * 64, OFF_BAR = OFF_PART + 4 * 64;
+  static constexpr int OFF_SEQ = OFF_CUT + 4 * 64;                                          // the sequences
+  static constexpr int OFF_PART = OFF_SEQ + kChunkTable * (int)sizeof(ChunkSeq), OFF_BAR = OFF_PART + 4 * 64;
   static constexpr int THREADS = 32 * 20;
   static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 4, O = P + 4,
                        OM = O + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2,
                        PARTFREE = PARTFULL + 4, GROUP = PARTFREE + 4, REFS = GROUP + 4, SUMS = REFS + 2, DONE = SUMS + 2,
-                       N_BARS = DONE + 1, OFF_VOTE = 8 * N_BARS + 32;
+                       N_BARS = DONE + 1, OFF_VOTE = 8 * N_BARS + 48;
   static constexpr int SMEM_BYTES = OFF_BAR + (OFF_VOTE + 64 + 127) / 128 * 128 + 1024;   // + alignment slack
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of an SM");
 };
@@ -88,8 +90,7 @@ struct alignas(16) Part {
 static_assert(sizeof(Part) == 64, "four 16-byte words");
 
 // The CTA's parts one after the other.
-__device__ __forceinline__ Part next_part(const ChunkArgs& a, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols, int pass) {
-  const ChunkSched& s = a.sched;
+__device__ __forceinline__ Part next_part(const ChunkArgs& a, const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols, int pass) {
   Part p{};
   if (w.pos >= w.end) return p;
   p.b = w.b;
@@ -271,9 +272,9 @@ struct TcArgs {
 };
 
 // The CTA's n parts of items that are cut (at most its first part and its last) are written: joins those of which it was the last
-// to finish.  (All 128 threads; x: row tile.)
-template <int HD, bool ROW_MAJOR>
-__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, Group& group) {
+// to finish.  (All 256 threads of stream x; sync: their barrier.)
+template <int HD, bool ROW_MAJOR, class Sync>
+__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, float2* rows, Sync sync) {
 #pragma unroll 1
   for (int i = 0; i < n; ++i) {
     const Part p = cuts[i];
@@ -281,18 +282,21 @@ __device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, 
       const int32_t at = p.first * 2 + x;
       const bool is_last = atomicAdd(a.tickets + at, 1) == p.parts - 1;
       if (is_last) a.tickets[at] = 0;   // for the next call
-      *flag = is_last;
+      flag[i] = is_last;
       __threadfence();
     }
-    if (!group.sync()) return;
-    if (*flag != 0) {
-      const int my_tok = p.form() == PAIR ? x * tile_tok : 0;
-      ChunkParts parts;
-      parts.first = p.first;
-      parts.parts = p.parts;
-      chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 128, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads);
-    }
-    if (!group.sync()) return;   // (the flag has been read)
+  }
+  if (!sync()) return;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    if (flag[i] == 0) continue;
+    const Part p = cuts[i];
+    const int my_tok = p.form() == PAIR ? x * tile_tok : 0;
+    ChunkParts parts;
+    parts.first = p.first;
+    parts.parts = p.parts;
+    if (!sync()) return;   // (the numbers of the rows before have been read)
+    chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 256, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, rows, sync);
   }
 }
 __device__ __forceinline__ int64_t part_slot(const Part& p, int x) {
@@ -501,7 +505,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + C::OFF_BAR + 8 * C::N_BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 8);
   volatile int* redo = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 12);       // a sum left the range: all parts again
-  volatile int* last_part = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 16);  // [2]
+  volatile int* last_part = reinterpret_cast<volatile int*>(gen + C::OFF_BAR + 8 * C::N_BARS + 16);  // [stream][2]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -550,7 +554,8 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   const uint32_t tmem = *tmem_slot;   // S_x (and P_x over it) at x * 128, O_x at (2 + x) * 128
   pdl_launch_dependents();
   pdl_wait();
-  ChunkWalk w = chunk_share(a.sched, reinterpret_cast<int64_t*>(gen));
+  ChunkSched sched = a.sched;
+  ChunkWalk w = chunk_share(sched, reinterpret_cast<int64_t*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ));
   const bool cols = w.longest * a.block_heads <= MAX_COLS, wide = w.longest * a.block_heads > 16;   // (wide: two warpgroups a stream)
   fence_async_smem();   // (the copies that come next land where the shares' scratch was)
   __syncthreads();
@@ -603,23 +608,24 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     // ------------------------------------------------------------------ parts; TMA producer: Q tiles; rows of V behind the last key
     const ChunkWalk begin = w;
     ChunkSeq q{};
-    if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
+    if (w.pos < w.end) q = chunk_seq(sched, w.b);
     int e = 0, n_q[2] = {0, 0}, made = 0;   // ring entries passed, Q tiles loaded, parts handed out so far
     bool ok = true, more = true;
     int pass = FAST;
     Part again{};   // EXACT: the part whose maxima were just asked for
     const uint32_t bytes = (uint32_t)(ta.q_box_tok * a.block_heads) * (HD * 2);
     for (int k = 0; ok; ++k) {
-      while (more && made <= k + 2) {   // two parts ahead of the one whose Q is loaded (four places: this warp reads its own there)
+      auto hand_out = [&](int upto) {
+      while (more && made <= upto) {
         const int at = made & 3;
-        if (made >= 4 && !wait(C::PARTFREE + at, (made >> 2) - 1)) { ok = false; break; }
+        if (made >= 4 && !wait(C::PARTFREE + at, (made >> 2) - 1)) return false;
         Part fresh{};
         if (pass == EXACT && again.n > 0) {
           fresh = again;
           fresh.kind += 4 * (EXACT - MAXIMA);
           again.n = 0;
         } else if (w.pos < w.end) {
-          fresh = next_part(a, w, q, ta.tile_tok, cols, pass == FAST ? FAST : MAXIMA);
+          fresh = next_part(a, sched, w, q, ta.tile_tok, cols, pass == FAST ? FAST : MAXIMA);
           if (pass == EXACT) again = fresh;
         } else if (cols || pass == EXACT) {
           fresh.n = -1;
@@ -634,6 +640,9 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (lane == 0) mbar_arrive(bar(C::PARTFULL + at));
         ++made;
       }
+      return true;
+      };
+      ok = hand_out(k);
       if (!ok) break;
       const Part p = *reinterpret_cast<const Part*>(gen + C::OFF_PART + (k & 3) * 64);
       if (p.n < 0) break;
@@ -642,7 +651,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         pass = EXACT;
         if (*redo != 0) {
           w = begin;
-          if (w.pos < w.end) q = chunk_seq(a.sched, w.b);
+          if (w.pos < w.end) q = chunk_seq(sched, w.b);
         }
         more = true;
         continue;
@@ -657,6 +666,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
         ++n_q[x];
       }
+      ok = ok && hand_out(k + 2);   // two parts ahead (four places: this warp reads its own there)
       for (int i = 0; i < 2 * p.n && ok; ++i, ++e) {
         const int st = e % C::NSTAGE;
         ok = wait(C::FULL + st, e / C::NSTAGE);
@@ -847,12 +857,12 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     Part p;
     if (cols) {
       for (int k = 0; ok && get_part(k, p); ++k) {
-        if (x >= p.n || (b == 1 && !wide)) continue;   // no key tile for stream 1, or no row for the second warpgroup
-        ok = softmax_cols<HD>(a, sl2, p, x, b, wide, tmem, base, bars, abort_flag, n, group);
         if (x == 0 && p.parts > 1) {
           if (b == 0 && row == 0) cuts[n_cuts] = p;
           ++n_cuts;
         }
+        if (x >= p.n || (b == 1 && !wide)) continue;   // no key tile for stream 1, or no row for the second warpgroup
+        ok = softmax_cols<HD>(a, sl2, p, x, b, wide, tmem, base, bars, abort_flag, n, group);
       }
     } else {
       const int per_head = 65536 / a.block_heads + 1;   // row * per_head >> 16 = row / block_heads for rows below 128
@@ -1046,13 +1056,17 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
       }
     }
-    // ---- items that are cut: both halves have written their columns (COLS: rows) of the parts
+    // ---- items that are cut: both warpgroups have written their columns (COLS: rows) of the parts
     if (ok && *abort_flag == 0) {
+      auto sync = [&]() {
+        warp_arrive(bar(C::SUMS + x));
+        return wait(C::SUMS + x, n.sum++);
+      };
       __threadfence();
-      warp_arrive(bar(C::SUMS + x));
-      if (wait(C::SUMS + x, n.sum) && b == 0) {
-        if (cols) join_cuts<HD, true>(a, cuts, n_cuts, ta.tile_tok, x, row, last_part + x, group);
-        else join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, row, last_part + x, group);
+      if (sync() && n_cuts > 0) {
+        float2* rows = reinterpret_cast<float2*>(gen + C::OFF_SUM + x * 1024);
+        if (cols) join_cuts<HD, true>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, rows, sync);
+        else join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, rows, sync);
       }
     }
   }
