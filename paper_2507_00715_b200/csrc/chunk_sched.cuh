@@ -12,7 +12,7 @@
 // columns: item i of the order above stands in column i % CTAs, and a column's items follow one another.  A CTA's share is then
 // about one column, and neighbouring CTAs are at neighbouring items.  (8 sequences of 1024 new tokens over 16000-31000 rows:
 // DRAM traffic 13.4 -> 1.9 GB a layer.)  All of it is whole-number arithmetic on
-// the lengths: every CTA finds its own share and, for an item in parts, who else holds one, without a planning kernel.
+// the lengths, in 32 bits (a call with 2^31 units or more is refused): every CTA finds its own share and, for an item in parts, who else holds one, without a planning kernel.
 #pragma once
 #include <stdint.h>
 
@@ -31,7 +31,7 @@ struct ChunkSched {
   int grid, min_share;      // CTAs launched; units a CTA takes at least
   const ChunkSeq* table;    // the sequences, where a CTA has them in shared memory (up to kChunkTable), or null
 };
-constexpr int kChunkTable = 1024;
+constexpr int kChunkTable = 960;
 
 // Offsets that run past the batch or backwards are cut off, so that no row outside q and o is touched.
 __host__ __device__ inline ChunkSeq chunk_seq(const ChunkSched& s, int b) {
@@ -56,12 +56,12 @@ __host__ __device__ inline int chunk_units(const ChunkSched& s, const ChunkSeq& 
   const int u = (chunk_keys(s, q, m) + s.key_tile - 1) / s.key_tile;
   return u > 0 ? u : 1;
 }
-// sum over i < n of floor((a i + b) / m), by the Euclidean recursion; a n + b below 2^32
-__host__ __device__ inline int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
-  int64_t sum = 0;
+// sum over i < n of floor((a i + b) / m), by the Euclidean recursion; a n + b and the sum below 2^32
+__host__ __device__ inline uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+  uint32_t sum = 0;
   while (true) {
-    if (a >= m) { const uint32_t k = a / m; sum += (int64_t)n * (n - 1) / 2 * k; a -= k * m; }
-    if (b >= m) { const uint32_t k = b / m; sum += (int64_t)n * k; b -= k * m; }
+    if (a >= m) { const uint32_t k = a / m; sum += (uint32_t)((uint64_t)n * (n - 1) / 2) * k; a -= k * m; }
+    if (b >= m) { const uint32_t k = b / m; sum += n * k; b -= k * m; }
     const uint32_t y = a * n + b;
     if (y < m) return sum;
     n = y / m;
@@ -72,12 +72,12 @@ __host__ __device__ inline int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a,
   }
 }
 // units of the first `count` items of a sequence under one head block
-__host__ __device__ inline int64_t chunk_units_before(const ChunkSched& s, const ChunkSeq& q, int count) {
+__host__ __device__ inline uint32_t chunk_units_before(const ChunkSched& s, const ChunkSeq& q, int count) {
   const int items = q.items;
   if (count == 1 || items == 1) return count > 0 ? chunk_units(s, q, 0) : 0;
   int whole = count < items ? count : items - 1;   // items whose end is a multiple of item_tok
   if (whole < 0) whole = 0;
-  int64_t sum = 0;
+  uint32_t sum = 0;
   int skip = 0;
   if (q.base < 0) {   // leading items that see less than one key
     skip = (int)((1 - (int64_t)q.base + s.item_tok - 1) / s.item_tok) - 1;
@@ -91,29 +91,36 @@ __host__ __device__ inline int64_t chunk_units_before(const ChunkSched& s, const
 }
 
 struct ChunkWalk {
-  int64_t pos, end;    // units of the line: next one, and the end of this CTA's share
-  int64_t total, tol;  // units in all; a cut closer than this to an item's edge is moved there
-  int shares;          // shares the line is cut into
-  int b, h, m, off;    // where pos is: unit `off` of item m under head block h of sequence b
-  int longest;         // most new tokens of a sequence
-  int cols, col;       // columns of the line (1: the items' own order), and the one that pos is in
+  uint32_t pos, end;    // units of the line: next one, and the end of this CTA's share
+  uint32_t total, tol;  // units in all; a cut closer than this to an item's edge is moved there
+  int shares;           // shares the line is cut into: share c begins at c * quot + c * rem / shares
+  uint32_t quot, rem;
+  int b, h, m, off;     // where pos is: unit `off` of item m under head block h of sequence b
+  int longest;          // most new tokens of a sequence
+  int cols, col;        // columns of the line (1: the items' own order), and the one that pos is in
 };
-
-__host__ __device__ inline int64_t chunk_cut(const ChunkWalk& w, int c) { return (int64_t)c * w.total / w.shares; }
+__host__ __device__ inline void chunk_cuts(const ChunkSched& s, ChunkWalk& w) {
+  const uint32_t shares = (w.total + s.min_share - 1) / s.min_share;
+  w.shares = (int)(shares < (uint32_t)s.grid ? (shares > 0 ? shares : 1) : (uint32_t)s.grid);
+  w.quot = w.total / w.shares;
+  w.rem = w.total - w.quot * w.shares;
+  w.tol = w.quot / 16;
+}
+__host__ __device__ inline uint32_t chunk_cut(const ChunkWalk& w, int c) { return c * w.quot + c * w.rem / w.shares; }
 
 // `count` items further in the order (sequence, head block, item); w.b = n_seq behind the last one
 __host__ __device__ inline void chunk_skip(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int count) {
   if (w.m + count < q.items) { w.m += count; return; }
-  int64_t at = (int64_t)w.h * q.items + w.m + count, all;
-  while (at >= (all = (int64_t)s.heads * q.items)) {
+  uint32_t at = (uint32_t)w.h * q.items + w.m + count, all;
+  while (at >= (all = (uint32_t)s.heads * q.items)) {
     at -= all;
     do {
       if (++w.b >= s.n_seq) return;
       q = chunk_seq(s, w.b);
     } while (q.n == 0);
   }
-  w.h = (int)(at / q.items);
-  w.m = (int)(at - (int64_t)w.h * q.items);
+  w.h = q.items == 1 ? at : at / q.items;
+  w.m = at - w.h * q.items;
 }
 // the first item of a column (there is one: no more columns than items)
 __host__ __device__ inline void chunk_column(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int col) {
@@ -130,8 +137,8 @@ __host__ __device__ inline void chunk_next(const ChunkSched& s, ChunkWalk& w, Ch
 }
 // Moves unit x of the line, which lies at unit w.off of the item where w is, to the item's edge where it is close to one.
 // Returns the cut; w moves with it.
-__host__ __device__ inline int64_t chunk_settle(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int64_t x) {
-  const int off = w.off, left = chunk_units(s, q, w.m) - off;
+__host__ __device__ inline uint32_t chunk_settle(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, uint32_t x) {
+  const uint32_t off = w.off, left = chunk_units(s, q, w.m) - off;
   if (off <= w.tol) {
     w.off = 0;
     return x - off;
@@ -141,7 +148,7 @@ __host__ __device__ inline int64_t chunk_settle(const ChunkSched& s, ChunkWalk& 
   return x + left;
 }
 // Own order (w.cols = 1): w to unit `r` of sequence b's items under its head block h.
-__host__ __device__ inline void chunk_find(const ChunkSched& s, ChunkWalk& w, const ChunkSeq& q, int64_t r) {
+__host__ __device__ inline void chunk_find(const ChunkSched& s, ChunkWalk& w, const ChunkSeq& q, uint32_t r) {
   int lo = 0, hi = q.items;   // the last item that starts at or before r lies in lo .. hi - 1
 #ifdef __CUDA_ARCH__
   while (hi - lo > 1) {       // (the whole warp: 32 places at once)
@@ -157,73 +164,76 @@ __host__ __device__ inline void chunk_find(const ChunkSched& s, ChunkWalk& w, co
   }
 #endif
   w.m = lo;
-  w.off = (int)(r - chunk_units_before(s, q, lo));
+  w.off = lo > 0 ? (int)(r - chunk_units_before(s, q, lo)) : (int)r;
 }
 
 // An item in parts: CTAs first .. first + parts - 1 hold one each (parts = 1: the item is whole).
 struct ChunkParts {
   int first, parts;
 };
-__host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, int64_t start, int units) {
-  const int64_t g = w.shares, u = w.total;
-  const int64_t lo = ((start + w.tol + 1) * g + u - 1) / u;            // first cut more than tol behind the start
-  const int64_t hi = ((start + units - w.tol) * g + u - 1) / u - 1;    // last cut more than tol in front of the end
-  ChunkParts p;
-  p.parts = hi >= lo ? (int)(hi - lo) + 2 : 1;
-  p.first = (int)lo - 1;
+// the first cut at or behind unit y
+__host__ __device__ inline int chunk_cut_from(const ChunkWalk& w, uint32_t y) {
+  int c = (int)((float)y * ((float)w.shares / (float)w.total));
+  c = c < w.shares ? c : w.shares;
+  while (c > 0 && chunk_cut(w, c - 1) >= y) --c;
+  while (chunk_cut(w, c) < y) ++c;
+  return c;
+}
+__host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, uint32_t start, int units) {
+  ChunkParts p{0, 1};
+  if ((uint32_t)units <= 2 * w.tol + 1) return p;
+  const int lo = chunk_cut_from(w, start + w.tol + 1), hi = chunk_cut_from(w, start + units - w.tol) - 1;   // cuts further than tol inside
+  p.parts = hi >= lo ? hi - lo + 2 : 1;
+  p.first = lo - 1;
   return p;
 }
 
 // columns of the line, see above; `threads`: a column's units are summed up by a thread
-__host__ __device__ inline int chunk_columns(int64_t items, int64_t lists, int n_seq, int shares, int threads) {
-  return shares <= threads && n_seq <= 64 && items >= 2 * (int64_t)shares && items >= 4 * lists ? shares : 1;
+__host__ __device__ inline int chunk_columns(uint32_t items, uint32_t lists, int n_seq, int shares, int threads) {
+  return shares <= threads && n_seq <= 64 && items >= 2u * shares && items / 4 >= lists ? shares : 1;
 }
 
 #ifdef __CUDACC__
 struct ChunkCounts {
-  int64_t units;
+  uint32_t units;
   int items, lists, longest;   // (items and lists: of sequences)
 };
 // Sums (units, items, lists) and maximum (longest) over the block; returns the units of the threads in front of this one.
-__device__ inline int64_t chunk_scan(ChunkCounts& c, int64_t* scratch) {
+__device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
-  int64_t incl = c.units;
+  uint32_t incl = c.units;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, incl, d);
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, d);
     if (lane >= d) incl += v;
   }
-  const int64_t inside = incl - c.units;
-  c.items = __reduce_add_sync(0xffffffffu, c.items);
-  c.lists = __reduce_add_sync(0xffffffffu, c.lists);
-  c.longest = __reduce_max_sync(0xffffffffu, c.longest);
+  const uint32_t inside = incl - c.units;
+  const int items = __reduce_add_sync(0xffffffffu, c.items), lists = __reduce_add_sync(0xffffffffu, c.lists);
+  const int longest = __reduce_max_sync(0xffffffffu, c.longest);
   __syncthreads();
-  if (lane == 31) {
-    scratch[warp] = incl;
-    reinterpret_cast<int4*>(scratch + 32)[warp] = make_int4(c.items, c.lists, c.longest, 0);
-  }
+  if (lane == 31) scratch[warp] = make_int4((int)incl, items, lists, longest);
   __syncthreads();
-  const int64_t mine = lane < warps ? scratch[lane] : 0;
-  const int4 n = lane < warps ? reinterpret_cast<int4*>(scratch + 32)[lane] : make_int4(0, 0, 0, 0);
-  int64_t sum = mine;
+  const int4 n = lane < warps ? scratch[lane] : make_int4(0, 0, 0, 0);
+  uint32_t sum = (uint32_t)n.x;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, sum, d);
+    const uint32_t v = __shfl_up_sync(0xffffffffu, sum, d);
     if (lane >= d) sum += v;
   }
   c.units = __shfl_sync(0xffffffffu, sum, 31);
-  c.items = __reduce_add_sync(0xffffffffu, n.x);
-  c.lists = __reduce_add_sync(0xffffffffu, n.y);
-  c.longest = __reduce_max_sync(0xffffffffu, n.z);
-  return __shfl_sync(0xffffffffu, sum - mine, warp) + inside;
+  c.items = __reduce_add_sync(0xffffffffu, n.y);
+  c.lists = __reduce_add_sync(0xffffffffu, n.z);
+  c.longest = __reduce_max_sync(0xffffffffu, n.w);
+  return __shfl_sync(0xffffffffu, sum - (uint32_t)n.x, warp) + inside;
 }
 
-// This CTA's share of the line; every thread of the CTA calls it (`scratch`: 16-byte aligned shared memory for 96 64-bit words;
-// `table`: for kChunkTable sequences, or null).  From then on s reads the sequences from the table, where they fit.
-__device__ inline ChunkWalk chunk_share(ChunkSched& s, int64_t* scratch, ChunkSeq* table) {
+// This CTA's share of the line; every thread of the CTA calls it (`scratch`: 16-byte aligned shared memory for 48 16-byte words;
+// `table`: for kChunkTable sequences, or null).  From then on s reads the sequences from the table, where they fit.  Nothing
+// is worked out (pos = end) if the longest chunk is not within least .. most tokens: the call is another kernel's.
+__device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* table, int least, int most) {
   const int t = threadIdx.x, threads = blockDim.x, c = blockIdx.x;
   const bool in_table = table != nullptr && s.n_seq <= kChunkTable;
-  const int per = (s.n_seq + threads - 1) / threads, b0 = min(t * per, s.n_seq), b1 = min(b0 + per, s.n_seq);
+  const int per = s.n_seq <= threads ? 1 : (s.n_seq + threads - 1) / threads, b0 = min(t * per, s.n_seq), b1 = min(b0 + per, s.n_seq);
   ChunkCounts n{};
   for (int b = b0; b < b1; ++b) {
     const ChunkSeq q = chunk_seq(s, b);
@@ -234,15 +244,14 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int64_t* scratch, ChunkSe
     ++n.lists;
     n.units += s.heads * chunk_units_before(s, q, q.items);
   }
-  int64_t mine = n.units, before = chunk_scan(n, scratch);
+  uint32_t mine = n.units, before = chunk_scan(n, scratch);
   if (in_table) s.table = table;   // (written in front of the scan's barriers)
   ChunkWalk w{};
   w.total = n.units;
   w.longest = n.longest;
-  const int64_t shares = (w.total + s.min_share - 1) / s.min_share;
-  w.shares = (int)(shares < s.grid ? (shares > 0 ? shares : 1) : s.grid);
-  w.tol = w.total / (w.shares * 16);
-  w.cols = chunk_columns((int64_t)n.items * s.heads, (int64_t)n.lists * s.heads, s.n_seq, w.shares, threads);
+  if (n.longest < least || n.longest > most) return w;
+  chunk_cuts(s, w);
+  w.cols = chunk_columns((uint32_t)n.items * s.heads, (uint32_t)n.lists * s.heads, s.n_seq, w.shares, threads);
   if (w.cols > 1) {
     ChunkCounts col{};
     if (t < w.cols) {
@@ -254,26 +263,26 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int64_t* scratch, ChunkSe
     before = chunk_scan(col, scratch);
   }
   // who knows where the cuts lie says so, and a warp each finds the place
-  const int64_t x0 = chunk_cut(w, c), x1 = chunk_cut(w, c + 1);
-  int64_t* place = scratch + 80;   // [2]: first thread's number and units in front of it
+  const uint32_t x0 = chunk_cut(w, c), x1 = chunk_cut(w, c + 1);
+  uint32_t* place = reinterpret_cast<uint32_t*>(scratch + 32);   // two of: thread's number, units in front of it
   if (c < w.shares && mine > 0) {
     if (x0 >= before && x0 < before + mine) { place[0] = t; place[1] = before; }
     if (x1 >= before && x1 < before + mine) { place[2] = t; place[3] = before; }
   }
   __syncthreads();
-  int64_t* found = scratch + 84;
+  uint32_t* found = place + 4;
   if (t < 64) {
     const int side = t >> 5;
-    const int64_t x = side ? x1 : x0;
+    const uint32_t x = side ? x1 : x0;
     ChunkWalk v = w;
-    int64_t cut = w.total;
+    uint32_t cut = w.total;
     if (c < w.shares && x < w.total) {
       const int owner = (int)place[2 * side];
-      int64_t at = place[2 * side + 1];
+      uint32_t at = place[2 * side + 1];
       ChunkSeq q;
       if (w.cols > 1) {
         chunk_column(s, v, q, owner);
-        for (int u = chunk_units(s, q, v.m); at + u <= x; u = chunk_units(s, q, v.m)) {
+        for (uint32_t u = chunk_units(s, q, v.m); at + u <= x; u = chunk_units(s, q, v.m)) {
           at += u;
           chunk_skip(s, v, q, w.cols);
         }
@@ -282,7 +291,7 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int64_t* scratch, ChunkSe
         for (v.b = owner * per;; ++v.b) {
           q = chunk_seq(s, v.b);
           if (q.n == 0) continue;
-          const int64_t per_head = chunk_units_before(s, q, q.items);
+          const uint32_t per_head = chunk_units_before(s, q, q.items);
           if (x < at + s.heads * per_head) {
             v.h = (int)((x - at) / per_head);
             chunk_find(s, v, q, x - at - v.h * per_head);

@@ -21,20 +21,20 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   float* Ks = Qs + RT * D;   // float4 c of row r lies at c ^ (r & 7): sixteen rows are read at once
   float* Vs = Ks + KT * D;
   float* Ps = Vs + KT * D;
-  __shared__ alignas(16) int64_t scratch[96];
+  __shared__ int4 scratch[48];
   __shared__ int last_part;
   __shared__ float2 weights[RT];
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
   ChunkSched s = a.sched;
   pdl_launch_dependents();
   pdl_wait();
-  ChunkWalk w = chunk_share(s, scratch, nullptr);
+  ChunkWalk w = chunk_share(s, scratch, nullptr, 1, INT32_MAX);
   if (w.pos >= w.end) return;
   ChunkSeq q = chunk_seq(s, w.b);
   while (w.pos < w.end) {
     const int units = chunk_units(s, q, w.m);
-    const int64_t start = w.pos - w.off;
-    const int stop = (int)min((int64_t)units, w.end - start);   // this part: units off .. stop
+    const uint32_t start = w.pos - w.off;
+    const int stop = (int)min((uint32_t)units, w.end - start);   // this part: units off .. stop
     const int kvh = w.h / a.blocks, head0 = kvh * a.g + (w.h % a.blocks) * a.block_heads;
     const int n_heads = min(a.block_heads, (kvh + 1) * a.g - head0);
     const int tok_in = w.m * s.item_tok, n_tok = min(s.item_tok, q.n - tok_in), tok0 = q.tok0 + tok_in;
@@ -211,7 +211,7 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int d
   // no more CTAs than there can be units
   const int64_t items = (int64_t)n_tokens / (p.tile_tok * p.tiles) + std::min(n_seq, n_tokens);
   const int64_t units = items * n_kv_heads * p.blocks * ((max_len + p.keys - 1) / p.keys);
-  p.grid = (int)std::min<int64_t>(sm_count() * (tc ? 1 : D == 64 ? 3 : 2), std::max<int64_t>(units, 1));
+  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(sm_count() * (tc ? 1 : D == 64 ? 3 : 2), std::max<int64_t>(units, 1));
   return p;
 }
 

@@ -52,7 +52,12 @@ struct ChunkPlan {
 };
 ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int dtype, int n_tokens, int max_len);
 cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st);                      // fp32
-cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);    // bf16
+// bf16: a call whose sequences have at most chunk_short_tokens() new tokens each (0: none such) is the first kernel's, any other
+// the second's.  The lengths are on the device, so both are launched, unless n_tokens tells, and one of them finds nothing to do.
+cudaError_t launch_chunk_short(const ChunkArgs& a, cudaStream_t st);
+cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);
+constexpr int kShortRows = 32;   // rows (token, query head of a kv head)
+inline int chunk_short_tokens(const ChunkArgs& a) { return a.blocks == 1 ? kShortRows / a.g : 0; }
 
 // Softmax denominator of a row, natural log: once per row, so the logarithm is taken in 64 bits (the fast 32-bit one is off by
 // a few 1e-7, which is all of what fp32 callers see).  A row that sees nothing: -inf.

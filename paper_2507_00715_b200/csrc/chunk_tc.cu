@@ -6,8 +6,8 @@
 //
 //   PAIR   more than 128 rows: two row tiles of 128 against the same K/V tiles
 //   ROWS   up to 128 rows: one row tile, even and odd key tiles as two streams that meet in the end
-//   COLS   where no item of the call has more than 32 rows (decoded tokens, drafts): the same two streams transposed,
-//          S^T = K Q^T and O^T = V^T P^T, so that all threads have a key each instead of a few threads a row each
+//
+// (A call whose chunks all have at most 32 rows is the other kernel's, chunk_short.cu.)
 //
 //   warp 0      TMA: the pages of the K and V tiles -> shared memory (128-byte swizzle), 16 rows x 64 columns a copy, a ring that
 //               runs on across items
@@ -15,18 +15,17 @@
 //               one has read them; and the rows behind the last key in the last page of an item, zeroed in V (a weight of zero
 //               does not undo a NaN)
 //   warps 2, 3  tcgen05.mma, one warp per stream (row tile, or half of the key tiles): S into tensor memory, O += P V with P read
-//               from tensor memory (COLS: shared memory).  What a warp waits for and how long it takes to issue is hidden behind
+//               from tensor memory.  What a warp waits for and how long it takes to issue is hidden behind
 //               the other's products: one warp for both was 1.4 times slower on long lists
 //   warps 4..   softmax, two warpgroups per stream
 //
-// PAIR and ROWS: a key tile is taken in two halves of 64 keys, each with an accumulator and a warpgroup of its own, one row per
+// A key tile is taken in two halves of 64 keys, each with an accumulator and a warpgroup of its own, one row per
 // thread, so that the tensor core has the other halves to multiply while one is in the exponentials (P lies over S: the next S
 // of a half follows its P V).  With whole tiles a product of 128 x 128 costs the tensor core less (the halves read Q twice), but
 // it waits more: 1152 us instead of 920 for 4096 new tokens over 12000 rows, 32/8 heads.  The reference of a row's exponentials is its largest logit among its first 32 visible keys, and
 // stays: fp32 and bf16 hold 2^127, so a row needs another one only if a logit exceeds that by 44 nats or more.  If the sums tell
 // that one did (or that the first keys had no finite logit), the CTA takes all its parts again, each twice: for the rows' maxima,
 // and with them.  (A test per half and a rescaling of O in place, with one warpgroup per row tile, took 1.4 times as long.)
-// COLS: one key per thread, 16 rows per warpgroup, references common to the warpgroup and raised tile by tile.
 //
 // An item that is cut leaves fp32 parts; the CTA that finishes last joins them (chunk_join), once it has nothing else to do.  Every mbarrier wait is bounded:
 // when one runs out the CTA raises its abort flag, writes EARN_ERR_TIMEOUT to the status word, waits for what it has in flight,
@@ -34,16 +33,11 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "chunk_step.cuh"
-#include "sm100_ptx.cuh"
+#include "chunk_part.cuh"
 #include "tc_maps.cuh"
 
 namespace earn {
 namespace {
-using namespace ptx;
-
-constexpr int BM = 128, BN = 128;
-constexpr long long WAIT_LIMIT = 2000000000LL;   // about one second of SM clocks
 
 template <int HD>
 struct Cfg {
@@ -51,74 +45,24 @@ struct Cfg {
   static constexpr int NHALF = HD / 64;
   static constexpr int NSTAGE = HD == 128 ? 4 : 8;
   static constexpr int OFF_Q = 0, OFF_RING = OFF_Q + 2 * TILE, RING_END = OFF_RING + NSTAGE * TILE;
-  static constexpr int OFF_PT = HD == 128 ? OFF_Q + TILE : RING_END;                   // COLS: P^T of either stream (no second Q tile then)
-  static constexpr int OFF_REF = HD == 128 ? RING_END : OFF_PT + 2 * 16384;            // references [stream][row]
+  static constexpr int OFF_REF = RING_END;                                             // references [stream][row]
   static constexpr int OFF_SUM = OFF_REF + 2 * 128 * 4;                                // sums [parity][stream][half][row]
   static constexpr int OFF_MAX = OFF_SUM + 2 * 2 * 2 * 128 * 4;                        // maxima [stream][half][row]
-  static constexpr int OFF_RED = OFF_MAX + 2 * 2 * 128 * 4, RED = 1024;                // COLS: a warpgroup's scratch
-  static constexpr int OFF_SUM1 = OFF_RED + 4 * RED;                                    // stream 1's sums [half][row] for a merge
+  static constexpr int OFF_SUM1 = OFF_MAX + 2 * 2 * 128 * 4;                           // stream 1's sums [half][row] for a merge
   static constexpr int OFF_CUT = OFF_SUM1 + 2 * 128 * 4;                               // parts of items that are cut [stream][2]
   static constexpr int OFF_SEQ = OFF_CUT + 4 * 64;                                          // the sequences
   static constexpr int OFF_PART = OFF_SEQ + kChunkTable * (int)sizeof(ChunkSeq), OFF_BAR = OFF_PART + 4 * 64;
   static constexpr int THREADS = 32 * 20;
   static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 4, O = P + 4,
                        OM = O + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2,
-                       PARTFREE = PARTFULL + 4, GROUP = PARTFREE + 4, REFS = GROUP + 4, SUMS = REFS + 2, DONE = SUMS + 2,
-                       N_BARS = DONE + 1, OFF_VOTE = 8 * N_BARS + 48;
-  static constexpr int SMEM_BYTES = OFF_BAR + (OFF_VOTE + 64 + 127) / 128 * 128 + 1024;   // + alignment slack
+                       PARTFREE = PARTFULL + 4, REFS = PARTFREE + 4, SUMS = REFS + 2, DONE = SUMS + 2,
+                       N_BARS = DONE + 1;
+  static constexpr int SMEM_BYTES = OFF_BAR + (8 * N_BARS + 48 + 127) / 128 * 128 + 1024;   // + alignment slack
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of an SM");
 };
 
-enum Form { PAIR, ROWS, COLS };
-enum Pass { FAST, MAXIMA, EXACT };
 constexpr float SUM_LIMIT = 1.8446744e19f;   // 2^64: sums up to here leave O's below 2^64 |v|
-constexpr int MAX_COLS = 32;   // rows of an item in the transposed form
 
-// One item's share of this CTA, as warp 1 hands it to the others (16 words in shared memory).
-struct alignas(16) Part {
-  __device__ __forceinline__ int pass() const { return kind >> 2; }
-  __device__ __forceinline__ int form() const { return kind & 3; }
-  int b, kvh, head0, n_heads;   // sequence, kv head, first query head, query heads
-  int tok0, tok_in, n_tok;      // first token in the batch and in the chunk, tokens
-  int base, keys;               // rows in front of the chunk; keys that the item's last token sees
-  int u0, n;                    // key tiles u0 .. u0 + n - 1; n = 0: all parts have been handed out, n < 0: that was it
-  int kind;                     // form, pass
-  int n_rows;                   // rows of the first row tile
-  int last;                     // the item's last key tile is among them
-  int first, parts;             // CTAs first .. first + parts - 1 hold one part each
-};
-static_assert(sizeof(Part) == 64, "four 16-byte words");
-
-// The CTA's parts one after the other.
-__device__ __forceinline__ Part next_part(const ChunkArgs& a, const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int tile_tok, bool cols, int pass) {
-  Part p{};
-  if (w.pos >= w.end) return p;
-  p.b = w.b;
-  p.kvh = a.blocks > 1 ? w.h / a.blocks : w.h;
-  p.head0 = p.kvh * a.g + (w.h - p.kvh * a.blocks) * a.block_heads;
-  p.n_heads = min(a.block_heads, (p.kvh + 1) * a.g - p.head0);
-  p.tok_in = w.m * s.item_tok;
-  p.n_tok = min(s.item_tok, q.n - p.tok_in);
-  p.tok0 = q.tok0 + p.tok_in;
-  p.base = q.base;
-  p.keys = chunk_keys(s, q, w.m);
-  const int units = chunk_units(s, q, w.m);
-  p.u0 = w.off;
-  p.n = (int)min((int64_t)(units - w.off), w.end - w.pos);
-  p.n_rows = min(p.n_tok, tile_tok) * a.block_heads;
-  p.kind = (cols ? COLS : p.n_tok > tile_tok ? PAIR : ROWS) + 4 * pass;
-  p.last = w.off + p.n == units;
-  p.parts = 1;
-  if (w.off > 0 || !p.last) {
-    const ChunkParts parts = chunk_parts(w, w.pos - w.off, units);
-    p.first = parts.first;
-    p.parts = parts.parts;
-  }
-  w.pos += p.n;
-  if (p.last) chunk_next(s, w, q);
-  else w.off += p.n;
-  return p;
-}
 // Ring entries of a part, 2 n of them.  PAIR: K0 V0 K1 V1 ..; two streams: K0 K1 V0 K2 V1 K3 .. V(n-1), as they are consumed (a
 // stream's next S follows its P V).
 __device__ __forceinline__ int entry_k(const Part& p, int j) { return p.form() == PAIR ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
@@ -177,55 +121,8 @@ __device__ __forceinline__ void tmem_st_8(uint32_t taddr, const uint32_t (&r)[8]
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// v[c] of all lanes combined; the result for column `lane % N` is returned
-template <int N, class Op>
-__device__ __forceinline__ float across_lanes(float (&v)[N], int lane, Op op) {
-#pragma unroll
-  for (int d = N / 2; d > 0; d >>= 1) {
-#pragma unroll
-    for (int i = 0; i < d; ++i) {
-      const float give = (lane & d) ? v[i] : v[i + d], keep = (lane & d) ? v[i + d] : v[i];
-      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, d));
-    }
-  }
-  if (N == 16) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
-  return v[0];
-}
 constexpr float NO_REF = 3.0e38f;   // added to a logit that has no reference yet: 2^(that) is inf unless the logit is -inf
 
-// The warp's arrival: what its lanes did before is visible to who waits.
-__device__ __forceinline__ void warp_arrive(uint32_t bar) {
-  __syncwarp();
-  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar) : "memory");
-}
-// Warp-wide bounded wait, the same answer in every lane.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, (uint32_t)parity & 1u, abort_flag, WAIT_LIMIT)) != 0;
-}
-// The four warps of a softmax warpgroup wait for one another, on an mbarrier: a named barrier would wait for good for a warp
-// that has given up.  False: a wait ran out.
-struct Group {
-  uint32_t bar, votes;   // votes: four words, that of phase n is n & 3
-  volatile int* abort_flag;
-  int n;
-  __device__ __forceinline__ bool sync() {
-    warp_arrive(bar);
-    return warp_wait(bar, n++, abort_flag);
-  }
-  __device__ __forceinline__ bool any(bool mine, bool& result) {
-    const uint32_t at = votes + 4u * (uint32_t)(n & 3);
-    if (__any_sync(0xffffffffu, mine)) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(1u) : "memory");
-    const bool ok = sync();
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    result = v != 0;
-    // (this word's next phase is four on; the others have read it before they get there, and it is cleared in between)
-    return ok;
-  }
-  __device__ __forceinline__ void clear() {   // by the first warp, after each phase: the word of the phase after the next
-    asm volatile("st.shared.u32 [%0], %1;" ::"r"(votes + 4u * (uint32_t)((n + 1) & 3)), "r"(0u) : "memory");
-  }
-};
 // The same instructions as in sm100_ptx.cuh, issued by one elected lane of a converged warp, so that the descriptors stay
 // warp-uniform arithmetic (a branch on the lane around them cost 1.1 times the time on long lists).
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
@@ -258,237 +155,19 @@ __device__ __forceinline__ void st_global_32b(void* at, const uint32_t (&v)[8]) 
 }
 __device__ __forceinline__ float lds(uint32_t at) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; }
 __device__ __forceinline__ void sts(uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
-__device__ __forceinline__ float2 lds2(uint32_t at) {
-  float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ void sts2(uint32_t at, float u, float v) { asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(u), "f"(v) : "memory"); }
 
 struct TcArgs {
   ChunkArgs a;
   int tile_tok, q_box_tok;   // tokens of a row tile; tokens that a copy of Q brings
+  int least;                 // the call is this kernel's if its longest chunk has that many tokens
   float scale_log2;
 };
-
-// The CTA's n parts of items that are cut (at most its first part and its last) are written: joins those of which it was the last
-// to finish.  (All 256 threads of stream x; sync: their barrier.)
-template <int HD, bool ROW_MAJOR, class Sync>
-__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, float2* rows, Sync sync) {
-#pragma unroll 1
-  for (int i = 0; i < n; ++i) {
-    const Part p = cuts[i];
-    if (t == 0) {
-      const int32_t at = p.first * 2 + x;
-      const bool is_last = atomicAdd(a.tickets + at, 1) == p.parts - 1;
-      if (is_last) a.tickets[at] = 0;   // for the next call
-      flag[i] = is_last;
-      __threadfence();
-    }
-  }
-  if (!sync()) return;
-#pragma unroll 1
-  for (int i = 0; i < n; ++i) {
-    if (flag[i] == 0) continue;
-    const Part p = cuts[i];
-    const int my_tok = p.form() == PAIR ? x * tile_tok : 0;
-    ChunkParts parts;
-    parts.first = p.first;
-    parts.parts = p.parts;
-    if (!sync()) return;   // (the numbers of the rows before have been read)
-    chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 256, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, rows, sync);
-  }
-}
-__device__ __forceinline__ int64_t part_slot(const Part& p, int x) {
-  return (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == p.first ? 1 : 0)) * 2 + x;
-}
 
 // Phases that a warpgroup has consumed: S, O, references, sums, merges of the streams.
 struct Phases {
   int s, o, ref, sum, ml;
   bool pending;   // stream 1: stream 0 may still be reading what the last merge needs
 };
-
-// Rows 16 h .. 16 h + 15 of stream x of a transposed part: thread = key, column = row.  Sums stay with the threads until the part
-// ends; the references (negated, log2 domain) are shared by the warpgroup.  Returns false when a wait ran out.
-template <int HD>
-__device__ __forceinline__ bool softmax_cols(const ChunkArgs& a, float sl2, const Part& p, int x, int h, bool wide, uint32_t tmem, uint32_t base,
-                                             uint32_t bars, volatile int* abort_flag, Phases& n, Group& group) {
-  using C = Cfg<HD>;
-  constexpr int NC = 16;
-  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
-  const uint32_t lane0 = (uint32_t)(warp * 32) << 16, t_s = tmem + lane0 + x * 128 + h * NC, t_o = tmem + lane0 + (2 + x) * 128 + h * NC;
-  const uint32_t pt = base + C::OFF_PT + (uint32_t)x * 16384 + (uint32_t)key * 128;   // P^T [key][row], 128 bytes a key
-  // scratch: 4 x 16 numbers of the warps, 16 factors, 16 references, 16 pairs, and the same of the other stream's end
-  const uint32_t red = base + C::OFF_RED + (uint32_t)(2 * x + h) * C::RED, scale = red + 256, refs = red + 320, fac = red + 384, ends = red + 512;
-  const uint32_t ends1 = base + C::OFF_RED + (uint32_t)(2 + h) * C::RED + 512;
-  const int row0 = h * NC, rows = min(p.n_rows - row0, NC);
-  auto wait = [&](int i, int parity) { return warp_wait(bars + 8u * (uint32_t)i, parity, abort_flag); };
-  auto sync = [&]() {
-    const bool ok = group.sync();
-    if (warp == 0) group.clear();
-    return ok;
-  };
-  if (n.pending) {   // the other stream may be reading this one's scratch and accumulator
-    n.pending = false;
-    if (!wait(C::MERGED, n.ml - 1)) return false;
-  }
-  const int first_seen = p.base + p.tok_in + 1;   // keys that the first token sees
-  float l[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) l[c] = 0.f;
-  for (int j = x; j < p.n; j += 2) {
-    if (!wait(C::S + 2 * x + h, n.s++)) return false;
-    tc_fence_after();
-    const bool first = j < 2, interior = (p.u0 + j + 1) * BN <= first_seen;
-    const int at = (p.u0 + j) * BN + key;
-    // the tile's logits; what the row does not see is -inf
-    auto logits = [&](uint32_t (&s)[NC]) {
-      tmem_ld_32x16(t_s, s);
-      if (!interior) {
-        int tok = row0 / a.block_heads, head = row0 - tok * a.block_heads;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if (at >= first_seen + tok) s[c] = 0xff800000u;
-          if (++head == a.block_heads) { head = 0; ++tok; }
-        }
-      }
-    };
-    // references from the tile's own maxima, where the old ones (none in front of the first tile) do not hold
-    auto raise = [&]() {
-      uint32_t s[NC];
-      float v[NC];
-      logits(s);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) v[c] = __uint_as_float(s[c]) * sl2;
-      const float mine = across_lanes<NC>(v, lane, [](float u, float t) { return fmaxf(u, t); });
-      if (lane < NC) sts(red + (uint32_t)(warp * NC + lane) * 4, mine);
-      if (!sync()) return false;
-      if (warp == 0 && lane < NC) {
-        const float top = fmaxf(fmaxf(lds(red + lane * 4), lds(red + (NC + lane) * 4)), fmaxf(lds(red + (2 * NC + lane) * 4), lds(red + (3 * NC + lane) * 4)));
-        const float old = first ? NO_REF : lds(refs + lane * 4);
-        // (rows that hold nothing get -inf: their weights are 0, or NaN, and go nowhere)
-        const float fresh = lane >= rows ? -INFINITY : top == -INFINITY ? old : old == NO_REF ? -top : top + old > 8.f ? -top : old;
-        sts(scale + lane * 4, old == NO_REF ? 0.f : lane >= rows ? 1.f : ex2(fresh - old));
-        sts(refs + lane * 4, fresh);
-      }
-      return sync();
-    };
-    if (first && !raise()) return false;
-    uint32_t pk[NC / 2];
-    float e[NC];
-#pragma unroll 1
-    for (int attempt = 0;; ++attempt) {
-      uint32_t s[NC];
-      logits(s);
-      float top = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; c += 2) {
-        const float2 r = lds2(refs + c * 4);
-        fma2(e[c], e[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), sl2, r.x, r.y);
-        e[c] = ex2(e[c]);
-        e[c + 1] = ex2(e[c + 1]);
-        top = max3(top, e[c], e[c + 1]);
-        pk[c >> 1] = pack_bf16(e[c], e[c + 1]);
-      }
-      if (first || attempt > 0) break;   // (the references are this tile's)
-      bool grown;
-      if (!group.any(top > 256.f, grown)) return false;
-      if (warp == 0) group.clear();
-      if (!grown) break;
-      if (!raise()) return false;
-      // what has been accumulated, to the new references: O^T is quiescent (S was issued behind the stream's last product)
-      tmem_ld_32x16(t_o, s);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const float f = lds(scale + c * 4);
-        l[c] *= f;
-        s[c] = __float_as_uint(__uint_as_float(s[c]) * f);
-      }
-      tmem_st_32x16(t_o, s);
-      tmem_wait_st();
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) l[c] += e[c];
-#pragma unroll
-    for (int ch = 0; ch < NC / 8; ++ch)
-      st_shared_v4(pt + (uint32_t)(((2 * h + ch) ^ (key & 7)) << 4), pk[ch * 4], pk[ch * 4 + 1], pk[ch * 4 + 2], pk[ch * 4 + 3]);
-    fence_async_smem();
-    tc_fence_before();
-    warp_arrive(bars + 8u * (C::P + 2 * x + h));
-  }
-  // ---- end of the part: the warps' sums, and stream 1's references, meet in stream 0's first warp
-  const bool merge = p.n > 1;
-  const float sum = across_lanes<NC>(l, lane, [](float u, float t) { return u + t; });
-  if (lane < NC) sts2(ends + (uint32_t)(warp * NC + lane) * 8, lds(refs + lane * 4), sum);
-  if (merge && x == 1) {
-    tc_fence_before();
-    warp_arrive(bars + 8u * C::ML);
-    if (!wide) warp_arrive(bars + 8u * C::ML);   // (in the place of the second warpgroup)
-    ++n.ml;
-    n.pending = true;
-    return true;
-  }
-  if (!wait(C::O + x, n.o++)) return false;
-  if (merge && !(wait(C::OM, n.ml) && wait(C::ML, n.ml))) return false;
-  tc_fence_after();
-  if (merge) ++n.ml;
-  const bool whole = p.parts == 1;
-  const int64_t slot = part_slot(p, x);
-  if (!sync()) return false;
-  if (warp == 0 && lane < NC) {
-    auto end_of = [&](uint32_t from, float& m, float& sum_of) {
-      const float2 v0 = lds2(from + lane * 8), v1 = lds2(from + (NC + lane) * 8), v2 = lds2(from + (2 * NC + lane) * 8), v3 = lds2(from + (3 * NC + lane) * 8);
-      m = v0.x == NO_REF ? -INFINITY : -v0.x;
-      sum_of = (v0.y + v1.y) + (v2.y + v3.y);
-    };
-    float m, l0, w0 = 1.f, w1 = 0.f;
-    end_of(ends, m, l0);
-    if (merge) {
-      float m1, l1;
-      end_of(ends1, m1, l1);
-      const float mx = fmaxf(m, m1), ref = mx == -INFINITY ? 0.f : mx;
-      w0 = ex2(m - ref);
-      w1 = ex2(m1 - ref);
-      l0 = l0 * w0 + l1 * w1;
-      m = mx;
-    }
-    const float inv = !whole ? 1.f : l0 == 0.f ? 0.f : __frcp_rn(l0);
-    sts2(fac + lane * 8, l0 == 0.f ? -1.f : w0 * inv, w1 * inv);   // (-1: nothing visible, O holds nothing)
-    const int row = row0 + lane, tok = row / a.block_heads, head = row - tok * a.block_heads;
-    if (lane < rows && head < p.n_heads) {
-      if (!whole) a.part_ml[slot * BM + row] = make_float2(m, l0);
-      else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + p.tok0 + tok] = chunk_lse<true>(m, l0);
-    }
-  }
-  if (!sync()) return false;
-  if (key < HD) {   // (whole warps) lane = element of the head
-    uint32_t s0[NC], s1[NC];
-    tmem_ld_32x16(t_o, s0);
-    if (merge) tmem_ld_32x16(t_o + 128, s1);
-    int tok = row0 / a.block_heads, head = row0 - tok * a.block_heads;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if (c < rows) {
-        const float2 f = lds2(fac + c * 8);
-        float y = __uint_as_float(s0[c]) * f.x;
-        if (merge) y += __uint_as_float(s1[c]) * f.y;
-        if (f.x < 0.f) y = 0.f;
-        if (head < p.n_heads) {
-          if (whole) reinterpret_cast<__nv_bfloat16*>(a.o)[((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + key] = __float2bfloat16(y);
-          else reinterpret_cast<float*>(a.part_o)[(slot * BM + row0 + c) * HD + key] = y;
-        }
-        if (++head == a.block_heads) { head = 0; ++tok; }
-      }
-    }
-  }
-  tc_fence_before();
-  if (merge) {
-    warp_arrive(bars + 8u * C::MERGED);
-    if (!wide) warp_arrive(bars + 8u * C::MERGED);
-  }
-  return sync();   // (the scratch's numbers have been read)
-}
 
 template <int HD>
 __global__ void __launch_bounds__(Cfg<HD>::THREADS, 1)
@@ -531,8 +210,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     mbar_init(bar(C::DONE), 16);
     mbar_init(bar(C::DRAIN), 1);
     mbar_init(bar(C::DRAIN + 1), 1);
-    for (int i = 0; i < 4; ++i) mbar_init(bar(C::GROUP + i), 4);
-    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t*>(gen + C::OFF_BAR + C::OFF_VOTE)[i] = 0;
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(C::PARTFULL + i), 1);
       mbar_init(bar(C::PARTFREE + i), 19);   // warps 0, 2, 3 and the softmax warps
@@ -555,24 +232,12 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   pdl_launch_dependents();
   pdl_wait();
   ChunkSched sched = a.sched;
-  ChunkWalk w = chunk_share(sched, reinterpret_cast<int64_t*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ));
-  const bool cols = w.longest * a.block_heads <= MAX_COLS, wide = w.longest * a.block_heads > 16;   // (wide: two warpgroups a stream)
+  ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ), ta.least, INT32_MAX);
   fence_async_smem();   // (the copies that come next land where the shares' scratch was)
   __syncthreads();
   auto wait = [&](int i, int parity) { return warp_wait(bar(i), parity, abort_flag); };
 
-  // Part k of this CTA, from warp 1; false: that was it, or a wait ran out.
-  auto get_part = [&](int k, Part& p) {
-    const int at = k & 3;
-    if (!wait(C::PARTFULL + at, k >> 2)) return false;
-    const int4* from = reinterpret_cast<const int4*>(gen + C::OFF_PART + at * 64);
-    int4* to = reinterpret_cast<int4*>(&p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to[i] = from[i];
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar(C::PARTFREE + at));
-    return p.n >= 0;
-  };
+  auto get_part = [&](int k, Part& p) { return take_part(gen + C::OFF_PART, bar(C::PARTFULL), bar(C::PARTFREE), k, abort_flag, p); };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer: K/V ring
@@ -616,31 +281,24 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const uint32_t bytes = (uint32_t)(ta.q_box_tok * a.block_heads) * (HD * 2);
     for (int k = 0; ok; ++k) {
       auto hand_out = [&](int upto) {
-      while (more && made <= upto) {
-        const int at = made & 3;
-        if (made >= 4 && !wait(C::PARTFREE + at, (made >> 2) - 1)) return false;
-        Part fresh{};
-        if (pass == EXACT && again.n > 0) {
-          fresh = again;
-          fresh.kind += 4 * (EXACT - MAXIMA);
-          again.n = 0;
-        } else if (w.pos < w.end) {
-          fresh = next_part(a, sched, w, q, ta.tile_tok, cols, pass == FAST ? FAST : MAXIMA);
-          if (pass == EXACT) again = fresh;
-        } else if (cols || pass == EXACT) {
-          fresh.n = -1;
-          more = false;
-        } else {
-          more = false;   // n = 0: this warp goes on once it has come to it
+        while (more && made <= upto) {
+          Part fresh;
+          if (pass == EXACT && again.n > 0) {
+            fresh = again;
+            fresh.kind += 4 * (EXACT - MAXIMA);
+            again.n = 0;
+          } else {
+            fresh = next_part(a, sched, w, q, ta.tile_tok, pass == FAST ? FAST : MAXIMA);
+            if (fresh.n > 0 && pass == EXACT) again = fresh;
+            if (fresh.n < 0) {
+              more = false;
+              if (pass == FAST) fresh.n = 0;   // (this warp goes on once it has come to it)
+            }
+          }
+          if (!give_part(gen + C::OFF_PART, bar(C::PARTFULL), bar(C::PARTFREE), made, abort_flag, fresh)) return false;
+          ++made;
         }
-        if (lane < 4) reinterpret_cast<int4*>(gen + C::OFF_PART + at * 64)[lane] = lane == 0 ? make_int4(fresh.b, fresh.kvh, fresh.head0, fresh.n_heads)
-                          : lane == 1 ? make_int4(fresh.tok0, fresh.tok_in, fresh.n_tok, fresh.base)
-                          : lane == 2 ? make_int4(fresh.keys, fresh.u0, fresh.n, fresh.kind) : make_int4(fresh.n_rows, fresh.last, fresh.first, fresh.parts);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::PARTFULL + at));
-        ++made;
-      }
-      return true;
+        return true;
       };
       ok = hand_out(k);
       if (!ok) break;
@@ -697,7 +355,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     constexpr uint32_t idesc_o = idesc_bf16_f32(BM, HD, 0, 1);       // P (TMEM) x V (MN-major)
     constexpr uint32_t desc_hi = smem_desc_hi_sw128(1024);
     const uint32_t q_lo = smem_desc_lo(sQ, 16), k_lo = smem_desc_lo(sRing, 16), v_lo = smem_desc_lo(sRing, C::HALF);
-    const uint32_t p_lo = smem_desc_lo(base + C::OFF_PT + x * 16384, 16);
     const uint32_t t_s = tmem + x * 128, t_o = tmem + (2 + x) * 128;
     auto free_entry = [&](int e) { mma_commit(bar(C::EMPTY + e % C::NSTAGE)); };
     // S of half b of a row tile: Q_y times keys 64 b .. of the K tile of ring entry e
@@ -721,25 +378,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll 1
         for (int kk = 0; 4 * b + kk < pages; ++kk) mma_ts(t_o, t_s + b * 64 + kk * 8, b0 + kk * (2048 >> 4), desc_hi, idesc_o, kk > 0 ? 1u : more);
       }
-    };
-    // COLS: S^T = K Q^T, and O^T (+)= V^T P^T with P^T [key][row] in shared memory.  (head_dim 64: O^T has 64 rows more than V has
-    // columns; what they are computed from lies within the ring or behind it, and nobody reads them.)
-    auto issue_st = [&](int e, uint32_t idesc) {
-      const uint32_t a0 = k_lo + (e % C::NSTAGE) * (C::TILE >> 4);
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) {
-        const uint32_t off = ((kk >> 2) * C::HALF + (kk & 3) * 32) >> 4;
-        mma_ss(t_s, a0 + off, q_lo + off, desc_hi, idesc, kk > 0);
-      }
-      mma_commit(bar(C::S + 2 * x));
-      if (wide) mma_commit(bar(C::S + 2 * x + 1));
-      free_entry(e);
-    };
-    auto issue_vp = [&](int e, int pages, bool first, uint32_t idesc) {
-      const uint32_t a0 = v_lo + (e % C::NSTAGE) * (C::TILE >> 4);
-#pragma unroll 1
-      for (int kk = 0; kk < pages; ++kk) mma_ss(t_o, a0 + kk * (2048 >> 4), p_lo + kk * (2048 >> 4), desc_hi, idesc, (!first || kk > 0) ? 1u : 0u);
-      free_entry(e);
     };
     int eb = 0, n_q = 0, n_q0 = 0;   // ring entry of the part's K_0; parts with a second Q tile, and all
     int filled = 0;                  // ring entries waited for
@@ -782,7 +420,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         auto wait_v = [&](int j) { return wait_full(eb + entry_v(p, j)) && (!fixed || j + 1 < n || wait(C::FIX + fix_st, fix_phase >> fix_st)); };
         auto pages_of = [&](int j) { return min(n_pages - (p.u0 + j) * 8, 8); };
         auto free_q = [&]() { mma_commit(bar(C::QFREE + y)); };   // the stream's last S has been issued
-        if (p.form() != COLS) {
+        {
           issue_s(0, y, eb + entry_k(p, j0));
           issue_s(1, y, eb + entry_k(p, j0));
           free_entry(eb + entry_k(p, j0));
@@ -809,25 +447,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
               }
             }
           }
-        } else {
-          const uint32_t idesc_st = idesc_bf16_f32(BM, wide ? 32 : 16, 0, 0);   // K (K-major) x Q^T (K-major)
-          const uint32_t idesc_ot = idesc_bf16_f32(BM, wide ? 32 : 16, 1, 1);   // V^T (MN-major) x P^T (MN-major)
-          issue_st(eb + entry_k(p, j0), idesc_st);
-          if (j0 + 2 >= n) free_q();
-          for (int j = j0; j < n && ok; j += 2) {
-            const int ek = eb + entry_k(p, j + 2);
-            ok = wait_p(0) && (!wide || wait_p(1)) && wait_v(j);
-            if (!ok) break;
-            tc_fence_after();
-            issue_vp(eb + entry_v(p, j), pages_of(j), j == j0, idesc_ot);
-            if (j + 2 < n) {
-              ok = wait_full(ek);
-              if (!ok) break;
-              tc_fence_after();
-              issue_st(ek, idesc_st);
-              if (j + 4 >= n) free_q();
-            }
-          }
         }
         if (ok) mma_commit(bar(p.form() == PAIR || x == 0 ? C::O + x : C::OM));
       }
@@ -844,7 +463,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
     __syncwarp();
   } else {
-    // ------------------------------------------------------------------ softmax: stream x, half b of its key tiles (COLS: of its rows)
+    // ------------------------------------------------------------------ softmax: stream x, half b of its key tiles
     const int x = (warp - 4) >> 3, b = ((warp - 4) >> 2) & 1;
     const int wq = warp & 3;            // a warp may only touch TMEM lanes 32*(warp % 4) ..
     const int row = wq * 32 + lane;
@@ -852,19 +471,9 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     Phases n{};
     Part* cuts = reinterpret_cast<Part*>(gen + C::OFF_CUT + x * 128);   // (written by the first half's threads)
     int n_cuts = 0;
-    Group group{bar(C::GROUP + 2 * x + b), bars + C::OFF_VOTE + 16u * (uint32_t)(2 * x + b), abort_flag, 0};
     bool ok = true, again = false;
     Part p;
-    if (cols) {
-      for (int k = 0; ok && get_part(k, p); ++k) {
-        if (x == 0 && p.parts > 1) {
-          if (b == 0 && row == 0) cuts[n_cuts] = p;
-          ++n_cuts;
-        }
-        if (x >= p.n || (b == 1 && !wide)) continue;   // no key tile for stream 1, or no row for the second warpgroup
-        ok = softmax_cols<HD>(a, sl2, p, x, b, wide, tmem, base, bars, abort_flag, n, group);
-      }
-    } else {
+    {
       const int per_head = 65536 / a.block_heads + 1;   // row * per_head >> 16 = row / block_heads for rows below 128
       const int tok = row * per_head >> 16, head = row - tok * a.block_heads;
       const uint32_t lane0 = (uint32_t)(wq * 32) << 16;
@@ -1056,18 +665,13 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
       }
     }
-    // ---- items that are cut: both warpgroups have written their columns (COLS: rows) of the parts
-    if (ok && *abort_flag == 0) {
+    // ---- items that are cut: both warpgroups have written their columns of the parts
+    if (ok && *abort_flag == 0 && n_cuts > 0) {
       auto sync = [&]() {
         warp_arrive(bar(C::SUMS + x));
         return wait(C::SUMS + x, n.sum++);
       };
-      __threadfence();
-      if (sync() && n_cuts > 0) {
-        float2* rows = reinterpret_cast<float2*>(gen + C::OFF_SUM + x * 1024);
-        if (cols) join_cuts<HD, true>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, rows, sync);
-        else join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, rows, sync);
-      }
+      join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, reinterpret_cast<float2*>(gen + C::OFF_SUM + x * 1024), sync);
     }
   }
 
@@ -1102,6 +706,7 @@ cudaError_t launch(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st) {
   ta.tile_tok = p.tile_tok;
   ta.q_box_tok = std::min(p.tile_tok, a.sched.n_tokens);
   ta.scale_log2 = a.scale * kLog2e;
+  ta.least = chunk_short_tokens(a) + 1;
   const int rows = a.cache.n_pages * EARN_PAGE_TOKENS;
   if (!make_q_map(&mq, a, ta.q_box_tok) || !tcmap::make_map(&mk, a.cache.k, a.Hkv, rows, EARN_PAGE_TOKENS, HD) ||
       !tcmap::make_map(&mv, a.cache.v, a.Hkv, rows, EARN_PAGE_TOKENS, HD))

@@ -893,6 +893,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   if (n_seq == 0 || n_tokens == 0) return EARN_OK;
   if (!cu_new || !q || !o || !aligned4(cu_new) || !aligned16(q) || !aligned16(o) || !aligned4(lse_or_null)) return EARN_ERR_INVALID_ARG;
   const ChunkLayout l = chunk_layout(model, n_seq, n_tokens, cache);
+  if (l.plan.grid == 0) return EARN_ERR_UNSUPPORTED;   // more work than 32 bits count
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < l.total) return EARN_ERR_WORKSPACE;
   char* ws = reinterpret_cast<char*>(workspace);
   ChunkArgs a{};
@@ -910,7 +911,14 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   a.g = model->n_q_heads / model->n_kv_heads; a.block_heads = l.plan.block_heads; a.blocks = l.plan.blocks;
   a.scale = scale_of(model);
   note_call(stream, CALL_UNKNOWN);
-  const cudaError_t e = a.dtype == EARN_BF16 ? launch_chunk_tc(a, l.plan, (cudaStream_t)stream) : launch_chunk_simt(a, (cudaStream_t)stream);
+  cudaError_t e = cudaSuccess;
+  if (a.dtype == EARN_BF16) {
+    const int few = chunk_short_tokens(a);
+    if (few > 0) e = launch_chunk_short(a, (cudaStream_t)stream);
+    if (e == cudaSuccess && n_tokens > few) e = launch_chunk_tc(a, l.plan, (cudaStream_t)stream);
+  } else {
+    e = launch_chunk_simt(a, (cudaStream_t)stream);
+  }
   return e == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }
 
