@@ -98,9 +98,9 @@ __device__ __forceinline__ bool give_part(void* places, uint32_t full, uint32_t 
 }
 
 // The CTA's n parts of items that are cut (at most its first part and its last) are written: joins those of which it was the last
-// to finish.  (256 threads; x: row tile; flag: a word per part; sync: the threads' barrier, false if it gave up.)
+// to finish.  (256 threads; x: row tile; flag: a word per part; weights: shared memory for 128 rows x 148 parts; sync: the threads' barrier, false if it gave up.)
 template <int HD, bool ROW_MAJOR, class Sync>
-__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, float2* rows, Sync sync) {
+__device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, int n, int tile_tok, int x, int t, volatile int* flag, float* weights, Sync sync) {
   __threadfence();
   if (!sync()) return;
   if (t < n) {
@@ -120,8 +120,8 @@ __device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, 
     ChunkParts parts;
     parts.first = p.first;
     parts.parts = p.parts;
-    if (!sync()) return;   // (the numbers of the rows before have been read)
-    chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 256, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, rows, sync);
+    if (!sync()) return;   // (the weights before have been read)
+    chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 256, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, weights, sync);
   }
 }
 

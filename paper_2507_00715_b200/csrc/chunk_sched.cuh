@@ -104,7 +104,9 @@ __host__ __device__ inline void chunk_cuts(const ChunkSched& s, ChunkWalk& w) {
   w.shares = (int)(shares < (uint32_t)s.grid ? (shares > 0 ? shares : 1) : (uint32_t)s.grid);
   w.quot = w.total / w.shares;
   w.rem = w.total - w.quot * w.shares;
-  w.tol = w.quot / 16;
+  // (a part more costs its writing and the join, about three key tiles' worth of time)
+  const uint32_t few = w.quot / 6 < 3 ? w.quot / 6 : 3;
+  w.tol = w.quot / 16 > few ? w.quot / 16 : few;
 }
 __host__ __device__ inline uint32_t chunk_cut(const ChunkWalk& w, int c) { return c * w.quot + c * w.rem / w.shares; }
 

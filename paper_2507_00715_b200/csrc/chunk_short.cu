@@ -1,5 +1,5 @@
 // Causal attention over paged lists of calls whose sequences have few new tokens each (decoded tokens, drafts): at most 32 rows
-// (token, query head of a kv head) per sequence.
+// (token, query head of a kv head) per sequence; an item is 16 of them.
 //
 // Bound by HBM: every K and V row is read once for all rows, 2 D flop per byte and row, so the work is to keep the copies going.
 // A CTA (one per SM) walks its share of the work line (chunk_sched.cuh).  One warp finds the parts and brings their tiles of 128
@@ -28,7 +28,7 @@ struct Cfg {
   static constexpr int TILE = 128 * HD * 2, HALF = 128 * 128, NHALF = HD / 64;   // bytes of a tile, and of its 64-column blocks
   static constexpr int OFF_OUT = NSTAGE * 2 * TILE;                              // Q, later the warps' outputs, 16 KB
   static constexpr int OFF_SEQ = OFF_OUT + 16384, OFF_ML = OFF_SEQ + kChunkTable * (int)sizeof(ChunkSeq);   // [warp][row]
-  static constexpr int ML_BYTES = WARPS * kShortRows * 8;
+  static constexpr int ML_BYTES = WARPS * 16 * 8;
   static constexpr int OFF_PART = OFF_ML + ML_BYTES, OFF_CUT = OFF_PART + 4 * 64, OFF_BAR = OFF_CUT + 2 * 64;
   static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, PARTFULL = EMPTY + NSTAGE, PARTFREE = PARTFULL + 4, GROUP = PARTFREE + 4, N_BARS = GROUP + 1;
   static constexpr int SMEM_BYTES = OFF_BAR + 8 * N_BARS + 32 + 1024;            // + alignment slack
@@ -47,50 +47,85 @@ struct Consumer {
   }
 };
 
-// All parts of the CTA, MT row tiles of 16 rows.
-template <int HD, int MT>
-__device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl2, int item_tok) {
+// The warps' outputs meet: R rows (of 16) x 512 / R columns at a time.  f: the lane's rows' factors.  out(row, column, y): two
+// columns' sums, in the threads that hold them.
+template <int HD, int R, class Out>
+__device__ __forceinline__ bool exchange(Consumer& c, const float (&o)[HD / 8][4], const float (&f)[2], Out out) {
+  using C = Cfg<HD>;
+  constexpr int COLS = 512 / R < HD ? 512 / R : HD, PAIRS = COLS / 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = threadIdx.x;
+  float2* all = reinterpret_cast<float2*>(c.gen + C::OFF_OUT);   // [warp][row][column pair], a row's pairs turned by four times its number
+#pragma unroll
+  for (int d0 = 0; d0 < HD; d0 += COLS) {
+#pragma unroll
+    for (int d = 0; d < COLS / 8; ++d) {
+#pragma unroll
+      for (int h = 0; h < (R > 8 ? 2 : 1); ++h) {
+        const int r = h * 8 + (lane >> 2);
+        if (R >= 8 || r < R)
+          all[warp * 256 + r * PAIRS + ((d * 4 + (lane & 3) + 4 * r) & (PAIRS - 1))] = make_float2(o[d0 / 8 + d][h * 2] * f[h], o[d0 / 8 + d][h * 2 + 1] * f[h]);
+      }
+    }
+    if (!c.template sync<C>()) return false;
+    if (t < R * PAIRS) {
+      const int r = t / PAIRS, pair = t % PAIRS;
+      float2 y = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) {
+        const float2 v = all[i * 256 + r * PAIRS + ((pair + 4 * r) & (PAIRS - 1))];
+        y.x += v.x;
+        y.y += v.y;
+      }
+      out(r, d0 + pair * 2, y);
+    }
+    if (!c.template sync<C>()) return false;
+  }
+  return true;
+}
+
+// All parts of the CTA.
+template <int HD>
+__device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl2) {
   using C = Cfg<HD>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = threadIdx.x;
   const uint32_t out = c.base + C::OFF_OUT;
   float2* ml = reinterpret_cast<float2*>(c.gen + C::OFF_ML);
   Part* cuts = reinterpret_cast<Part*>(c.gen + C::OFF_CUT);
   volatile int* flag = reinterpret_cast<volatile int*>(c.gen + C::OFF_BAR + 8 * C::N_BARS + 8);
+  auto take = [&](int k, Part& p) { return take_part(c.gen + C::OFF_PART, c.bars + 8u * C::PARTFULL, c.bars + 8u * C::PARTFREE, k, c.abort_flag, p); };
+  // Q: a thread brings 16 bytes of a row (shared memory: 128-byte lines of 64 columns, 16-byte chunk i of row r at i ^ (r % 8))
+  const int q_row = t / (HD / 8), q_ch = t % (HD / 8), q_tok = q_row / a.block_heads, q_head = q_row - q_tok * a.block_heads;
+  auto load_q = [&](const Part& p) {   // (rows that hold nothing are 0)
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (q_row < 16 && q_tok < p.n_tok && q_head < p.n_heads)
+      v = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + ((int64_t)(p.tok0 + q_tok) * a.Hq + p.head0 + q_head) * HD + q_ch * 8);
+    return v;
+  };
   int n_cuts = 0, e = 0;   // ring entries taken so far
   Part p;
-  for (int k = 0; take_part(c.gen + C::OFF_PART, c.bars + 8u * C::PARTFULL, c.bars + 8u * C::PARTFREE, k, c.abort_flag, p); ++k) {
-    // ---- Q to shared memory (128-byte lines of 64 columns, 16-byte chunk i of row r at i ^ (r % 8)); rows that hold nothing are 0
-    for (int i = t; i < MT * 16 * HD / 8; i += 32 * WARPS) {
-      const int r = i / (HD / 8), ch = i % (HD / 8), tok = r / a.block_heads, head = r - tok * a.block_heads;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (tok < p.n_tok && head < p.n_heads)
-        v = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + ((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + ch * 8);
-      st_shared_v4(out + (uint32_t)((ch >> 3) * (MT * 16 * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)), v.x, v.y, v.z, v.w);
-    }
+  bool more = take(0, p);
+  if (!more) return;
+  uint4 q_mine = load_q(p);
+  for (int k = 0; more; ++k) {
+    if (q_row < 16) st_shared_v4(out + (uint32_t)((q_ch >> 3) * (16 * 128) + q_row * 128 + (((q_ch & 7) ^ (q_row & 7)) << 4)), q_mine.x, q_mine.y, q_mine.z, q_mine.w);
     if (!c.template sync<C>()) return;
-    auto q_fragment = [&](int mt, int kk, uint32_t (&f)[4]) {
-      const int r = mt * 16 + (lane & 15), ch = (kk & 3) * 2 + (lane >> 4);
-      mma::ldsm_x4(out + (uint32_t)((kk >> 2) * (MT * 16 * 128) + r * 128 + ((ch ^ (r & 7)) << 4)), f[0], f[1], f[2], f[3]);
-    };
-    uint32_t qf[MT == 1 ? HD / 16 : 1][4];   // (two row tiles leave no registers for it: read again for every page)
-    if (MT == 1) {
+    uint32_t qf[HD / 16][4];
 #pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) q_fragment(0, kk, qf[MT == 1 ? kk : 0]);
+    for (int kk = 0; kk < HD / 16; ++kk) {
+      const int r = lane & 15, ch = (kk & 3) * 2 + (lane >> 4);
+      mma::ldsm_x4(out + (uint32_t)((kk >> 2) * (16 * 128) + r * 128 + ((ch ^ (r & 7)) << 4)), qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3]);
     }
-    // a lane's rows: lane / 4 and 8 more of each row tile; `seen`: keys that they see
-    int seen[MT][2];
-    float m[MT][2], l[MT][2], o[MT][HD / 8][4];
+    // a lane's rows: lane / 4 and 8 more; `seen`: keys that they see
+    int seen[2];
+    float m[2], l[2], o[HD / 8][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        seen[mt][h] = p.base + p.tok_in + (mt * 16 + h * 8 + (lane >> 2)) / a.block_heads + 1;
-        m[mt][h] = -INFINITY;
-        l[mt][h] = 0.f;
-      }
-#pragma unroll
-      for (int d = 0; d < HD / 8; ++d) o[mt][d][0] = o[mt][d][1] = o[mt][d][2] = o[mt][d][3] = 0.f;
+    for (int h = 0; h < 2; ++h) {
+      seen[h] = p.base + p.tok_in + (h * 8 + (lane >> 2)) / a.block_heads + 1;
+      m[h] = -INFINITY;
+      l[h] = 0.f;
     }
+#pragma unroll
+    for (int d = 0; d < HD / 8; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
     const int all_see = p.base + p.tok_in + 1;   // what every row sees
     for (int u = 0; u < p.n; ++u, ++e) {
       const int st = e % NSTAGE, key0 = (p.u0 + u) * BN + warp * EARN_PAGE_TOKENS;
@@ -106,73 +141,57 @@ __device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl
           fence_async_smem();   // (the stage's next copy comes behind these writes)
           __syncwarp();
         }
-        float s[MT][2][4];
+        float s[2][4], s1[2][4];   // (two chains of products each)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s[mt][i >> 2][i & 3] = 0.f;
+        for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = s1[i >> 2][i & 3] = 0.f;
         const int kr = warp * EARN_PAGE_TOKENS + ((lane >> 4) << 3) + (lane & 7);   // K: matrices (keys 0-7, k 0-7), (0-7, 8-15), (8-15, 0-7), ..
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
-          uint32_t b[4], f[4];
+          uint32_t b[4];
           const int ch = (kk & 3) * 2 + ((lane >> 3) & 1);
           mma::ldsm_x4(sk + (kk >> 2) * C::HALF + kr * 128 + ((ch ^ (kr & 7)) << 4), b[0], b[1], b[2], b[3]);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            if (MT > 1) q_fragment(mt, kk, f);
-            mma::mma_bf16(s[mt][0], MT == 1 ? qf[MT == 1 ? kk : 0] : f, b[0], b[1]);
-            mma::mma_bf16(s[mt][1], MT == 1 ? qf[MT == 1 ? kk : 0] : f, b[2], b[3]);
-          }
+          mma::mma_bf16((kk & 1) ? s1[0] : s[0], qf[kk], b[0], b[1]);
+          mma::mma_bf16((kk & 1) ? s1[1] : s[1], qf[kk], b[2], b[3]);
         }
-        uint32_t pf[MT][4];
-        bool raise = false;
-        float top[MT][2];
+        float top[2];
+        bool raise[2];
         const bool interior = key0 + EARN_PAGE_TOKENS <= all_see;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int h = 0; h < 2; ++h) {
+          float mx = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float mx = -INFINITY;
+          for (int n = 0; n < 2; ++n) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                float& x = s[mt][n][h * 2 + i];
-                x = interior || key0 + n * 8 + (lane & 3) * 2 + i < seen[mt][h] ? x * sl2 : -INFINITY;
-                mx = fmaxf(mx, x);
-              }
+            for (int i = 0; i < 2; ++i) {
+              float& x = s[n][h * 2 + i];
+              x = interior || key0 + n * 8 + (lane & 3) * 2 + i < seen[h] ? (x + s1[n][h * 2 + i]) * sl2 : -INFINITY;
+              mx = fmaxf(mx, x);
             }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            top[mt][h] = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            raise |= top[mt][h] > m[mt][h] + 8.f || (m[mt][h] == -INFINITY && top[mt][h] > -INFINITY);
           }
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          top[h] = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          raise[h] = top[h] > m[h] + 8.f || (m[h] == -INFINITY && top[h] > -INFINITY);
         }
         // A row's reference is raised when a logit exceeds it by more than 8 (no term exceeds 2^8): the first page as a rule.
-        if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const bool mine = top[mt][h] > m[mt][h] + 8.f || (m[mt][h] == -INFINITY && top[mt][h] > -INFINITY);
-              const float alpha = mine ? ex2(m[mt][h] - top[mt][h]) : 1.f;
-              if (mine) m[mt][h] = top[mt][h];
-              l[mt][h] *= alpha;
-#pragma unroll
-              for (int d = 0; d < HD / 8; ++d) { o[mt][d][h * 2] *= alpha; o[mt][d][h * 2 + 1] *= alpha; }
-            }
-          }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        if (__any_sync(0xffffffffu, raise[0] || raise[1])) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float ref = m[mt][h] == -INFINITY ? 0.f : m[mt][h];   // (nothing seen so far: every term is 2^-inf = 0)
+            const float alpha = raise[h] ? ex2(m[h] - top[h]) : 1.f;
+            if (raise[h]) m[h] = top[h];
+            l[h] *= alpha;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              const float p0 = ex2(s[mt][n][h * 2] - ref), p1 = ex2(s[mt][n][h * 2 + 1] - ref);
-              l[mt][h] += p0 + p1;
-              pf[mt][n * 2 + h] = pack_bf16(p0, p1);
-            }
+            for (int d = 0; d < HD / 8; ++d) { o[d][h * 2] *= alpha; o[d][h * 2 + 1] *= alpha; }
+          }
+        }
+        uint32_t pf[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float ref = m[h] == -INFINITY ? 0.f : m[h];   // (nothing seen so far: every term is 2^-inf = 0)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const float p0 = ex2(s[n][h * 2] - ref), p1 = ex2(s[n][h * 2 + 1] - ref);
+            l[h] += p0 + p1;
+            pf[n * 2 + h] = pack_bf16(p0, p1);
           }
         }
         const int vr = warp * EARN_PAGE_TOKENS + (((lane >> 3) & 1) << 3) + (lane & 7);   // V: matrices (keys 0-7, d 0-7), (8-15, 0-7), (0-7, 8-15), ..
@@ -181,97 +200,71 @@ __device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl
           uint32_t b[4];
           const int ch = (d & 3) * 2 + (lane >> 4);
           mma::ldsm_x4_t(sv + (d >> 2) * C::HALF + vr * 128 + ((ch ^ (vr & 7)) << 4), b[0], b[1], b[2], b[3]);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            mma::mma_bf16(o[mt][2 * d], pf[mt], b[0], b[1]);
-            mma::mma_bf16(o[mt][2 * d + 1], pf[mt], b[2], b[3]);
-          }
+          mma::mma_bf16(o[2 * d], pf, b[0], b[1]);
+          mma::mma_bf16(o[2 * d + 1], pf, b[2], b[3]);
         }
       }
       warp_arrive(c.bars + 8u * (C::EMPTY + st));
     }
-    // ---- the warps' sums and references meet, then their outputs, 16 rows x 32 columns at a time
+    // ---- the warps' sums and references meet, then their outputs; the next part's Q is on its way meanwhile
+    Part next;
+    more = take(k + 1, next);
+    if (more) q_mine = load_q(next);
     const bool whole = p.parts == 1;
     const int64_t slot = part_slot(p, 0);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        l[mt][h] += __shfl_xor_sync(0xffffffffu, l[mt][h], 1);
-        l[mt][h] += __shfl_xor_sync(0xffffffffu, l[mt][h], 2);
-        if ((lane & 3) == 0) ml[warp * kShortRows + mt * 16 + h * 8 + (lane >> 2)] = make_float2(m[mt][h], l[mt][h]);
-      }
+    for (int h = 0; h < 2; ++h) {
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      if ((lane & 3) == 0) ml[warp * 16 + h * 8 + (lane >> 2)] = make_float2(m[h], l[h]);
     }
     if (!c.template sync<C>()) return;   // (and Q has been read)
+    // the lane's rows' factors, 2^(reference - the warps' largest) over the denominator
+    float f[2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int used = p.n_tok * a.block_heads;
-      if (mt > 0 && used <= mt * 16) break;   // (the same for all threads)
-      float f[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) mx = fmaxf(mx, ml[i * kShortRows + mt * 16 + h * 8 + (lane >> 2)].x);
-        f[h] = mx == -INFINITY ? 0.f : ex2(m[mt][h] - mx);
-      }
-      // this thread's outputs: row t / 16 and columns 2 (t % 16) of each block
-      const int row = mt * 16 + t / 16, tok = row / a.block_heads, head = row - tok * a.block_heads;
-      const bool valid = tok < p.n_tok && head < p.n_heads;
+    for (int h = 0; h < 2; ++h) {
+      const int row = h * 8 + (lane >> 2);
       float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) mx = fmaxf(mx, ml[i * kShortRows + row].x);
+      for (int i = 0; i < WARPS; ++i) mx = fmaxf(mx, ml[i * 16 + row].x);
+      const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
       for (int i = 0; i < WARPS; ++i) {
-        const float2 v = ml[i * kShortRows + row];
-        sum += mx == -INFINITY ? 0.f : v.y * ex2(v.x - mx);
+        const float2 v = ml[i * 16 + row];
+        sum += v.y * ex2(v.x - ref);
       }
-      if (valid && t % 16 == 0) {
+      f[h] = ex2(m[h] - ref);
+      if (whole) f[h] *= sum == 0.f ? 0.f : __frcp_rn(sum);
+      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+      if (warp == 0 && (lane & 3) == 0 && tok < p.n_tok && head < p.n_heads) {
         if (!whole) a.part_ml[slot * BM + row] = make_float2(mx, sum);
         else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + p.tok0 + tok] = chunk_lse<true>(mx, sum);
       }
-      const float inv = !whole ? 1.f : sum == 0.f ? 0.f : __frcp_rn(sum);
-#pragma unroll
-      for (int d0 = 0; d0 < HD / 32; ++d0) {
-        float2* box = reinterpret_cast<float2*>(c.gen + C::OFF_OUT) + warp * 256;   // [row][column pair], rows shifted by their number
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = h * 8 + (lane >> 2);
-            box[r * 16 + ((d * 4 + (lane & 3) + 4 * (r & 3)) & 15)] = make_float2(o[mt][d0 * 4 + d][h * 2] * f[h], o[mt][d0 * 4 + d][h * 2 + 1] * f[h]);
-          }
-        }
-        if (!c.template sync<C>()) return;
-        if (valid) {
-          float2 y = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int i = 0; i < WARPS; ++i) {
-            const float2 v = reinterpret_cast<float2*>(c.gen + C::OFF_OUT)[i * 256 + (t / 16) * 16 + ((t % 16 + 4 * ((t / 16) & 3)) & 15)];
-            y.x += v.x;
-            y.y += v.y;
-          }
-          const int col = d0 * 32 + (t % 16) * 2;
-          if (whole)
-            *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.o) + ((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + col) = pack_bf16(y.x * inv, y.y * inv);
-          else
-            *reinterpret_cast<float2*>(reinterpret_cast<float*>(a.part_o) + (slot * BM + row) * HD + col) = y;
-        }
-        if (!c.template sync<C>()) return;
-      }
     }
+    auto store = [&](int row, int col, float2 y) {
+      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+      if (tok >= p.n_tok || head >= p.n_heads) return;
+      if (whole)
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.o) + ((int64_t)(p.tok0 + tok) * a.Hq + p.head0 + head) * HD + col) = pack_bf16(y.x, y.y);
+      else
+        *reinterpret_cast<float2*>(reinterpret_cast<float*>(a.part_o) + (slot * BM + row) * HD + col) = y;
+    };
+    const int used = p.n_tok * a.block_heads;
+    const bool met = used <= 4 ? exchange<HD, 4>(c, o, f, store) : used <= 8 ? exchange<HD, 8>(c, o, f, store) : exchange<HD, 16>(c, o, f, store);
+    if (!met) return;
     if (!whole) {
       if (t == 0) cuts[n_cuts] = p;
       ++n_cuts;
     }
+    p = next;
   }
-  if (*c.abort_flag == 0 && n_cuts > 0)
-    join_cuts<HD, true>(a, cuts, n_cuts, item_tok, 0, t, flag, ml, [&]() { return c.template sync<C>(); });
+  if (*c.abort_flag == 0 && n_cuts > 0)   // (the ring's memory holds the weights: nothing is on its way any more)
+    join_cuts<HD, true>(a, cuts, n_cuts, a.sched.item_tok, 0, t, flag, reinterpret_cast<float*>(c.gen), [&]() { return c.template sync<C>(); });
 }
 
 template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
-chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2) {
+chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2, int most) {
   using C = Cfg<HD>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;    // swizzled tiles need 1024-byte alignment
@@ -299,7 +292,7 @@ chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   pdl_wait();
   pdl_launch_dependents();
   ChunkSched sched = a.sched;
-  ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ), 1, sched.item_tok);
+  ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ), 1, most);
   if (w.pos >= w.end) return;   // (the same for all threads)
   fence_async_smem();           // (the copies that come next land where the shares' scratch was)
   __syncthreads();
@@ -333,8 +326,7 @@ chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
   } else {
     Consumer c{gen, base, bars, abort_flag, 0};
-    if (w.longest * a.block_heads <= 16) consume<HD, 1>(a, c, sl2, sched.item_tok);
-    else consume<HD, 2>(a, c, sl2, sched.item_tok);
+    consume<HD>(a, c, sl2);
   }
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(a.status, (int32_t)EARN_ERR_TIMEOUT);
@@ -347,11 +339,14 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
   if (!tcmap::make_map(&mk, a.cache.k, a.Hkv, rows, EARN_PAGE_TOKENS, HD) || !tcmap::make_map(&mv, a.cache.v, a.Hkv, rows, EARN_PAGE_TOKENS, HD))
     return cudaErrorInvalidValue;
   ChunkArgs s = a;
-  s.sched.item_tok = chunk_short_tokens(a);
+  s.blocks = (a.g + 15) / 16;   // head blocks of at most 16 heads
+  s.block_heads = (a.g + s.blocks - 1) / s.blocks;
+  s.sched.heads = a.Hkv * s.blocks;
+  s.sched.item_tok = 16 / s.block_heads;
   s.sched.min_share = 1;
   cudaError_t e = ensure_dynamic_smem<chunk_short_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
   if (e == cudaSuccess)
-    e = launch_pdl(chunk_short_kernel<HD>, dim3(s.sched.grid), dim3(THREADS), Cfg<HD>::SMEM_BYTES, st, mk, mv, s, a.scale * kLog2e);
+    e = launch_pdl(chunk_short_kernel<HD>, dim3(s.sched.grid), dim3(THREADS), Cfg<HD>::SMEM_BYTES, st, mk, mv, s, a.scale * kLog2e, chunk_short_tokens(a));
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -11,7 +11,11 @@ namespace {
 
 constexpr int KT = 64, THREADS = 256;
 
-template <int D, int RT> constexpr int smem_floats() { return RT * D + 2 * KT * D + RT * KT; }
+constexpr int MAX_GRID = 320;   // CTAs, which is how many parts an item can have: the join wants a number per part and row
+template <int D, int RT> constexpr int smem_floats() {
+  constexpr int tiles = RT * D + 2 * KT * D + RT * KT;
+  return tiles > MAX_GRID * RT ? tiles : MAX_GRID * RT;
+}
 
 template <typename T, int D, int RT>
 __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
@@ -23,7 +27,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   float* Ps = Vs + KT * D;
   __shared__ int4 scratch[48];
   __shared__ int last_part;
-  __shared__ float2 weights[RT];
+
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
   ChunkSched s = a.sched;
   pdl_launch_dependents();
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
         __threadfence();
       }
       __syncthreads();
-      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads, weights, [] { __syncthreads(); return true; });
+      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads, Qs, [] { __syncthreads(); return true; });   // (in the tiles' memory)
     }
     w.pos += stop - w.off;
     if (stop == units) chunk_next(s, w, q);
@@ -197,7 +201,7 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int dtype, int n_tokens, int max_len) {
+ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, int n_tokens, int max_len) {
   ChunkPlan p{};
   const bool tc = dtype == EARN_BF16;
   p.rows = tc ? 128 : 64;
@@ -211,7 +215,7 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int d
   // no more CTAs than there can be units
   const int64_t items = (int64_t)n_tokens / (p.tile_tok * p.tiles) + std::min(n_seq, n_tokens);
   const int64_t units = items * n_kv_heads * p.blocks * ((max_len + p.keys - 1) / p.keys);
-  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(sm_count() * (tc ? 1 : D == 64 ? 3 : 2), std::max<int64_t>(units, 1));
+  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(tc ? sm_count() : std::min(2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
   return p;
 }
 

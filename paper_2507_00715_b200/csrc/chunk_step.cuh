@@ -50,14 +50,14 @@ struct ChunkArgs {
 struct ChunkPlan {
   int rows, tiles, keys, block_heads, blocks, tile_tok, grid, min_share;
 };
-ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int D, int dtype, int n_tokens, int max_len);
+ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, int n_tokens, int max_len);
 cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st);                      // fp32
 // bf16: a call whose sequences have at most chunk_short_tokens() new tokens each (0: none such) is the first kernel's, any other
 // the second's.  The lengths are on the device, so both are launched, unless n_tokens tells, and one of them finds nothing to do.
 cudaError_t launch_chunk_short(const ChunkArgs& a, cudaStream_t st);
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);
 constexpr int kShortRows = 32;   // rows (token, query head of a kv head)
-inline int chunk_short_tokens(const ChunkArgs& a) { return a.blocks == 1 ? kShortRows / a.g : 0; }
+inline int chunk_short_tokens(const ChunkArgs& a) { return kShortRows / a.g; }
 
 // Softmax denominator of a row, natural log: once per row, so the logarithm is taken in 64 bits (the fast 32-bit one is off by
 // a few 1e-7, which is all of what fp32 callers see).  A row that sees nothing: -inf.
@@ -68,62 +68,75 @@ __device__ __forceinline__ float chunk_lse(float ref, float sum) {
 }
 
 // Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows, by `threads` threads of
-// which this is number t: first a row's reference and denominator (into `rows`, shared memory for ROWS pairs), then four columns
-// of a row at a time.  The parts are added in their order along the keys, so the result does not depend on which of them came
-// last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else [D / 4][rows][4].  sync():
-// barrier of the threads, false if it gave up.
+// which this is number t (whole warps): first every part's weight in a row (2^(its reference - the largest) over the row's
+// denominator, into `weights`, shared memory for used rows x parts numbers), a thread per row or, for many parts, a warp; then
+// four columns of a row at a time.  The parts are added in their order along the keys, so the result does not depend on which
+// of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else
+// [D / 4][rows][4].  sync(): barrier of the threads, false if it gave up.
 template <typename T, int D, int ROWS, bool LOG2, bool ROW_MAJOR, class Sync>
 __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t, int threads,
-                                           int tok0, int n_tok, int head0, int n_heads, float2* rows, Sync sync) {
+                                           int tok0, int n_tok, int head0, int n_heads, float* weights, Sync sync) {
   constexpr int C4 = D / 4;
   const int used = n_tok * a.block_heads, n = parts.parts;   // rows of the tile that hold a token
   auto slot = [&](int p) { return (int64_t)(2 * (parts.first + p) + (p == 0 ? 1 : 0)) * tiles + x; };
-  auto weight = [&](float from, float ref) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
-  for (int row = t; row < used; row += threads) {
+  auto power = [&](float from, float ref) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
+  const bool by_warp = n > 4;
+  const int lane = t & 31, lanes = by_warp ? 32 : 1;
+  for (int row = by_warp ? t >> 5 : t; row < used; row += by_warp ? threads >> 5 : threads) {
     const int tok = row / a.block_heads, head = row - tok * a.block_heads;
-    if (head >= n_heads) { rows[row] = make_float2(0.f, -1.f); continue; }
+    if (head >= n_heads) continue;
     float m = -INFINITY, l = 0.f;
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) m = fmaxf(m, __ldcg(a.part_ml + slot(p) * ROWS + row).x);
+    for (int p = by_warp ? lane : 0; p < n; p += lanes) m = fmaxf(m, __ldcg(a.part_ml + slot(p) * ROWS + row).x);
+    if (by_warp) {
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    }
     const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen: every weight is 2^-inf = 0)
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) {
+    for (int p = by_warp ? lane : 0; p < n; p += lanes) {
       const float2 ml = __ldcg(a.part_ml + slot(p) * ROWS + row);
-      l += ml.y * weight(ml.x, ref);
+      l += ml.y * power(ml.x, ref);
     }
-    rows[row] = make_float2(ref, l == 0.f ? 0.f : __frcp_rn(l));
-    if (a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+    if (by_warp) {
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    }
+    const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+#pragma unroll 4
+    for (int p = by_warp ? lane : 0; p < n; p += lanes) weights[p * used + row] = power(__ldcg(a.part_ml + slot(p) * ROWS + row).x, ref) * inv;
+    if ((!by_warp || lane == 0) && a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
   }
   if (!sync()) return;
-  constexpr int BATCH = 4;   // elements of a thread, or parts, in flight
+  constexpr int BATCH = 2;   // elements of a thread in flight, four parts of each
   const int all = ROW_MAJOR ? used * C4 : ROWS * C4;
   for (int i0 = t; i0 < all; i0 += BATCH * threads) {
     float4 acc[BATCH];
-    float2 of[BATCH];
+    int at[BATCH], row[BATCH];   // element within a part; -1: none
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
-      const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS;
+      const int i = i0 + k * threads;
+      row[k] = ROW_MAJOR ? i / C4 : i % ROWS;
+      at[k] = i < all && row[k] < used ? i : -1;
       acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      of[k] = i < all && row < used ? rows[row] : make_float2(0.f, -1.f);
     }
 #pragma unroll 4
     for (int p = 0; p < n; ++p) {
-      const int64_t from = slot(p);
+      const float4* from = a.part_o + slot(p) * ROWS * C4;
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS, c4 = ROW_MAJOR ? i % C4 : i / ROWS;
-        if (of[k].y < 0.f) continue;
-        const float w = weight(__ldcg(a.part_ml + from * ROWS + row).x, of[k].x);
-        const float4 v = __ldcg(a.part_o + (ROW_MAJOR ? (from * ROWS + row) * C4 + c4 : (from * C4 + c4) * ROWS + row));
+        if (at[k] < 0) continue;
+        const float w = weights[p * used + row[k]];
+        const float4 v = __ldcg(from + at[k]);   // (either layout: the element's number is its place)
         acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
       }
     }
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
-      const int i = i0 + k * threads, row = ROW_MAJOR ? i / C4 : i % ROWS, c4 = ROW_MAJOR ? i % C4 : i / ROWS;
-      if (of[k].y < 0.f) continue;
-      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
-      const float y[4] = {acc[k].x * of[k].y, acc[k].y * of[k].y, acc[k].z * of[k].y, acc[k].w * of[k].y};
+      if (at[k] < 0) continue;
+      const int tok = row[k] / a.block_heads, head = row[k] - tok * a.block_heads, c4 = ROW_MAJOR ? at[k] % C4 : at[k] / ROWS;
+      if (head >= n_heads) continue;
+      const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
       Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D + c4 * 4, y);
     }
   }

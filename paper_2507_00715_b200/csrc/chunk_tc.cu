@@ -666,12 +666,13 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     }
     // ---- items that are cut: both warpgroups have written their columns of the parts
-    if (ok && *abort_flag == 0 && n_cuts > 0) {
+    warp_arrive(bar(C::DONE));
+    if (ok && n_cuts > 0 && wait(C::DONE, 1)) {   // (the other stream is through as well: the join's weights go over Q and the ring)
       auto sync = [&]() {
         warp_arrive(bar(C::SUMS + x));
         return wait(C::SUMS + x, n.sum++);
       };
-      join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, reinterpret_cast<float2*>(gen + C::OFF_SUM + x * 1024), sync);
+      join_cuts<HD, false>(a, cuts, n_cuts, ta.tile_tok, x, b * 128 + row, last_part + 2 * x, reinterpret_cast<float*>(gen + x * (128 * 160 * 4)), sync);
     }
   }
 

@@ -278,7 +278,7 @@ struct ChunkLayout {
 };
 static ChunkLayout chunk_layout(const earn_model_t* m, int32_t n_seq, int32_t n_tokens, const earn_paged_cache_t* c) {
   ChunkLayout l{};
-  l.plan = plan_chunk_attn(n_seq, m->n_q_heads, m->n_kv_heads, m->head_dim, m->dtype, n_tokens, c->max_len);
+  l.plan = plan_chunk_attn(n_seq, m->n_q_heads, m->n_kv_heads, m->dtype, n_tokens, c->max_len);
   const size_t tiles = (size_t)l.plan.grid * l.plan.tiles, rows = 2 * tiles * l.plan.rows;
   l.tickets = kStatusBytes;
   l.part_ml = l.tickets + round_up(tiles * 4, 256);
