@@ -212,9 +212,10 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   p.blocks = (g + p.rows - 1) / p.rows;
   p.block_heads = (g + p.blocks - 1) / p.blocks;
   p.tile_tok = p.rows / p.block_heads;
-  // no more CTAs than there can be units
-  const int64_t items = (int64_t)n_tokens / (p.tile_tok * p.tiles) + std::min(n_seq, n_tokens);
-  const int64_t units = items * n_kv_heads * p.blocks * ((max_len + p.keys - 1) / p.keys);
+  // no more CTAs than there can be units (bf16: of the kernel for few tokens, whose items are the smaller ones)
+  const int heads = tc ? std::min(p.block_heads, 16) : p.block_heads, tokens = tc ? 16 / heads : p.tile_tok;
+  const int64_t items = (int64_t)n_tokens / tokens + std::min(n_seq, n_tokens);
+  const int64_t units = items * n_kv_heads * ((g + heads - 1) / heads) * ((max_len + p.keys - 1) / p.keys);
   p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(tc ? sm_count() : std::min(2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
   return p;
 }
