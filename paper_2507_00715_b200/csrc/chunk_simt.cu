@@ -1,7 +1,9 @@
 // Causal attention of every sequence's new tokens over its paged list, on the CUDA cores.
 //
-// A CTA walks its share of the work (chunk_sched.cuh) item by item: 64 rows (token, head) against tiles of 64 keys, logits in
-// registers (4 x 4 a thread), a running maximum and sum per row, probabilities through shared memory into the product with V.
+// fp32: products on the CUDA cores.  A CTA walks its share of the work (chunk_sched.cuh) item by item: 64 rows (token, head; 32 or
+// 16 where there is less work than CTAs, or fewer rows in a sequence) against tiles of 64 keys, logits in registers (4 x 4 a
+// thread), a running maximum and sum per row, probabilities through shared memory into the product with V.  Bound by the FMA
+// pipes (2 x 1024 new tokens over 2000 rows, 12/2 heads: 30 TFLOP/s, half of what they can); few rows by shared memory reads.
 #include <algorithm>
 
 #include "chunk_step.cuh"
@@ -190,13 +192,17 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   }
 }
 
-template <int D>
+template <int D, int RT>
 cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
-  constexpr int RT = 64, bytes = smem_floats<D, RT>() * 4;
+  constexpr int bytes = smem_floats<D, RT>() * 4;
   cudaError_t e = ensure_dynamic_smem<chunk_simt_kernel<float, D, RT>>(bytes);
   if (e == cudaSuccess) e = launch_pdl(chunk_simt_kernel<float, D, RT>, dim3(a.sched.grid), dim3(THREADS), bytes, st, a);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <int D>
+cudaError_t launch_rows(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st) {
+  return p.rows == 64 ? launch<D, 64>(a, st) : p.rows == 32 ? launch<D, 32>(a, st) : launch<D, 16>(a, st);
 }
 
 }  // namespace
@@ -209,6 +215,13 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   p.keys = tc ? 128 : KT;
   p.min_share = tc ? 2 : 1;
   const int g = n_q_heads / n_kv_heads;
+  if (!tc) {
+    // the largest row tile that is not twice the rows of an average sequence and leaves two units for every CTA (2 prompts of
+    // 90-156 new tokens, 4 heads: 31 us with 64 rows, 19 with 16; 16 single tokens over 2000 rows: 93 and 62 us)
+    const int64_t rows = std::max<int64_t>((int64_t)n_tokens * g / std::max(std::min(n_seq, n_tokens), 1), 1);
+    auto work = [&](int r) { return (rows + r - 1) / r * std::min(n_seq, n_tokens) * n_kv_heads * ((max_len + KT - 1) / KT); };
+    while (p.rows > 16 && (p.rows >= 2 * rows || work(p.rows) < 4 * sm_count())) p.rows /= 2;
+  }
   p.blocks = (g + p.rows - 1) / p.rows;
   p.block_heads = (g + p.blocks - 1) / p.blocks;
   p.tile_tok = p.rows / p.block_heads;
@@ -220,6 +233,8 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   return p;
 }
 
-cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st) { return a.D == 64 ? launch<64>(a, st) : launch<128>(a, st); }
+cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st) {
+  return a.D == 64 ? launch_rows<64>(a, p, st) : launch_rows<128>(a, p, st);
+}
 
 }  // namespace earn

@@ -51,7 +51,7 @@ struct ChunkPlan {
   int rows, tiles, keys, block_heads, blocks, tile_tok, grid, min_share;
 };
 ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, int n_tokens, int max_len);
-cudaError_t launch_chunk_simt(const ChunkArgs& a, cudaStream_t st);                      // fp32
+cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);   // fp32
 // bf16: a call whose sequences have at most chunk_short_tokens() new tokens each (0: none such) is the first kernel's, any other
 // the second's.  The lengths are on the device, so both are launched, unless n_tokens tells, and one of them finds nothing to do.
 cudaError_t launch_chunk_short(const ChunkArgs& a, cudaStream_t st);

@@ -917,7 +917,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
     if (few > 0) e = launch_chunk_short(a, (cudaStream_t)stream);
     if (e == cudaSuccess && n_tokens > few) e = launch_chunk_tc(a, l.plan, (cudaStream_t)stream);
   } else {
-    e = launch_chunk_simt(a, (cudaStream_t)stream);
+    e = launch_chunk_simt(a, l.plan, (cudaStream_t)stream);
   }
   return e == cudaSuccess ? EARN_OK : EARN_ERR_CUDA;
 }

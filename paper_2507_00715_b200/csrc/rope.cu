@@ -13,7 +13,7 @@
 namespace earn {
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, MAX_TOKENS = 8;
 
 enum Form { HALF, INTERLEAVED, STAGED };   // STAGED: half layout whose second half does not start on a 16-byte vector
 
@@ -63,115 +63,140 @@ __device__ __forceinline__ Row row_of(const RopeArgs& a, int tok, int h, int slo
   return r;
 }
 
-template <typename T, int D, int FORM, int TOKENS>
-__global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, int head_from, int per_block) {
+// A block takes `tokens` tokens and `per_block` of their heads, as one list of units.  A thread's first two units are on their
+// way while the angles are worked out.
+template <typename T, int D, int FORM>
+__global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, int head_from, int per_block, int tokens) {
   constexpr int N = Vec<T>::N, HEAD_BYTES = D * (int)sizeof(T);
   constexpr int UNITS = FORM == HALF ? D / (2 * N) : D / N;   // HALF: a unit is two vectors, a pair's halves or two that are copied
-  __shared__ float2 cs[TOKENS][D / 2];
-  __shared__ int place[TOKENS][2];   // position, slot
-  extern __shared__ uint4 rows[];    // STAGED: the rows of the token
-  const int t = threadIdx.x, tok0 = blockIdx.x * TOKENS, half = a.rot / 2;
+  constexpr int VECS = FORM == HALF ? 2 : 1, AHEAD = 2;
+  __shared__ float2 cs[MAX_TOKENS][D / 2];
+  __shared__ int place[MAX_TOKENS][2];   // position, slot
+  extern __shared__ uint4 rows[];        // STAGED: the rows
+  const int t = threadIdx.x, tok0 = blockIdx.x * tokens, half = a.rot / 2;
   head_from += (int)blockIdx.y * per_block;   // this block's heads
   heads = min(per_block, heads - (int)blockIdx.y * per_block);
+  tokens = min(tokens, a.n_tokens - tok0);
+  const int units = heads * UNITS, all = tokens * units, turned = half / N;
   pdl_launch_dependents();
   pdl_wait();
-  if (t < TOKENS) {
-    place[t][0] = tok0 + t < a.n_tokens ? a.positions[tok0 + t] : -1;
-    place[t][1] = tok0 + t < a.n_tokens && a.slots != nullptr ? a.slots[tok0 + t] : -1;
+  if (t < tokens) {
+    place[t][0] = a.positions[tok0 + t];
+    place[t][1] = a.slots != nullptr ? a.slots[tok0 + t] : -1;
   }
-  for (int i = t; i < TOKENS * half; i += THREADS) {
+  // unit i of the block: its token, head, number; HALF: pairs' units first (vectors u and u + half / N), then the copied ones, two
+  // by two behind the turned share
+  auto load = [&](int i, uint4 (&w)[VECS]) {
+    const int k = tokens == 1 ? 0 : i / units, r = i - k * units, u = r % UNITS;
+    const uint4* src = reinterpret_cast<const uint4*>(row_of(a, tok0 + k, head_from + r / UNITS, -1, HEAD_BYTES).src);
+    if constexpr (FORM == HALF) {
+      w[0] = src[u < turned ? u : 2 * u];
+      w[1] = src[u < turned ? u + turned : 2 * u + 1];
+    } else {
+      w[0] = src[u];
+    }
+  };
+  uint4 ahead[AHEAD][VECS];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n)
+    if (t + n * THREADS < all) load(t + n * THREADS, ahead[n]);
+  for (int i = t; i < tokens * half; i += THREADS) {
     const int k = i / half, p = i - k * half;
-    const int pos = tok0 + k < a.n_tokens ? a.positions[tok0 + k] : -1;
-    const double turns = (double)pos * a.freq[p] * 0.15915494309189533577;   // 1 / (2 pi)
+    const double turns = (double)a.positions[tok0 + k] * a.freq[p] * 0.15915494309189533577, rest = turns - rint(turns);   // 1 / (2 pi)
     float sn, cn;
-    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cn);
-    cs[k][p] = make_float2(a.amplitude * cn, a.sign * a.amplitude * sn);
+    const float by = (float)(2.0 * rest), lost = (float)(2.0 * rest - (double)by) * 3.14159265f;
+    sincospif(by, &sn, &cn);
+    // (what the angle lost to 32 bits is put back to first order)
+    cs[k][p] = make_float2(a.amplitude * fmaf(-lost, sn, cn), a.sign * a.amplitude * fmaf(lost, cn, sn));
+  }
+  if constexpr (FORM == STAGED) {
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n)
+      if (t + n * THREADS < all) rows[t + n * THREADS] = ahead[n][0];
+    for (int i = t + AHEAD * THREADS; i < all; i += THREADS) load(i, *reinterpret_cast<uint4(*)[VECS]>(&rows[i]));
   }
   __syncthreads();
-  const int all = heads * UNITS;
-#pragma unroll 1
-  for (int k = 0; k < TOKENS; ++k) {
-    if (place[k][0] < 0) continue;   // a token that takes no part (the whole block skips it)
-    const int tok = tok0 + k, slot = place[k][1];
-    if constexpr (FORM == STAGED) {
-      for (int i = t; i < all; i += THREADS) rows[i] = reinterpret_cast<const uint4*>(row_of(a, tok, head_from + i / UNITS, slot, HEAD_BYTES).src)[i % UNITS];
-      __syncthreads();
-    }
-#pragma unroll 2
-    for (int i = t; i < all; i += THREADS) {
-      const int h = i / UNITS, u = i % UNITS;
-      const Row r = row_of(a, tok, head_from + h, slot, HEAD_BYTES);
-      if (r.dst == nullptr) continue;
-      if constexpr (FORM == HALF) {
-        // pairs' units first: vectors u and u + half / N; then the copied ones, two by two behind the turned share
-        const int turned = half / N, va = u < turned ? u : 2 * u, vb = u < turned ? u + turned : 2 * u + 1;
-        uint4 wa = reinterpret_cast<const uint4*>(r.src)[va], wb = reinterpret_cast<const uint4*>(r.src)[vb];
-        if (r.turn && u < turned) {
-          float x[N], y[N];
-          unpack<T>(wa, x);
-          unpack<T>(wb, y);
+  auto finish = [&](int i, uint4 (&w)[VECS]) {
+    const int k = tokens == 1 ? 0 : i / units, r = i - k * units, h = r / UNITS, u = r % UNITS;
+    const Row to = row_of(a, tok0 + k, head_from + h, place[k][1], HEAD_BYTES);
+    if (place[k][0] < 0 || to.dst == nullptr) return;   // a token that takes no part, a row without a slot
+    if constexpr (FORM == HALF) {
+      if (to.turn && u < turned) {
+        float x[N], y[N];
+        unpack<T>(w[0], x);
+        unpack<T>(w[1], y);
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const float2 c = cs[k][u * N + e];
-            const float p = x[e] * c.x - y[e] * c.y, q = x[e] * c.y + y[e] * c.x;
-            x[e] = p;
-            y[e] = q;
-          }
-          wa = packed<T>(x);
-          wb = packed<T>(y);
+        for (int e = 0; e < N; ++e) {
+          const float2 c = cs[k][u * N + e];
+          const float p = x[e] * c.x - y[e] * c.y, q = x[e] * c.y + y[e] * c.x;
+          x[e] = p;
+          y[e] = q;
         }
-        reinterpret_cast<uint4*>(r.dst)[va] = wa;
-        reinterpret_cast<uint4*>(r.dst)[vb] = wb;
-      } else if constexpr (FORM == INTERLEAVED) {
-        uint4 w = reinterpret_cast<const uint4*>(r.src)[u];
-        if (r.turn && u * N < a.rot) {
-          float x[N];
-          unpack<T>(w, x);
-#pragma unroll
-          for (int e = 0; e < N; e += 2) {
-            if (u * N + e < a.rot) {
-              const float2 c = cs[k][(u * N + e) / 2];
-              const float p = x[e] * c.x - x[e + 1] * c.y, q = x[e] * c.y + x[e + 1] * c.x;
-              x[e] = p;
-              x[e + 1] = q;
-            }
-          }
-          w = packed<T>(x);
-        }
-        reinterpret_cast<uint4*>(r.dst)[u] = w;
-      } else {
-        uint4 w = rows[i];
-        if (r.turn && u * N < a.rot) {
-          const T* row = reinterpret_cast<const T*>(rows + h * UNITS);
-          float x[N];
-          unpack<T>(w, x);
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const int at = u * N + e;
-            if (at < half) {
-              const float2 c = cs[k][at];
-              x[e] = x[e] * c.x - (float)row[at + half] * c.y;
-            } else if (at < a.rot) {
-              const float2 c = cs[k][at - half];
-              x[e] = (float)row[at - half] * c.y + x[e] * c.x;
-            }
-          }
-          w = packed<T>(x);
-        }
-        reinterpret_cast<uint4*>(r.dst)[u] = w;
+        w[0] = packed<T>(x);
+        w[1] = packed<T>(y);
       }
+      reinterpret_cast<uint4*>(to.dst)[u < turned ? u : 2 * u] = w[0];
+      reinterpret_cast<uint4*>(to.dst)[u < turned ? u + turned : 2 * u + 1] = w[1];
+    } else if constexpr (FORM == INTERLEAVED) {
+      if (to.turn && u * N < a.rot) {
+        float x[N];
+        unpack<T>(w[0], x);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          if (u * N + e < a.rot) {
+            const float2 c = cs[k][(u * N + e) / 2];
+            const float p = x[e] * c.x - x[e + 1] * c.y, q = x[e] * c.y + x[e + 1] * c.x;
+            x[e] = p;
+            x[e + 1] = q;
+          }
+        }
+        w[0] = packed<T>(x);
+      }
+      reinterpret_cast<uint4*>(to.dst)[u] = w[0];
+    } else {
+      w[0] = rows[i];
+      if (to.turn && u * N < a.rot) {
+        const T* row = reinterpret_cast<const T*>(rows + i - u);
+        float x[N];
+        unpack<T>(w[0], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int at = u * N + e;
+          if (at < half) {
+            const float2 c = cs[k][at];
+            x[e] = x[e] * c.x - (float)row[at + half] * c.y;
+          } else if (at < a.rot) {
+            const float2 c = cs[k][at - half];
+            x[e] = (float)row[at - half] * c.y + x[e] * c.x;
+          }
+        }
+        w[0] = packed<T>(x);
+      }
+      reinterpret_cast<uint4*>(to.dst)[u] = w[0];
     }
-    if constexpr (FORM == STAGED) __syncthreads();
+  };
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n)
+    if (t + n * THREADS < all) finish(t + n * THREADS, ahead[n]);
+#pragma unroll 2
+  for (int i = t + AHEAD * THREADS; i < all; i += THREADS) {
+    uint4 w[VECS];
+    if (FORM != STAGED) load(i, w);
+    finish(i, w);
   }
 }
 
-template <typename T, int D, int FORM, int TOKENS>
+template <typename T, int D, int FORM>
 cudaError_t launch_form(const RopeArgs& a, int heads, int head_from, cudaStream_t st) {
-  // a block takes up to 64 heads of a token (STAGED keeps their rows in shared memory: 32 KB at most)
+  // Up to 64 heads of a token (STAGED keeps the rows in shared memory: 32 KB at most), and so many tokens that every thread has
+  // two units, as long as there are eight blocks for every SM all the same.
+  constexpr int UNITS = FORM == HALF ? D / (2 * Vec<T>::N) : D / Vec<T>::N;
   const int per_block = std::min(heads, 64);
-  const int bytes = FORM == STAGED ? per_block * D * (int)sizeof(T) : 0;
-  const dim3 grid((a.n_tokens + TOKENS - 1) / TOKENS, (heads + per_block - 1) / per_block);
-  const cudaError_t e = launch_pdl(rope_kernel<T, D, FORM, TOKENS>, grid, dim3(THREADS), bytes, st, a, heads, head_from, per_block);
+  int tokens = std::max(1, std::min(MAX_TOKENS, 2 * THREADS / (per_block * UNITS)));
+  while (tokens > 1 && a.n_tokens / tokens < 8 * sm_count()) tokens /= 2;
+  const int bytes = FORM == STAGED ? tokens * per_block * D * (int)sizeof(T) : 0;
+  const dim3 grid((a.n_tokens + tokens - 1) / tokens, (heads + per_block - 1) / per_block);
+  const cudaError_t e = launch_pdl(rope_kernel<T, D, FORM>, grid, dim3(THREADS), bytes, st, a, heads, head_from, per_block, tokens);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -180,9 +205,9 @@ template <typename T, int D>
 cudaError_t launch_type(const RopeArgs& a, cudaStream_t st) {
   const int head_from = a.q != nullptr ? 0 : a.Hq;
   const int heads = (a.q != nullptr ? a.Hq : 0) + (a.k != nullptr ? a.Hkv : 0) + (a.v != nullptr ? a.Hkv : 0);
-  if (a.interleaved) return launch_form<T, D, INTERLEAVED, 1>(a, heads, head_from, st);
-  if (a.rot / 2 % Vec<T>::N == 0) return launch_form<T, D, HALF, 1>(a, heads, head_from, st);
-  return launch_form<T, D, STAGED, 1>(a, heads, head_from, st);
+  if (a.interleaved) return launch_form<T, D, INTERLEAVED>(a, heads, head_from, st);
+  if (a.rot / 2 % Vec<T>::N == 0) return launch_form<T, D, HALF>(a, heads, head_from, st);
+  return launch_form<T, D, STAGED>(a, heads, head_from, st);
 }
 
 }  // namespace
