@@ -545,15 +545,20 @@ def _rows(t, what: str, dtype: torch.dtype, n: int, heads: int, d: int, device: 
     """Address and token stride (elements) of [>= n, heads, d] rows whose heads are dense."""
     if t is None:
         return None, 0
-    shape = t.shape
-    if len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != d:
-        raise ValueError(f"{what}: {tuple(shape)}, expected at least [{n}, {heads}, {d}]")
-    stride = t.stride()
-    if stride[2] != 1 or (heads > 1 and stride[1] != d) or (shape[0] > 1 and stride[0] < heads * d):
-        raise ValueError(f"{what}: strides {stride}, expected a token's heads one after the other")
+    try:
+        n0, n1, n2 = t.shape
+        s0, s1, s2 = t.stride()
+    except (AttributeError, ValueError):
+        raise ValueError(f"{what}: {tuple(t.shape) if isinstance(t, torch.Tensor) else type(t).__name__}, expected [{n}, {heads}, {d}]") from None
+    if n0 >= n and n1 == heads and n2 == d and s2 == 1 and s1 == d and s0 >= heads * d and t.dtype is dtype and t.get_device() == device:
+        return t.data_ptr(), s0
+    if n0 < n or n1 != heads or n2 != d:
+        raise ValueError(f"{what}: {tuple(t.shape)}, expected at least [{n}, {heads}, {d}]")
+    if s2 != 1 or (heads > 1 and s1 != d) or (n0 > 1 and s0 < heads * d):
+        raise ValueError(f"{what}: strides {t.stride()}, expected a token's heads one after the other")
     if t.dtype is not dtype or t.get_device() != device:
         raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {dtype} on the current CUDA device ({device})")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
+    return t.data_ptr(), s0 if n0 > 1 else heads * d
 
 
 def earn_rope(model: EarnModel, rope: EarnRope, n_tokens: int, positions, q, k, q_out, k_out, inverse: bool = False) -> None:

@@ -213,7 +213,10 @@ static cudaError_t launch(const PageTableArgs& a, cudaStream_t st) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-// 256 threads where they have the sequences in one pass: fewer warps to scan and to wait for
-cudaError_t launch_page_tables(const PageTableArgs& a, cudaStream_t st) { return a.n_seq <= 256 ? launch<256>(a, st) : launch<1024>(a, st); }
+// Few threads have fewer warps to scan and to wait for, and more CTAs share the tokens: 512 sequences of a mixed step take 10.6 us
+// with 512 threads, 10.5 with 256, 12.5 with 1024; 1000 of them 12.3, 13.7 and 13.9.
+cudaError_t launch_page_tables(const PageTableArgs& a, cudaStream_t st) {
+  return a.n_seq <= 256 ? launch<256>(a, st) : a.n_seq <= 1024 ? launch<512>(a, st) : launch<1024>(a, st);
+}
 
 }  // namespace earn

@@ -292,3 +292,69 @@ class BudgetedLayers:
         (after one of those the rows kept may be the wrong ones), and of the workspace of the pages."""
         status = self.session.device_status()
         return status if status != B.EARN_OK or not self.caches else B.earn_device_status(self.workspace)
+
+
+class PagedLayers:
+    """The full layers (``l < split_k``) of up to ``n_seq`` sequences whose rows come in steps: pieces of a prompt, the items a
+    history has gained, drafted tokens, single tokens, all in one batch; or go again (a rejected draft, a request that ends).
+
+    A step is ``begin_step(target)`` with the lengths the sequences are to have, then ``layer`` for every full layer with the
+    step's packed Q, K, V (unrotated; ``cu_new`` says where a sequence's tokens begin).  The pages come from one pool: a sequence
+    holds those of its rows.  Without frequencies Q and K are taken as rotated.  Nothing here waits for the device; ``refused``
+    does, and tells how many sequences the last step left as they were for want of pages or room.
+    """
+
+    def __init__(self, n_layers: int, split_k: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seq: int,
+                 n_pages: int, max_len: int, n_tokens: int, freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 amplitude: float = 1.0, softmax_scale: float = 0.0, device="cuda"):
+        self.device, self.dtype, self.n_seq, self.n_tokens = torch.device(device), dtype, n_seq, n_tokens
+        self.Hq, self.Hkv, self.D, self.split_k = n_q_heads, n_kv_heads, head_dim, split_k
+        self.model = B.make_model(n_layers, split_k, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        pages_per_seq = -(-max_len // B.PAGE_TOKENS)
+        self.block_table = torch.zeros(n_seq, pages_per_seq, **i32)
+        self.held, self.seq_len, self.cu_new = torch.zeros(n_seq, **i32), torch.zeros(n_seq, **i32), torch.zeros(n_seq + 1, **i32)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, **i32)   # (a stack: page 0 is taken first)
+        self.n_free, self.n_refused = torch.full((1,), n_pages, **i32), torch.zeros(1, **i32)
+        self.positions, self.slots = torch.full((n_tokens,), -1, **i32), torch.full((n_tokens,), -1, **i32)
+        self.pool = B.make_page_pool(self.block_table, self.held, self.free_pages, self.n_free)
+        self.step = B.make_step(self.cu_new, self.seq_len, self.positions, self.slots, self.n_refused)
+        self.freq = None if freq is None else freq.to(device=self.device, dtype=torch.float64).contiguous()
+        self.rope = B.make_rope(self.freq, interleaved, amplitude)
+        shape = (n_pages, B.PAGE_TOKENS, n_kv_heads, head_dim)
+        self.k_pages = [torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(split_k)]
+        self.v_pages = [torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(split_k)]
+        self.caches = [B.make_paged_cache(k, v, self.block_table, self.seq_len, max_len) for k, v in zip(self.k_pages, self.v_pages)]
+        self.q_turned = torch.empty(n_tokens, n_q_heads, head_dim, dtype=dtype, device=self.device)
+        need = B.earn_page_tables_workspace_bytes(n_seq)
+        self.table_workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        B.earn_workspace_init(self.table_workspace)
+        self.workspace = None
+        if self.caches:
+            need = B.earn_paged_chunk_workspace_bytes(self.model, n_seq, n_tokens, self.caches[0])
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            B.earn_workspace_init(self.workspace)
+
+    def begin_step(self, target: torch.Tensor) -> None:
+        """target: int32 device [n_seq], the lengths after the step (0: the sequence ends and its pages are free)."""
+        B.earn_page_tables(self.n_seq, target, self.pool, self.step, self.held, self.n_free, self.table_workspace)
+
+    def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None,
+              lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q [n_tokens, Hq, D], k, v [n_tokens, Hkv, D] of the step's new tokens (they may be parts of a projection's output) ->
+        O [n_tokens, Hq, D]; rows of padding tokens stay as they are."""
+        o = out if out is not None else torch.zeros_like(self.q_turned)
+        B.earn_rope_append(self.model, layer, self.rope, self.n_tokens, self.positions, self.slots, q, k, v, self.q_turned, self.caches[layer])
+        B.earn_paged_chunk_attn(self.model, self.n_seq, layer, self.n_tokens, self.cu_new, self.q_turned, self.caches[layer], o, lse,
+                                self.workspace)
+        return o
+
+    def refused(self) -> int:
+        return int(self.n_refused)
+
+    def kv_entries(self) -> int:
+        """KV entries per kv head that the sequences hold in all full layers."""
+        return int(self.held.sum()) * self.split_k
+
+    def device_status(self) -> int:
+        return B.EARN_OK if self.workspace is None else B.earn_device_status(self.workspace)

@@ -473,3 +473,44 @@ def test_a_run_of_steps(dtype, hq, hkv, d):
             assert (err <= weight * mag + EPS[dtype] * np.abs(ref) + 1e-30).all()
             assert (o[cu[-1]:] == 7).all()
     assert p.refused.item() == 0 and rng is not None
+
+
+@pytest.mark.parametrize("dtype,interleaved", [("bf16", False), ("f32", True)])
+def test_paged_layers_agree_with_the_session(dtype, interleaved):
+    """Prompts taken by PagedLayers in three uneven steps give the rows that a session's prefill of the whole prompts gives, and
+    one more token those of its decode; then every sequence ends and the pool is full again."""
+    from paper_2507_00715_b200.rope import frequencies
+    from paper_2507_00715_b200.session import EarnSession, PagedLayers
+    lens, hq, hkv, d, room = [200, 33, 129], 8, 2, 128, 256
+    f, amp = frequencies(d, scaling="ramp", factor=2.0, original=256)
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    ses = EarnSession(2, 1, hq, hkv, d, DT[dtype], cu, 0, 0, max_new=1)
+    lay = PagedLayers(2, 1, hq, hkv, d, DT[dtype], 3, 40, 256, room, f, interleaved, amp)
+    g = gen(11)
+    qkv = torch.randn(sum(lens) + 3, hq + 2 * hkv, d, generator=g, device="cuda").to(DT[dtype])   # (the last three rows: a token each)
+    pos = i32(np.concatenate([np.arange(n) for n in lens] + [lens]))
+    q, k = torch.empty(len(pos), hq, d, device="cuda", dtype=DT[dtype]), torch.empty(len(pos), hkv, d, device="cuda", dtype=DT[dtype])
+    B.earn_rope(lay.model, lay.rope, len(pos), pos, qkv[:, :hq], qkv[:, hq:hq + hkv], q, k)
+    v = qkv[:, hq + hkv:].contiguous()
+    n = int(cu[-1])
+    whole = ses.prefill_layer(0, q[:n], k[:n], v[:n])
+    last = ses.decode_layer(0, 1, q[n:], k[n:], v[n:])
+    tol = 2e-2 if dtype == "bf16" else 1e-5                # (the bounds of a single attention call on outputs of order one)
+    done = [0, 0, 0]
+    for target in ([70, 33, 1], [71, 33, 129], [200, 33, 129]):
+        lay.begin_step(i32(target))
+        rows = np.concatenate([np.arange(cu[b] + done[b], cu[b] + target[b]) for b in range(3)])
+        step = torch.full((room, hq + 2 * hkv, d), float("nan"), device="cuda", dtype=DT[dtype])
+        step[:len(rows)] = qkv[rows]
+        o = lay.layer(0, step[:, :hq], step[:, hq:hq + hkv], step[:, hq + hkv:])
+        assert lay.refused() == 0 and lay.device_status() == B.EARN_OK and lay.kv_entries() == sum(target)
+        assert (o[:len(rows)].float() - whole[rows].float()).abs().max() <= 2 * tol
+        assert (o[len(rows):] == 0).all()
+        done = target
+    lay.begin_step(i32([x + 1 for x in lens]))
+    step = torch.zeros(room, hq + 2 * hkv, d, device="cuda", dtype=DT[dtype])
+    step[:3] = qkv[n:]
+    o = lay.layer(0, step[:, :hq], step[:, hq:hq + hkv], step[:, hq + hkv:])
+    assert (o[:3].float() - last.float()).abs().max() <= 2 * tol
+    lay.begin_step(i32([0, 0, 0]))
+    assert int(lay.n_free) == 40 and sorted(lay.free_pages.tolist()) == list(range(40))
