@@ -550,7 +550,7 @@ def _rows(t, what: str, dtype: torch.dtype, n: int, heads: int, d: int, device: 
         s0, s1, s2 = t.stride()
     except (AttributeError, ValueError):
         raise ValueError(f"{what}: {tuple(t.shape) if isinstance(t, torch.Tensor) else type(t).__name__}, expected [{n}, {heads}, {d}]") from None
-    if n0 >= n and n1 == heads and n2 == d and s2 == 1 and s1 == d and s0 >= heads * d and t.dtype is dtype and t.get_device() == device:
+    if n0 >= n and n0 > 1 and n1 == heads and n2 == d and s2 == 1 and s1 == d and s0 >= heads * d and t.dtype is dtype and t.get_device() == device:
         return t.data_ptr(), s0
     if n0 < n or n1 != heads or n2 != d:
         raise ValueError(f"{what}: {tuple(t.shape)}, expected at least [{n}, {heads}, {d}]")
