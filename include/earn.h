@@ -414,7 +414,7 @@ typedef struct {
  * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
  * must not overlap it).  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
  * or above the new height hold nothing.
- * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter.
+ * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes may use it in turn.
  * Errors: n_seq < 0, n_tokens < 0, n_pages < 1, pages_per_seq < 1, NULL or misaligned arrays -> INVALID_ARG; n_seq > 16384,
  * row or slot numbers beyond 2^31 - 32 -> UNSUPPORTED; workspace -> WORKSPACE. */
 size_t earn_page_tables_workspace_bytes(int32_t n_seq);
@@ -467,9 +467,11 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  * are accumulated (earn_paged_decode_attn does that for a single token).
  * Logits, softmax and sums in fp32; with bf16 the probabilities are rounded to bf16 in front of the product with V only.
  * Lists are cut at places that depend on the lengths only, and joined in the order of the keys: equal calls, equal results.
- * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init.
+ * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init; calls of any shapes whose bytes it holds may
+ * use it in turn (not entry points of other kinds in between: those leave other things where this one's counters are).
  * Errors: layer outside [0, k), n_seq < 0, n_tokens < 0, a malformed cache, NULL or misaligned tensors -> INVALID_ARG;
- * n_seq > 65535, 16 * n_pages beyond 2^31 - 1 -> UNSUPPORTED; workspace -> WORKSPACE. */
+ * n_seq > 65535, 16 * n_pages beyond 2^31 - 1, more than 2^31 - 1 products of a row tile and a key tile (128 x 128; fp32: 64 x
+ * 64 or fewer rows) that n_tokens and max_len allow -> UNSUPPORTED; workspace -> WORKSPACE. */
 size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
                                         const earn_paged_cache_t* cache);
 earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, int32_t n_tokens,

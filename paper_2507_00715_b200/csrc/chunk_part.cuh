@@ -121,7 +121,7 @@ __device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, 
     parts.first = p.first;
     parts.parts = p.parts;
     if (!sync()) return;   // (the weights before have been read)
-    chunk_join<__nv_bfloat16, HD, BM, true, ROW_MAJOR>(a, parts, 2, x, t, 256, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, weights, sync);
+    chunk_join<__nv_bfloat16, HD, BM, 256, true, ROW_MAJOR>(a, parts, 2, x, t, p.tok0 + my_tok, min(tile_tok, p.n_tok - my_tok), p.head0, p.n_heads, weights, sync);
   }
 }
 

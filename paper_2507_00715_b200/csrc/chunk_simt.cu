@@ -13,6 +13,7 @@ namespace {
 
 constexpr int KT = 64, THREADS = 256;
 
+static_assert(2 * 320 <= kChunkTickets, "two row tiles a CTA");
 constexpr int MAX_GRID = 320;   // CTAs, which is how many parts an item can have: the join wants a number per part and row
 template <int D, int RT> constexpr int smem_floats() {
   constexpr int tiles = RT * D + 2 * KT * D + RT * KT;
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
         __threadfence();
       }
       __syncthreads();
-      if (last_part) chunk_join<T, D, RT, false, false>(a, parts, 1, 0, t, THREADS, tok0, n_tok, head0, n_heads, Qs, [] { __syncthreads(); return true; });   // (in the tiles' memory)
+      if (last_part) chunk_join<T, D, RT, THREADS, false, false>(a, parts, 1, 0, t, tok0, n_tok, head0, n_heads, Qs, [] { __syncthreads(); return true; });   // (in the tiles' memory)
     }
     w.pos += stop - w.off;
     if (stop == units) chunk_next(s, w, q);
@@ -229,7 +230,7 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   const int heads = tc ? std::min(p.block_heads, 16) : p.block_heads, tokens = tc ? 16 / heads : p.tile_tok;
   const int64_t items = (int64_t)n_tokens / tokens + std::min(n_seq, n_tokens);
   const int64_t units = items * n_kv_heads * ((g + heads - 1) / heads) * ((max_len + p.keys - 1) / p.keys);
-  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(tc ? sm_count() : std::min(2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
+  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(std::min(tc ? sm_count() : 2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
   return p;
 }
 

@@ -32,6 +32,8 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
 
+constexpr int kChunkTickets = 640;   // row tiles of all CTAs' items, at most
+
 struct ChunkArgs {
   const void* q;
   void* o;
@@ -40,7 +42,7 @@ struct ChunkArgs {
   ChunkSched sched;
   float4* part_o;              // [2 * grid][row tiles][D / 4][rows], or [rows][D / 4]
   float2* part_ml;             // [2 * grid][row tiles][rows]: reference of the exponentials, their sum
-  int32_t* tickets;            // [grid][row tiles], zero between calls
+  int32_t* tickets;            // [kChunkTickets >= grid * row tiles], zero between calls
   int32_t* status;
   int Hq, Hkv, D, dtype, g;
   int block_heads, blocks;     // query heads of a head block, head blocks of a kv head
@@ -67,14 +69,14 @@ __device__ __forceinline__ float chunk_lse(float ref, float sum) {
   return (float)((LOG2 ? (double)ref * 0.69314718055994530942 : (double)ref) + log((double)sum));
 }
 
-// Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows, by `threads` threads of
-// which this is number t (whole warps): first every part's weight in a row (2^(its reference - the largest) over the row's
+// Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows, by THREADS threads of
+// which this is number t: first every part's weight in a row (2^(its reference - the largest) over the row's
 // denominator, into `weights`, shared memory for used rows x parts numbers), a thread per row or, for many parts, a warp; then
 // four columns of a row at a time.  The parts are added in their order along the keys, so the result does not depend on which
 // of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else
 // [D / 4][rows][4].  sync(): barrier of the threads, false if it gave up.
-template <typename T, int D, int ROWS, bool LOG2, bool ROW_MAJOR, class Sync>
-__device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t, int threads,
+template <typename T, int D, int ROWS, int THREADS, bool LOG2, bool ROW_MAJOR, class Sync>
+__device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t,
                                            int tok0, int n_tok, int head0, int n_heads, float* weights, Sync sync) {
   constexpr int C4 = D / 4;
   const int used = n_tok * a.block_heads, n = parts.parts;   // rows of the tile that hold a token
@@ -82,7 +84,7 @@ __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts&
   auto power = [&](float from, float ref) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
   const bool by_warp = n > 4;
   const int lane = t & 31, lanes = by_warp ? 32 : 1;
-  for (int row = by_warp ? t >> 5 : t; row < used; row += by_warp ? threads >> 5 : threads) {
+  for (int row = by_warp ? t >> 5 : t; row < used; row += by_warp ? THREADS >> 5 : THREADS) {
     const int tok = row / a.block_heads, head = row - tok * a.block_heads;
     if (head >= n_heads) continue;
     float m = -INFINITY, l = 0.f;
@@ -108,36 +110,59 @@ __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts&
     if ((!by_warp || lane == 0) && a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
   }
   if (!sync()) return;
-  constexpr int BATCH = 2;   // elements of a thread in flight, four parts of each
-  const int all = ROW_MAJOR ? used * C4 : ROWS * C4;
-  for (int i0 = t; i0 < all; i0 += BATCH * threads) {
-    float4 acc[BATCH];
-    int at[BATCH], row[BATCH];   // element within a part; -1: none
+  if constexpr (!ROW_MAJOR) {
+    // a thread has consecutive columns of one row, neighbouring threads neighbouring rows
+    constexpr int PER = C4 * ROWS / THREADS, AHEAD = PER < 4 ? PER : 4;
+    const int row = t % ROWS, from4 = t / ROWS * PER, tok = row / a.block_heads, head = row - tok * a.block_heads;
+    if (row >= used || head >= n_heads) return;
+    T* out = reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D;
+#pragma unroll 1
+    for (int c = from4; c < from4 + PER; c += AHEAD) {
+      float4 acc[AHEAD];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      const int i = i0 + k * threads;
-      row[k] = ROW_MAJOR ? i / C4 : i % ROWS;
-      at[k] = i < all && row[k] < used ? i : -1;
-      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const float4* from = a.part_o + slot(p) * ROWS * C4;
+      for (int k = 0; k < AHEAD; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+      for (int p = 0; p < n; ++p) {
+        const float4* from = a.part_o + (slot(p) * C4 + c) * ROWS + row;
+        const float w = weights[p * used + row];
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k) {
-        if (at[k] < 0) continue;
-        const float w = weights[p * used + row[k]];
-        const float4 v = __ldcg(from + at[k]);   // (either layout: the element's number is its place)
-        acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
+        for (int k = 0; k < AHEAD; ++k) {
+          const float4 v = __ldcg(from + k * ROWS);
+          acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
+        Elem<T>::store4(out + (c + k) * 4, y);
       }
     }
+  } else {
+    constexpr int BATCH = 2;   // elements of a thread in flight, four parts of each
+    const int all = used * C4;
+    for (int i0 = t; i0 < all; i0 += BATCH * THREADS) {
+      float4 acc[BATCH];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k) {
-      if (at[k] < 0) continue;
-      const int tok = row[k] / a.block_heads, head = row[k] - tok * a.block_heads, c4 = ROW_MAJOR ? at[k] % C4 : at[k] / ROWS;
-      if (head >= n_heads) continue;
-      const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
-      Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D + c4 * 4, y);
+      for (int k = 0; k < BATCH; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int p = 0; p < n; ++p) {
+        const float4* from = a.part_o + slot(p) * ROWS * C4;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          const int i = i0 + k * THREADS;
+          if (i >= all) continue;
+          const float w = weights[p * used + i / C4];
+          const float4 v = __ldcg(from + i);
+          acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const int i = i0 + k * THREADS, row = i / C4, tok = row / a.block_heads, head = row - tok * a.block_heads;
+        if (i >= all || head >= n_heads) continue;
+        const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
+        Elem<T>::store4(reinterpret_cast<T*>(a.o) + ((int64_t)(tok0 + tok) * a.Hq + head0 + head) * D + i % C4 * 4, y);
+      }
     }
   }
 }

@@ -202,7 +202,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
     for (int i = 0; i < 4; ++i) {   // stream, half of the key tile
       mbar_init(bar(C::S + i), 1);
-      mbar_init(bar(C::P + i), 4);   // (one lane a warp: 128 arrivals took as long as a quarter of the tile's exponentials)
+      mbar_init(bar(C::P + i), 4);   // (one lane a warp)
     }
     mbar_init(bar(C::OM), 1);
     mbar_init(bar(C::ML), 8);

@@ -271,7 +271,8 @@ static RopeArgs rope_args(const earn_model_t* m, const earn_rope_t* r, int32_t n
   a.amplitude = r->amplitude > 0.f ? r->amplitude : 1.f; a.sign = 1.f;
   return a;
 }
-// Workspace of the chunk attention: status block, tickets, the parts' sums and references, the parts.
+// Workspace of the chunk attention: status block, tickets (as many for every call, so that no other call's parts lie on them:
+// they are zero between calls), the parts' sums and references, the parts.
 struct ChunkLayout {
   size_t tickets, part_ml, part_o, total;
   ChunkPlan plan;
@@ -281,7 +282,7 @@ static ChunkLayout chunk_layout(const earn_model_t* m, int32_t n_seq, int32_t n_
   l.plan = plan_chunk_attn(n_seq, m->n_q_heads, m->n_kv_heads, m->dtype, n_tokens, c->max_len);
   const size_t tiles = (size_t)l.plan.grid * l.plan.tiles, rows = 2 * tiles * l.plan.rows;
   l.tickets = kStatusBytes;
-  l.part_ml = l.tickets + round_up(tiles * 4, 256);
+  l.part_ml = l.tickets + round_up(kChunkTickets * 4, 256);
   l.part_o = l.part_ml + round_up(rows * 8, 256);
   l.total = l.part_o + rows * (size_t)m->head_dim * 4;
   return l;
@@ -901,7 +902,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   a.sched.cu_new = cu_new; a.sched.seq_len = cache->seq_len;
   a.sched.n_seq = n_seq; a.sched.n_tokens = n_tokens; a.sched.max_len = cache->max_len;
   a.sched.heads = model->n_kv_heads * l.plan.blocks;
-  a.sched.item_tok = l.plan.tile_tok * l.plan.tiles; a.sched.key_tile = l.plan.keys;
+  a.sched.item_tok = l.plan.tile_tok * l.plan.tiles; a.sched.key_shift = l.plan.keys == 128 ? 7 : 6;
   a.sched.grid = l.plan.grid; a.sched.min_share = l.plan.min_share;
   a.tickets = reinterpret_cast<int32_t*>(ws + l.tickets);
   a.part_ml = reinterpret_cast<float2*>(ws + l.part_ml);

@@ -402,6 +402,55 @@ def test_chunk_offsets_are_cut_off():
     assert B.earn_device_status(c.ws) == B.EARN_OK
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_chunk_workspace_serves_calls_of_all_shapes(dtype):
+    """One workspace for calls whose parts lie at different places, and for the block tables between them."""
+    shapes = [([1] * 6, [900, 3000, 17, 2048, 1, 555]), ([300, 1], [4000, 900]), ([1], [5]), ([40, 2, 33], [1500, 16, 33]), ([1], [6000])]
+    chunks = [Chunk(new, lens, 8, 2, 128, dtype, seed=i) for i, (new, lens) in enumerate(shapes)]
+    ws = torch.empty(max(c.ws.numel() for c in chunks), dtype=torch.uint8, device="cuda")
+    B.earn_workspace_init(ws)
+    p = Pool([3, 0], 4, 8, n_tokens=8)
+    p.ws = ws
+    for i in [0, 1, 2, 3, 4, 1, 0, 2, 4, 3, 0]:
+        c = chunks[i]
+        c.ws = ws
+        c.o.fill_(7)
+        c.lse.fill_(7)
+        c.call().check()
+        p.check([4 + i, i], *p.call([4 + i, i]))
+    assert B.earn_device_status(ws) == B.EARN_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("longest", [3, 40])
+def test_chunk_many_sequences(dtype, longest):
+    """More sequences than a CTA keeps in shared memory."""
+    r = np.random.default_rng(longest)
+    new = r.integers(0, longest + 1, 1200)
+    Chunk(new.tolist(), (new + r.integers(0, 30, 1200)).tolist(), 4, 2, 64, dtype, seed=8).call().check()
+
+
+def test_chunk_long_chunks_and_one_long_list():
+    """Items worked on by columns, and lists that every CTA has a part of."""
+    Chunk([1100, 900, 1200], [1100, 1000, 1203], 28, 4, 64, "bf16", seed=9).call().check()
+    Chunk([700] * 4, [700, 1300, 705, 900], 16, 16, 64, "bf16", seed=10).call().check()
+    for dtype in ("bf16", "f32"):
+        Chunk([1], [24001], 8, 1, 128, dtype, seed=11).call().check()
+        Chunk([40], [9001], 8, 1, 128, dtype, seed=12).call().check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,lens", [([200, 3], [900, 70]), ([1, 2], [600, 70])])
+def test_chunk_rows_16_bytes_past_a_32_byte_boundary(dtype, new, lens):
+    c = Chunk(new, lens, 8, 2, 64, dtype, seed=13)
+    for name in ("q", "o"):
+        t = getattr(c, name)
+        by = 16 // t.element_size()
+        moved = torch.empty(t.numel() + by, dtype=t.dtype, device="cuda")[by:].view(t.shape)
+        setattr(c, name, moved.copy_(t))
+    c.call().check()
+
+
 def test_chunk_on_another_stream_and_captured():
     """A step captured once and replayed with other lengths, tables and offsets, on a stream of its own."""
     c = Chunk([5, 1, 40, 0], [300, 40, 90, 10], 8, 2, 128, "bf16", seed=6, pad=14)
