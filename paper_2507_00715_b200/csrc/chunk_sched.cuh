@@ -35,15 +35,19 @@ struct ChunkSched {
 };
 constexpr int kChunkTable = 960;
 
-// Offsets that run past the batch or backwards are cut off, so that no row outside q and o is touched.
+// Offsets that run past the batch or backwards are cut off, so that no row outside q and o is touched: lo to where it belongs.
+__host__ __device__ inline int chunk_new(const ChunkSched& s, int& lo, int hi) {   // returns the new tokens
+  lo = lo < 0 ? 0 : lo > s.n_tokens ? s.n_tokens : lo;
+  hi = hi < lo ? lo : hi > s.n_tokens ? s.n_tokens : hi;
+  return hi - lo;
+}
 __host__ __device__ inline ChunkSeq chunk_seq(const ChunkSched& s, int b) {
   if (s.table != nullptr) return s.table[b];
   ChunkSeq q;
-  int lo = s.cu_new[b], hi = s.cu_new[b + 1], len = s.seq_len[b];
-  lo = lo < 0 ? 0 : lo > s.n_tokens ? s.n_tokens : lo;
-  hi = hi < lo ? lo : hi > s.n_tokens ? s.n_tokens : hi;
+  int lo = s.cu_new[b], len = s.seq_len[b];
+  q.n = chunk_new(s, lo, s.cu_new[b + 1]);
   len = len < 0 ? 0 : len > s.max_len ? s.max_len : len;
-  q.tok0 = lo; q.n = hi - lo; q.base = len - q.n;
+  q.tok0 = lo; q.base = len - q.n;
   q.items = (q.n + s.item_tok - 1) / s.item_tok;
   return q;
 }
@@ -111,7 +115,6 @@ struct ChunkWalk {
   int shares;           // shares the line is cut into: share c begins at c * quot + c * rem / shares
   uint32_t quot, rem;
   int b, h, m, off;     // where pos is: unit `off` of item m under head block h of sequence b
-  int longest;          // most new tokens of a sequence
   int cols, col;        // columns of the line (1: the items' own order), and the one that pos is in
 };
 __host__ __device__ inline void chunk_cuts(const ChunkSched& s, ChunkWalk& w) {
@@ -213,9 +216,18 @@ __host__ __device__ inline int chunk_columns(uint32_t items, uint32_t lists, int
 #ifdef __CUDACC__
 struct ChunkCounts {
   uint32_t units;
-  int items, lists, longest;   // (items and lists: of sequences)
+  int items, lists;   // of sequences
 };
-// Sums (units, items, lists) and maximum (longest) over the block; returns the units of the threads in front of this one.
+// Whether a sequence has more than n new tokens, the same answer in every thread of the block.
+__device__ inline bool chunk_longer(const ChunkSched& s, int n) {
+  bool mine = false;
+  for (int b = threadIdx.x; b < s.n_seq; b += blockDim.x) {
+    int lo = s.cu_new[b];
+    mine |= chunk_new(s, lo, s.cu_new[b + 1]) > n;
+  }
+  return __syncthreads_or(mine) != 0;
+}
+// Sums (units, items, lists) over the block; returns the units of the threads in front of this one.
 __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
   uint32_t incl = c.units;
@@ -226,9 +238,8 @@ __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   }
   const uint32_t inside = incl - c.units;
   const int items = __reduce_add_sync(0xffffffffu, c.items), lists = __reduce_add_sync(0xffffffffu, c.lists);
-  const int longest = __reduce_max_sync(0xffffffffu, c.longest);
   __syncthreads();
-  if (lane == 31) scratch[warp] = make_int4((int)incl, items, lists, longest);
+  if (lane == 31) scratch[warp] = make_int4((int)incl, items, lists, 0);
   __syncthreads();
   const int4 n = lane < warps ? scratch[lane] : make_int4(0, 0, 0, 0);
   uint32_t sum = (uint32_t)n.x;
@@ -240,14 +251,12 @@ __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   c.units = __shfl_sync(0xffffffffu, sum, 31);
   c.items = __reduce_add_sync(0xffffffffu, n.y);
   c.lists = __reduce_add_sync(0xffffffffu, n.z);
-  c.longest = __reduce_max_sync(0xffffffffu, n.w);
   return __shfl_sync(0xffffffffu, sum - (uint32_t)n.x, warp) + inside;
 }
 
 // This CTA's share of the line; every thread of the CTA calls it (`scratch`: 16-byte aligned shared memory for 48 16-byte words;
-// `table`: for kChunkTable sequences, or null).  From then on s reads the sequences from the table, where they fit.  Nothing
-// is worked out (pos = end) if the longest chunk is not within least .. most tokens: the call is another kernel's.
-__device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* table, int least, int most) {
+// `table`: for kChunkTable sequences, or null).  From then on s reads the sequences from the table, where they fit.
+__device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* table) {
   const int t = threadIdx.x, threads = blockDim.x, c = blockIdx.x;
   const bool in_table = table != nullptr && s.n_seq <= kChunkTable;
   const int per = s.n_seq <= threads ? 1 : (s.n_seq + threads - 1) / threads, b0 = min(t * per, s.n_seq), b1 = min(b0 + per, s.n_seq);
@@ -256,7 +265,6 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
     const ChunkSeq q = chunk_seq(s, b);
     if (in_table) table[b] = q;
     if (q.n == 0) continue;
-    n.longest = max(n.longest, q.n);
     n.items += q.items;
     ++n.lists;
     n.units += s.heads * chunk_units_before(s, q, q.items);
@@ -265,8 +273,7 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
   if (in_table) s.table = table;   // (written in front of the scan's barriers)
   ChunkWalk w{};
   w.total = n.units;
-  w.longest = n.longest;
-  if (n.longest < least || n.longest > most) return w;
+  if (n.units == 0) return w;
   chunk_cuts(s, w);
   w.cols = chunk_columns((uint32_t)n.items * s.heads, (uint32_t)n.lists * s.heads, s.n_seq, w.shares, threads);
   if (w.cols > 1) {

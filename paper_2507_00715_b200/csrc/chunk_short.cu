@@ -264,7 +264,7 @@ __device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl
 
 template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
-chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2, int most) {
+chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2, int few) {
   using C = Cfg<HD>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;    // swizzled tiles need 1024-byte alignment
@@ -291,8 +291,9 @@ chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
+  if (a.sched.n_tokens > few && chunk_longer(a.sched, few)) return;   // (the call is the other kernel's)
   ChunkSched sched = a.sched;
-  ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ), 1, most);
+  ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ));
   if (w.pos >= w.end) return;   // (the same for all threads)
   fence_async_smem();           // (the copies that come next land where the shares' scratch was)
   __syncthreads();

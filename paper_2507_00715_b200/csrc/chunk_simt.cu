@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
   ChunkSched s = a.sched;
   pdl_launch_dependents();
   pdl_wait();
-  ChunkWalk w = chunk_share(s, scratch, nullptr, 1, INT32_MAX);
+  ChunkWalk w = chunk_share(s, scratch, nullptr);
   if (w.pos >= w.end) return;
   ChunkSeq q = chunk_seq(s, w.b);
   while (w.pos < w.end) {
