@@ -32,8 +32,9 @@ struct ChunkSched {
   int item_tok, key_shift;  // tokens of an item; keys of a key tile, as a power of two
   int grid, min_share;      // CTAs launched; units a CTA takes at least
   const ChunkSeq* table;    // the sequences, where a CTA has them in shared memory (up to kChunkTable), or null
+  const int* first;         // with columns: every sequence's first item in the order above, and their number
 };
-constexpr int kChunkTable = 960;
+constexpr int kChunkTable = 960, kChunkFirst = 64;   // columns: of up to kChunkFirst sequences
 
 // Offsets that run past the batch or backwards are cut off, so that no row outside q and o is touched: lo to where it belongs.
 __host__ __device__ inline int chunk_new(const ChunkSched& s, int& lo, int hi) {   // returns the new tokens
@@ -115,7 +116,7 @@ struct ChunkWalk {
   int shares;           // shares the line is cut into: share c begins at c * quot + c * rem / shares
   uint32_t quot, rem;
   int b, h, m, off;     // where pos is: unit `off` of item m under head block h of sequence b
-  int cols, col;        // columns of the line (1: the items' own order), and the one that pos is in
+  int cols, col, i;     // columns of the line (1: the items' own order), the one that pos is in, and that item's number in the order
 };
 __host__ __device__ inline void chunk_cuts(const ChunkSched& s, ChunkWalk& w) {
   const uint32_t shares = (w.total + s.min_share - 1) / s.min_share;
@@ -128,32 +129,35 @@ __host__ __device__ inline void chunk_cuts(const ChunkSched& s, ChunkWalk& w) {
 }
 __host__ __device__ inline uint32_t chunk_cut(const ChunkWalk& w, int c) { return c * w.quot + c * w.rem / w.shares; }
 
-// `count` items further in the order (sequence, head block, item); w.b = n_seq behind the last one
-__host__ __device__ inline void chunk_skip(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int count) {
-  if (w.m + count < q.items) { w.m += count; return; }
-  uint32_t at = (uint32_t)w.h * q.items + w.m + count, all;
-  while (at >= (all = (uint32_t)s.heads * q.items)) {
-    at -= all;
-    do {
-      if (++w.b >= s.n_seq) return;
-      q = chunk_seq(s, w.b);
-    } while (q.n == 0);
-  }
-  w.h = q.items == 1 ? at : at / q.items;
+// w to the item that stands at w.i in the order (sequence, head block, item); w.b = n_seq behind the last one
+__host__ __device__ inline void chunk_place(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q) {
+  if (w.i >= s.first[s.n_seq]) { w.b = s.n_seq; return; }
+  int b = 0;
+  for (int step = kChunkFirst / 2; step > 0; step >>= 1)
+    if (b + step < s.n_seq && s.first[b + step] <= w.i) b += step;   // the last one that starts there or before: it is not empty
+  w.b = b;
+  q = chunk_seq(s, b);
+  const int at = w.i - s.first[b];
+  w.h = at / q.items;
   w.m = at - w.h * q.items;
-}
-// the first item of a column (there is one: no more columns than items)
-__host__ __device__ inline void chunk_column(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, int col) {
-  w.col = col;
-  w.h = w.m = w.off = w.b = 0;
-  for (q = chunk_seq(s, 0); q.n == 0; q = chunk_seq(s, w.b)) ++w.b;
-  chunk_skip(s, w, q, col);
 }
 // the item that follows on the line
 __host__ __device__ inline void chunk_next(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q) {
   w.off = 0;
-  chunk_skip(s, w, q, w.cols);
-  if (w.b >= s.n_seq && w.col + 1 < w.cols) chunk_column(s, w, q, w.col + 1);
+  if (w.cols > 1) {
+    w.i += w.cols;
+    if (w.i >= s.first[s.n_seq] && w.col + 1 < w.cols) w.i = ++w.col;
+    chunk_place(s, w, q);
+    return;
+  }
+  if (++w.m < q.items) return;
+  w.m = 0;
+  if (++w.h < s.heads) return;
+  w.h = 0;
+  do {
+    if (++w.b >= s.n_seq) return;
+    q = chunk_seq(s, w.b);
+  } while (q.n == 0);
 }
 // Moves unit x of the line, which lies at unit w.off of the item where w is, to the item's edge where it is close to one.
 // Returns the cut; w moves with it.
@@ -208,9 +212,9 @@ __host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, uint32_t s
   return p;
 }
 
-// columns of the line, see above; `threads`: a column's units are summed up by a thread
+// columns of the line, see above; `threads`: a column's units are summed up by a thread or several
 __host__ __device__ inline int chunk_columns(uint32_t items, uint32_t lists, int n_seq, int shares, int threads) {
-  return shares <= threads && n_seq <= 64 && items >= 2u * shares && items / 4 >= lists ? shares : 1;
+  return shares <= threads && n_seq <= kChunkFirst && items >= 2u * shares && items / 4 >= lists ? shares : 1;
 }
 
 #ifdef __CUDACC__
@@ -269,20 +273,43 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
     ++n.lists;
     n.units += s.heads * chunk_units_before(s, q, q.items);
   }
+  int own_items = n.items;
   uint32_t mine = n.units, before = chunk_scan(n, scratch);
   if (in_table) s.table = table;   // (written in front of the scan's barriers)
   ChunkWalk w{};
   w.total = n.units;
   if (n.units == 0) return w;
   chunk_cuts(s, w);
-  w.cols = chunk_columns((uint32_t)n.items * s.heads, (uint32_t)n.lists * s.heads, s.n_seq, w.shares, threads);
+  w.cols = in_table ? chunk_columns((uint32_t)n.items * s.heads, (uint32_t)n.lists * s.heads, s.n_seq, w.shares, threads) : 1;
+  int each = 1;   // threads of a column, a power of two
   if (w.cols > 1) {
+    int* first = reinterpret_cast<int*>(table + kChunkFirst);
+    if (t < kChunkFirst) {   // (a sequence a thread)
+      int incl = own_items;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, d);
+        if ((t & 31) >= d) incl += v;
+      }
+      if (t >= 32) incl += scratch[0].y;   // (the first warp's items)
+      if (t < s.n_seq) first[t + 1] = incl * s.heads;
+      if (t == 0) first[0] = 0;
+    }
+    s.first = first;
+    __syncthreads();
+    const int items = n.items * s.heads;
+    while (each < 32 && 2 * each * w.cols <= threads) each *= 2;
     ChunkCounts col{};
-    if (t < w.cols) {
+    if (t < w.cols * each) {
       ChunkWalk v = w;
       ChunkSeq q;
-      for (chunk_column(s, v, q, t); v.b < s.n_seq; chunk_skip(s, v, q, w.cols)) col.units += chunk_units(s, q, v.m);
+      for (v.i = t / each + t % each * w.cols; v.i < items; v.i += each * w.cols) {
+        chunk_place(s, v, q);
+        col.units += chunk_units(s, q, v.m);
+      }
     }
+    for (int d = 1; d < each; d <<= 1) col.units += __shfl_xor_sync(0xffffffffu, col.units, d);
+    if (t % each != 0) col.units = 0;
     mine = col.units;
     before = chunk_scan(col, scratch);
   }
@@ -305,11 +332,28 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
       uint32_t at = place[2 * side + 1];
       ChunkSeq q;
       if (w.cols > 1) {
-        chunk_column(s, v, q, owner);
-        for (uint32_t u = chunk_units(s, q, v.m); at + u <= x; u = chunk_units(s, q, v.m)) {
-          at += u;
-          chunk_skip(s, v, q, w.cols);
+        v.col = owner / each;
+        for (int i = v.col;; i += 32 * w.cols) {   // (32 of the column's items at once)
+          v.i = i + (t & 31) * w.cols;
+          chunk_place(s, v, q);
+          const uint32_t u = v.b < s.n_seq ? chunk_units(s, q, v.m) : 0;
+          uint32_t incl = u;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+            if ((t & 31) >= d) incl += y;
+          }
+          const uint32_t behind = __ballot_sync(0xffffffffu, at + incl > x);
+          if (behind == 0) {
+            at += __shfl_sync(0xffffffffu, incl, 31);
+            continue;
+          }
+          const int lane = __ffs(behind) - 1;
+          at += __shfl_sync(0xffffffffu, incl - u, lane);
+          v.i = i + lane * w.cols;
+          break;
         }
+        chunk_place(s, v, q);
         v.off = (int)(x - at);
       } else {
         for (v.b = owner * per;; ++v.b) {
@@ -328,12 +372,12 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
     }
     if ((t & 31) == 0) {
       found[side] = cut;
-      if (side == 0) { found[2] = v.b; found[3] = v.h; found[4] = v.m; found[5] = v.off; found[6] = v.col; }
+      if (side == 0) { found[2] = v.b; found[3] = v.h; found[4] = v.m; found[5] = v.off; found[6] = v.col; found[7] = v.i; }
     }
   }
   __syncthreads();
   w.pos = found[0]; w.end = found[1];
-  w.b = (int)found[2]; w.h = (int)found[3]; w.m = (int)found[4]; w.off = (int)found[5]; w.col = (int)found[6];
+  w.b = (int)found[2]; w.h = (int)found[3]; w.m = (int)found[4]; w.off = (int)found[5]; w.col = (int)found[6]; w.i = (int)found[7];
   __syncthreads();
   return w;
 }
