@@ -2,6 +2,7 @@
 #pragma once
 #include "chunk_sched.cuh"
 #include "paged_cache.cuh"
+#include "sm100_ptx.cuh"
 
 namespace earn {
 
@@ -131,10 +132,17 @@ __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts&
           acc[k].x += v.x * w; acc[k].y += v.y * w; acc[k].z += v.z * w; acc[k].w += v.w * w;
         }
       }
+      if constexpr (sizeof(T) == 2 && AHEAD % 2 == 0) {   // 16 bytes a store: neighbouring threads' rows are apart
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
-        Elem<T>::store4(out + (c + k) * 4, y);
+        for (int k = 0; k < AHEAD; k += 2)
+          *reinterpret_cast<uint4*>(out + (c + k) * 4) = make_uint4(ptx::pack_bf16(acc[k].x, acc[k].y), ptx::pack_bf16(acc[k].z, acc[k].w),
+                                                                   ptx::pack_bf16(acc[k + 1].x, acc[k + 1].y), ptx::pack_bf16(acc[k + 1].z, acc[k + 1].w));
+      } else {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const float y[4] = {acc[k].x, acc[k].y, acc[k].z, acc[k].w};
+          Elem<T>::store4(out + (c + k) * 4, y);
+        }
       }
     }
   } else {
