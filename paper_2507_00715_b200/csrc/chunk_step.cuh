@@ -72,9 +72,8 @@ __device__ __forceinline__ float chunk_lse(float ref, float sum) {
 
 // Joins the parts of a row tile (all of them written, and seen by this thread) into its output rows, by THREADS threads of
 // which this is number t: first every part's weight in a row (2^(its reference - the largest) over the row's
-// denominator, into `weights`, shared memory for used rows x parts numbers), a thread per row or, for many parts, a warp; then
-// four columns of a row at a time.  The parts are added in their order along the keys, so the result does not depend on which
-// of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else
+// denominator, into `weights`, shared memory for used rows x parts numbers); then four columns of a row at a time.  The parts
+// are added in their order along the keys, so the result does not depend on which of them came last.  LOG2: references are in the log2 domain, else natural.  ROW_MAJOR: a part is [rows][D], else
 // [D / 4][rows][4].  sync(): barrier of the threads, false if it gave up.
 template <typename T, int D, int ROWS, int THREADS, bool LOG2, bool ROW_MAJOR, class Sync>
 __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts& parts, int tiles, int x, int t,
@@ -83,32 +82,60 @@ __device__ __forceinline__ void chunk_join(const ChunkArgs& a, const ChunkParts&
   const int used = n_tok * a.block_heads, n = parts.parts;   // rows of the tile that hold a token
   auto slot = [&](int p) { return (int64_t)(2 * (parts.first + p) + (p == 0 ? 1 : 0)) * tiles + x; };
   auto power = [&](float from, float ref) { return LOG2 ? exp2f(from - ref) : exp2f((from - ref) * kLog2e); };
-  const bool by_warp = n > 4;
-  const int lane = t & 31, lanes = by_warp ? 32 : 1;
-  for (int row = by_warp ? t >> 5 : t; row < used; row += by_warp ? THREADS >> 5 : THREADS) {
-    const int tok = row / a.block_heads, head = row - tok * a.block_heads;
-    if (head >= n_heads) continue;
-    float m = -INFINITY, l = 0.f;
+  if constexpr (ROW_MAJOR) {
+    // few rows: a lane per part, one trip to memory for all weights of a row (512 rows of one token: 11.9 -> 11.2 us; where a
+    // part is a full row tile this code cost the kernel around it registers: 8 x 512 tokens of 64-wide heads 128 -> 136 us)
+    const int lanes = n <= 4 ? 4 : 32, sub = t & (lanes - 1);
+    const uint32_t mask = n <= 4 ? 0xfu << (t & 28) : 0xffffffffu;
+    for (int row = t / lanes; row < used; row += THREADS / lanes) {
+      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+      if (head >= n_heads) continue;
+      auto part = [&](int p) { return __ldcg(a.part_ml + slot(p) * ROWS + row); };
+      const float2 mine = sub < n ? part(sub) : make_float2(-INFINITY, 0.f);
+      float m = mine.x;
+      for (int p = sub + lanes; p < n; p += lanes) m = fmaxf(m, part(p).x);
+      for (int d = lanes / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(mask, m, d));
+      const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen: every weight is 2^-inf = 0)
+      float l = mine.y * power(mine.x, ref);
+      for (int p = sub + lanes; p < n; p += lanes) {
+        const float2 ml = part(p);
+        l += ml.y * power(ml.x, ref);
+      }
+      for (int d = lanes / 2; d > 0; d >>= 1) l += __shfl_xor_sync(mask, l, d);
+      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+      if (sub < n) weights[sub * used + row] = power(mine.x, ref) * inv;
+      for (int p = sub + lanes; p < n; p += lanes) weights[p * used + row] = power(part(p).x, ref) * inv;
+      if (sub == 0 && a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+    }
+  } else {
+    // a thread per row or, for many parts, a warp
+    const bool by_warp = n > 4;
+    const int lane = t & 31, lanes = by_warp ? 32 : 1;
+    for (int row = by_warp ? t >> 5 : t; row < used; row += by_warp ? THREADS >> 5 : THREADS) {
+      const int tok = row / a.block_heads, head = row - tok * a.block_heads;
+      if (head >= n_heads) continue;
+      float m = -INFINITY, l = 0.f;
 #pragma unroll 4
-    for (int p = by_warp ? lane : 0; p < n; p += lanes) m = fmaxf(m, __ldcg(a.part_ml + slot(p) * ROWS + row).x);
-    if (by_warp) {
+      for (int p = by_warp ? lane : 0; p < n; p += lanes) m = fmaxf(m, __ldcg(a.part_ml + slot(p) * ROWS + row).x);
+      if (by_warp) {
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    }
-    const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen: every weight is 2^-inf = 0)
+        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      }
+      const float ref = m == -INFINITY ? 0.f : m;   // (nothing seen: every weight is 2^-inf = 0)
 #pragma unroll 4
-    for (int p = by_warp ? lane : 0; p < n; p += lanes) {
-      const float2 ml = __ldcg(a.part_ml + slot(p) * ROWS + row);
-      l += ml.y * power(ml.x, ref);
-    }
-    if (by_warp) {
+      for (int p = by_warp ? lane : 0; p < n; p += lanes) {
+        const float2 ml = __ldcg(a.part_ml + slot(p) * ROWS + row);
+        l += ml.y * power(ml.x, ref);
+      }
+      if (by_warp) {
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-    }
-    const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+      }
+      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
 #pragma unroll 4
-    for (int p = by_warp ? lane : 0; p < n; p += lanes) weights[p * used + row] = power(__ldcg(a.part_ml + slot(p) * ROWS + row).x, ref) * inv;
-    if ((!by_warp || lane == 0) && a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+      for (int p = by_warp ? lane : 0; p < n; p += lanes) weights[p * used + row] = power(__ldcg(a.part_ml + slot(p) * ROWS + row).x, ref) * inv;
+      if ((!by_warp || lane == 0) && a.lse != nullptr) a.lse[(int64_t)(head0 + head) * a.sched.n_tokens + tok0 + tok] = chunk_lse<LOG2>(m, l);
+    }
   }
   if (!sync()) return;
   if constexpr (!ROW_MAJOR) {
