@@ -44,20 +44,21 @@ __device__ __forceinline__ Part next_part(const ChunkArgs& a, const ChunkSched& 
   p.base = q.base;
   p.keys = chunk_keys(s, q, w.m);
   const int units = chunk_units(s, q, w.m);
-  p.u0 = w.off;
-  p.n = (int)min((uint32_t)(units - w.off), w.end - w.pos);
+  const int cost = chunk_cost(s, q, w.m), end = w.off + (int)min((uint32_t)(units - w.off), w.end - w.pos);
+  p.u0 = max(w.off - cost, 0);
+  p.n = end - cost - p.u0;
   p.n_rows = min(p.n_tok, tile_tok) * a.block_heads;
   p.kind = (p.n_tok > tile_tok ? PAIR : ROWS) + 4 * pass;
-  p.last = w.off + p.n == units;
+  p.last = end == units;
   p.parts = 1;
   if (w.off > 0 || !p.last) {
-    const ChunkParts parts = chunk_parts(w, w.pos - w.off, units);
+    const ChunkParts parts = chunk_parts(w, w.pos - w.off, units, cost);
     p.first = parts.first;
     p.parts = parts.parts;
   }
-  w.pos += p.n;
+  w.pos += end - w.off;
   if (p.last) chunk_next(s, w, q);
-  else w.off += p.n;
+  else w.off = end;
   return p;
 }
 // where this CTA's part of row tile x goes in the scratch

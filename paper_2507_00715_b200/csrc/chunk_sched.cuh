@@ -2,7 +2,8 @@
 //
 // A row tile holds the query rows (token, head) of `tile_tok` consecutive new tokens of one sequence under one head block (the
 // query heads of a kv head, or a part of them where a group is larger than a tile).  A work item is `item_tok` tokens (one or
-// two row tiles) against every key that its last token sees; its cost is counted in units, one per key tile.  The units of all
+// two row tiles) against every key that its last token sees; its cost is counted in units, one per key tile, with a few in front
+// for what an item takes besides.  The units of all
 // items, in the order (sequence, head block, item, key tile), form one line, which is cut into equal shares, one per CTA: long
 // lists are split over CTAs, short ones share one, whatever the mix of single tokens and long chunks.  A cut that falls close
 // to an item's edge is moved there, so that only cuts that pay make partial results.
@@ -30,6 +31,7 @@ struct ChunkSched {
   int n_seq, n_tokens, max_len;
   int heads;                // head blocks: Hkv * ceil(g / heads of a block)
   int item_tok, key_shift;  // tokens of an item; keys of a key tile, as a power of two
+  int item_cost, free_tok;  // units at the beginning of an item that stand for no key tile; items of up to free_tok tokens have none
   int grid, min_share;      // CTAs launched; units a CTA takes at least
   const ChunkSeq* table;    // the sequences, where a CTA has them in shared memory (up to kChunkTable), or null
   const int* first;         // with columns: every sequence's first item in the order above, and their number
@@ -58,10 +60,11 @@ __host__ __device__ inline int chunk_keys(const ChunkSched& s, const ChunkSeq& q
   const int seen = q.base + (int)(end < q.n ? end : q.n);
   return seen > 0 ? seen : 0;
 }
-// units of item m: at least one, so that rows that see nothing are written too
+__host__ __device__ inline int chunk_cost(const ChunkSched& s, const ChunkSeq& q, int m) { return q.n - m * s.item_tok <= s.free_tok ? 0 : s.item_cost; }
+// units of item m: at least one with a key tile, so that rows that see nothing are written too
 __host__ __device__ inline int chunk_units(const ChunkSched& s, const ChunkSeq& q, int m) {
   const int u = (chunk_keys(s, q, m) + (1 << s.key_shift) - 1) >> s.key_shift;
-  return u > 0 ? u : 1;
+  return (u > 0 ? u : 1) + chunk_cost(s, q, m);
 }
 // sum over i < n of floor((a i + b) / 2^shift), by the Euclidean recursion; a n + b and the sum below 2^32
 __host__ __device__ inline uint32_t floor_sum(uint32_t n, int shift, uint32_t a, uint32_t b) {
@@ -97,7 +100,7 @@ __host__ __device__ inline uint32_t chunk_units_before(const ChunkSched& s, cons
   if (count == 1 || items == 1) return count > 0 ? chunk_units(s, q, 0) : 0;
   int whole = count < items ? count : items - 1;   // items whose end is a multiple of item_tok
   if (whole < 0) whole = 0;
-  uint32_t sum = 0;
+  uint32_t sum = whole * s.item_cost;   // (free_tok < item_tok)
   int skip = 0;
   if (q.base < 0) {   // leading items that see less than one key
     skip = (int)((1 - (int64_t)q.base + s.item_tok - 1) / s.item_tok) - 1;
@@ -162,8 +165,8 @@ __host__ __device__ inline void chunk_next(const ChunkSched& s, ChunkWalk& w, Ch
 // Moves unit x of the line, which lies at unit w.off of the item where w is, to the item's edge where it is close to one.
 // Returns the cut; w moves with it.
 __host__ __device__ inline uint32_t chunk_settle(const ChunkSched& s, ChunkWalk& w, ChunkSeq& q, uint32_t x) {
-  const uint32_t off = w.off, left = chunk_units(s, q, w.m) - off;
-  if (off <= w.tol) {
+  const uint32_t off = w.off, cost = chunk_cost(s, q, w.m), left = chunk_units(s, q, w.m) - off;
+  if (off <= w.tol + cost) {
     w.off = 0;
     return x - off;
   }
@@ -203,10 +206,10 @@ __host__ __device__ inline int chunk_cut_from(const ChunkWalk& w, uint32_t y) {
   while (chunk_cut(w, c) < y) ++c;
   return c;
 }
-__host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, uint32_t start, int units) {
+__host__ __device__ inline ChunkParts chunk_parts(const ChunkWalk& w, uint32_t start, int units, int cost) {
   ChunkParts p{0, 1};
-  if ((uint32_t)units <= 2 * w.tol + 1) return p;
-  const int lo = chunk_cut_from(w, start + w.tol + 1), hi = chunk_cut_from(w, start + units - w.tol) - 1;   // cuts further than tol inside
+  if ((uint32_t)units <= 2 * w.tol + cost + 1) return p;
+  const int lo = chunk_cut_from(w, start + cost + w.tol + 1), hi = chunk_cut_from(w, start + units - w.tol) - 1;   // cuts further than tol inside
   p.parts = hi >= lo ? hi - lo + 2 : 1;
   p.first = lo - 1;
   return p;

@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
     for (int i = 0; i < RI; ++i)
 #pragma unroll
       for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
-    const ChunkParts parts = chunk_parts(w, start, units);
+    const ChunkParts parts = chunk_parts(w, start, units, 0);
     if (parts.parts == 1) {
 #pragma unroll
       for (int i = 0; i < RI; ++i) {
@@ -229,7 +229,7 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   // no more CTAs than there can be units (bf16: of the kernel for few tokens, whose items are the smaller ones)
   const int heads = tc ? std::min(p.block_heads, 16) : p.block_heads, tokens = tc ? 16 / heads : p.tile_tok;
   const int64_t items = (int64_t)n_tokens / tokens + std::min(n_seq, n_tokens);
-  const int64_t units = items * n_kv_heads * ((g + heads - 1) / heads) * ((max_len + p.keys - 1) / p.keys);
+  const int64_t units = items * n_kv_heads * ((g + heads - 1) / heads) * ((max_len + p.keys - 1) / p.keys + (tc ? kItemCost : 0));
   p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(std::min(tc ? sm_count() : 2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
   return p;
 }

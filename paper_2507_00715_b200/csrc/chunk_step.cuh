@@ -33,6 +33,7 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
 
+constexpr int kItemCost = 2;   // of the tensor-core kernel's items of two row tiles, see there
 constexpr int kChunkTickets = 640;   // row tiles of all CTAs' items, at most
 
 struct ChunkArgs {

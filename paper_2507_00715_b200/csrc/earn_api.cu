@@ -903,6 +903,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   a.sched.n_seq = n_seq; a.sched.n_tokens = n_tokens; a.sched.max_len = cache->max_len;
   a.sched.heads = model->n_kv_heads * l.plan.blocks;
   a.sched.item_tok = l.plan.tile_tok * l.plan.tiles; a.sched.key_shift = l.plan.keys == 128 ? 7 : 6;
+  a.sched.item_cost = a.sched.free_tok = 0;
   a.sched.grid = l.plan.grid; a.sched.min_share = l.plan.min_share;
   a.tickets = reinterpret_cast<int32_t*>(ws + l.tickets);
   a.part_ml = reinterpret_cast<float2*>(ws + l.part_ml);
