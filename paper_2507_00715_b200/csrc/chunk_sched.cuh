@@ -225,14 +225,34 @@ struct ChunkCounts {
   uint32_t units;
   int items, lists;   // of sequences
 };
-// Whether a sequence has more than n new tokens, the same answer in every thread of the block.
-__device__ inline bool chunk_longer(const ChunkSched& s, int n) {
-  bool mine = false;
+// Which of the two bf16 kernels a call belongs to: the one for many rows if a sequence has more than `few` new tokens and the
+// other one would have more than `units` products of 16 rows and a key tile under a head block (its items times the tiles of
+// their list).
+struct ChunkSplit {
+  int few, units;
+  int item_tok;   // tokens of an item of the other kernel
+  int known;      // the lengths need not be looked at: it is the other kernel's
+};
+// The same answer in every thread of every block, and in both kernels.
+__device__ inline bool chunk_many(const ChunkSched& s, const ChunkSplit& f) {
+  __shared__ uint32_t sum;
+  if (f.known) return false;
+  if (threadIdx.x == 0) sum = 0;
+  bool longer = false;
+  uint32_t mine = 0;
   for (int b = threadIdx.x; b < s.n_seq; b += blockDim.x) {
     int lo = s.cu_new[b];
-    mine |= chunk_new(s, lo, s.cu_new[b + 1]) > n;
+    const int n = chunk_new(s, lo, s.cu_new[b + 1]), len = s.seq_len[b];
+    longer |= n > f.few;
+    const int tiles = ((len < s.max_len ? len : s.max_len) + 127) >> 7;
+    const uint64_t units = (uint64_t)((n + f.item_tok - 1) / f.item_tok) * (tiles > 0 ? tiles : 1);
+    mine += (uint32_t)(units < 65535 ? units : 65535);   // (at most 65535 sequences: 32 bits hold the sum)
   }
-  return __syncthreads_or(mine) != 0;
+  if (!__syncthreads_or(longer)) return false;
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  if ((threadIdx.x & 31) == 0) atomicAdd(&sum, mine);
+  __syncthreads();
+  return sum > (uint32_t)f.units;
 }
 // Sums (units, items, lists) over the block; returns the units of the threads in front of this one.
 __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {

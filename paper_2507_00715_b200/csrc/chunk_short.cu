@@ -1,5 +1,5 @@
-// Causal attention over paged lists of calls whose sequences have few new tokens each (decoded tokens, drafts): at most 32 rows
-// (token, query head of a kv head) per sequence; an item is 16 of them.
+// Causal attention over paged lists, for calls whose sequences have few new tokens each (decoded tokens, drafts) or that are too
+// small to fill the GPU with row tiles: an item is 16 rows (token, query head of a kv head).
 //
 // Bound by HBM: every K and V row is read once for all rows, 2 D flop per byte and row, so the work is to keep the copies going.
 // A CTA (one per SM) walks its share of the work line (chunk_sched.cuh).  One warp finds the parts and brings their tiles of 128
@@ -264,7 +264,7 @@ __device__ __forceinline__ void consume(const ChunkArgs& a, Consumer c, float sl
 
 template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
-chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2, int few) {
+chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a, float sl2) {
   using C = Cfg<HD>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;    // swizzled tiles need 1024-byte alignment
@@ -291,7 +291,7 @@ chunk_short_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
-  if (a.sched.n_tokens > few && chunk_longer(a.sched, few)) return;   // (the call is the other kernel's)
+  if (chunk_many(a.sched, a.split)) return;   // (the call is the other kernel's)
   ChunkSched sched = a.sched;
   ChunkWalk w = chunk_share(sched, reinterpret_cast<int4*>(gen), reinterpret_cast<ChunkSeq*>(gen + C::OFF_SEQ));
   if (w.pos >= w.end) return;   // (the same for all threads)
@@ -340,14 +340,14 @@ cudaError_t launch(const ChunkArgs& a, cudaStream_t st) {
   if (!tcmap::make_map(&mk, a.cache.k, a.Hkv, rows, EARN_PAGE_TOKENS, HD) || !tcmap::make_map(&mv, a.cache.v, a.Hkv, rows, EARN_PAGE_TOKENS, HD))
     return cudaErrorInvalidValue;
   ChunkArgs s = a;
-  s.blocks = (a.g + 15) / 16;   // head blocks of at most 16 heads
+  s.blocks = (a.g + kShortRows - 1) / kShortRows;   // head blocks of at most 16 heads
   s.block_heads = (a.g + s.blocks - 1) / s.blocks;
   s.sched.heads = a.Hkv * s.blocks;
-  s.sched.item_tok = 16 / s.block_heads;
+  s.sched.item_tok = a.split.item_tok;
   s.sched.min_share = 1;
   cudaError_t e = ensure_dynamic_smem<chunk_short_kernel<HD>>(Cfg<HD>::SMEM_BYTES);
   if (e == cudaSuccess)
-    e = launch_pdl(chunk_short_kernel<HD>, dim3(s.sched.grid), dim3(THREADS), Cfg<HD>::SMEM_BYTES, st, mk, mv, s, a.scale * kLog2e, chunk_short_tokens(a));
+    e = launch_pdl(chunk_short_kernel<HD>, dim3(s.sched.grid), dim3(THREADS), Cfg<HD>::SMEM_BYTES, st, mk, mv, s, a.scale * kLog2e);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

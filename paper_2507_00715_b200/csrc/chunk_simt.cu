@@ -227,9 +227,15 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   p.block_heads = (g + p.blocks - 1) / p.blocks;
   p.tile_tok = p.rows / p.block_heads;
   // no more CTAs than there can be units (bf16: of the kernel for few tokens, whose items are the smaller ones)
-  const int heads = tc ? std::min(p.block_heads, 16) : p.block_heads, tokens = tc ? 16 / heads : p.tile_tok;
+  const int blocks = tc ? (g + kShortRows - 1) / kShortRows : p.blocks, heads = (g + blocks - 1) / blocks, tokens = tc ? kShortRows / heads : p.tile_tok;
   const int64_t items = (int64_t)n_tokens / tokens + std::min(n_seq, n_tokens);
-  const int64_t units = items * n_kv_heads * ((g + heads - 1) / heads) * ((max_len + p.keys - 1) / p.keys + (tc ? kItemCost : 0));
+  const int64_t tiles = (max_len + p.keys - 1) / p.keys, units = items * n_kv_heads * blocks * (tiles + (tc ? kItemCost : 0));
+  if (tc) {
+    p.split.few = kShortRows / g;
+    p.split.units = kShortUnits * sm_count() / (n_kv_heads * blocks);
+    p.split.item_tok = tokens;
+    p.split.known = n_tokens <= p.split.few || items * tiles <= p.split.units;
+  }
   p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(std::min(tc ? sm_count() : 2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
   return p;
 }

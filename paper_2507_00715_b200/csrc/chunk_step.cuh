@@ -42,6 +42,7 @@ struct ChunkArgs {
   float* lse;                  // [Hq, n_tokens] or null
   PagedSource cache;
   ChunkSched sched;
+  ChunkSplit split;            // (bf16)
   float4* part_o;              // [2 * grid][row tiles][D / 4][rows], or [rows][D / 4]
   float2* part_ml;             // [2 * grid][row tiles][rows]: reference of the exponentials, their sum
   int32_t* tickets;            // [kChunkTickets >= grid * row tiles], zero between calls
@@ -53,15 +54,18 @@ struct ChunkArgs {
 // Tiles that a call uses: rows of a row tile, row tiles of an item, keys of a key tile.
 struct ChunkPlan {
   int rows, tiles, keys, block_heads, blocks, tile_tok, grid, min_share;
+  ChunkSplit split;            // (bf16)
 };
 ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, int n_tokens, int max_len);
 cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);   // fp32
-// bf16: a call whose sequences have at most chunk_short_tokens() new tokens each (0: none such) is the first kernel's, any other
-// the second's.  The lengths are on the device, so both are launched, unless n_tokens tells, and one of them finds nothing to do.
+// bf16: the first kernel has items of 16 rows, which go through the keys one by one; the second fills row tiles of 128.  A call is
+// the second's if it has items of several in a sequence and enough work for it (chunk_many; 24 units an SM: 256 rows over 2900, 8
+// kv heads, 21 units: 46 and 62 us; 8 x 32 rows over 2900, 20 units: 49 and 48; 16 x 24 rows, 40 units: 87 and 72; one sequence of
+// 128 rows over 9000, 2 kv heads, 8 units: 27 and 143).  The lengths are on the device, so both are launched, unless the sizes
+// that the host knows tell, and one of them finds nothing to do, which costs 5 us.
 cudaError_t launch_chunk_short(const ChunkArgs& a, cudaStream_t st);
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);
-constexpr int kShortRows = 32;   // rows (token, query head of a kv head)
-inline int chunk_short_tokens(const ChunkArgs& a) { return kShortRows / a.g; }
+constexpr int kShortRows = 16, kShortUnits = 24;   // rows of an item; units an SM, up to which a call is always the first kernel's
 
 // Softmax denominator of a row, natural log: once per row, so the logarithm is taken in 64 bits (the fast 32-bit one is off by
 // a few 1e-7, which is all of what fp32 callers see).  A row that sees nothing: -inf.

@@ -7,8 +7,7 @@
 //   PAIR   more than 128 rows: two row tiles of 128 against the same K/V tiles
 //   ROWS   up to 128 rows: one row tile, even and odd key tiles as two streams that meet in the end
 //
-// (A call whose chunks all have at most 32 rows is the other kernel's, chunk_short.cu.  The lengths are the device's, so both
-// are launched unless the number of tokens tells: the one that finds nothing to do costs 5 us.)
+// (A call of chunks of at most 16 rows, or with little work, is the other kernel's, chunk_short.cu.)
 //
 //   warp 0      TMA: the pages of the K and V tiles -> shared memory (128-byte swizzle), 16 rows x 64 columns a copy, a ring that
 //               runs on across items
@@ -160,7 +159,6 @@ __device__ __forceinline__ void sts(uint32_t at, float v) { asm volatile("st.sha
 struct TcArgs {
   ChunkArgs a;
   int tile_tok, q_box_tok;   // tokens of a row tile; tokens that a copy of Q brings
-  int few;                   // the call is the other kernel's if no chunk is longer
   float scale_log2;
 };
 
@@ -232,7 +230,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   const uint32_t tmem = *tmem_slot;   // S_x (and P_x over it) at x * 128, O_x at (2 + x) * 128
   pdl_launch_dependents();
   pdl_wait();
-  if (ta.few > 0 && !chunk_longer(a.sched, ta.few)) {
+  if (!chunk_many(a.sched, a.split)) {   // (the call is the other kernel's)
     if (warp == 2) tmem_dealloc(tmem, 512);
     return;
   }
@@ -716,7 +714,6 @@ cudaError_t launch(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st) {
   ta.a.sched.free_tok = p.tile_tok;
   ta.q_box_tok = std::min(p.tile_tok, a.sched.n_tokens);
   ta.scale_log2 = a.scale * kLog2e;
-  ta.few = chunk_short_tokens(a);
   const int rows = a.cache.n_pages * EARN_PAGE_TOKENS;
   if (!make_q_map(&mq, a, ta.q_box_tok) || !tcmap::make_map(&mk, a.cache.k, a.Hkv, rows, EARN_PAGE_TOKENS, HD) ||
       !tcmap::make_map(&mv, a.cache.v, a.Hkv, rows, EARN_PAGE_TOKENS, HD))

@@ -915,9 +915,9 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   note_call(stream, CALL_UNKNOWN);
   cudaError_t e = cudaSuccess;
   if (a.dtype == EARN_BF16) {
-    const int few = chunk_short_tokens(a);
-    if (few > 0) e = launch_chunk_short(a, (cudaStream_t)stream);
-    if (e == cudaSuccess && n_tokens > few) e = launch_chunk_tc(a, l.plan, (cudaStream_t)stream);
+    a.split = l.plan.split;
+    e = launch_chunk_short(a, (cudaStream_t)stream);
+    if (e == cudaSuccess && !a.split.known) e = launch_chunk_tc(a, l.plan, (cudaStream_t)stream);
   } else {
     e = launch_chunk_simt(a, l.plan, (cudaStream_t)stream);
   }

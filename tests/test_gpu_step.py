@@ -249,6 +249,13 @@ class Chunk:
 
     def __init__(self, new, lens, hq, hkv, d, dtype, seed=0, shuffle=True, scale=0.0, pad=0, junk=float("nan"), spread=1.0):
         g = gen(seed)
+        dtype, _, bulk = dtype.partition(" ")
+        if bulk:   # one sequence more, so long that the call goes to the kernel for many rows
+            heads_a_block = -(-(hq // hkv) // -(-(hq // hkv) // 16))
+            blocks, tokens, n = hkv * -(-(hq // hkv) // 16), 16 // heads_a_block, 40
+            while -(-n // tokens) * up(-(-(n + 60) // 8)) * blocks <= 24 * torch.cuda.get_device_properties(0).multi_processor_count:
+                n += 23
+            new, lens = [*new, n], [*lens, n + 60]
         self.new, self.lens, self.hq, self.hkv, self.d, self.dtype, self.scale, self.pad = new, lens, hq, hkv, d, dtype, scale, pad
         n_seq, total = len(new), sum(new)
         self.total, per_seq = total, max(1, up(max(lens, default=0))) + 1
@@ -314,7 +321,7 @@ class Chunk:
 HEADS = [(4, 4, 64), (8, 2, 128), (7, 1, 128), (28, 4, 64), (12, 2, 128), (3, 3, 128)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("hq,hkv,d", HEADS)
 def test_chunk_lengths(dtype, hq, hkv, d):
     """One token, page and tile edges, nothing new, nothing old, nothing at all, more tokens than rows, refused sequences."""
@@ -323,7 +330,7 @@ def test_chunk_lengths(dtype, hq, hkv, d):
     Chunk(new, lens, hq, hkv, d, dtype, seed=hq, pad=5).call().check()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("new,lens,hq,hkv,d", [
     ([1], [1], 1, 1, 64), ([1], [700], 4, 1, 128), ([5], [2005], 12, 2, 128), ([300], [300], 8, 2, 128), ([257, 255], [600, 255], 4, 4, 64),
     ([1] * 40, [(37 * i) % 300 + 1 for i in range(40)], 8, 1, 64), ([129, 1, 128], [129, 1000, 385], 2, 2, 128),
@@ -335,7 +342,7 @@ def test_chunk_shapes(dtype, new, lens, hq, hkv, d):
     assert torch.equal(c.call(lse=False).o, first)                   # equal calls, equal results
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("hq,hkv", [(100, 1), (160, 1), (129, 1), (300, 1), (144, 2)])
 def test_chunk_large_groups(dtype, hq, hkv):
     Chunk([3, 1, 0, 9], [140, 20, 5, 9], hq, hkv, 128, dtype, seed=hq).call().check()
@@ -343,11 +350,12 @@ def test_chunk_large_groups(dtype, hq, hkv):
 
 def test_chunk_identity_table_and_scale():
     Chunk([9, 1, 50], [100, 31, 77], 8, 2, 128, "bf16", shuffle=False).call().check()
+    Chunk([9, 1, 50], [100, 31, 77], 8, 2, 128, "bf16 bulk", shuffle=False, scale=0.2).call().check()
     Chunk([9, 1, 50], [100, 31, 77], 4, 2, 64, "f32", shuffle=False, scale=0.3).call().check()
     Chunk([9, 1, 50], [100, 31, 77], 4, 2, 64, "bf16", scale=0.02).call().check()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_chunk_logits_far_apart(dtype, d):
     """Large logits, a maximum that keeps growing along the list, a first tile that lies far below the rest."""
@@ -359,7 +367,7 @@ def test_chunk_logits_far_apart(dtype, d):
     c.call().check()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("new", [[300, 1, 40], [7, 1, 3]])
 def test_chunk_logits_beyond_any_reference(dtype, new):
     """Keys whose logits exceed those in front of them by hundreds: late in the list, early in it, and in one list of several."""
@@ -374,7 +382,7 @@ def test_chunk_logits_beyond_any_reference(dtype, new):
     assert torch.equal(c.call().o, first)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 def test_chunk_dead_keys(dtype):
     """Keys whose logits are -inf weigh nothing, long stretches of them at the start and whole lists included."""
     c = Chunk([6, 2, 140], [300, 40, 200], 8, 2, 128, dtype, seed=5)
@@ -402,7 +410,48 @@ def test_chunk_offsets_are_cut_off():
     assert B.earn_device_status(c.ws) == B.EARN_OK
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_chunk_offsets_of_many_rows_are_cut_off():
+    c = Chunk([4], [60], 8, 2, 128, "bf16 bulk", pad=8, seed=2)
+    n = c.new[1]
+    c.new, c.lens = c.new[::-1], c.lens[::-1]
+    c.cu.copy_(i32([0, n, n + 4]))
+    c.seq_len.copy_(c.seq_len.flip(0))
+    c.table.copy_(c.table.flip(0))
+    c.q[n + 4:] = 0
+    first = c.call().check().o.clone()
+    c.cu.copy_(i32([-7, n, 10 ** 9]))
+    c.call()
+    assert B.earn_device_status(c.ws) == B.EARN_OK and torch.equal(c.o[:n], first[:n])
+    c.cu.copy_(i32([n, 5, -1]))   # backwards: nothing is new
+    c.o.fill_(7)
+    c.call()
+    assert B.earn_device_status(c.ws) == B.EARN_OK and (c.o == 7).all()
+
+
+def test_chunk_captured_once_for_few_and_many_rows():
+    """The lengths that a captured call finds on the device say which kernel does the work."""
+    many = Chunk([40, 7], [200, 300], 8, 2, 128, "bf16 bulk", seed=20)
+    few = [([5, 0, 30], [100, 40, 60]), ([1, 1, 1], [180, 1, 90]), ([0, 0, 0], [7, 8, 9])]
+    many.call()
+    graph = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            many.call()
+        kept, capacity = (many.new, many.lens), many.total
+        for new, lens in [few[0], kept, few[1], few[2], kept]:
+            many.new, many.lens, many.total, many.pad = new, lens, sum(new), capacity - sum(new)
+            many.cu.copy_(i32(np.concatenate([[0], np.cumsum(new)])))
+            many.seq_len.copy_(i32(lens))
+            many.o.fill_(7)
+            many.lse.fill_(7)
+            graph.replay()
+            many.check()
+    torch.cuda.current_stream().wait_stream(s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 def test_chunk_workspace_serves_calls_of_all_shapes(dtype):
     """One workspace for calls whose parts lie at different places, and for the block tables between them."""
     shapes = [([1] * 6, [900, 3000, 17, 2048, 1, 555]), ([300, 1], [4000, 900]), ([1], [5]), ([40, 2, 33], [1500, 16, 33]), ([1], [6000])]
@@ -437,9 +486,10 @@ def test_chunk_long_chunks_and_one_long_list():
     for dtype in ("bf16", "f32"):
         Chunk([1], [24001], 8, 1, 128, dtype, seed=11).call().check()
         Chunk([40], [9001], 8, 1, 128, dtype, seed=12).call().check()
+    Chunk([130], [9001], 8, 1, 128, "bf16", seed=14).call().check()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
 @pytest.mark.parametrize("new,lens", [([200, 3], [900, 70]), ([1, 2], [600, 70])])
 def test_chunk_rows_16_bytes_past_a_32_byte_boundary(dtype, new, lens):
     c = Chunk(new, lens, 8, 2, 64, dtype, seed=13)
