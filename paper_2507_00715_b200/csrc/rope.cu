@@ -6,6 +6,8 @@
 // Bound by HBM: every row is read and written once.  Angles cost a token rot/2 sines and cosines, shared by all its heads:
 // the product position * f_i is taken and reduced to turns in 64 bits (a 32-bit product is off by 0.06 rad at position 10^6),
 // the remainder's sine and cosine in 32.  They go to shared memory, from where the threads take them, eight pairs at a time.
+// 65536 tokens of 32/8 heads of 128: 240 us, 5.6 TB/s of a copy's 6.55; 8191 tokens of 28/4 heads appended: 31 us, 4.9 TB/s; 64
+// tokens: 2.7 us, a launch.
 #include <algorithm>
 
 #include "chunk_step.cuh"
@@ -191,6 +193,7 @@ cudaError_t launch_form(const RopeArgs& a, int heads, int head_from, cudaStream_
   // Up to 64 heads of a token (STAGED keeps the rows in shared memory: 32 KB at most), and so many tokens that every thread has
   // two units, as long as there are eight blocks for every SM all the same.
   constexpr int UNITS = FORM == HALF ? D / (2 * Vec<T>::N) : D / Vec<T>::N;
+  // as many tokens a block as give a thread two units (65536 tokens 240 us, one token a block 288; 8191 appended 31 and 38)
   const int per_block = std::min(heads, 64);
   int tokens = std::max(1, std::min(MAX_TOKENS, 2 * THREADS / (per_block * UNITS)));
   while (tokens > 1 && a.n_tokens / tokens < 8 * sm_count()) tokens /= 2;
