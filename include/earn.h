@@ -413,7 +413,7 @@ typedef struct {
  * sequence keeps its rows; its tokens stay in the packed batch with position and slot -1, and its seq_len is 0.
  * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
  * must not overlap it).  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
- * or above the new height hold nothing.
+ * or above the new height hold nothing.  Without sequences (n_seq = 0) nothing is done.
  * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes may use it in turn.
  * Errors: n_seq < 0, n_tokens < 0, n_pages < 1, pages_per_seq < 1, NULL or misaligned arrays -> INVALID_ARG; n_seq > 16384,
  * row or slot numbers beyond 2^31 - 32 -> UNSUPPORTED; workspace -> WORKSPACE. */
@@ -459,7 +459,7 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
 /* Causal attention of every sequence's new tokens over its rows in the paged cache of a layer l < k, the new ones (stored
  * before) included: new token i of the n of sequence b is row p = seq_len[b] - n + i and sees rows 0 .. p,
  *   o = sum_{j <= p} softmax_j( q . k_j * scale ) v_j .
- * q, o: device [n_tokens, Hq, D]; lse_or_null: device fp32 [Hq, n_tokens], natural-log softmax denominators.  A token that
+ * q, o: device [n_tokens, Hq, D], apart from one another; lse_or_null: device fp32 [Hq, n_tokens], natural-log softmax denominators.  A token that
  * sees nothing (its sequence has seq_len 0, or fewer rows than new tokens; every logit -inf): o = 0, lse = -inf.  Rows of q
  * past cu_new[n_seq] are not read, those of o and lse are left as they were.  Rows at or past seq_len are not used, whatever
  * they hold; every row of a sequence below seq_len is to hold finite values (a row that some new token sees meets the earlier

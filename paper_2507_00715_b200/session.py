@@ -324,7 +324,7 @@ class PagedLayers:
         shape = (n_pages, B.PAGE_TOKENS, n_kv_heads, head_dim)
         self.k_pages = [torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(split_k)]
         self.v_pages = [torch.zeros(shape, dtype=dtype, device=self.device) for _ in range(split_k)]
-        self.caches = [B.make_paged_cache(k, v, self.block_table, self.seq_len, max_len) for k, v in zip(self.k_pages, self.v_pages)]
+        self.caches = [B.make_paged_cache(k, v, self.block_table, self.seq_len) for k, v in zip(self.k_pages, self.v_pages)]
         self.q_turned = torch.empty(n_tokens, n_q_heads, head_dim, dtype=dtype, device=self.device)
         need = B.earn_page_tables_workspace_bytes(n_seq)
         self.table_workspace = torch.empty(need, dtype=torch.uint8, device=self.device)

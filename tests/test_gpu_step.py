@@ -574,6 +574,21 @@ def test_a_run_of_steps(dtype, hq, hkv, d):
     assert p.refused.item() == 0 and rng is not None
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_paged_layers_use_the_last_page_to_its_end(dtype):
+    """A greatest length inside a page: the page tables grant rows up to the page's end, and the attention has to see them."""
+    from paper_2507_00715_b200.session import PagedLayers
+    g = gen(3)
+    q, k, v = (torch.randn(30, h, 64, generator=g, device="cuda").to(DT[dtype]) for h in (4, 2, 2))
+    outs = []
+    for max_len in (20, 32):
+        lay = PagedLayers(1, 1, 4, 2, 64, DT[dtype], 1, 4, max_len, 30)
+        lay.begin_step(i32([25]))
+        outs.append(lay.layer(0, q, k, v))
+        assert lay.refused() == 0 and lay.kv_entries() == 25
+    assert torch.equal(outs[0], outs[1]) and not torch.equal(outs[0][24], outs[0][19])
+
+
 @pytest.mark.parametrize("dtype,interleaved", [("bf16", False), ("f32", True)])
 def test_paged_layers_agree_with_the_session(dtype, interleaved):
     """Prompts taken by PagedLayers in three uneven steps give the rows that a session's prefill of the whole prompts gives, and
