@@ -10,6 +10,8 @@
 // instructions want 128 rows: the same calls on them, transposed to fill the rows with keys, spent most of their time in the
 // waits between the product, the exponentials and the next product, with two such chains per SM: 84 us for 64 x 700-1044 rows.)
 //
+// The probabilities are rounded to bf16 for the product with V (chunk_tc.cu), their sum is that of the unrounded ones.
+//
 // Measured: 64 single tokens over 700-1044 rows, 32/8 heads, 58 us (3.9 TB/s; 41 us of them the main loop); 8 over 20000-32000 rows
 // 157 us (5.4 TB/s); 5 tokens over 2000 rows, 12/2 heads, 16 us.
 //
