@@ -501,6 +501,47 @@ def test_chunk_rows_16_bytes_past_a_32_byte_boundary(dtype, new, lens):
     c.call().check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "bf16 bulk", "f32"])
+def test_chunk_pages_behind_2_31_elements(dtype):
+    """Rows stored and read behind the first 2^31 elements of the pools."""
+    c = Chunk([20, 1], [60, 33], 8, 8, 128, dtype, seed=21)
+    first = 2 ** 31 // (PAGE * 8 * 128) + 3
+    pools = [torch.empty(first + c.n_pages, PAGE, 8, 128, device="cuda", dtype=c.k.dtype) for _ in range(2)]
+    for big, small in zip(pools, (c.k, c.v)):
+        big[first:] = small
+    c.k, c.v = pools
+    c.table += first
+    c.cache = B.make_paged_cache(c.k, c.v, c.table, c.seq_len, max_len=max(c.lens))
+    c.call().check()
+    k, v = (torch.randn(1, 8, 128, device="cuda").to(c.k.dtype) for _ in range(2))
+    slot = int(c.table[1, 0]) * PAGE + 5
+    B.earn_rope_append(c.model, 0, B.make_rope(None), 1, i32([0]), i32([slot]), None, k, v, None, c.cache)
+    assert torch.equal(c.k.view(-1, 8, 128)[slot], k[0]) and torch.equal(c.v.view(-1, 8, 128)[slot], v[0])
+
+
+def test_chunk_two_graphs_share_a_workspace():
+    """Captured calls of different shapes, replayed in turn on one stream."""
+    chunks = [Chunk([3, 1, 2], [900, 3000, 40], 8, 2, 128, "bf16", seed=30), Chunk([50], [500], 8, 2, 128, "bf16 bulk", seed=31)]
+    ws = torch.empty(max(c.ws.numel() for c in chunks), dtype=torch.uint8, device="cuda")
+    B.earn_workspace_init(ws)
+    s, graphs = torch.cuda.Stream(), []
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for c in chunks:
+            c.ws = ws
+            c.call()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=s):
+                c.call()
+        for i in (0, 1, 1, 0, 0, 1):
+            chunks[i].o.fill_(7)
+            chunks[i].lse.fill_(7)
+            graphs[i].replay()
+        for c in chunks:
+            c.check()
+    torch.cuda.current_stream().wait_stream(s)
+
+
 def test_chunk_on_another_stream_and_captured():
     """A step captured once and replayed with other lengths, tables and offsets, on a stream of its own."""
     c = Chunk([5, 1, 40, 0], [300, 40, 90, 10], 8, 2, 128, "bf16", seed=6, pad=14)
