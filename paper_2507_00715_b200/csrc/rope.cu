@@ -6,8 +6,8 @@
 // Bound by HBM: every row is read and written once.  Angles cost a token rot/2 sines and cosines, shared by all its heads:
 // the product position * f_i is taken and reduced to turns in 64 bits (a 32-bit product is off by 0.06 rad at position 10^6),
 // the remainder's sine and cosine in 32.  They go to shared memory, from where the threads take them, eight pairs at a time.
-// 65536 tokens of 32/8 heads of 128: 240 us, 5.6 TB/s of a copy's 6.55; 8191 tokens of 28/4 heads appended: 31 us, 4.9 TB/s; 64
-// tokens: 2.7 us, a launch.
+// 65536 tokens of 32/8 heads of 128: 233 us, 5.8 TB/s of a copy's 6.55; 8191 tokens of 28/4 heads appended: 26 us, 5.8 TB/s; 64
+// tokens: 2.5 us, a launch.
 #include <algorithm>
 
 #include "chunk_step.cuh"
@@ -15,7 +15,7 @@
 namespace earn {
 namespace {
 
-constexpr int THREADS = 256, MAX_TOKENS = 8;
+constexpr int MAX_TOKENS = 8;
 
 enum Form { HALF, INTERLEAVED, STAGED };   // STAGED: half layout whose second half does not start on a 16-byte vector
 
@@ -66,8 +66,10 @@ __device__ __forceinline__ Row row_of(const RopeArgs& a, int tok, int h, int slo
 }
 
 // A block takes `tokens` tokens and `per_block` of their heads, as one list of units.  A thread's first two units are on their
-// way while the angles are worked out.
-template <typename T, int D, int FORM>
+// way while the angles are worked out.  Loads and stores are marked as streaming: the rows are read once, and what is written is
+// read by another kernel or not soon (65536 tokens 237 us without, 233 with; the attention behind an append of 8 x 1024 tokens is
+// as fast).
+template <typename T, int D, int FORM, int THREADS>
 __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, int head_from, int per_block, int tokens) {
   constexpr int N = Vec<T>::N, HEAD_BYTES = D * (int)sizeof(T);
   constexpr int UNITS = FORM == HALF ? D / (2 * N) : D / N;   // HALF: a unit is two vectors, a pair's halves or two that are copied
@@ -92,10 +94,10 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, in
     const int k = tokens == 1 ? 0 : i / units, r = i - k * units, u = r % UNITS;
     const uint4* src = reinterpret_cast<const uint4*>(row_of(a, tok0 + k, head_from + r / UNITS, -1, HEAD_BYTES).src);
     if constexpr (FORM == HALF) {
-      w[0] = src[u < turned ? u : 2 * u];
-      w[1] = src[u < turned ? u + turned : 2 * u + 1];
+      w[0] = __ldcs(src + (u < turned ? u : 2 * u));
+      w[1] = __ldcs(src + (u < turned ? u + turned : 2 * u + 1));
     } else {
-      w[0] = src[u];
+      w[0] = __ldcs(src + u);
     }
   };
   uint4 ahead[AHEAD][VECS];
@@ -137,8 +139,8 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, in
         w[0] = packed<T>(x);
         w[1] = packed<T>(y);
       }
-      reinterpret_cast<uint4*>(to.dst)[u < turned ? u : 2 * u] = w[0];
-      reinterpret_cast<uint4*>(to.dst)[u < turned ? u + turned : 2 * u + 1] = w[1];
+      __stcs(reinterpret_cast<uint4*>(to.dst) + (u < turned ? u : 2 * u), w[0]);
+      __stcs(reinterpret_cast<uint4*>(to.dst) + (u < turned ? u + turned : 2 * u + 1), w[1]);
     } else if constexpr (FORM == INTERLEAVED) {
       if (to.turn && u * N < a.rot) {
         float x[N];
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, in
         }
         w[0] = packed<T>(x);
       }
-      reinterpret_cast<uint4*>(to.dst)[u] = w[0];
+      __stcs(reinterpret_cast<uint4*>(to.dst) + u, w[0]);
     } else {
       w[0] = rows[i];
       if (to.turn && u * N < a.rot) {
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, in
         }
         w[0] = packed<T>(x);
       }
-      reinterpret_cast<uint4*>(to.dst)[u] = w[0];
+      __stcs(reinterpret_cast<uint4*>(to.dst) + u, w[0]);
     }
   };
 #pragma unroll
@@ -190,16 +192,19 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeArgs a, int heads, in
 
 template <typename T, int D, int FORM>
 cudaError_t launch_form(const RopeArgs& a, int heads, int head_from, cudaStream_t st) {
-  // Up to 64 heads of a token (STAGED keeps the rows in shared memory: 32 KB at most), and so many tokens that every thread has
-  // two units, as long as there are eight blocks for every SM all the same.
+  // Up to 64 heads of a token (STAGED keeps the rows in shared memory: 32 KB at most), and so many tokens as make 512 units, as
+  // long as there are eight blocks for every SM all the same (8191 appended 38 us with one token a block, 31 so).  Where there are,
+  // blocks of 128 threads, more of which fit an SM at different stages (65536 tokens 239 us with 256, 233 with 128; 8191 appended 30
+  // and 26); else 256, which are through sooner (64 tokens 2.5 and 2.9).
   constexpr int UNITS = FORM == HALF ? D / (2 * Vec<T>::N) : D / Vec<T>::N;
-  // as many tokens a block as give a thread two units (65536 tokens 240 us, one token a block 288; 8191 appended 31 and 38)
   const int per_block = std::min(heads, 64);
-  int tokens = std::max(1, std::min(MAX_TOKENS, 2 * THREADS / (per_block * UNITS)));
+  int tokens = std::max(1, std::min(MAX_TOKENS, 512 / (per_block * UNITS)));
   while (tokens > 1 && a.n_tokens / tokens < 8 * sm_count()) tokens /= 2;
   const int bytes = FORM == STAGED ? tokens * per_block * D * (int)sizeof(T) : 0;
   const dim3 grid((a.n_tokens + tokens - 1) / tokens, (heads + per_block - 1) / per_block);
-  const cudaError_t e = launch_pdl(rope_kernel<T, D, FORM>, grid, dim3(THREADS), bytes, st, a, heads, head_from, per_block, tokens);
+  const cudaError_t e = grid.x * (int64_t)grid.y >= 8 * sm_count()
+      ? launch_pdl(rope_kernel<T, D, FORM, 128>, grid, dim3(128), bytes, st, a, heads, head_from, per_block, tokens)
+      : launch_pdl(rope_kernel<T, D, FORM, 256>, grid, dim3(256), bytes, st, a, heads, head_from, per_block, tokens);
   note_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
