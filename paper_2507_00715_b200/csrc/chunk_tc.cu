@@ -63,7 +63,7 @@ struct Cfg {
   static constexpr int FULL = 0, EMPTY = FULL + NSTAGE, QFULL = EMPTY + NSTAGE, QFREE = QFULL + 2, S = QFREE + 2, P = S + 4, O = P + 4,
                        OM = O + 2, ML = OM + 1, MERGED = ML + 1, FIX = MERGED + 1, DRAIN = FIX + NSTAGE, PARTFULL = DRAIN + 2,
                        PARTFREE = PARTFULL + 4, REFS = PARTFREE + 4, SUMS = REFS + 2, DONE = SUMS + 2,
-                       N_BARS = DONE + 1;
+                       OFREE = DONE + 1, N_BARS = OFREE + 2;
   static constexpr int SMEM_BYTES = OFF_BAR + (8 * N_BARS + 48 + 127) / 128 * 128 + 1024;   // + alignment slack
   static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of an SM");
 };
@@ -205,6 +205,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       mbar_init(bar(C::O + x), 1);
       mbar_init(bar(C::REFS + x), 4);
       mbar_init(bar(C::SUMS + x), 8);
+      mbar_init(bar(C::OFREE + x), 8);   // the warps that read O_x: its stream's, or stream 0's where the streams meet
     }
     for (int i = 0; i < 4; ++i) {   // stream, half of the key tile
       mbar_init(bar(C::S + i), 1);
@@ -390,6 +391,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     };
     int eb = 0, n_q = 0, n_q0 = 0;   // ring entry of the part's K_0; parts with a second Q tile, and all
+    int n_o = 0;                     // parts that had their sums in O_x
     int filled = 0;                  // ring entries waited for
     uint32_t p_phase = 0;            // a bit per P barrier
     uint32_t fix_phase = 0;          // a bit per ring stage: warp 1 may be several items ahead, but not on one stage
@@ -435,6 +437,8 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           issue_s(1, y, eb + entry_k(p, j0));
           free_entry(eb + entry_k(p, j0));
           if (j0 + stride >= n) free_q();
+          if (n_o > 0) ok = wait(C::OFREE + x, n_o - 1);   // the first P V overwrites what both halves' warps read at the last part's end
+          ++n_o;
           for (int j = j0; j < n && ok; j += stride) {
             const int ev = eb + entry_v(p, j), ek = eb + entry_k(p, j + stride), pages = pages_of(j);
             const bool more = j + stride < n;
@@ -667,8 +671,12 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             else if (a.lse != nullptr) a.lse[(int64_t)(p.head0 + head) * a.sched.n_tokens + at_tok] = chunk_lse<true>(m_ref, l);
           }
         }
-        tc_fence_before();   // the next P V over O_x is issued after both halves' next arrivals on P
-        if (merge) warp_arrive(bar(C::MERGED));
+        tc_fence_before();
+        warp_arrive(bar(C::OFREE + x));   // this warp has read O_x: the next part's first P V waits for all of them
+        if (merge) {
+          warp_arrive(bar(C::OFREE + 1));
+          warp_arrive(bar(C::MERGED));
+        }
         if (!whole && pass != MAXIMA) {
           if (b == 0 && row == 0) cuts[n_cuts] = p;
           ++n_cuts;
