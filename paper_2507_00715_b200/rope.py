@@ -7,9 +7,12 @@ trained on (``original`` of them) by ``factor``:
   "linear"  all frequencies divided by the factor
   "base"    theta times factor^(rot_dim / (rot_dim - 2)): the fastest pair keeps its frequency, the slowest is divided by the factor
   "ramp"    pairs that make more than ``fast`` turns over the original length keep their frequency, those with less than ``slow``
-            turns are divided by the factor, between them the weight of the old frequency grows linearly with the pair's number;
-            amplitude 0.1 ln(factor) + 1
+            turns are divided by the factor, between them the weight of the old frequency falls linearly with the pair's number,
+            from 1 to 0 between the two pairs that make ``fast`` and ``slow`` turns, as real numbers and rounded outward to whole
+            ones (as the models that were trained with such a ramp have it); amplitude 0.1 ln(factor) + 1
   "bands"   the same, but the weight grows linearly with the number of turns, and the amplitude is 1
+
+The amplitude is an argument of its own of make_rope, so any of these goes with any amplitude.
 """
 from __future__ import annotations
 
@@ -41,7 +44,7 @@ def frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str] = N
     elif scaling == "ramp":
         # the pairs (as real numbers) that make `fast` and `slow` turns: original * theta^(-2i / rot_dim) = 2 pi turns
         first, last = (rot_dim * math.log(original / (2.0 * math.pi * n)) / (2.0 * math.log(theta)) for n in (fast, slow))
-        first, last = max(first, 0.0), min(max(last, 0.0), rot_dim / 2 - 1.0)
-        keep = 1.0 - ((torch.arange(rot_dim // 2, dtype=torch.float64) - first) / max(last - first, 1e-3)).clamp(0.0, 1.0)
+        first, last = math.floor(first), math.ceil(last)
+        keep = ((last - torch.arange(rot_dim // 2, dtype=torch.float64)) / (last - first)).clamp(0.0, 1.0)
         f = f * (keep + (1.0 - keep) / factor)
     return f, 0.1 * math.log(factor) + 1.0 if scaling == "ramp" else 1.0
