@@ -29,7 +29,9 @@ def frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str] = N
         raise ValueError(f"rot_dim: {rot_dim}, expected an even number of at least 2")
     if scaling not in (None, "linear", "base", "ramp", "bands"):
         raise ValueError(f"scaling: {scaling!r}")
-    if scaling is not None and not factor >= 1.0:
+    if not 0.0 < theta < math.inf or (scaling == "ramp" and theta <= 1.0):
+        raise ValueError(f"theta: {theta}, expected a positive number{' greater than 1' if scaling == 'ramp' else ''}")
+    if scaling is not None and not 1.0 <= factor < math.inf:
         raise ValueError(f"factor: {factor}, expected at least 1")
     if scaling in ("ramp", "bands") and (original < 1 or not 0 < slow < fast):
         raise ValueError("original length and 0 < slow < fast are needed")
