@@ -33,6 +33,7 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st);
 
+constexpr int kChunkMaxLen = INT32_MAX - 127;   // the end of a list's last key tile is a 32-bit number
 constexpr int kItemCost = 2;   // of the tensor-core kernel's items of two row tiles, see there
 constexpr int kChunkTickets = 640;   // row tiles of all CTAs' items, at most
 

@@ -876,7 +876,8 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
 
 size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
                                         const earn_paged_cache_t* cache) {
-  if (check_model(model) != EARN_OK || n_seq < 0 || n_seq > 65535 || n_tokens < 0 || check_paged(cache, n_seq, false) != EARN_OK)
+  if (check_model(model) != EARN_OK || n_seq < 0 || n_seq > 65535 || n_tokens < 0 || check_paged(cache, n_seq, false) != EARN_OK ||
+      cache->max_len > kChunkMaxLen)
     return kStatusBytes;
   return chunk_layout(model, n_seq, n_tokens, cache).total;
 }
@@ -891,6 +892,7 @@ earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, in
   s = check_paged(cache, n_seq, true);
   if (s != EARN_OK) return s;
   if (cache->n_pages > INT32_MAX / EARN_PAGE_TOKENS) return EARN_ERR_UNSUPPORTED;   // the copy engine's row numbers are 32-bit
+  if (cache->max_len > kChunkMaxLen) return EARN_ERR_UNSUPPORTED;
   if (n_seq == 0 || n_tokens == 0) return EARN_OK;
   if (!cu_new || !q || !o || !aligned4(cu_new) || !aligned16(q) || !aligned16(o) || !aligned4(lse_or_null)) return EARN_ERR_INVALID_ARG;
   const ChunkLayout l = chunk_layout(model, n_seq, n_tokens, cache);
