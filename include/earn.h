@@ -470,8 +470,10 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init; calls of any shapes whose bytes it holds may
  * use it in turn (not entry points of other kinds in between: those leave other things where this one's counters are).
  * Errors: layer outside [0, k), n_seq < 0, n_tokens < 0, a malformed cache, NULL or misaligned tensors -> INVALID_ARG;
- * n_seq > 65535, 16 * n_pages beyond 2^31 - 1, max_len beyond 2^31 - 128, more than 2^31 - 1 products of a row tile and a key tile (128 x 128; fp32: 64 x
- * 64 or fewer rows) that n_tokens and max_len allow -> UNSUPPORTED; workspace -> WORKSPACE. */
+ * n_seq > 65535, 16 * n_pages beyond 2^31 - 1, max_len beyond 2^31 - 128, sizes that allow 2^31 units of work or more ->
+ * UNSUPPORTED; workspace -> WORKSPACE.  The units of sizes: (n_tokens / t + min(n_seq, n_tokens)) * Hkv * tiles; bf16: t tokens
+ * fill 256 rows (token, query head of a kv head; of 128 heads at most, more count as several kv heads), tiles of 128 keys and
+ * two more; fp32: 64 rows or, where that makes too few units, 32 or 16, tiles of 64 keys. */
 size_t earn_paged_chunk_workspace_bytes(const earn_model_t* model, int32_t n_seq, int32_t n_tokens,
                                         const earn_paged_cache_t* cache);
 earn_status_t earn_paged_chunk_attn(const earn_model_t* model, int32_t n_seq, int32_t layer, int32_t n_tokens,

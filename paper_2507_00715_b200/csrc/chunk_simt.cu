@@ -228,15 +228,20 @@ ChunkPlan plan_chunk_attn(int n_seq, int n_q_heads, int n_kv_heads, int dtype, i
   p.tile_tok = p.rows / p.block_heads;
   // no more CTAs than there can be units (bf16: of the kernel for few tokens, whose items are the smaller ones)
   const int blocks = tc ? (g + kShortRows - 1) / kShortRows : p.blocks, heads = (g + blocks - 1) / blocks, tokens = tc ? kShortRows / heads : p.tile_tok;
-  const int64_t items = (int64_t)n_tokens / tokens + std::min(n_seq, n_tokens);
-  const int64_t tiles = (max_len + p.keys - 1) / p.keys, units = items * n_kv_heads * blocks * (tiles + (tc ? kItemCost : 0));
+  const int64_t lists = std::min(n_seq, n_tokens), items = (int64_t)n_tokens / tokens + lists, tiles = (max_len + p.keys - 1) / p.keys;
   if (tc) {
     p.split.few = kShortRows / g;
     p.split.units = kShortUnits * sm_count() / (n_kv_heads * blocks);
     p.split.item_tok = tokens;
     p.split.known = n_tokens <= p.split.few || items * tiles <= p.split.units;
   }
-  p.grid = units > INT32_MAX ? 0 : (int)std::min<int64_t>(std::min(tc ? sm_count() : 2 * sm_count(), MAX_GRID), std::max<int64_t>(units, 1));
+  // Units are counted in 31 bits, by the kernel that works: for few tokens these are one item a list at most, or no more than
+  // split.units.  (In floating point: the sizes' product may pass 64 bits.)
+  const double units = (double)items * n_kv_heads * blocks * (tiles + (tc ? kItemCost : 0));
+  const double counted = !tc ? units : p.split.known ? (double)lists * n_kv_heads * blocks * tiles
+                         : (double)((int64_t)n_tokens / (p.tile_tok * p.tiles) + lists) * n_kv_heads * p.blocks * (tiles + kItemCost);
+  const int most = std::min(tc ? sm_count() : 2 * sm_count(), MAX_GRID);
+  p.grid = counted > (double)INT32_MAX ? 0 : units < most ? std::max((int)units, 1) : most;
   return p;
 }
 
