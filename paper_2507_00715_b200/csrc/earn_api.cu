@@ -831,8 +831,9 @@ earn_status_t earn_rope(const earn_model_t* model, const earn_rope_t* rope, int3
   if (s != EARN_OK) return s;
   s = check_rope(model, rope, n_tokens);
   if (s != EARN_OK) return s;
+  if (n_tokens == 0) return EARN_OK;   // (tensors of no rows may come as NULL)
   if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return EARN_ERR_INVALID_ARG;
-  if (n_tokens == 0 || (q == nullptr && k == nullptr)) return EARN_OK;
+  if (q == nullptr && k == nullptr) return EARN_OK;
   if (!positions || !aligned4(positions) || !aligned16(q_out) || !aligned16(k_out)) return EARN_ERR_INVALID_ARG;
   if ((q != nullptr && bad_rows(model, q, q_stride, model->n_q_heads)) || (k != nullptr && bad_rows(model, k, k_stride, model->n_kv_heads)))
     return EARN_ERR_INVALID_ARG;
@@ -857,8 +858,8 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
   s = check_paged(cache, 0, false);
   if (s != EARN_OK) return s;
   if (cache->n_pages > INT32_MAX / EARN_PAGE_TOKENS) return EARN_ERR_UNSUPPORTED;   // slot numbers are 32-bit
+  if (n_tokens == 0) return EARN_OK;   // (as above)
   if ((q == nullptr) != (q_out == nullptr)) return EARN_ERR_INVALID_ARG;
-  if (n_tokens == 0) return EARN_OK;
   if (!positions || !slots || !k || !v || !aligned4(positions) || !aligned4(slots) || !aligned16(q_out)) return EARN_ERR_INVALID_ARG;
   if ((q != nullptr && bad_rows(model, q, q_stride, model->n_q_heads)) || bad_rows(model, k, k_stride, model->n_kv_heads) ||
       bad_rows(model, v, v_stride, model->n_kv_heads))
