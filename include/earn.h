@@ -41,7 +41,7 @@ typedef enum {
   EARN_OK = 0,
   EARN_ERR_INVALID_ARG = 1, /* null/misaligned pointer, bad shape, layer on the wrong side of k, R > L_b ... */
   EARN_ERR_UNSUPPORTED = 2, /* legal request this build has no kernel for (e.g. head_dim not in {64,128}) */
-  EARN_ERR_WORKSPACE = 3,   /* workspace NULL or smaller than earn_workspace_bytes() */
+  EARN_ERR_WORKSPACE = 3,   /* workspace NULL, smaller than needed, or (earn_device_status) overwritten */
   EARN_ERR_CUDA = 4,        /* the CUDA runtime reported an error at launch */
   EARN_ERR_TIMEOUT = 5      /* a bounded device-side wait ran out (read back by earn_device_status) */
 } earn_status_t;
@@ -110,7 +110,8 @@ size_t earn_workspace_bytes(const earn_model_t* model, const earn_batch_t* batch
 earn_status_t earn_workspace_init(void* workspace, size_t workspace_bytes, earn_stream_t stream);
 
 /* Synchronises `stream` and returns the device status word of the workspace: EARN_OK, or
- * EARN_ERR_TIMEOUT if a bounded wait inside a kernel ran out since earn_workspace_init. */
+ * EARN_ERR_TIMEOUT if a bounded wait inside a kernel ran out since earn_workspace_init, or EARN_ERR_WORKSPACE if a call of
+ * earn_page_tables or earn_paged_chunk_attn found something else than its counters there (its outputs are then not complete). */
 earn_status_t earn_device_status(const void* workspace, earn_stream_t stream);
 
 /* Failure-path self-test (the paper has no counterpart): launches one small kernel that waits, with the bounded
@@ -414,7 +415,8 @@ typedef struct {
  * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
  * must not overlap it).  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
  * or above the new height hold nothing.  Without sequences (n_seq = 0) nothing is done.
- * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes may use it in turn.
+ * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes, and those of
+ * earn_paged_chunk_attn, may use it in turn (others leave other things there: see earn_device_status).
  * Errors: n_seq < 0, n_tokens < 0, n_pages < 1, pages_per_seq < 1, NULL or misaligned arrays -> INVALID_ARG; n_seq > 16384,
  * row or slot numbers beyond 2^31 - 32 -> UNSUPPORTED; workspace -> WORKSPACE. */
 size_t earn_page_tables_workspace_bytes(int32_t n_seq);
@@ -468,7 +470,8 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  * Logits, softmax and sums in fp32; with bf16 the probabilities are rounded to bf16 in front of the product with V only.
  * Lists are cut at places that depend on the lengths only, and joined in the order of the keys: equal calls, equal results.
  * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init; calls of any shapes whose bytes it holds may
- * use it in turn (not entry points of other kinds in between: those leave other things where this one's counters are).
+ * use it in turn (not entry points of other kinds but earn_page_tables in between: those leave other things where this one's
+ * counters are, which earn_device_status then reports, and earn_workspace_init mends).
  * Errors: layer outside [0, k), n_seq < 0, n_tokens < 0, a malformed cache, NULL or misaligned tensors -> INVALID_ARG;
  * n_seq > 65535, 16 * n_pages beyond 2^31 - 1, max_len beyond 2^31 - 128, sizes that allow 2^31 units of work or more ->
  * UNSUPPORTED; workspace -> WORKSPACE.  The units of sizes: (n_tokens / t + min(n_seq, n_tokens)) * Hkv * tiles; bf16: t tokens

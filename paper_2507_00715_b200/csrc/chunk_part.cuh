@@ -106,10 +106,7 @@ __device__ __forceinline__ void join_cuts(const ChunkArgs& a, const Part* cuts, 
   if (!sync()) return;
   if (t < n) {
     const Part& p = cuts[t];
-    const int32_t at = p.first * 2 + x;
-    const bool is_last = atomicAdd(a.tickets + at, 1) == p.parts - 1;
-    if (is_last) a.tickets[at] = 0;   // for the next call
-    flag[t] = is_last;
+    flag[t] = last_arrival(a.tickets + p.first * 2 + x, p.parts, a.status);
     __threadfence();
   }
   if (!sync()) return;

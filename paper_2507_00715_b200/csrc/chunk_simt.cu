@@ -180,8 +180,7 @@ __global__ void __launch_bounds__(THREADS) chunk_simt_kernel(ChunkArgs a) {
       __threadfence();
       __syncthreads();
       if (t == 0) {
-        last_part = atomicAdd(a.tickets + parts.first, 1) == parts.parts - 1;
-        if (last_part) a.tickets[parts.first] = 0;   // for the next call
+        last_part = last_arrival(a.tickets + parts.first, parts.parts, a.status);
         __threadfence();
       }
       __syncthreads();

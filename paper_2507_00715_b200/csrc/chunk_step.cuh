@@ -6,6 +6,19 @@
 
 namespace earn {
 
+// An arrival at a ticket that is zero between calls: true for the last of `all`, who sets it to zero again.  A ticket counts in steps
+// of a large odd number, so that what other entry points leave in a workspace (counts, floats) is not taken for one of its states:
+// whoever finds something else reports EARN_ERR_WORKSPACE.
+constexpr uint32_t kTicketStep = 2654435769u, kTicketInverse = 340573321u;
+static_assert(kTicketStep * kTicketInverse == 1u, "inverse modulo 2^32");
+__device__ __forceinline__ bool last_arrival(int32_t* ticket, int all, int32_t* status) {
+  const uint32_t before = (uint32_t)atomicAdd(ticket, (int32_t)kTicketStep) * kTicketInverse;
+  if (before >= (uint32_t)all) atomicExch(status, (int32_t)EARN_ERR_WORKSPACE);
+  if (before != (uint32_t)all - 1) return false;
+  *ticket = 0;   // for the next call
+  return true;
+}
+
 struct PageTableArgs {
   const int32_t* target;       // [n_seq] lengths to bring the sequences to
   const int32_t* held;         // [n_seq] rows held
@@ -15,7 +28,7 @@ struct PageTableArgs {
   const int32_t* n_free;
   int32_t* n_free_out;         // may be n_free
   int32_t *cu_new, *seq_len, *positions, *slots, *n_refused;
-  int32_t* ticket;
+  int32_t *ticket, *status;
   int n_seq, n_tokens, pages_per_seq, n_pages;
 };
 constexpr int kPageTablesMaxSeqs = 16384;   // three numbers per sequence in shared memory

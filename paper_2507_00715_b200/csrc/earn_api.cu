@@ -303,7 +303,7 @@ const char* earn_status_string(earn_status_t s) {
     case EARN_OK: return "ok";
     case EARN_ERR_INVALID_ARG: return "invalid argument";
     case EARN_ERR_UNSUPPORTED: return "unsupported configuration";
-    case EARN_ERR_WORKSPACE: return "workspace missing or too small";
+    case EARN_ERR_WORKSPACE: return "workspace missing, too small or overwritten";
     case EARN_ERR_CUDA: return "CUDA error at launch";
     case EARN_ERR_TIMEOUT: return "device-side wait timed out";
   }
@@ -328,7 +328,7 @@ earn_status_t earn_device_status(const void* workspace, earn_stream_t stream) {
   if (cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess)
     return EARN_ERR_CUDA;
   if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return EARN_ERR_CUDA;
-  return word == 0 ? EARN_OK : EARN_ERR_TIMEOUT;
+  return word == 0 ? EARN_OK : word == EARN_ERR_WORKSPACE ? EARN_ERR_WORKSPACE : EARN_ERR_TIMEOUT;
 }
 
 earn_status_t earn_prefill_attn(const earn_model_t* model, const earn_batch_t* batch, int32_t layer, const void* q,
@@ -818,6 +818,7 @@ earn_status_t earn_page_tables(int32_t n_seq, const int32_t* target, const earn_
   a.free_pages = pool->free_pages; a.n_free = pool->n_free; a.n_free_out = n_free_out;
   a.cu_new = step->cu_new; a.seq_len = step->seq_len; a.positions = step->positions; a.slots = step->slots;
   a.n_refused = step->n_refused;
+  a.status = reinterpret_cast<int32_t*>(workspace);
   a.ticket = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) + kStatusBytes);
   a.n_seq = n_seq; a.n_tokens = step->n_tokens; a.pages_per_seq = pool->pages_per_seq; a.n_pages = pool->n_pages;
   note_call(stream, CALL_UNKNOWN);

@@ -186,8 +186,7 @@ __global__ void __launch_bounds__(THREADS) page_tables_kernel(PageTableArgs a) {
   if (gridDim.x > 1) {
     if (t == 0) {
       __threadfence();
-      last = atomicAdd(a.ticket, 1) == (int)gridDim.x - 1;
-      if (last) *a.ticket = 0;   // for the next call
+      last = last_arrival(a.ticket, (int)gridDim.x, a.status);
       __threadfence();
     }
     __syncthreads();

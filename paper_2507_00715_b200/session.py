@@ -357,4 +357,5 @@ class PagedLayers:
         return int(self.held.sum()) * self.split_k
 
     def device_status(self) -> int:
-        return B.EARN_OK if self.workspace is None else B.earn_device_status(self.workspace)
+        status = B.earn_device_status(self.table_workspace)
+        return status if status != B.EARN_OK or self.workspace is None else B.earn_device_status(self.workspace)
