@@ -465,8 +465,9 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  * sees nothing (its sequence has seq_len 0, or fewer rows than new tokens; every logit -inf): o = 0, lse = -inf.  Rows of q
  * past cu_new[n_seq] are not read, those of o and lse are left as they were.  Rows at or past seq_len are not used, whatever
  * they hold; every row of a sequence below seq_len is to hold finite values (a row that some new token sees meets the earlier
- * ones with a weight of zero).  cu_new: device [n_seq + 1], increasing; offsets past n_tokens count as n_tokens.  No weights
- * are accumulated (earn_paged_decode_attn does that for a single token).
+ * ones with a weight of zero).  cu_new: device [n_seq + 1], increasing; offsets past n_tokens count as n_tokens.  (Offsets that
+ * run backwards touch nothing outside the tensors, but a token that they give to several sequences has one of its rows, or none.)
+ * No weights are accumulated (earn_paged_decode_attn does that for a single token).
  * Logits, softmax and sums in fp32; with bf16 the probabilities are rounded to bf16 in front of the product with V only.
  * Lists are cut at places that depend on the lengths only, and joined in the order of the keys: equal calls, equal results.
  * workspace: earn_paged_chunk_workspace_bytes, prepared by earn_workspace_init; calls of any shapes whose bytes it holds may

@@ -254,7 +254,8 @@ __device__ inline bool chunk_many(const ChunkSched& s, const ChunkSplit& f) {
   __syncthreads();
   return sum > (uint32_t)f.units;
 }
-// Sums (units, items, lists) over the block; returns the units of the threads in front of this one.
+// Sums (units, items, lists) over the block; returns the units of the threads in front of this one.  2^31 units or more, which
+// only offsets that run backwards can make (tokens that belong to several sequences): no units.
 __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x / 32;
   uint32_t incl = c.units;
@@ -265,8 +266,9 @@ __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
   }
   const uint32_t inside = incl - c.units;
   const int items = __reduce_add_sync(0xffffffffu, c.items), lists = __reduce_add_sync(0xffffffffu, c.lists);
+  const uint32_t high = __reduce_add_sync(0xffffffffu, c.units >> 16);   // (65536 units each: what the sum would be without its 32 bits)
   __syncthreads();
-  if (lane == 31) scratch[warp] = make_int4((int)incl, items, lists, 0);
+  if (lane == 31) scratch[warp] = make_int4((int)incl, items, lists, (int)high);
   __syncthreads();
   const int4 n = lane < warps ? scratch[lane] : make_int4(0, 0, 0, 0);
   uint32_t sum = (uint32_t)n.x;
@@ -275,7 +277,7 @@ __device__ inline uint32_t chunk_scan(ChunkCounts& c, int4* scratch) {
     const uint32_t v = __shfl_up_sync(0xffffffffu, sum, d);
     if (lane >= d) sum += v;
   }
-  c.units = __shfl_sync(0xffffffffu, sum, 31);
+  c.units = __reduce_add_sync(0xffffffffu, (uint32_t)n.w) < 32768u ? __shfl_sync(0xffffffffu, sum, 31) : 0u;
   c.items = __reduce_add_sync(0xffffffffu, n.y);
   c.lists = __reduce_add_sync(0xffffffffu, n.z);
   return __shfl_sync(0xffffffffu, sum - (uint32_t)n.x, warp) + inside;
@@ -288,14 +290,16 @@ __device__ inline ChunkWalk chunk_share(ChunkSched& s, int4* scratch, ChunkSeq* 
   const bool in_table = table != nullptr && s.n_seq <= kChunkTable;
   const int per = s.n_seq <= threads ? 1 : (s.n_seq + threads - 1) / threads, b0 = min(t * per, s.n_seq), b1 = min(b0 + per, s.n_seq);
   ChunkCounts n{};
+  uint64_t units = 0;
   for (int b = b0; b < b1; ++b) {
     const ChunkSeq q = chunk_seq(s, b);
     if (in_table) table[b] = q;
     if (q.n == 0) continue;
     n.items += q.items;
     ++n.lists;
-    n.units += s.heads * chunk_units_before(s, q, q.items);
+    units += s.heads * chunk_units_before(s, q, q.items);
   }
+  n.units = (uint32_t)(units < 0x80000000u ? units : 0x80000000u);
   int own_items = n.items;
   uint32_t mine = n.units, before = chunk_scan(n, scratch);
   if (in_table) s.table = table;   // (written in front of the scan's barriers)

@@ -118,3 +118,26 @@ def test_chunk_offsets_of_many_rows():
     for a, b in ((0, 1), (2, 3)):
         assert torch.equal(rows[a][0], rows[b][0]) and torch.equal(rows[a][1], rows[b][1])
     assert (rows[2][0][:9] == 7).all() and (rows[2][1][:, :9] == 7).all() and (rows[2][0][9:] != 7).any(-1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_seq", [65535, 40000])
+def test_chunk_offsets_that_give_every_token_to_thousands_of_sequences(dtype, n_seq):
+    """More work than 31 bits (or 32) count, which increasing offsets cannot make: nothing is written, and the next call is right."""
+    rows, heads, d = 32768, 8, 64
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q = torch.zeros(rows, heads, d, device="cuda", dtype=dt)
+    o = torch.full((rows + 32, heads, d), 7.0, device="cuda", dtype=dt)
+    pages = [torch.randn(8, 16, heads, d, device="cuda").to(dt) for _ in range(2)]
+    table, lens = torch.zeros(n_seq, rows // 16, dtype=torch.int32, device="cuda"), torch.full((n_seq,), rows, dtype=torch.int32, device="cuda")
+    cache = B.make_paged_cache(*pages, table, lens)
+    cu = torch.zeros(n_seq + 1, dtype=torch.int32, device="cuda")
+    cu[1::2] = rows
+    model = B.make_model(2, 1, heads, heads, d, dtype)
+    ws = torch.empty(B.earn_paged_chunk_workspace_bytes(model, n_seq, rows, cache), dtype=torch.uint8, device="cuda")
+    B.earn_workspace_init(ws)
+    B.earn_paged_chunk_attn(model, n_seq, 0, rows, cu, q, cache, o[16:-16], None, ws)
+    assert B.earn_device_status(ws) == B.EARN_OK and (o == 7).all()
+    c = Chunk([40, 3], [200, 90], heads, heads, d, dtype, seed=4)
+    c.ws = ws
+    c.call().check()
