@@ -413,7 +413,7 @@ typedef struct {
  * the pages that it and the sequences before it want (refused ones included: nobody is overtaken) are not there.  A refused
  * sequence keeps its rows; its tokens stay in the packed batch with position and slot -1, and its seq_len is 0.
  * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
- * must not overlap it).  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
+ * must not overlap it), target may be held; the arrays do not overlap otherwise.  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
  * or above the new height hold nothing.  Without sequences (n_seq = 0) nothing is done.
  * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes, and those of
  * earn_paged_chunk_attn, may use it in turn (others leave other things there: see earn_device_status).

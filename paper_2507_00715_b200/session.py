@@ -342,7 +342,8 @@ class PagedLayers:
     def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None,
               lse: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [n_tokens, Hq, D], k, v [n_tokens, Hkv, D] of the step's new tokens (they may be parts of a projection's output) ->
-        O [n_tokens, Hq, D]; rows of padding tokens stay as they are."""
+        O [n_tokens, Hq, D]; rows of padding tokens stay as they are (0 in an output that is made here, which costs its clearing:
+        a loop passes its own as ``out``)."""
         o = out if out is not None else torch.zeros_like(self.q_turned)
         B.earn_rope_append(self.model, layer, self.rope, self.n_tokens, self.positions, self.slots, q, k, v, self.q_turned, self.caches[layer])
         B.earn_paged_chunk_attn(self.model, self.n_seq, layer, self.n_tokens, self.cu_new, self.q_turned, self.caches[layer], o, lse,
