@@ -413,8 +413,9 @@ typedef struct {
  * the pages that it and the sequences before it want (refused ones included: nobody is overtaken) are not there.  A refused
  * sequence keeps its rows; its tokens stay in the packed batch with position and slot -1, and its seq_len is 0.
  * held_out[b] = t, or h where refused; n_free_out: the stack's new height; each may be the input array itself (otherwise it
- * must not overlap it), target may be held; the arrays do not overlap otherwise.  cu_new is cut off at n_tokens.  Table entries of pages given back stay as they are; stack entries at
- * or above the new height hold nothing.  Without sequences (n_seq = 0) nothing is done.
+ * must not overlap it), and target may be held; the arrays do not overlap otherwise.  cu_new is cut off at n_tokens.  Table
+ * entries of pages given back stay as they are; stack entries at or above the new height hold nothing.  Without sequences
+ * (n_seq = 0) nothing is done.
  * The workspace (earn_page_tables_workspace_bytes, earn_workspace_init) holds a counter; calls of any sizes, and those of
  * earn_paged_chunk_attn, may use it in turn (others leave other things there: see earn_device_status).
  * Errors: n_seq < 0, n_tokens < 0, n_pages < 1, pages_per_seq < 1, NULL or misaligned arrays -> INVALID_ARG; n_seq > 16384,
@@ -463,7 +464,7 @@ earn_status_t earn_rope_append(const earn_model_t* model, int32_t layer, const e
  *   o = sum_{j <= p} softmax_j( q . k_j * scale ) v_j .
  * q, o: device [n_tokens, Hq, D], apart from one another; lse_or_null: device fp32 [Hq, n_tokens], natural-log softmax denominators.  A token that
  * sees nothing (its sequence has seq_len 0, or fewer rows than new tokens; every logit -inf): o = 0, lse = -inf.  Rows of q
- * past cu_new[n_seq] are not read, those of o and lse are left as they were.  Rows at or past seq_len are not used, whatever
+ * past cu_new[n_seq] are not used, those of o and lse are left as they were.  Rows at or past seq_len are not used, whatever
  * they hold; every row of a sequence below seq_len is to hold finite values (a row that some new token sees meets the earlier
  * ones with a weight of zero).  cu_new: device [n_seq + 1], increasing; offsets past n_tokens count as n_tokens.  (Offsets that
  * run backwards touch nothing outside the tensors, but a token that they give to several sequences has one of its rows, or none.)
