@@ -75,7 +75,9 @@ cudaError_t launch_chunk_simt(const ChunkArgs& a, const ChunkPlan& p, cudaStream
 // bf16: the first kernel has items of 16 rows, which go through the keys one by one; the second fills row tiles of 128.  A call is
 // the second's if it has items of several in a sequence and enough work for it (chunk_many; 24 units an SM: 256 rows over 2900, 8
 // kv heads, 21 units: 46 and 62 us; 8 x 32 rows over 2900, 20 units: 49 and 48; 16 x 24 rows, 40 units: 87 and 72; one sequence of
-// 128 rows over 9000, 2 kv heads, 8 units: 27 and 143).  The lengths are on the device, so both are launched, unless the sizes
+// 128 rows over 9000, 2 kv heads, 8 units: 27 and 143; and at 16, 24, 32 and 40 units by their lists' length, 8 x 32 rows 41 and 44,
+// 54 and 56, 65 and 67, 78 and 73; 8 x 96 rows 41 and 37, 55 and 39, 68 and 42, 81 and 41; one of 256 rows 40 and 59, 52 and 67, 63
+// and 73, 75 and 73: level between 14 and 40 units, as the row tiles are filled).  The lengths are on the device, so both are launched, unless the sizes
 // that the host knows tell, and one of them finds nothing to do, which costs 5 us.
 cudaError_t launch_chunk_short(const ChunkArgs& a, cudaStream_t st);
 cudaError_t launch_chunk_tc(const ChunkArgs& a, const ChunkPlan& p, cudaStream_t st);

@@ -28,7 +28,8 @@
 // and with them.  (A test per half and a rescaling of O in place, with one warpgroup per row tile, took 1.4 times as long.)
 //
 // The probabilities are rounded to bf16 for the product with V, the type of its instruction: outputs are off by 2.3e-3 of
-// themselves, of which their own rounding makes 1.7e-3.  Everything else, the row's sum included, is fp32.
+// themselves, of which their own rounding makes 1.7e-3.  (A second number per probability would add the 1024 clocks of another
+// product with V to a unit's 2560.)  Everything else, the row's sum included, is fp32.
 //
 // Measured: 4096 new tokens over 12000 rows, 32/8 heads, 850-900 us (1.05-1.1 PFLOP/s); 8 x 1024 over 16000-31000 rows 3200-3550 us (0.95-1.05,
 // at the power cap); 14 chunks of 130-700 and 34 single tokens, 28/4 heads, 216 us.  A unit (256 rows x 128 keys) takes 3200 clocks,
